@@ -211,6 +211,74 @@ typedef struct apmm_problem {
 apmm_status apmm_gemm_grouped(int count, const apmm_problem *problems, int p, int q,
                               void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- A key/value cache held in four bits, and attention over it: what stands between the q/k/v and the output linears of a
+ * decoder layer (paper Sec. 5.2 setting).  Keys and values are bipolar-INT codes of four bits (paper Sec. 3.1, Eq. 1), a scale for each token and head.
+ *
+ * The cache is two buffers of the caller's, in pages of page_size tokens:
+ *   codes   pages x kv_heads x 2 x (page_size * head_dim / 2) bytes, 16-byte aligned; of the 2 the first are keys, the second values
+ *             keys    token by token, channel c in byte c / 2, in its low four bits where c is even, else in its high ones
+ *             values  by eights of tokens; in one, for channels 4 m to 4 m + 3 (m from 0 to head_dim / 4 - 1) eight 16-bit words, one a
+ *                     token, channel 4 m + e in bits 4 e to 4 e + 3
+ *   scales  pages x kv_heads x 2 x page_size numbers of the type of the tensors, 16-byte aligned
+ * A code u with the scale s stands for (2 u - 15) s.  A page may be copied, moved or shared by several sequences; nothing else refers to its place.
+ * Scales are not negative and finite, or NaN (see apmm_kv_write); codes are any.
+ *
+ * A call works on a batch of sequences: */
+typedef enum { APMM_F16 = 0, APMM_BF16 = 1 } apmm_dtype;
+
+typedef struct apmm_kv_cache {
+    void *codes, *scales;  /* device */
+    int64_t pages;
+    int page_size;         /* tokens of a page: a power of two from 16 to 1048576 */
+    int kv_heads;          /* 1 to 1024 */
+    int head_dim;          /* 64 or 128 */
+    int dtype;             /* apmm_dtype of scales, keys, values, queries and results */
+} apmm_kv_cache;
+
+typedef struct apmm_kv_batch {
+    int sequences;              /* 0 to 65536 */
+    int64_t tokens;             /* new tokens of all sequences, up to 2^30: rows of the tensors that the call takes */
+    const int32_t *lengths;     /* device, sequences: tokens of each sequence, its new ones included; up to 2^30 */
+    const int32_t *starts;      /* device, sequences + 1, ascending from 0 to `tokens`: the new tokens of sequence b, its last ones, are rows starts[b]
+                                   to starts[b + 1] - 1; or NULL: each sequence has one (tokens == sequences) */
+    const int32_t *page_table;  /* device: token t of sequence b is in page page_table[b * table_stride + t / page_size] */
+    int64_t table_stride;       /* elements between rows of the table, >= table_width */
+    int64_t table_width;        /* pages of a row, 1 to 2^26; tokens beyond table_width * page_size have no place */
+} apmm_kv_batch;
+/* Lengths, starts and page numbers are read on the device and cannot be refused; whatever they are, nothing outside of the buffers is
+ * read or written.  A token whose position is negative (more new tokens than the length says), beyond the table or in a page outside of 0 to pages - 1 has no place: it is not written,
+ * reads as zeros and is seen by no query.
+ * Tensors are tokens x heads x head_dim with head_dim contiguous elements and strides in elements, at any address of their type's
+ * alignment; rows that all start at multiples of 16 bytes are read and written faster. */
+
+/* Quantises new keys and values as they are written: of each row x of head_dim numbers
+ *   s = max |x| / 15, rounded once to its type,  u = (v + 15) / 2, v the odd integer of [-15, 15] nearest to x / s, the upper one on a tie
+ * decided as in exact arithmetic, as apmm_quantize_pack_activations does; a scale that rounds to zero has the code of +1 everywhere.  A row with a
+ * number that is not finite gets the scale NaN.  Two tokens of a call must not have the same place. */
+apmm_status apmm_kv_write(const apmm_kv_cache *cache, const apmm_kv_batch *batch,
+                          const void *k, int64_t k_token_stride, int64_t k_head_stride,
+                          const void *v, int64_t v_token_stride, int64_t v_head_stride, void *stream);
+
+/* Reads keys and values of the batch's new tokens back (all tokens of a sequence: as many new ones as its length): (2 u - 15) s rounded once to
+ * nearest even; what would round past the type's largest number becomes that. */
+apmm_status apmm_kv_read(const apmm_kv_cache *cache, const apmm_kv_batch *batch,
+                         void *k, int64_t k_token_stride, int64_t k_head_stride,
+                         void *v, int64_t v_token_stride, int64_t v_head_stride, void *stream);
+
+/* Attention of the batch's new tokens over the cache.  Query head h belongs to key/value head h / (q_heads / kv_heads).  The query at position p (its
+ * sequence's length less its new tokens, plus its place among them) sees key j of its sequence where
+ *   j <= p, and where window > 0 also j > p - window or j < sinks
+ * and its result is sum_j softmax_j(scale * q . k_j) v_j over these, zeros where there is none.  Statistics and sums are of 32 bits, the weights of the values are
+ * rounded to 11 significant bits, the result once.  Accuracy holds for value scales from 2^-103 on (bfloat16; below, values lose bits).
+ *   scale     > 0 and finite, 1 / sqrt(head_dim) in most models
+ *   window    0 (all keys) to 2^30;  sinks  0 to 2^30, without effect where window is 0
+ *   workspace device, 16-byte aligned, apmm_kv_attention_workspace_bytes() bytes of the same arguments (0 for most large calls); calls that may overlap need one each */
+size_t apmm_kv_attention_workspace_bytes(const apmm_kv_cache *cache, const apmm_kv_batch *batch, int q_heads);
+apmm_status apmm_kv_attention(const apmm_kv_cache *cache, const apmm_kv_batch *batch, int q_heads,
+                              const void *q, int64_t q_token_stride, int64_t q_head_stride,
+                              void *out, int64_t out_token_stride, int64_t out_head_stride,
+                              float scale, int64_t window, int64_t sinks, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Measurement aid.  The next apmm_gemm / apmm_gemm_ex / apmm_gemm_from_codes call of the calling thread, if it
  * runs the large-tile MFMA kernel or a small-M kernel in one launch, attaches the two hipEvent_t (created by the
  * caller; either may be NULL) to that kernel's dispatch itself (hipExtLaunchKernel): afterwards they hold the

@@ -20,7 +20,7 @@ ALGO_PLANE_PAIRS_GLOBAL, ALGO_PLANES_REGISTERS, ALGO_MFMA_KSPLIT = 6, 7, 8
 EXPORTS = [
     "apmm_packed_bytes", "apmm_packed_activation_bytes", "apmm_workspace_bytes", "apmm_pack_weights", "apmm_pack_activations",
     "apmm_quantize_pack_activations", "apmm_unpack", "apmm_unpack_activations", "apmm_gemm", "apmm_gemm_ex", "apmm_gemm_from_codes", "apmm_gemm_from_codes_noalloc", "apmm_gemm_grouped",
-    "apmm_time_next_gemm", "apmm_last_gemm_kernel", "apmm_status_string", "apmm_last_error", "apmm_version",
+    "apmm_kv_write", "apmm_kv_read", "apmm_kv_attention", "apmm_kv_attention_workspace_bytes", "apmm_time_next_gemm", "apmm_last_gemm_kernel", "apmm_status_string", "apmm_last_error", "apmm_version",
 ]
 
 
@@ -31,6 +31,18 @@ class ApmmProblem(ctypes.Structure):
                 ("a_packed", ctypes.c_void_p), ("w_packed", ctypes.c_void_p),
                 ("c_i32", ctypes.c_void_p), ("c_f16", ctypes.c_void_p),
                 ("w_scale", ctypes.c_void_p), ("a_scale", ctypes.c_void_p), ("a_codes", ctypes.c_void_p)]
+
+
+class ApmmKvCache(ctypes.Structure):
+    """struct apmm_kv_cache of include/apmm.h"""
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("pages", ctypes.c_int64), ("page_size", ctypes.c_int),
+                ("kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int), ("dtype", ctypes.c_int)]
+
+
+class ApmmKvBatch(ctypes.Structure):
+    """struct apmm_kv_batch of include/apmm.h"""
+    _fields_ = [("sequences", ctypes.c_int), ("tokens", ctypes.c_int64), ("lengths", ctypes.c_void_p), ("starts", ctypes.c_void_p),
+                ("page_table", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("table_width", ctypes.c_int64)]
 
 
 _lib = None
@@ -86,6 +98,15 @@ def load():
     lib.apmm_gemm_from_codes_noalloc.argtypes = [i64, i64, i64, ci, ci, vp, vp, vp, vp, vp, vp, vp]
     lib.apmm_gemm_grouped.restype = ci
     lib.apmm_gemm_grouped.argtypes = [ci, ctypes.POINTER(ApmmProblem), ci, ci, vp, ctypes.c_size_t, vp]
+    cache, batch, rows = ctypes.POINTER(ApmmKvCache), ctypes.POINTER(ApmmKvBatch), [vp, i64, i64]
+    for name in ("apmm_kv_write", "apmm_kv_read"):
+        fn = getattr(lib, name)
+        fn.restype = ci
+        fn.argtypes = [cache, batch] + rows + rows + [vp]
+    lib.apmm_kv_attention.restype = ci
+    lib.apmm_kv_attention.argtypes = [cache, batch, ci] + rows + rows + [ctypes.c_float, i64, i64, vp, ctypes.c_size_t, vp]
+    lib.apmm_kv_attention_workspace_bytes.restype = ctypes.c_size_t
+    lib.apmm_kv_attention_workspace_bytes.argtypes = [cache, batch, ci]
     lib.apmm_time_next_gemm.restype = ci
     lib.apmm_time_next_gemm.argtypes = [vp, vp]
     lib.apmm_last_gemm_kernel.restype = ctypes.c_char_p
@@ -271,6 +292,101 @@ def apmm_gemm_grouped(problems, p, q):
             t = pr.get(key)
             setattr(arr[i], key, t.data_ptr() if t is not None else None)
     _check(load().apmm_gemm_grouped(len(problems), arr, p, q, None, 0, _stream()))
+
+
+_KV_DTYPES = {torch.float16: 0, torch.bfloat16: 1}
+
+
+def apmm_kv_cache(pages, page_size, kv_heads, head_dim, dtype=torch.float16, device="cuda"):
+    """A four-bit key/value cache (layout: include/apmm.h) of zeros: (codes, scales)."""
+    return (torch.zeros((pages, kv_heads, 2, page_size * head_dim // 2), dtype=torch.uint8, device=device),
+            torch.zeros((pages, kv_heads, 2, page_size), dtype=dtype, device=device))
+
+
+def _kv_cache(codes, scales):
+    if codes.dtype != torch.uint8 or scales.dtype not in _KV_DTYPES or codes.dim() != 4 or scales.dim() != 4 or codes.shape[:3] != scales.shape[:3] or \
+            codes.shape[2] != 2 or not codes.is_contiguous() or not scales.is_contiguous() or not codes.is_cuda or scales.device != codes.device:
+        raise ValueError("codes and scales must be contiguous CUDA tensors, uint8 pages x heads x 2 x page_size * head_dim / 2 and float16 or bfloat16 pages x heads x 2 x page_size")
+    pages, heads, _, page_size = scales.shape
+    if page_size < 1 or codes.shape[3] * 2 % page_size:
+        raise ValueError("codes must hold a whole number of channels a token")
+    return ApmmKvCache(codes.data_ptr(), scales.data_ptr(), pages, page_size, heads, codes.shape[3] * 2 // page_size, _KV_DTYPES[scales.dtype])
+
+
+def _kv_batch(codes, page_table, lengths, starts, tokens):
+    for t, what, dim in ((page_table, "page_table", 2), (lengths, "lengths", 1), (starts, "starts", 1)):
+        if t is None and what == "starts":
+            continue
+        if t.dtype != torch.int32 or t.dim() != dim or t.device != codes.device or (t.shape[-1] > 1 and t.stride(-1) != 1):
+            raise ValueError("%s must be a %d-D int32 tensor on the cache's device, contiguous in its last dimension" % (what, dim))
+    n = lengths.shape[0]
+    if page_table.shape[0] != n or (starts is not None and starts.shape[0] != n + 1) or (starts is None and tokens != n):
+        raise ValueError("page_table needs a row, starts (if given) one element more than there are lengths; without starts each sequence has one token")
+    width = page_table.shape[1]
+    return ApmmKvBatch(n, tokens, lengths.data_ptr(), _ptr(starts), page_table.data_ptr(), page_table.stride(0) if n > 1 else width, width)
+
+
+def _kv_rows(t, codes, scales, heads, head_dim, tokens, what):
+    if t.dtype != scales.dtype or t.device != codes.device or t.dim() != 3 or t.shape[1] != heads or t.shape[2] != head_dim or t.shape[0] != tokens or t.stride(2) != 1:
+        raise ValueError("%s must be tokens x %d x %d of the scales' type on the cache's device, contiguous in its last dimension" % (what, heads, head_dim))
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def apmm_kv_write(k, v, codes, scales, page_table, lengths, starts=None):
+    """Quantise new keys and values (tokens x kv heads x head_dim) into the cache.
+
+    lengths (int32, one a sequence) counts the new tokens; starts (int32, sequences + 1) says which rows of k and v are whose, None: one a
+    sequence.  page_table: int32, sequences x pages.
+    """
+    cache = _kv_cache(codes, scales)
+    batch = _kv_batch(codes, page_table, lengths, starts, k.shape[0])
+    _check(load().apmm_kv_write(cache, batch, *_kv_rows(k, codes, scales, cache.kv_heads, cache.head_dim, batch.tokens, "k"),
+                                *_kv_rows(v, codes, scales, cache.kv_heads, cache.head_dim, batch.tokens, "v"), _stream()))
+
+
+def apmm_kv_read(codes, scales, page_table, lengths, tokens, starts=None, k_out=None, v_out=None):
+    """Keys and values of the last starts[b + 1] - starts[b] tokens (None: of the last one) of each sequence, `tokens` in all: (k, v)."""
+    cache = _kv_cache(codes, scales)
+    batch = _kv_batch(codes, page_table, lengths, starts, tokens)
+    if k_out is None:
+        k_out = torch.empty((tokens, cache.kv_heads, cache.head_dim), dtype=scales.dtype, device=codes.device)
+    if v_out is None:
+        v_out = torch.empty((tokens, cache.kv_heads, cache.head_dim), dtype=scales.dtype, device=codes.device)
+    _check(load().apmm_kv_read(cache, batch, *_kv_rows(k_out, codes, scales, cache.kv_heads, cache.head_dim, tokens, "k_out"),
+                               *_kv_rows(v_out, codes, scales, cache.kv_heads, cache.head_dim, tokens, "v_out"), _stream()))
+    return k_out, v_out
+
+
+def apmm_kv_attention(q, codes, scales, page_table, lengths, starts=None, window=0, sinks=0, scale=None, out=None, workspace=None):
+    """Causal attention of the new tokens' queries (tokens x query heads x head_dim) over the cache, which holds their keys and values already.
+
+    window > 0: only the last `window` keys up to the query's own and the first `sinks` of the sequence are seen.  scale: 1 / sqrt(head_dim) if None.
+    workspace: uint8 tensor of apmm_kv_attention_workspace_bytes(...) bytes; allocated if None.  A query that sees no key gets zeros.
+    """
+    cache = _kv_cache(codes, scales)
+    if q.dim() != 3 or q.shape[2] != cache.head_dim:
+        raise ValueError("q must be tokens x query heads x %d" % cache.head_dim)
+    tokens, heads, head_dim = q.shape
+    batch = _kv_batch(codes, page_table, lengths, starts, tokens)
+    if out is None:
+        out = torch.empty((tokens, heads, head_dim), dtype=q.dtype, device=q.device)
+    rows = _kv_rows(q, codes, scales, heads, head_dim, tokens, "q") + _kv_rows(out, codes, scales, heads, head_dim, tokens, "out")
+    lib = load()
+    if workspace is None:
+        need = lib.apmm_kv_attention_workspace_bytes(cache, batch, heads)
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    elif workspace.device != codes.device or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the cache's device")
+    _check(lib.apmm_kv_attention(cache, batch, heads, *rows, head_dim ** -0.5 if scale is None else scale, window, sinks,
+                                 _ptr(workspace), 0 if workspace is None else workspace.nbytes, _stream()))
+    return out
+
+
+def apmm_kv_attention_workspace_bytes(tokens, q_heads, codes, scales, page_table, lengths):
+    """Bytes of workspace that apmm_kv_attention needs for `tokens` queries."""
+    batch = _kv_batch(codes, page_table, lengths, None, lengths.shape[0])
+    batch.tokens = tokens
+    return int(load().apmm_kv_attention_workspace_bytes(_kv_cache(codes, scales), batch, q_heads))
 
 
 def apmm_last_gemm_kernel():

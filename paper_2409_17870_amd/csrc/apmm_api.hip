@@ -5,11 +5,16 @@
 #include <mutex>
 
 #include "../../include/apmm.h"
+#include "apmm_api.h"
 #include "apmm_kernels.h"
 
 namespace {
 
 thread_local char g_error[256] = "";
+
+}  // namespace
+
+namespace apmm {
 
 apmm_status fail(apmm_status st, const char *msg)
 {
@@ -22,6 +27,13 @@ apmm_status fail_hip(hipError_t e, const char *where)
     std::snprintf(g_error, sizeof(g_error), "%s: %s", where, hipGetErrorString(e));
     return APMM_ERR_HIP;
 }
+
+}  // namespace apmm
+
+namespace {
+
+using apmm::fail;
+using apmm::fail_hip;
 
 bool bits_ok(int bits) { return bits >= 1 && bits <= 8; }
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }

@@ -1,0 +1,169 @@
+// The four-bit key/value cache: its layout, the batch that a call works on, and the launchers of its kernels (the public ABI is include/apmm.h).
+//
+// codes:  [page][head][2][page tokens * head_dim / 2 bytes], keys then values
+//   keys    token by token, channel c in the low (even c) or high (odd c) four bits of byte c / 2: a lane of the matrix unit's operand K takes 8
+//           channels of one token, one word, and gets them as binary16 pairs (c, c + 4) with one AND each (kv_operand)
+//   values  by eights of tokens; of one, for each m the channels 4 m to 4 m + 3 of the eight tokens, 16 bits a token: a lane of the operand V^T takes
+//           8 tokens of one channel, and a word of two tokens gives the pairs of four channels the same way
+// scales: [page][head][2][page tokens] of the type of the tensors
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+namespace apmm {
+
+constexpr int kKvMost = 1 << 30;  // tokens, positions, window
+
+struct KvArgs {
+    uint8_t *codes;
+    uint16_t *scales;
+    const int32_t *table;    // sequences x table_stride, the first `width` of a row are pages
+    const int32_t *lengths;  // tokens of each sequence
+    const int32_t *starts;   // sequences + 1, or null: one new token a sequence
+    int64_t pages, table_stride;
+    int sequences, tokens, width, heads, page_shift, head_dim;
+    bool bf16;
+};
+
+struct KvTensor {  // rows of head_dim contiguous elements
+    uint16_t *data;
+    int64_t token_stride, head_stride;  // elements
+    bool aligned;                       // every row starts at a multiple of 16 bytes
+};
+
+struct KvAttentionArgs {
+    KvArgs c;
+    KvTensor q, out;
+    int groups;        // query heads to a key/value head
+    int window, sinks; // window 0: none
+    float scale;
+    float *partial;    // results of pieces of sequences: see KvPlan
+};
+
+// How the work of an attention call is cut, the same on host and device.  Rows are the queries of the heads that share a key/value head, `tile` of them to a
+// workgroup; the keys that a tile sees are cut in pieces so that there are about `target` workgroups whatever the lengths are, which the host does not know.
+struct KvPlan {
+    int tile;     // rows of a workgroup
+    int target;   // pieces wanted for each key/value head over all sequences; 0: none is cut
+    int slots;    // most pieces there can be
+};
+KvPlan kv_plan(int sequences, int64_t tokens, int heads, int groups, int head_dim);
+size_t kv_partial_bytes(const KvPlan &plan, int heads, int head_dim);
+
+hipError_t launch_kv_write(const KvArgs &c, const KvTensor &k, const KvTensor &v, hipStream_t stream);
+hipError_t launch_kv_read(const KvArgs &c, const KvTensor &k, const KvTensor &v, hipStream_t stream);
+hipError_t launch_kv_attention(const KvAttentionArgs &a, const KvPlan &plan, hipStream_t stream);
+
+#ifdef __HIPCC__
+constexpr int kKvStep = 32;  // keys of one step of attention
+
+// Place of lane `lane` within its wave of a workgroup of whole waves
+__device__ __forceinline__ int kv_lane() { return threadIdx.x & 63; }
+
+// A sequence of the batch.  Whatever lies in lengths and starts, rows start .. start + n - 1 are rows of the tensors and keys below `keys` have a place in the table.
+struct KvSequence {
+    int start, n;  // new tokens
+    int first;     // position of the first new token; may be negative
+    int keys;
+};
+__device__ __forceinline__ KvSequence kv_sequence(const KvArgs &c, int b)
+{
+    KvSequence s;
+    int end;
+    if (c.starts) {
+        s.start = min(max(c.starts[b], 0), c.tokens);
+        end = min(max(c.starts[b + 1], s.start), c.tokens);
+    } else {
+        s.start = b;
+        end = b + 1;
+    }
+    s.n = end - s.start;
+    const int length = min(max(c.lengths[b], 0), kKvMost);
+    s.first = length - s.n;
+    s.keys = (int)min((int64_t)length, (int64_t)c.width << c.page_shift);
+    return s;
+}
+
+// Sum over the lanes up to this one
+__device__ __forceinline__ int kv_scan(int v)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int o = __shfl_up(v, d);
+        v += kv_lane() >= d ? o : 0;
+    }
+    return v;
+}
+
+// The sequence that has unit `unit` where sequence b has count(b) of them, and the unit's number within it; false: there are fewer.  All lanes take part, all get the same.
+template <class Count>
+__device__ __forceinline__ bool kv_find(int sequences, int unit, int &b, int &rest, Count count)
+{
+    int before = 0;
+    for (int base = 0; base < sequences; base += 64) {
+        const int at = base + kv_lane();
+        const int n = at < sequences ? count(at) : 0;
+        const int to = before + kv_scan(n);
+        const uint64_t past = __ballot(to > unit);
+        if (past) {
+            const int l = __ffsll((long long)past) - 1;
+            b = __builtin_amdgcn_readfirstlane(base + l);
+            rest = __builtin_amdgcn_readfirstlane(unit - (__shfl(to, l) - __shfl(n, l)));
+            return true;
+        }
+        before = __builtin_amdgcn_readfirstlane(__shfl(to, 63));
+    }
+    return false;
+}
+
+__device__ __forceinline__ float kv_scale_value(uint32_t bits, bool bf16)
+{
+    if (bf16) return __uint_as_float(bits << 16);
+    return (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
+}
+
+__device__ __forceinline__ uint16_t kv_round(float x, bool bf16)
+{
+    if (bf16) return __builtin_bit_cast(uint16_t, (__bf16)x);
+    return __builtin_bit_cast(uint16_t, (_Float16)x);
+}
+
+// Words of a row's 16-bit elements, two at a time; rows that are not aligned element by element
+template <int N>
+__device__ __forceinline__ void kv_load(const uint16_t *src, bool aligned, uint32_t (&w)[N])
+{
+    if (aligned) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            const uint4 x = *reinterpret_cast<const uint4 *>(src + 2 * i);
+            w[i] = x.x; w[i + 1] = x.y; w[i + 2] = x.z; w[i + 3] = x.w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = src[2 * i] | (uint32_t)src[2 * i + 1] << 16;
+    }
+}
+template <int N>
+__device__ __forceinline__ void kv_store(uint16_t *dst, bool aligned, const uint32_t (&w)[N])
+{
+    if (aligned) {
+        if constexpr (N % 4 == 0) {
+#pragma unroll
+            for (int i = 0; i < N; i += 4) *reinterpret_cast<uint4 *>(dst + 2 * i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+        } else {
+            static_assert(N % 2 == 0, "pairs of words");
+#pragma unroll
+            for (int i = 0; i < N; i += 2) *reinterpret_cast<uint2 *>(dst + 2 * i) = make_uint2(w[i], w[i + 1]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            dst[2 * i] = (uint16_t)w[i];
+            dst[2 * i + 1] = (uint16_t)(w[i] >> 16);
+        }
+    }
+}
+#endif
+
+}  // namespace apmm

@@ -1,0 +1,210 @@
+// Attention over the four-bit key/value cache (layout: apmm_kv.h): what its kernels share.
+//
+// For a query q of a row and keys j that it sees, with key codes u, value codes w, scales a, b of a token and c = scale log2(e):
+//   x_j = c a_j sum_d q_d (2 u_jd - 15)        p_j = 2^(x_j - m)        o_d = sum_j p_j b_j (2 w_jd - 15) / sum_j p_j
+// Both sums over products are matrix instructions on binary16 operands with 32-bit accumulators.
+//
+//   Codes as operands   A code in the low mantissa bits of a binary16 number is the subnormal u 2^-24 (bits 0 to 3) or u 2^-20 (bits 4 to 7), which the matrix unit takes exactly:
+//                       five operations make four operand words of one word of eight codes.  The -15 is added outside: -15 sum_d q_d is where the accumulators of the first product start
+//                       from, and 15 times the sum of the weights is taken off the second one's result.
+//   Queries             times a power of two for each row, so that its largest number is just below 2^11 (2^15 for the channels that meet u 2^-24): binary16 numbers as they are, bfloat16
+//                       ones exactly as far as 2^-35 of the row's largest.
+//   Weights             p_j b_j, rounded once to binary16 (bfloat16 would cost an output of binary16 numbers eight times its own rounding).  The value scales may lie anywhere, so a
+//                       wave holds a power of two 2^E above all that it has met, and weights carry the factor 2^(9 - E) until the end: at most 2^15, and 2^-21 of the largest without loss.
+//                       The sum of the rounded weights goes with them (dot products with ones).
+//   Running maximum     m (and E) are only moved where a score passes m + 6: until then weights are at most 2^6 times larger, for which there is room.  Then the accumulators are scaled;
+//                       -m + 9 - E is one number, `base`.
+//   Products transposed S^T = K Q^T and O^T = V^T P^T: the rows of S^T in a lane's accumulators are eight (or sixteen) keys that follow each other, if key rows are dealt to the operand's
+//                       rows in that order, and those are the lane's part of the operand P^T of the second product.  No weight passes through LDS.
+// A row that sees no key has the weight sum 0 and gets zeros.
+#pragma once
+
+#include "apmm_kv.h"
+
+namespace apmm {
+
+constexpr int kRowsTile = 16;    // rows of a workgroup of kv_attention_rows_kernel
+constexpr int kTilesTile = 128;  // and of kv_attention_tiles_kernel
+
+#ifdef __HIPCC__
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef float float2v __attribute__((ext_vector_type(2)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef float float16v __attribute__((ext_vector_type(16)));
+
+constexpr float kLowest = -3.402823466e38f;
+constexpr float kSlack = 6.0f, kRoom = 9.0f;
+
+// A workgroup's part of the call: keys of steps `from` to `to` - 1 (of kKvStep keys, the hidden ones between the first tokens and the window left out) for rows of one sequence
+struct KvItem {
+    KvSequence s;
+    int b, row0, rows;   // first row, rows that there are from there on (may be more than a tile)
+    int from, to;
+    int sink_steps, gap; // step v lies at v < sink_steps ? v : v + gap
+    int pieces, slot;
+    __device__ __forceinline__ int key_of(int v) const { return (v < sink_steps ? v : v + gap) * kKvStep; }
+};
+
+// Steps of one tile whose queries lie at positions first_pos to last_pos
+struct KvSteps {
+    int sink_steps, gap, count;
+};
+__device__ __forceinline__ KvSteps kv_steps(const KvAttentionArgs &a, const KvSequence &s, int first_pos, int last_pos)
+{
+    KvSteps r;
+    const int end = min(last_pos + 1, s.keys), steps = end > 0 ? (end + kKvStep - 1) / kKvStep : 0;
+    const int low = min(a.window ? max(first_pos - a.window + 1, 0) / kKvStep : 0, steps);
+    r.sink_steps = min((int)(((int64_t)a.sinks + kKvStep - 1) / kKvStep), low);
+    r.gap = low - r.sink_steps;
+    r.count = steps - r.gap;
+    return r;
+}
+
+// Tiles of a sequence, and steps of the one with most (or a few more)
+__device__ __forceinline__ void kv_extent(const KvAttentionArgs &a, const KvSequence &s, int tile, int &tiles, int &steps)
+{
+    tiles = (int)(((int64_t)s.n * a.groups + tile - 1) / tile);
+    steps = (s.keys + kKvStep - 1) / kKvStep;
+    if (a.window) {
+        const int64_t span = (int64_t)a.window + (tile + a.groups - 2) / a.groups;  // positions that the queries of a tile see, without the first tokens
+        steps = (int)min((int64_t)steps, (span + kKvStep - 1) / kKvStep + 1 + ((int64_t)a.sinks + kKvStep - 1) / kKvStep);
+    }
+    if (!tiles) steps = 0;
+}
+
+// Steps of a piece, from the work of all sequences
+__device__ __forceinline__ int kv_piece(const KvAttentionArgs &a, const KvPlan &plan, int least)
+{
+    if (!plan.target) return 0x7fffffff;
+    int64_t work = 0;
+    for (int base = 0; base < a.c.sequences; base += 64) {
+        const int at = base + kv_lane();
+        if (at < a.c.sequences) {
+            int tiles, steps;
+            kv_extent(a, kv_sequence(a.c, at), plan.tile, tiles, steps);
+            work += (int64_t)tiles * steps;
+        }
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) work += __shfl_xor(work, d);
+    const int64_t piece = (work + plan.target - 1) / plan.target;
+    return __builtin_amdgcn_readfirstlane((int)min(max(piece, (int64_t)least), (int64_t)0x7fffffff));
+}
+
+__device__ __forceinline__ int kv_pieces(int steps, int piece) { return steps > piece ? (steps + piece - 1) / piece : 1; }
+
+// false: there is no piece `slot`
+__device__ __forceinline__ bool kv_item(const KvAttentionArgs &a, const KvPlan &plan, int piece, int slot, KvItem &it)
+{
+    int rest, tiles, steps;
+    auto count = [&](int at) {
+        int t, s;
+        kv_extent(a, kv_sequence(a.c, at), plan.tile, t, s);
+        return t * kv_pieces(s, piece);
+    };
+    if (!kv_find(a.c.sequences, slot, it.b, rest, count)) return false;
+    it.s = kv_sequence(a.c, it.b);
+    kv_extent(a, it.s, plan.tile, tiles, steps);
+    it.slot = slot;
+    it.pieces = kv_pieces(steps, piece);
+    const int tile = tiles - 1 - rest / it.pieces, part = rest % it.pieces;  // (the last queries see the most keys: those first)
+    it.row0 = tile * plan.tile;
+    it.rows = it.s.n * a.groups - it.row0;
+    const int last = min(it.rows, plan.tile) - 1;
+    const KvSteps r = kv_steps(a, it.s, it.s.first + it.row0 / a.groups, it.s.first + (it.row0 + last) / a.groups);
+    it.sink_steps = r.sink_steps;
+    it.gap = r.gap;
+    it.from = min(part * (int64_t)piece, (int64_t)r.count);
+    it.to = min((part + 1) * (int64_t)piece, (int64_t)r.count);
+    return true;
+}
+
+// Four words of a matrix operand from one word of codes: nibbles 0 and 4, 1 and 5, 2 and 6, 3 and 7, those of even number as u 2^-24, of odd number as u 2^-20
+__device__ __forceinline__ half8 kv_operand(uint32_t w)
+{
+    const uint32_t h = w >> 8;
+    uint4 r;
+    r.x = w & 0x000f000fu;
+    r.y = w & 0x00f000f0u;
+    r.z = h & 0x000f000fu;
+    r.w = h & 0x00f000f0u;
+    return __builtin_bit_cast(half8, r);
+}
+
+__device__ __forceinline__ uint32_t kv_half_pair(float a, float b)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((float2v{a, b}), half2v));
+}
+
+template <bool BF16>
+__device__ __forceinline__ float kv_low(uint32_t w) { return BF16 ? __uint_as_float(w << 16) : (float)__builtin_bit_cast(half2v, w)[0]; }
+template <bool BF16>
+__device__ __forceinline__ float kv_high(uint32_t w) { return BF16 ? __uint_as_float(w & 0xffff0000u) : (float)__builtin_bit_cast(half2v, w)[1]; }
+
+// The queries of a lane as operand words: x holds 8 channels to 4 words in their order.  `across` folds a value over the lanes that share the row.
+template <int N, bool BF16, class Max, class Sum>
+__device__ __forceinline__ void kv_queries(const uint32_t (&x)[N], float scale, Max max_across, Sum sum_across, half8 (&q)[N / 4], float &init, float &factor)
+{
+    float top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float a = fabsf(kv_low<BF16>(x[i])), b = fabsf(kv_high<BF16>(x[i]));
+        top = fmaxf(top, a <= -kLowest ? a : 0.0f);
+        top = fmaxf(top, b <= -kLowest ? b : 0.0f);
+    }
+    top = max_across(top);
+    int e = top > 0.0f ? 11 - (int)((__float_as_uint(top) >> 23) - 126u) : 0;  // top 2^e < 2^11
+    e = min(e, 100);                                                         // (a row of subnormal numbers)
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+        float f[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            f[2 * j] = ldexpf(kv_low<BF16>(x[4 * i + j]), e);
+            f[2 * j + 1] = ldexpf(kv_high<BF16>(x[4 * i + j]), e);
+        }
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float by = j & 1 ? 1.0f : 16.0f, back = j & 1 ? 1.0f : 0.0625f;
+            w[j] = kv_half_pair(f[j] * by, f[j + 4] * by);
+            sum += (kv_low<false>(w[j]) + kv_high<false>(w[j])) * back;
+        }
+        q[i] = __builtin_bit_cast(half8, make_uint4(w[0], w[1], w[2], w[3]));
+    }
+    init = -7.5f * 0x1p-20f * sum_across(sum);
+    factor = ldexpf(scale * 1.44269504088896341f, min(21 - e, 122));  // (queries of 2^115 and more: scores beyond any other's all the same)
+}
+
+// Page of half a step (16 keys); lane i of `ids` has that of half step i of the next 32 steps of a wave
+__device__ __forceinline__ int kv_page_ids(const KvAttentionArgs &a, const KvItem &it, int v, int stride)
+{
+    const int step = v + (kv_lane() >> 1) * stride;
+    if (step >= it.to) return -1;
+    const int key = it.key_of(step) + 16 * (kv_lane() & 1);
+    if (key >= it.s.keys) return -1;
+    const int page = a.c.table[it.b * a.c.table_stride + (key >> a.c.page_shift)];
+    return page < a.c.pages ? page : -1;
+}
+
+// Largest finite scale of two to a word
+__device__ __forceinline__ uint32_t kv_fold_max(uint32_t m, uint32_t w)
+{
+    typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(us2, m), __builtin_bit_cast(us2, w)));
+}
+template <bool BF16>
+__device__ __forceinline__ uint32_t kv_finite_max(uint32_t m, uint32_t bits)
+{
+    return bits < (BF16 ? 0x7f80u : 0x7c00u) ? max(m, bits) : m;
+}
+// E of a largest scale: s < 2^E.  Held above -80, so that sums of 2^(9 - E) stay in range (scales below 2^-103 lose bits).
+template <bool BF16>
+__device__ __forceinline__ int kv_exponent(uint32_t bits) { return BF16 ? max((int)(bits >> 7) - 126, -80) : (int)(bits >> 10) - 14; }
+template <bool BF16>
+__device__ __forceinline__ uint32_t kv_limit(uint32_t bits) { return bits | (BF16 ? 0x7fu : 0x3ffu); }
+#endif
+
+}  // namespace apmm
