@@ -77,13 +77,13 @@ apmm_status check_pair(const apmm_kv_cache *cache, const apmm_kv_batch *batch, c
     return APMM_OK;
 }
 
-apmm_status check_heads(const apmm_kv_cache *cache, const apmm_kv_batch *batch, int q_heads, apmm::KvPlan &plan)
+apmm_status check_heads(const apmm_kv_cache *cache, const apmm_kv_batch *batch, const apmm::KvArgs &a, int q_heads, apmm::KvPlan &plan)
 {
     if (q_heads < 1 || q_heads % cache->kv_heads) return fail(APMM_ERR_INVALID_ARG, "kv_attention: q_heads must be a multiple of kv_heads");
     const int groups = q_heads / cache->kv_heads;
     if (groups > 1024 || (batch->tokens + batch->sequences) * q_heads > INT32_MAX / 4)
         return fail(APMM_ERR_UNSUPPORTED, "kv_attention: more than 1024 query heads to a key/value head, or tokens * q_heads is more than one launch takes");
-    plan = apmm::kv_plan(batch->sequences, batch->tokens, cache->kv_heads, groups, cache->head_dim);
+    plan = apmm::kv_plan(a, groups);
     return APMM_OK;
 }
 
@@ -119,7 +119,7 @@ size_t apmm_kv_attention_workspace_bytes(const apmm_kv_cache *cache, const apmm_
 {
     apmm::KvArgs a;
     apmm::KvPlan plan;
-    if (check_sizes(cache, batch, a) != APMM_OK || batch->sequences == 0 || batch->tokens == 0 || check_heads(cache, batch, q_heads, plan) != APMM_OK) return 0;
+    if (check_sizes(cache, batch, a) != APMM_OK || batch->sequences == 0 || batch->tokens == 0 || check_heads(cache, batch, a, q_heads, plan) != APMM_OK) return 0;
     return apmm::kv_partial_bytes(plan, cache->kv_heads, cache->head_dim);
 }
 
@@ -132,7 +132,7 @@ apmm_status apmm_kv_attention(const apmm_kv_cache *cache, const apmm_kv_batch *b
     bool empty;
     apmm_status st = check_batch(cache, batch, a.c, empty);
     if (st != APMM_OK) return st;
-    if ((st = check_heads(cache, batch, q_heads, plan)) != APMM_OK) return st;
+    if ((st = check_heads(cache, batch, a.c, q_heads, plan)) != APMM_OK) return st;
     if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(APMM_ERR_INVALID_ARG, "kv_attention: scale must be positive and finite");
     if (window < 0 || sinks < 0) return fail(APMM_ERR_INVALID_ARG, "kv_attention: window < 0 or sinks < 0");
     if (window > apmm::kKvMost || sinks > apmm::kKvMost) return fail(APMM_ERR_UNSUPPORTED, "kv_attention: window or sinks > 2^30");

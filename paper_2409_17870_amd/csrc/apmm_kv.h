@@ -41,14 +41,17 @@ struct KvAttentionArgs {
     float *partial;    // results of pieces of sequences: see KvPlan
 };
 
-// How the work of an attention call is cut, the same on host and device.  Rows are the queries of the heads that share a key/value head, `tile` of them to a
-// workgroup; the keys that a tile sees are cut in pieces so that there are about `target` workgroups whatever the lengths are, which the host does not know.
+// How the work of an attention call is cut.  Rows are the queries of the heads that share a key/value head, `tile` of them to a workgroup; the keys that a tile sees are cut in
+// pieces of at least `least` steps so that there are about `target` workgroups for each key/value head whatever the lengths are, which the host does not know.
 struct KvPlan {
-    int tile;     // rows of a workgroup
-    int target;   // pieces wanted for each key/value head over all sequences; 0: none is cut
-    int slots;    // most pieces there can be
+    int tile;    // rows of a workgroup
+    int waves;   // of a workgroup
+    int target;  // 0: nothing is cut
+    int least;
+    int slots;   // most pieces there can be
 };
-KvPlan kv_plan(int sequences, int64_t tokens, int heads, int groups, int head_dim);
+KvPlan kv_plan(const KvArgs &c, int groups);
+// Workspace of a call that cuts: for every piece and head the sums of `tile` rows, base and total of each row, and a KvPieceNote
 size_t kv_partial_bytes(const KvPlan &plan, int heads, int head_dim);
 
 hipError_t launch_kv_write(const KvArgs &c, const KvTensor &k, const KvTensor &v, hipStream_t stream);
@@ -85,14 +88,15 @@ __device__ __forceinline__ KvSequence kv_sequence(const KvArgs &c, int b)
     return s;
 }
 
-// Sum over the lanes up to this one
+// Sum over the lanes up to this one, by moves within the vector unit
 __device__ __forceinline__ int kv_scan(int v)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int o = __shfl_up(v, d);
-        v += kv_lane() >= d ? o : 0;
-    }
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);   // one to four lanes up within sixteen
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // the last of sixteen to the next sixteen, of 32 to the next 32
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
     return v;
 }
 
@@ -108,11 +112,11 @@ __device__ __forceinline__ bool kv_find(int sequences, int unit, int &b, int &re
         const uint64_t past = __ballot(to > unit);
         if (past) {
             const int l = __ffsll((long long)past) - 1;
-            b = __builtin_amdgcn_readfirstlane(base + l);
-            rest = __builtin_amdgcn_readfirstlane(unit - (__shfl(to, l) - __shfl(n, l)));
+            b = base + l;
+            rest = unit - (__builtin_amdgcn_readlane(to, l) - __builtin_amdgcn_readlane(n, l));
             return true;
         }
-        before = __builtin_amdgcn_readfirstlane(__shfl(to, 63));
+        before = __builtin_amdgcn_readlane(to, 63);
     }
     return false;
 }

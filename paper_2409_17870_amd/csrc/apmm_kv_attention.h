@@ -26,6 +26,9 @@ namespace apmm {
 constexpr int kRowsTile = 16;    // rows of a workgroup of kv_attention_rows_kernel
 constexpr int kTilesTile = 128;  // and of kv_attention_tiles_kernel
 
+hipError_t launch_kv_attention_rows(const KvAttentionArgs &a, const KvPlan &plan, hipStream_t stream);
+hipError_t launch_kv_attention_tiles(const KvAttentionArgs &a, const KvPlan &plan, hipStream_t stream);
+
 #ifdef __HIPCC__
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
@@ -42,7 +45,7 @@ struct KvItem {
     int b, row0, rows;   // first row, rows that there are from there on (may be more than a tile)
     int from, to;
     int sink_steps, gap; // step v lies at v < sink_steps ? v : v + gap
-    int pieces, slot;
+    int pieces, part, slot;
     __device__ __forceinline__ int key_of(int v) const { return (v < sink_steps ? v : v + gap) * kKvStep; }
 };
 
@@ -73,42 +76,56 @@ __device__ __forceinline__ void kv_extent(const KvAttentionArgs &a, const KvSequ
     if (!tiles) steps = 0;
 }
 
-// Steps of a piece, from the work of all sequences
-__device__ __forceinline__ int kv_piece(const KvAttentionArgs &a, const KvPlan &plan, int least)
-{
-    if (!plan.target) return 0x7fffffff;
-    int64_t work = 0;
-    for (int base = 0; base < a.c.sequences; base += 64) {
-        const int at = base + kv_lane();
-        if (at < a.c.sequences) {
-            int tiles, steps;
-            kv_extent(a, kv_sequence(a.c, at), plan.tile, tiles, steps);
-            work += (int64_t)tiles * steps;
-        }
-    }
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) work += __shfl_xor(work, d);
-    const int64_t piece = (work + plan.target - 1) / plan.target;
-    return __builtin_amdgcn_readfirstlane((int)min(max(piece, (int64_t)least), (int64_t)0x7fffffff));
-}
-
 __device__ __forceinline__ int kv_pieces(int steps, int piece) { return steps > piece ? (steps + piece - 1) / piece : 1; }
 
-// false: there is no piece `slot`
-__device__ __forceinline__ bool kv_item(const KvAttentionArgs &a, const KvPlan &plan, int piece, int slot, KvItem &it)
+// Piece `slot` of the call; false: there is none
+__device__ __forceinline__ bool kv_item(const KvAttentionArgs &a, const KvPlan &plan, int slot, KvItem &it)
 {
-    int rest, tiles, steps;
-    auto count = [&](int at) {
-        int t, s;
-        kv_extent(a, kv_sequence(a.c, at), plan.tile, t, s);
-        return t * kv_pieces(s, piece);
-    };
-    if (!kv_find(a.c.sequences, slot, it.b, rest, count)) return false;
-    it.s = kv_sequence(a.c, it.b);
+    const int lane = kv_lane();
+    int piece = 0x7fffffff, tiles, steps;
+    KvSequence s = {};
+    if (lane < a.c.sequences) s = kv_sequence(a.c, lane);  // the first 64 stay in registers
+    kv_extent(a, s, plan.tile, tiles, steps);
+    if (plan.target) {
+        float work = (float)tiles * (float)steps;
+        for (int at = lane + 64; at < a.c.sequences; at += 64) {
+            int t, n;
+            kv_extent(a, kv_sequence(a.c, at), plan.tile, t, n);
+            work += (float)t * (float)n;
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) work += __shfl_xor(work, d);
+        // (rounding: a piece may be 2^-20 shorter than the work asks for, for which there is one slot more)
+        piece = __builtin_amdgcn_readfirstlane(max((int)ceilf(fminf(work / (float)plan.target * (1.0f - 0x1p-20f), 0x1p30f)), plan.least));
+    }
+    int rest, l;
+    const int own = tiles * kv_pieces(steps, piece), to = kv_scan(own);
+    const uint64_t past = __ballot(to > slot);
+    if (past) {
+        l = __ffsll((long long)past) - 1;
+        it.b = l;
+        rest = slot - (__builtin_amdgcn_readlane(to, l) - __builtin_amdgcn_readlane(own, l));
+        it.s.start = __builtin_amdgcn_readlane(s.start, l);
+        it.s.n = __builtin_amdgcn_readlane(s.n, l);
+        it.s.first = __builtin_amdgcn_readlane(s.first, l);
+        it.s.keys = __builtin_amdgcn_readlane(s.keys, l);
+    } else {
+        const int before = __builtin_amdgcn_readlane(to, 63);
+        auto count = [&](int at) {
+            int t, n;
+            if (at + 64 >= a.c.sequences) return 0;
+            kv_extent(a, kv_sequence(a.c, at + 64), plan.tile, t, n);
+            return t * kv_pieces(n, piece);
+        };
+        if (a.c.sequences <= 64 || !kv_find(a.c.sequences - 64, slot - before, it.b, rest, count)) return false;
+        it.b += 64;
+        it.s = kv_sequence(a.c, it.b);
+    }
     kv_extent(a, it.s, plan.tile, tiles, steps);
     it.slot = slot;
     it.pieces = kv_pieces(steps, piece);
     const int tile = tiles - 1 - rest / it.pieces, part = rest % it.pieces;  // (the last queries see the most keys: those first)
+    it.part = part;
     it.row0 = tile * plan.tile;
     it.rows = it.s.n * a.groups - it.row0;
     const int last = min(it.rows, plan.tile) - 1;
@@ -118,6 +135,32 @@ __device__ __forceinline__ bool kv_item(const KvAttentionArgs &a, const KvPlan &
     it.from = min(part * (int64_t)piece, (int64_t)r.count);
     it.to = min((part + 1) * (int64_t)piece, (int64_t)r.count);
     return true;
+}
+
+// For the joining of pieces: what lies at a slot and head
+struct KvPieceNote {
+    int start, row0, rows, pieces;  // pieces: of the tile, 0 where this is not the first of several
+};
+struct KvPartial {
+    float *sums;        // [slot][head][tile row][channel]
+    float2 *row;        // [slot][head][tile row]: base and total; the row is sum_i 2^base_i sums_i / sum_i 2^base_i total_i over its pieces
+    KvPieceNote *note;  // [slot][head]
+};
+__host__ __device__ inline KvPartial kv_partial(float *at, const KvPlan &plan, int heads, int head_dim)
+{
+    const int64_t rows = (int64_t)plan.slots * heads * plan.tile;
+    KvPartial p;
+    p.sums = at;
+    p.row = reinterpret_cast<float2 *>(at + rows * head_dim);
+    p.note = reinterpret_cast<KvPieceNote *>(p.row + rows);
+    return p;
+}
+__device__ __forceinline__ void kv_note(const KvAttentionArgs &a, const KvPlan &plan, int slot, int head, bool there, const KvItem &it)
+{
+    if (!plan.target || threadIdx.x) return;
+    KvPieceNote n = {};
+    if (there && it.part == 0 && it.pieces > 1) n = {it.s.start, it.row0, min(it.rows, plan.tile), it.pieces};
+    kv_partial(a.partial, plan, a.c.heads, a.c.head_dim).note[(int64_t)slot * a.c.heads + head] = n;
 }
 
 // Four words of a matrix operand from one word of codes: nibbles 0 and 4, 1 and 5, 2 and 6, 3 and 7, those of even number as u 2^-24, of odd number as u 2^-20

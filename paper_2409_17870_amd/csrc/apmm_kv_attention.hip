@@ -1,132 +1,112 @@
-// How an attention call over the four-bit cache is cut and launched, and the kernel that joins the pieces of rows whose keys were cut.
+// How an attention call over the four-bit cache is cut and launched, and the kernel that joins the pieces of tiles whose keys were cut.
 #include <algorithm>
 
 #include "apmm_kv_attention.h"
 
 namespace apmm {
 
-hipError_t launch_kv_attention_rows(const KvAttentionArgs &a, const KvPlan &plan, int least, hipStream_t stream);
-hipError_t launch_kv_attention_tiles(const KvAttentionArgs &a, const KvPlan &plan, int least, hipStream_t stream);
-
 namespace {
 
-constexpr int kWaves = 4;
-
-// One wave for each row that was cut.  The pieces' sums o_i and totals s_i stand for 2^base_i o_i and 2^base_i s_i: the row is sum 2^(base_i - M) o_i / sum 2^(base_i - M) s_i.
+// A workgroup looks at one piece and head (blockIdx.x) and 16 rows of its tile (blockIdx.y), and has work where the piece is the first of several.  16 lanes to a row; what is left of
+// the 256 for fewer rows shares out the pieces, each with its own running base, and meets in LDS.
 template <int D, bool BF16>
-__global__ __launch_bounds__(64 * kWaves) void kv_attention_join_kernel(KvAttentionArgs a, KvPlan plan, int least)
+__global__ __launch_bounds__(256) void kv_attention_join_kernel(KvAttentionArgs a, KvPlan plan)
 {
-    constexpr int C = D / 64;  // channels of a lane
-    const int lane = kv_lane(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int query_heads = a.c.heads * a.groups;
-    const int64_t unit = (int64_t)blockIdx.x * kWaves + wave;
-    const int token = (int)(unit / query_heads), query_head = (int)(unit % query_heads), head = query_head / a.groups;
-    if (token >= a.c.tokens) return;
-    const int piece = kv_piece(a, plan, least);
-    // the token's sequence and the slots before it
-    KvSequence s;
-    int b = -1, before = 0;
-    for (int from = 0; from < a.c.sequences && b < 0; from += 64) {
-        const int at = from + lane;
-        int count = 0, start = 0, n = 0;
-        if (at < a.c.sequences) {
-            int tiles, steps;
-            s = kv_sequence(a.c, at);
-            kv_extent(a, s, plan.tile, tiles, steps);
-            count = tiles * kv_pieces(steps, piece);
-            start = s.start;
-            n = s.n;
-        }
-        const int to = kv_scan(count);
-        const uint64_t here = __ballot(token >= start && token < start + n);
-        if (here) {
-            const int l = __ffsll((long long)here) - 1;
-            b = __builtin_amdgcn_readfirstlane(from + l);
-            before += __builtin_amdgcn_readfirstlane(__shfl(to, l) - __shfl(count, l));
-        } else {
-            before += __builtin_amdgcn_readfirstlane(__shfl(to, 63));
+    constexpr int C = D / 16;  // channels of a lane
+    __shared__ float bases[16][16], totals[16][16];  // by threadIdx.x / 16: share of the pieces, row
+    __shared__ __align__(16) float sums[256][C];
+    const KvPartial partial = kv_partial(a.partial, plan, a.c.heads, D);
+    const KvPieceNote note = partial.note[blockIdx.x];
+    const int first_row = blockIdx.y * 16, rows = min(note.rows - first_row, 16);
+    if (note.pieces == 0 || rows <= 0) return;
+    const int row_slots = rows > 8 ? 16 : rows > 4 ? 8 : rows > 2 ? 4 : rows, shares = 16 / row_slots;
+    const int group = threadIdx.x >> 4, row = group % row_slots, share = group / row_slots, c0 = (threadIdx.x & 15) * C;
+    const int head = blockIdx.x % a.c.heads;
+    float base = kLowest, total = 0.0f, o[C] = {};
+    if (row < rows) {
+        const int64_t place = (int64_t)blockIdx.x * plan.tile + first_row + row, step = (int64_t)a.c.heads * plan.tile;
+#pragma unroll 4
+        for (int i = share; i < note.pieces; i += shares) {
+            const int64_t at = place + i * step;
+            const float2 r = partial.row[at];
+            float x[C];
+#pragma unroll
+            for (int j = 0; j < C; j += 4) {
+                const float4v v = *reinterpret_cast<const float4v *>(partial.sums + at * D + c0 + j);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[j + k] = v[k];
+            }
+            const float top = fmaxf(base, r.x), old = __builtin_amdgcn_exp2f(base - top), by = __builtin_amdgcn_exp2f(r.x - top);
+            base = top;
+            total = fmaf(total, old, r.y * by);
+#pragma unroll
+            for (int j = 0; j < C; ++j) o[j] = fmaf(o[j], old, x[j] * by);
         }
     }
-    if (b < 0) return;
-    int tiles, steps;
-    s = kv_sequence(a.c, b);
-    kv_extent(a, s, plan.tile, tiles, steps);
-    const int pieces = kv_pieces(steps, piece);
-    if (pieces == 1) return;
-    const int row = (token - s.start) * a.groups + query_head % a.groups, tile = row / plan.tile;
-    const int64_t slot = before + (int64_t)(tiles - 1 - tile) * pieces;
-    if (slot < 0 || slot + pieces > plan.slots) return;  // (starts that are not ascending from 0 to tokens)
-    const int64_t place = (slot * a.c.heads + head) * plan.tile + row % plan.tile, step = (int64_t)a.c.heads * plan.tile;
-    const float *meta = a.partial + (int64_t)plan.slots * a.c.heads * plan.tile * D, *sums = a.partial + lane * C;
-    float most = kLowest, total = 0.0f, o[C] = {};
-    for (int from = 0; from < pieces; from += 64) {
-        const int here = min(pieces - from, 64);
-        float base = kLowest, t = 0.0f;
-        if (lane < here) {
-            const float2 m = *reinterpret_cast<const float2 *>(meta + (place + (from + lane) * step) * 2);
-            base = m.x;
-            t = m.y;
-        }
-        float top = base;
+    bases[group][0] = base;
+    totals[group][0] = total;
 #pragma unroll
-        for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-        top = fmaxf(top, most);
-        const float old = __builtin_amdgcn_exp2f(most - top), by = __builtin_amdgcn_exp2f(base - top);
-        most = top;
-        float part = t * by;
+    for (int j = 0; j < C; ++j) sums[threadIdx.x][j] = o[j];
+    __syncthreads();
+    if (share || row >= rows) return;
+    for (int i = 1; i < shares; ++i) {
+        const int other = group + i * row_slots;
+        const float b = bases[other][0], top = fmaxf(base, b), old = __builtin_amdgcn_exp2f(base - top), by = __builtin_amdgcn_exp2f(b - top);
+        base = top;
+        total = fmaf(total, old, totals[other][0] * by);
 #pragma unroll
-        for (int d = 1; d < 64; d *= 2) part += __shfl_xor(part, d);
-        total = fmaf(total, old, part);
-#pragma unroll
-        for (int j = 0; j < C; ++j) o[j] *= old;
-#pragma unroll 4
-        for (int i = 0; i < here; ++i) {
-            const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(by), i));
-            const float *from_piece = sums + (place + (from + i) * step) * D;
-#pragma unroll
-            for (int j = 0; j < C; ++j) o[j] = fmaf(from_piece[j], f, o[j]);
-        }
+        for (int j = 0; j < C; ++j) o[j] = fmaf(o[j], old, sums[threadIdx.x + 16 * i * row_slots][j] * by);
     }
     const float over = total == 0.0f ? 0.0f : 1.0f / total;
-    uint16_t *out = a.out.data + (int64_t)token * a.out.token_stride + (int64_t)query_head * a.out.head_stride + lane * C;
+    uint32_t w[C / 2];
 #pragma unroll
-    for (int j = 0; j < C; ++j) out[j] = kv_round(o[j] * over, BF16);
+    for (int j = 0; j < C / 2; ++j) w[j] = kv_round(o[2 * j] * over, BF16) | (uint32_t)kv_round(o[2 * j + 1] * over, BF16) << 16;
+    const int r = note.row0 + first_row + row;
+    kv_store(a.out.data + (int64_t)(note.start + r / a.groups) * a.out.token_stride + (int64_t)(head * a.groups + r % a.groups) * a.out.head_stride + c0, a.out.aligned, w);
 }
-
-// Fewest steps of a piece: one for each wave of the rows kernel, twice
-int least_steps(const KvPlan &plan) { return plan.tile == kRowsTile ? 8 : 16; }
 
 }  // namespace
 
-KvPlan kv_plan(int sequences, int64_t tokens, int heads, int groups, int)
+KvPlan kv_plan(const KvArgs &c, int groups)
 {
     KvPlan p;
-    const int64_t rows = tokens * groups;
-    p.tile = rows <= 32 * (int64_t)sequences ? kRowsTile : kTilesTile;
-    const int64_t tiles = std::min(tokens * ((groups + p.tile - 1) / p.tile), rows / p.tile + sequences);
-    const int wanted = p.tile == kRowsTile ? 1024 : 512;
-    p.target = tiles * heads >= 4 * wanted ? 0 : std::max(wanted / heads, 1);
-    p.slots = (int)(tiles + p.target);
+    const int64_t rows = (int64_t)c.tokens * groups, sequences = c.sequences;
+    p.tile = rows <= 32 * sequences ? kRowsTile : kTilesTile;
+    const int64_t tiles = std::min<int64_t>((int64_t)c.tokens * ((groups + p.tile - 1) / p.tile), rows / p.tile + sequences), work = tiles * c.heads;
+    const int64_t most_steps = (((int64_t)c.width << c.page_shift) + kKvStep - 1) / kKvStep;  // of a sequence, as far as the page table goes
+    int64_t wanted;
+    if (p.tile == kRowsTile) {
+        p.waves = work >= 512 ? 4 : 8;
+        p.least = p.waves == 4 ? 32 : 64;
+        wanted = p.waves == 4 ? 2048 : 256;
+    } else {
+        p.waves = 4;
+        p.least = 16;
+        wanted = 512;
+    }
+    p.target = work >= 4 * wanted || most_steps <= p.least ? 0 : (int)std::max<int64_t>(wanted / c.heads, 1);
+    p.slots = (int)(tiles + (p.target ? p.target + 1 : 0));
     return p;
 }
 
 size_t kv_partial_bytes(const KvPlan &plan, int heads, int head_dim)
 {
-    return plan.target ? (size_t)plan.slots * heads * plan.tile * (head_dim + 2) * sizeof(float) : 0;
+    if (!plan.target) return 0;
+    const KvPartial p = kv_partial(nullptr, plan, heads, head_dim);
+    return reinterpret_cast<size_t>(p.note + (int64_t)plan.slots * heads);
 }
 
 hipError_t launch_kv_attention(const KvAttentionArgs &a, const KvPlan &plan, hipStream_t stream)
 {
-    const int least = least_steps(plan);
-    const hipError_t e = plan.tile == kRowsTile ? launch_kv_attention_rows(a, plan, least, stream) : launch_kv_attention_tiles(a, plan, least, stream);
+    const hipError_t e = plan.tile == kRowsTile ? launch_kv_attention_rows(a, plan, stream) : launch_kv_attention_tiles(a, plan, stream);
     if (e != hipSuccess || !plan.target) return e;
-    const dim3 grid((uint32_t)(((int64_t)a.c.tokens * a.c.heads * a.groups + kWaves - 1) / kWaves)), block(64 * kWaves);
+    const dim3 grid((uint32_t)((int64_t)plan.slots * a.c.heads), plan.tile / 16), block(256);
     if (a.c.head_dim == 128) {
-        if (a.c.bf16) kv_attention_join_kernel<128, true><<<grid, block, 0, stream>>>(a, plan, least);
-        else kv_attention_join_kernel<128, false><<<grid, block, 0, stream>>>(a, plan, least);
+        if (a.c.bf16) kv_attention_join_kernel<128, true><<<grid, block, 0, stream>>>(a, plan);
+        else kv_attention_join_kernel<128, false><<<grid, block, 0, stream>>>(a, plan);
     } else {
-        if (a.c.bf16) kv_attention_join_kernel<64, true><<<grid, block, 0, stream>>>(a, plan, least);
-        else kv_attention_join_kernel<64, false><<<grid, block, 0, stream>>>(a, plan, least);
+        if (a.c.bf16) kv_attention_join_kernel<64, true><<<grid, block, 0, stream>>>(a, plan);
+        else kv_attention_join_kernel<64, false><<<grid, block, 0, stream>>>(a, plan);
     }
     return hipGetLastError();
 }

@@ -1,67 +1,35 @@
 // Attention of few rows over the four-bit cache (apmm_kv_attention.h): token generation.
 //
-// A workgroup has 16 rows (the query heads of a key/value head times its new tokens; fewer are there in most calls) and a piece of the keys, its four waves take steps of 32 keys
+// A workgroup has 16 rows (the query heads of a key/value head times its new tokens; fewer are there in most calls) and a piece of the keys, its waves take steps of 32 keys
 // in turn, each with its own maximum and sums, and meet in LDS at the end.  Matrix instructions 16 x 16 x 32: two for each 32 channels and 16 keys, one for each 16 channels of the result.
-// A lane loads its parts of keys and values from memory into registers, one step ahead: rows of keys whole, 16 bytes a lane.
+// Row i of the key operand is key i of 16, so that a lane's scores are those of keys 4 g to 4 g + 3 of both halves of a step (g = lane / 16).  Each half lies in one page: all loads are a base
+// that is the same for the wave plus the lane's offset, which does not change.  A step's loads leave one step ahead.
 #include "apmm_kv_attention.h"
 
 namespace apmm {
 
 namespace {
 
-constexpr int kWaves = 4;
-
 template <int D>
 struct Step {
     uint32_t k[2][D / 32];
-    uint4 v[D / 64];
-    uint4 ks, vs;
-    int key, page[2];
+    uint2 v[2][D / 64];
+    uint2 ks[2], vs[2];
 };
 
-template <int D>
-__device__ __forceinline__ void load_step(const KvAttentionArgs &a, int head, int key, int page0, int page1, Step<D> &s)
-{
-    const int lane = kv_lane(), r = lane & 15, g = lane >> 4, shift = a.c.page_shift, mask = (1 << shift) - 1;
-    s.key = key;
-    s.page[0] = page0;
-    s.page[1] = page1;
-    const int64_t block0 = ((int64_t)max(page0, 0) * a.c.heads + head) * 2, block1 = ((int64_t)max(page1, 0) * a.c.heads + head) * 2;
-    const int in0 = key & mask, in1 = (key + 16) & mask;
-    {   // operand row 4 g' + j of key tile t is key 8 g' + 4 t + j
-        const uint8_t *keys = a.c.codes + (((r < 8 ? block0 : block1) << shift) + (r < 8 ? in0 : in1)) * (D / 2) + (8 * ((r >> 2) & 1) + (r & 3)) * (D / 2) + g * (D / 8);
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            if constexpr (D == 128) {
-                const uint4 w = *reinterpret_cast<const uint4 *>(keys + 4 * t * (D / 2));
-                s.k[t][0] = w.x; s.k[t][1] = w.y; s.k[t][2] = w.z; s.k[t][3] = w.w;
-            } else {
-                const uint2 w = *reinterpret_cast<const uint2 *>(keys + 4 * t * (D / 2));
-                s.k[t][0] = w.x; s.k[t][1] = w.y;
-            }
-        }
-    }
-    const int64_t block = (g < 2 ? block0 : block1) << shift;
-    const int in = (g < 2 ? in0 : in1) + 8 * (g & 1);
-    const uint16_t *scales = a.c.scales + block + in;
-    s.ks = *reinterpret_cast<const uint4 *>(scales);
-    s.vs = *reinterpret_cast<const uint4 *>(scales + ((int64_t)1 << shift));
-    const uint4 *values = reinterpret_cast<const uint4 *>(a.c.codes + (block + in + ((int64_t)1 << shift)) * (D / 2)) + r;
-#pragma unroll
-    for (int i = 0; i < D / 64; ++i) s.v[i] = values[16 * i];
-}
-
-template <int D, bool BF16>
-__global__ __launch_bounds__(64 * kWaves) void kv_attention_rows_kernel(KvAttentionArgs a, KvPlan plan, int least)
+template <int D, bool BF16, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 2) void kv_attention_rows_kernel(KvAttentionArgs a, KvPlan plan)
 {
     constexpr int W = D / 32, V = D / 64, T = kRowsTile;
-    constexpr int kPitch = D + 4;
-    __shared__ __align__(16) float sums[kWaves][T][kPitch];
-    __shared__ float bases[kWaves][T], totals[kWaves][T];
+    constexpr int R = 4, kPitch = D + 4;  // rows that meet in LDS at a time
+    __shared__ __align__(16) float sums[WAVES][R][kPitch];
+    __shared__ float bases[WAVES][T], totals[WAVES][T];
     const int head = blockIdx.x % a.c.heads, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = kv_lane(), n = lane & 15, g = lane >> 4;
-    const int piece = kv_piece(a, plan, least);
+    const int slot = blockIdx.x / a.c.heads;
     KvItem it;
-    if (!kv_item(a, plan, piece, blockIdx.x / a.c.heads, it)) return;
+    const bool there = kv_item(a, plan, slot, it);
+    kv_note(a, plan, slot, head, there, it);
+    if (!there) return;
 
     const int rows = min(it.rows, T), row = it.row0 + min(n, rows - 1), at = row / a.groups;
     const int pos = it.s.first + at, first_pos = it.s.first + it.row0 / a.groups, last_pos = it.s.first + (it.row0 + rows - 1) / a.groups;
@@ -72,11 +40,36 @@ __global__ __launch_bounds__(64 * kWaves) void kv_attention_rows_kernel(KvAttent
     auto larger = [](float x, float y) { return fmaxf(x, y); };
     auto plus = [](float x, float y) { return x + y; };
 
+    const int shift = a.c.page_shift, mask = (1 << shift) - 1;
+    const uint32_t key_lane = n * (D / 2) + g * (D / 8), value_lane = ((g >> 1) * (D / 4) + n) * 16 + (g & 1) * 8, scale_lane = g * 8;
+    auto load = [&](int key, int page0, int page1, Step<D> &s) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int64_t place = ((((int64_t)max(t ? page1 : page0, 0) * a.c.heads + head) * 2) << shift) + ((key + 16 * t) & mask);
+            const uint8_t *keys = a.c.codes + place * (D / 2), *values = keys + ((int64_t)(D / 2) << shift);
+            const uint8_t *scales = reinterpret_cast<const uint8_t *>(a.c.scales + place), *value_scales = scales + ((int64_t)2 << shift);
+            if constexpr (D == 128) {
+                const uint4 w = *reinterpret_cast<const uint4 *>(keys + key_lane);
+                s.k[t][0] = w.x; s.k[t][1] = w.y; s.k[t][2] = w.z; s.k[t][3] = w.w;
+            } else {
+                const uint2 w = *reinterpret_cast<const uint2 *>(keys + key_lane);
+                s.k[t][0] = w.x; s.k[t][1] = w.y;
+            }
+            s.ks[t] = *reinterpret_cast<const uint2 *>(scales + scale_lane);
+            s.vs[t] = *reinterpret_cast<const uint2 *>(value_scales + scale_lane);
+#pragma unroll
+            for (int i = 0; i < V; ++i) s.v[t][i] = *reinterpret_cast<const uint2 *>(values + value_lane + 256 * i);
+        }
+    };
+
+    int v = it.from + wave, ids = kv_page_ids(a, it, v, WAVES), id = 0;
     half8 q[W];
     float init, factor;
+    Step<D> s0, s1;
     {
         uint32_t x[4 * W];
         kv_load(a.q.data + (int64_t)(it.s.start + at) * a.q.token_stride + (int64_t)(head * a.groups + row % a.groups) * a.q.head_stride + g * (D / 4), a.q.aligned, x);
+        if (v < it.to) load(it.key_of(v), __builtin_amdgcn_readlane(ids, 0), __builtin_amdgcn_readlane(ids, 1), s0);
         kv_queries<4 * W, BF16>(x, a.scale, [&](float v) { return over_row(v, larger); }, [&](float v) { return over_row(v, plus); }, q, init, factor);
     }
     const float4v init4 = {init, init, init, init};
@@ -89,16 +82,18 @@ __global__ __launch_bounds__(64 * kWaves) void kv_attention_rows_kernel(KvAttent
     float top = kLowest, base = -kLowest, total = 0.0f, weights = 0.0f;
     uint32_t limit = 0, met = 0;  // largest scale of values: where it is passed, met so far
 
-    int v = it.from + wave, ids = kv_page_ids(a, it, v, kWaves), id = 0;
-    Step<D> cur, next;
-    if (v < it.to) load_step<D>(a, head, it.key_of(v), __builtin_amdgcn_readlane(ids, 0), __builtin_amdgcn_readlane(ids, 1), cur);
-    for (; v < it.to; v += kWaves, cur = next) {
+    auto step = [&](const Step<D> &cur, Step<D> &next) {
+        const int key0 = it.key_of(v), page0 = __builtin_amdgcn_readlane(ids, id), page1 = __builtin_amdgcn_readlane(ids, id + 1);
+        v += WAVES;
         id += 2;
         if (id == 64) {
-            ids = kv_page_ids(a, it, v + kWaves, kWaves);
+            ids = kv_page_ids(a, it, v, WAVES);
             id = 0;
         }
-        if (v + kWaves < it.to) load_step<D>(a, head, it.key_of(v + kWaves), __builtin_amdgcn_readlane(ids, id), __builtin_amdgcn_readlane(ids, id + 1), next);
+        {   // (behind the last step the same one again: from the cache, and no branch)
+            const bool more = v < it.to;
+            load(more ? it.key_of(v) : key0, more ? __builtin_amdgcn_readlane(ids, id) : page0, more ? __builtin_amdgcn_readlane(ids, id + 1) : page1, next);
+        }
 
         // scores, without the row's factor
         float4v sc[2];
@@ -108,37 +103,31 @@ __global__ __launch_bounds__(64 * kWaves) void kv_attention_rows_kernel(KvAttent
 #pragma unroll
             for (int i = 0; i < W; ++i) sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv_operand(cur.k[t][i]), q[i], sc[t], 0, 0, 0);
         }
-        const uint32_t ks[4] = {cur.ks.x, cur.ks.y, cur.ks.z, cur.ks.w};
-        uint32_t vs[4] = {cur.vs.x, cur.vs.y, cur.vs.z, cur.vs.w};
+        const uint32_t ks[4] = {cur.ks[0].x, cur.ks[0].y, cur.ks[1].x, cur.ks[1].y};
+        uint32_t vs[4] = {cur.vs[0].x, cur.vs[0].y, cur.vs[1].x, cur.vs[1].y};
         float x[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = fmaf(sc[i / 4][i % 4], i & 1 ? kv_high<BF16>(ks[i / 2]) : kv_low<BF16>(ks[i / 2]), 0.0f);
-        const bool all = cur.key + kKvStep <= it.s.keys && cur.key + kKvStep - 1 <= first_pos && cur.page[0] >= 0 && cur.page[1] >= 0 &&
-                         (!a.window || cur.key > last_pos - a.window || cur.key + kKvStep <= a.sinks);
+        const bool all = key0 + kKvStep <= it.s.keys && key0 + kKvStep - 1 <= first_pos && page0 >= 0 && page1 >= 0 &&
+                         (!a.window || key0 > last_pos - a.window || key0 + kKvStep <= a.sinks);
         if (!all) {
-            const bool page = cur.page[g >> 1] >= 0;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const int key = cur.key + 8 * g + i;
-                if (!(page && key < it.s.keys && key <= pos && (!a.window || key > pos - a.window || key < a.sinks))) {
-                    x[i] = -__builtin_inff();
-                    vs[i / 2] &= i & 1 ? 0x0000ffffu : 0xffff0000u;  // weights of hidden keys are zero whatever their scale is
-                }
+                const int key = key0 + 16 * (i / 4) + 4 * g + i % 4, end = (i < 4 ? page0 : page1) >= 0 ? min(it.s.keys, pos + 1) : 0;
+                const bool hidden = (key >= end) | ((a.window != 0) & (key <= pos - a.window) & (key >= a.sinks));
+                x[i] = hidden ? -__builtin_inff() : x[i];
+                vs[i / 2] &= hidden ? (i & 1 ? 0x0000ffffu : 0xffff0000u) : 0xffffffffu;  // weights of hidden keys are zero whatever their scale is
             }
         }
         const uint32_t most2 = kv_fold_max(kv_fold_max(vs[0], vs[1]), kv_fold_max(vs[2], vs[3])), most = max(most2 & 0xffffu, most2 >> 16);
         const float high = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))) * factor;
-        if (__any(high > top + kSlack || most > limit)) {
+        if (__any((high > top + kSlack) | (most > limit))) {
             top = fmaxf(top, over_row(high, larger));
             uint32_t m = met;
 #pragma unroll
             for (int i = 0; i < 4; ++i) m = kv_finite_max<BF16>(kv_finite_max<BF16>(m, vs[i] & 0xffffu), vs[i] >> 16);
-            m = max(m, (uint32_t)__shfl_xor((int)m, 16));
-            m = max(m, (uint32_t)__shfl_xor((int)m, 32));
-            m = max(m, (uint32_t)__shfl_xor((int)m, 1));
-            m = max(m, (uint32_t)__shfl_xor((int)m, 2));
-            m = max(m, (uint32_t)__shfl_xor((int)m, 4));
-            m = max(m, (uint32_t)__shfl_xor((int)m, 8));  // (rows see different keys where some are hidden)
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) m = max(m, (uint32_t)__shfl_xor((int)m, d));  // (rows see different keys where some are hidden)
             met = m;
             limit = kv_limit<BF16>(met);
             const float to = -top + (kRoom - (float)kv_exponent<BF16>(met));
@@ -162,7 +151,7 @@ __global__ __launch_bounds__(64 * kWaves) void kv_attention_rows_kernel(KvAttent
         const half8 p = __builtin_bit_cast(half8, make_uint4(w[0], w[1], w[2], w[3]));
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const uint32_t c[4] = {cur.v[i].x, cur.v[i].y, cur.v[i].z, cur.v[i].w};
+            const uint32_t c[4] = {cur.v[0][i].x, cur.v[0][i].y, cur.v[1][i].x, cur.v[1][i].y};
             uint32_t o[4][4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -176,71 +165,86 @@ __global__ __launch_bounds__(64 * kWaves) void kv_attention_rows_kernel(KvAttent
             for (int e = 0; e < 4; ++e)
                 acc[e][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, make_uint4(o[e][0], o[e][1], o[e][2], o[e][3])), p, acc[e][i], 0, 0, 0);
         }
+    };
+    while (v < it.to) {
+        step(s0, s1);
+        if (v >= it.to) break;
+        step(s1, s0);
     }
 
-    // the four waves' sums: channel 64 i + 16 g + 4 j + e of row n is acc[e][i][j]
+    // the waves' sums, four rows at a time: channel 64 i + 16 g + 4 j + e of row n is acc[e][i][j]
     total = over_row(total, plus);
     weights = over_row(weights, plus);
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            float4v o;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = fmaf(acc[e][i][j], e & 1 ? 0x1p21f : 0x1p25f, -15.0f * weights);
-            *reinterpret_cast<float4v *>(&sums[wave][n][64 * i + 16 * g + 4 * j]) = o;
-        }
     if (g == 0) {
         bases[wave][n] = -base;
         totals[wave][n] = total;
     }
-    __syncthreads();
-    constexpr int C = D / 16;  // channels of a thread
-    const int mine = threadIdx.x >> 4, c0 = (threadIdx.x & 15) * C;
-    if (mine >= rows) return;
-    float most = bases[0][mine];
+    constexpr int kThreads = 64 * WAVES, C = kThreads >= R * D ? 1 : R * D / kThreads;  // channels of a thread
+    const int mine = threadIdx.x / (D / C), c0 = threadIdx.x % (D / C) * C;
+    const KvPartial partial = kv_partial(a.partial, plan, a.c.heads, D);
+    for (int r0 = 0; r0 < rows; r0 += R) {
+        if ((n & ~(R - 1)) == r0) {
 #pragma unroll
-    for (int i = 1; i < kWaves; ++i) most = fmaxf(most, bases[i][mine]);
-    float sum = 0.0f, o[C] = {};
+            for (int i = 0; i < V; ++i)
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
-        const float by = __builtin_amdgcn_exp2f(bases[i][mine] - most);
-        sum = fmaf(totals[i][mine], by, sum);
+                for (int j = 0; j < 4; ++j) {
+                    float4v o;
 #pragma unroll
-        for (int j = 0; j < C; ++j) o[j] = fmaf(sums[i][mine][c0 + j], by, o[j]);
-    }
-    if (it.pieces == 1) {
-        const int r = it.row0 + mine;
-        const float over = sum == 0.0f ? 0.0f : 1.0f / sum;
-        uint32_t w[C / 2];
-#pragma unroll
-        for (int j = 0; j < C / 2; ++j) w[j] = kv_round(o[2 * j] * over, BF16) | (uint32_t)kv_round(o[2 * j + 1] * over, BF16) << 16;
-        kv_store(a.out.data + (int64_t)(it.s.start + r / a.groups) * a.out.token_stride + (int64_t)(head * a.groups + r % a.groups) * a.out.head_stride + c0, a.out.aligned, w);
-    } else {
-        const int64_t place = ((int64_t)it.slot * a.c.heads + head) * T + mine;
-        float *to = a.partial + place * D + c0;
-#pragma unroll
-        for (int j = 0; j < C; j += 4) *reinterpret_cast<float4v *>(to + j) = float4v{o[j], o[j + 1], o[j + 2], o[j + 3]};
-        if (c0 == 0) {
-            float *meta = a.partial + (int64_t)plan.slots * a.c.heads * T * D + place * 2;
-            meta[0] = most;
-            meta[1] = sum;
+                    for (int e = 0; e < 4; ++e) o[e] = fmaf(acc[e][i][j], e & 1 ? 0x1p21f : 0x1p25f, -15.0f * weights);
+                    *reinterpret_cast<float4v *>(&sums[wave][n & (R - 1)][64 * i + 16 * g + 4 * j]) = o;
+                }
         }
+        __syncthreads();
+        const int r = r0 + mine;
+        if (mine < R && r < rows) {
+            float most = bases[0][r];
+#pragma unroll
+            for (int i = 1; i < WAVES; ++i) most = fmaxf(most, bases[i][r]);
+            float sum = 0.0f, o[C] = {};
+#pragma unroll
+            for (int i = 0; i < WAVES; ++i) {
+                const float by = __builtin_amdgcn_exp2f(bases[i][r] - most);
+                sum = fmaf(totals[i][r], by, sum);
+#pragma unroll
+                for (int j = 0; j < C; ++j) o[j] = fmaf(sums[i][mine][c0 + j], by, o[j]);
+            }
+            if (it.pieces == 1) {
+                const int to_row = it.row0 + r;
+                const float over = sum == 0.0f ? 0.0f : 1.0f / sum;
+                uint16_t *out = a.out.data + (int64_t)(it.s.start + to_row / a.groups) * a.out.token_stride +
+                                (int64_t)(head * a.groups + to_row % a.groups) * a.out.head_stride + c0;
+#pragma unroll
+                for (int j = 0; j < C; ++j) out[j] = kv_round(o[j] * over, BF16);
+            } else {
+                const int64_t place = ((int64_t)slot * a.c.heads + head) * T + r;
+#pragma unroll
+                for (int j = 0; j < C; ++j) partial.sums[place * D + c0 + j] = o[j];
+                if (c0 == 0) partial.row[place] = make_float2(most, sum);
+            }
+        }
+        __syncthreads();
+    }
+}
+
+template <int WAVES>
+void launch(const KvAttentionArgs &a, const KvPlan &plan, hipStream_t stream)
+{
+    const dim3 grid((uint32_t)((int64_t)plan.slots * a.c.heads)), block(64 * WAVES);
+    if (a.c.head_dim == 128) {
+        if (a.c.bf16) kv_attention_rows_kernel<128, true, WAVES><<<grid, block, 0, stream>>>(a, plan);
+        else kv_attention_rows_kernel<128, false, WAVES><<<grid, block, 0, stream>>>(a, plan);
+    } else {
+        if (a.c.bf16) kv_attention_rows_kernel<64, true, WAVES><<<grid, block, 0, stream>>>(a, plan);
+        else kv_attention_rows_kernel<64, false, WAVES><<<grid, block, 0, stream>>>(a, plan);
     }
 }
 
 }  // namespace
 
-hipError_t launch_kv_attention_rows(const KvAttentionArgs &a, const KvPlan &plan, int least, hipStream_t stream)
+hipError_t launch_kv_attention_rows(const KvAttentionArgs &a, const KvPlan &plan, hipStream_t stream)
 {
-    const dim3 grid((uint32_t)((int64_t)plan.slots * a.c.heads)), block(64 * kWaves);
-    if (a.c.head_dim == 128) {
-        if (a.c.bf16) kv_attention_rows_kernel<128, true><<<grid, block, 0, stream>>>(a, plan, least);
-        else kv_attention_rows_kernel<128, false><<<grid, block, 0, stream>>>(a, plan, least);
-    } else {
-        if (a.c.bf16) kv_attention_rows_kernel<64, true><<<grid, block, 0, stream>>>(a, plan, least);
-        else kv_attention_rows_kernel<64, false><<<grid, block, 0, stream>>>(a, plan, least);
-    }
+    if (plan.waves == 4) launch<4>(a, plan, stream);
+    else launch<8>(a, plan, stream);
     return hipGetLastError();
 }
 

@@ -48,13 +48,15 @@ __device__ __forceinline__ void load_step(const KvAttentionArgs &a, int head, in
 }
 
 template <int D, bool BF16>
-__global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAttentionArgs a, KvPlan plan, int least)
+__global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAttentionArgs a, KvPlan plan)
 {
     constexpr int W = D / 16, E = D / 32;  // words of a lane's key, blocks of 32 channels of the result
     const int head = blockIdx.x % a.c.heads, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = kv_lane(), n = lane & 31, h = lane >> 5;
-    const int piece = kv_piece(a, plan, least);
     KvItem it;
-    if (!kv_item(a, plan, piece, blockIdx.x / a.c.heads, it)) return;
+    const int slot = blockIdx.x / a.c.heads;
+    const bool there = kv_item(a, plan, slot, it);
+    kv_note(a, plan, slot, head, there, it);
+    if (!there) return;
 
     const int row0 = it.row0 + wave * kRows, rows = min(it.rows - wave * kRows, kRows);
     if (rows <= 0) return;
@@ -110,7 +112,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAt
         const bool all = cur.key + kKvStep <= it.s.keys && cur.key + kKvStep - 1 <= first_pos && cur.page[0] >= 0 && cur.page[1] >= 0 &&
                          (!a.window || cur.key > last_pos - a.window || cur.key + kKvStep <= a.sinks);
         if (!all) {
-            const bool page = cur.page[h] >= 0;
+            const bool page = (h ? cur.page[1] : cur.page[0]) >= 0;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int key = cur.key + 16 * h + i;
@@ -182,7 +184,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAt
     const float over = whole ? (total == 0.0f ? 0.0f : 1.0f / total) : 1.0f;
     uint16_t *out = a.out.data + (int64_t)(it.s.start + at) * a.out.token_stride + (int64_t)(head * a.groups + row % a.groups) * a.out.head_stride;
     const int64_t place = ((int64_t)it.slot * a.c.heads + head) * kTilesTile + wave * kRows + n;
-    float *partial = a.partial + place * D;
+    const KvPartial partial = kv_partial(a.partial, plan, a.c.heads, D);
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
         float o[16];
@@ -201,27 +203,23 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAt
             kv_store(out + c0, a.out.aligned, w);
         } else {
 #pragma unroll
-            for (int j = 0; j < 16; j += 4) *reinterpret_cast<float4v *>(partial + c0 + j) = float4v{o[j], o[j + 1], o[j + 2], o[j + 3]};
+            for (int j = 0; j < 16; j += 4) *reinterpret_cast<float4v *>(partial.sums + place * D + c0 + j) = float4v{o[j], o[j + 1], o[j + 2], o[j + 3]};
         }
     }
-    if (!whole && h == 0) {
-        float *meta = a.partial + (int64_t)plan.slots * a.c.heads * kTilesTile * D + place * 2;
-        meta[0] = -base;
-        meta[1] = total;
-    }
+    if (!whole && h == 0) partial.row[place] = make_float2(-base, total);
 }
 
 }  // namespace
 
-hipError_t launch_kv_attention_tiles(const KvAttentionArgs &a, const KvPlan &plan, int least, hipStream_t stream)
+hipError_t launch_kv_attention_tiles(const KvAttentionArgs &a, const KvPlan &plan, hipStream_t stream)
 {
     const dim3 grid((uint32_t)((int64_t)plan.slots * a.c.heads)), block(64 * kWaves);
     if (a.c.head_dim == 128) {
-        if (a.c.bf16) kv_attention_tiles_kernel<128, true><<<grid, block, 0, stream>>>(a, plan, least);
-        else kv_attention_tiles_kernel<128, false><<<grid, block, 0, stream>>>(a, plan, least);
+        if (a.c.bf16) kv_attention_tiles_kernel<128, true><<<grid, block, 0, stream>>>(a, plan);
+        else kv_attention_tiles_kernel<128, false><<<grid, block, 0, stream>>>(a, plan);
     } else {
-        if (a.c.bf16) kv_attention_tiles_kernel<64, true><<<grid, block, 0, stream>>>(a, plan, least);
-        else kv_attention_tiles_kernel<64, false><<<grid, block, 0, stream>>>(a, plan, least);
+        if (a.c.bf16) kv_attention_tiles_kernel<64, true><<<grid, block, 0, stream>>>(a, plan);
+        else kv_attention_tiles_kernel<64, false><<<grid, block, 0, stream>>>(a, plan);
     }
     return hipGetLastError();
 }

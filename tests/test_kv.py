@@ -404,7 +404,9 @@ def test_refusals(gpu):
     for kw in (dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(window=-1), dict(sinks=-1)):
         refused(binding.ApmmError, binding.apmm_kv_attention, x.q, c, s, t, n, status=1, **kw)
     refused(binding.ApmmError, binding.apmm_kv_attention, x.q, c, s, t, n, status=2, window=2 ** 30 + 1)
-    refused(binding.ApmmError, binding.apmm_kv_attention, x.q, c, s, t, n, status=4, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+    wide = torch.full((1, 1 << 20), -1, dtype=torch.int32, device="cuda")  # room for a sequence whose keys may be cut
+    assert binding.apmm_kv_attention_workspace_bytes(1, 4, c, s, wide, n) > 16
+    refused(binding.ApmmError, binding.apmm_kv_attention, x.q, c, s, wide, n, status=4, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
     refused(ValueError, binding.apmm_kv_write, x.k, x.v[:, :1], c, s, t, n)
     refused(ValueError, binding.apmm_kv_write, x.q, x.v, c, s, t, n)
     refused(ValueError, binding.apmm_kv_read, c, s, t, n, 2)
