@@ -52,7 +52,8 @@ except ImportError as _reason:  # not built, or built for another torch or Pytho
     _call = None
     warnings.warn("the calls' C++ marshalling is not used, each takes 2 to 3 us longer: %s" % _reason, RuntimeWarning)
 _CALL_FUNCTIONS = ("apmm_packed_bytes", "apmm_packed_activation_bytes", "apmm_pack_weights", "apmm_pack_activations",
-                   "apmm_quantize_pack_activations", "apmm_gemm_ex", "apmm_gemm_from_codes")
+                   "apmm_quantize_pack_activations", "apmm_gemm_ex", "apmm_gemm_from_codes", "apmm_kv_write", "apmm_kv_read", "apmm_kv_attention",
+                   "apmm_kv_attention_workspace_bytes")
 
 
 class ApmmError(RuntimeError):
@@ -307,6 +308,8 @@ def _kv_cache(codes, scales):
     if codes.dtype != torch.uint8 or scales.dtype not in _KV_DTYPES or codes.dim() != 4 or scales.dim() != 4 or codes.shape[:3] != scales.shape[:3] or \
             codes.shape[2] != 2 or not codes.is_contiguous() or not scales.is_contiguous() or not codes.is_cuda or scales.device != codes.device:
         raise ValueError("codes and scales must be contiguous CUDA tensors, uint8 pages x heads x 2 x page_size * head_dim / 2 and float16 or bfloat16 pages x heads x 2 x page_size")
+    if codes.get_device() != torch.cuda.current_device():
+        raise ValueError("the cache must be on the current device, whose stream the call goes to")
     pages, heads, _, page_size = scales.shape
     if page_size < 1 or codes.shape[3] * 2 % page_size:
         raise ValueError("codes must hold a whole number of channels a token")
@@ -402,7 +405,8 @@ def apmm_time_next_gemm(start_event, stop_event):
 
 _general = {}  # the Python functions behind the C++ calls
 if _call is not None:
-    for _name in ("apmm_pack_weights", "apmm_pack_activations", "apmm_quantize_pack_activations", "apmm_gemm", "apmm_gemm_from_codes"):
+    for _name in ("apmm_pack_weights", "apmm_pack_activations", "apmm_quantize_pack_activations", "apmm_gemm", "apmm_gemm_from_codes", "apmm_kv_write", "apmm_kv_read",
+                  "apmm_kv_attention"):
         _general[_name] = globals()[_name]
         _call.set_general(_name, _general[_name])
         globals()[_name] = getattr(_call, _name)

@@ -17,6 +17,7 @@
 #include <ATen/ops/empty.h>
 #include <c10/hip/HIPStream.h>
 
+#include <cmath>
 #include <cstring>
 
 #include "../../include/apmm.h"
@@ -32,13 +33,18 @@ struct Library {
     decltype(&apmm_quantize_pack_activations) quantize_pack_activations;
     decltype(&apmm_gemm_ex) gemm_ex;
     decltype(&apmm_gemm_from_codes) gemm_from_codes;
+    decltype(&apmm_kv_write) kv_write;
+    decltype(&apmm_kv_read) kv_read;
+    decltype(&apmm_kv_attention) kv_attention;
+    decltype(&apmm_kv_attention_workspace_bytes) kv_attention_workspace_bytes;
 };
+constexpr int kLibraryFunctions = 11;
 Library lib = {};
 bool loaded = false;
 PyObject *check = nullptr;  // binding.py's _check
 
 constexpr int kMaxArgs = 15;
-enum Function { kPackWeights, kPackActivations, kQuantize, kGemm, kFromCodes, kFunctions };
+enum Function { kPackWeights, kPackActivations, kQuantize, kGemm, kFromCodes, kKvWrite, kKvRead, kKvAttention, kFunctions };
 struct Signature {
     const char *name;
     int count, required;
@@ -53,6 +59,9 @@ Signature signatures[kFunctions] = {
     {"apmm_gemm", 15, 7,
      {"M", "N", "K", "p", "q", "a_packed", "w_packed", "want_i32", "want_f16", "w_scale", "a_scale", "c_i32", "c_f16", "workspace", "algo"}, {}, nullptr},
     {"apmm_gemm_from_codes", 12, 5, {"a_codes", "N", "p", "q", "w_packed", "want_i32", "want_f16", "w_scale", "a_scale", "c_i32", "c_f16", "workspace"}, {}, nullptr},
+    {"apmm_kv_write", 7, 6, {"k", "v", "codes", "scales", "page_table", "lengths", "starts"}, {}, nullptr},
+    {"apmm_kv_read", 8, 5, {"codes", "scales", "page_table", "lengths", "tokens", "starts", "k_out", "v_out"}, {}, nullptr},
+    {"apmm_kv_attention", 11, 5, {"q", "codes", "scales", "page_table", "lengths", "starts", "window", "sinks", "scale", "out", "workspace"}, {}, nullptr},
 };
 
 // Arguments by place, null where not given; false: not the plain case.
@@ -244,6 +253,105 @@ int from_codes(PyObject **v, PyObject *&result)
     return result_of(went ? 1 : -1, ci, &cf, result);
 }
 
+// The four-bit cache: its two tensors, the batch and rows of a call as binding.py checks them
+bool kv_cache(PyObject *codes_arg, PyObject *scales_arg, apmm_kv_cache &c)
+{
+    const at::Tensor *codes = tensor(codes_arg), *scales = tensor(scales_arg);
+    if (!codes || !scales || codes->scalar_type() != at::kByte || (scales->scalar_type() != at::kHalf && scales->scalar_type() != at::kBFloat16) || codes->dim() != 4 ||
+        scales->dim() != 4 || !codes->is_contiguous() || !scales->is_contiguous() || codes->get_device() != scales->get_device() ||
+        codes->get_device() != c10::hip::getCurrentHIPStream().device_index())
+        return false;
+    const int64_t pages = codes->size(0), heads = codes->size(1), page_size = scales->size(3);
+    if (scales->size(0) != pages || scales->size(1) != heads || codes->size(2) != 2 || scales->size(2) != 2 || page_size < 1 || codes->size(3) * 2 % page_size) return false;
+    const int64_t head_dim = codes->size(3) * 2 / page_size;
+    if (heads > INT32_MAX || page_size > INT32_MAX || head_dim > INT32_MAX) return false;
+    c = {codes->data_ptr(), scales->data_ptr(), pages, (int)page_size, (int)heads, (int)head_dim, scales->scalar_type() == at::kHalf ? APMM_F16 : APMM_BF16};
+    return true;
+}
+bool kv_indices(const at::Tensor *t, int64_t dim, int device)
+{
+    return t && t->scalar_type() == at::kInt && t->dim() == dim && t->get_device() == device && (t->size(dim - 1) <= 1 || t->stride(dim - 1) == 1);
+}
+bool kv_batch(PyObject *codes, PyObject *table_arg, PyObject *lengths_arg, PyObject *starts_arg, int64_t tokens, apmm_kv_batch &b)
+{
+    const int device = tensor(codes)->get_device();
+    const at::Tensor *table = tensor(table_arg), *lengths = tensor(lengths_arg), *starts = tensor(starts_arg);
+    if (!kv_indices(table, 2, device) || !kv_indices(lengths, 1, device) || (given(starts_arg) && !kv_indices(starts, 1, device))) return false;
+    const int64_t n = lengths->size(0);
+    if (n > INT32_MAX || table->size(0) != n || (starts ? starts->size(0) != n + 1 : tokens != n)) return false;
+    b = {(int)n, tokens, static_cast<const int32_t *>(lengths->data_ptr()), starts ? static_cast<const int32_t *>(starts->data_ptr()) : nullptr,
+         static_cast<const int32_t *>(table->data_ptr()), n > 1 ? table->stride(0) : table->size(1), table->size(1)};
+    return true;
+}
+bool kv_rows(const at::Tensor *t, PyObject *scales_arg, int64_t heads, int64_t head_dim, int64_t tokens)
+{
+    const at::Tensor *scales = tensor(scales_arg);
+    return t && t->scalar_type() == scales->scalar_type() && t->get_device() == scales->get_device() && t->dim() == 3 && t->size(0) == tokens && t->size(1) == heads &&
+           t->size(2) == head_dim && t->stride(2) == 1;
+}
+
+int kv_write(PyObject **v, PyObject *&result)
+{
+    apmm_kv_cache c;
+    apmm_kv_batch b;
+    const at::Tensor *k = tensor(v[0]), *x = tensor(v[1]);
+    if (!k || !x || k->dim() != 3 || !kv_cache(v[2], v[3], c) || !kv_batch(v[2], v[4], v[5], v[6], k->size(0), b) || !kv_rows(k, v[3], c.kv_heads, c.head_dim, b.tokens) ||
+        !kv_rows(x, v[3], c.kv_heads, c.head_dim, b.tokens))
+        return 0;
+    void *s = stream();
+    if (!called([&] { return lib.kv_write(&c, &b, k->data_ptr(), k->stride(0), k->stride(1), x->data_ptr(), x->stride(0), x->stride(1), s); })) return -1;
+    Py_INCREF(Py_None);
+    result = Py_None;
+    return 1;
+}
+
+int kv_read(PyObject **v, PyObject *&result)
+{
+    apmm_kv_cache c;
+    apmm_kv_batch b;
+    int64_t tokens;
+    if (!kv_cache(v[0], v[1], c) || !integer(v[4], 0, INT32_MAX, tokens) || !kv_batch(v[0], v[2], v[3], v[5], tokens, b)) return 0;
+    for (int i = 6; i < 8; ++i)
+        if (given(v[i]) && !kv_rows(tensor(v[i]), v[1], c.kv_heads, c.head_dim, tokens)) return 0;
+    const at::Tensor &like = *tensor(v[1]);
+    Output k, x;
+    if (!output(k, v[6], true, like, {tokens, c.kv_heads, c.head_dim}, like.scalar_type()) || !output(x, v[7], true, like, {tokens, c.kv_heads, c.head_dim}, like.scalar_type()))
+        return result_of(0, k, &x, result);
+    const at::Tensor &tk = *tensor(k.object), &tx = *tensor(x.object);
+    void *s = stream();
+    const bool went = called([&] { return lib.kv_read(&c, &b, k.address, tk.stride(0), tk.stride(1), x.address, tx.stride(0), tx.stride(1), s); });
+    return result_of(went ? 1 : -1, k, &x, result);
+}
+
+int kv_attention(PyObject **v, PyObject *&result)
+{
+    apmm_kv_cache c;
+    apmm_kv_batch b;
+    int64_t window = 0, sinks = 0;
+    const at::Tensor *q = tensor(v[0]);
+    if (!q || q->dim() != 3 || !kv_cache(v[1], v[2], c) || !kv_batch(v[1], v[3], v[4], v[5], q->size(0), b) || q->size(1) > INT32_MAX ||
+        !kv_rows(q, v[2], q->size(1), c.head_dim, b.tokens) || (given(v[9]) && !kv_rows(tensor(v[9]), v[2], q->size(1), c.head_dim, b.tokens)) ||
+        (v[6] && !integer(v[6], -kAny, kAny, window)) || (v[7] && !integer(v[7], -kAny, kAny, sinks)) || (given(v[8]) && !PyFloat_CheckExact(v[8])) ||
+        (given(v[10]) && (!tensor(v[10]) || !tensor(v[10])->is_contiguous() || tensor(v[10])->get_device() != q->get_device())))
+        return 0;
+    const int heads = (int)q->size(1);
+    const float scale = (float)(given(v[8]) ? PyFloat_AS_DOUBLE(v[8]) : 1.0 / std::sqrt((double)c.head_dim));
+    const size_t need = given(v[10]) ? 0 : lib.kv_attention_workspace_bytes(&c, &b, heads);
+    Output out, work;
+    int done = output(out, v[9], true, *q, {b.tokens, heads, c.head_dim}, q->scalar_type()) && output(work, v[10], need != 0, *q, {(int64_t)need}, at::kByte);
+    if (done) {
+        const at::Tensor &to = *tensor(out.object);
+        const size_t room = work.address ? bytes(*tensor(work.object)) : 0;
+        void *s = stream();
+        const bool went = called([&] {
+            return lib.kv_attention(&c, &b, heads, q->data_ptr(), q->stride(0), q->stride(1), out.address, to.stride(0), to.stride(1), scale, window, sinks, work.address, room, s);
+        });
+        done = went ? 1 : -1;
+    }
+    if (work.made) Py_DECREF(work.object);
+    return result_of(done, out, nullptr, result);
+}
+
 template <Function F>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *names)
 {
@@ -252,20 +360,29 @@ PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *n
     const int done = end_exceptions(
         [&] {
             if (!place(s, args, nargs, names, v)) return 0;
-            return F <= kPackActivations ? pack(F, v, result) : F == kQuantize ? quantize(v, result) : F == kGemm ? gemm(v, result) : from_codes(v, result);
+            return F <= kPackActivations ? pack(F, v, result) : F == kQuantize ? quantize(v, result) : F == kGemm ? gemm(v, result) : F == kFromCodes ? from_codes(v, result) :
+                   F == kKvWrite ? kv_write(v, result) : F == kKvRead ? kv_read(v, result) : kv_attention(v, result);
         },
         [] { return 0; });  // (torch's own refusal of a tensor: the general form meets the same one and reports it)
     if (done > 0) return result;
     return done < 0 ? nullptr : general(s, args, nargs, names);
 }
 
-// set_library(addresses of the seven functions in Library's order, _check)
+// set_library(addresses of the functions in Library's order, _check)
 PyObject *set_library(PyObject *, PyObject *args)
 {
-    unsigned long long at[7];
-    PyObject *fn;
-    if (!PyArg_ParseTuple(args, "(KKKKKKK)O", &at[0], &at[1], &at[2], &at[3], &at[4], &at[5], &at[6], &fn)) return nullptr;
-    static_assert(sizeof(lib) == sizeof(at), "seven functions");
+    unsigned long long at[kLibraryFunctions];
+    PyObject *addresses, *fn;
+    if (!PyArg_ParseTuple(args, "O!O", &PyTuple_Type, &addresses, &fn)) return nullptr;
+    if (PyTuple_GET_SIZE(addresses) != kLibraryFunctions) {
+        PyErr_SetString(PyExc_ValueError, "apmm: other functions than this module was built for");
+        return nullptr;
+    }
+    for (int i = 0; i < kLibraryFunctions; ++i) {
+        at[i] = PyLong_AsUnsignedLongLong(PyTuple_GET_ITEM(addresses, i));
+        if (PyErr_Occurred()) return nullptr;
+    }
+    static_assert(sizeof(lib) == sizeof(at), "addresses of functions alone");
     std::memcpy(&lib, at, sizeof(at));
     Py_INCREF(fn);
     Py_XDECREF(check);
@@ -305,6 +422,13 @@ PyMethodDef methods[] = {
     {"apmm_gemm_from_codes", ENTRY(kFromCodes),
      "apmm_gemm_from_codes(a_codes, N, p, q, w_packed, want_i32=True, want_f16=False, w_scale=None, a_scale=None, c_i32=None, c_f16=None, "
      "workspace=None)\n--\n\nC = A W^T straight from the M x K uint8 activation codes."},
+    {"apmm_kv_write", ENTRY(kKvWrite),
+     "apmm_kv_write(k, v, codes, scales, page_table, lengths, starts=None)\n--\n\nQuantise new keys and values (tokens x kv heads x head_dim) into the cache."},
+    {"apmm_kv_read", ENTRY(kKvRead),
+     "apmm_kv_read(codes, scales, page_table, lengths, tokens, starts=None, k_out=None, v_out=None)\n--\n\nKeys and values of the last tokens of each sequence: (k, v)."},
+    {"apmm_kv_attention", ENTRY(kKvAttention),
+     "apmm_kv_attention(q, codes, scales, page_table, lengths, starts=None, window=0, sinks=0, scale=None, out=None, workspace=None)\n--\n\n"
+     "Causal attention of the new tokens' queries over the cache, which holds their keys and values already."},
     {"set_library", set_library, METH_VARARGS, nullptr},
     {"set_general", set_general, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr},
