@@ -87,6 +87,11 @@ apmm_status check_heads(const apmm_kv_cache *cache, const apmm_kv_batch *batch, 
     return APMM_OK;
 }
 
+size_t partial_bytes(const apmm::KvPlan &plan, const apmm::KvArgs &a)
+{
+    return apmm::kv_partial_bytes(plan.rows, a.heads, a.head_dim) + apmm::kv_partial_bytes(plan.tiles, a.heads, a.head_dim);
+}
+
 }  // namespace
 
 extern "C" {
@@ -120,7 +125,7 @@ size_t apmm_kv_attention_workspace_bytes(const apmm_kv_cache *cache, const apmm_
     apmm::KvArgs a;
     apmm::KvPlan plan;
     if (check_sizes(cache, batch, a) != APMM_OK || batch->sequences == 0 || batch->tokens == 0 || check_heads(cache, batch, a, q_heads, plan) != APMM_OK) return 0;
-    return apmm::kv_partial_bytes(plan, cache->kv_heads, cache->head_dim);
+    return partial_bytes(plan, a);
 }
 
 apmm_status apmm_kv_attention(const apmm_kv_cache *cache, const apmm_kv_batch *batch, int q_heads, const void *q, int64_t q_token_stride,
@@ -138,7 +143,7 @@ apmm_status apmm_kv_attention(const apmm_kv_cache *cache, const apmm_kv_batch *b
     if (window > apmm::kKvMost || sinks > apmm::kKvMost) return fail(APMM_ERR_UNSUPPORTED, "kv_attention: window or sinks > 2^30");
     if (empty) return APMM_OK;
     if ((st = check_tensor(q, q_token_stride, q_head_stride, a.q)) != APMM_OK || (st = check_tensor(out, out_token_stride, out_head_stride, a.out)) != APMM_OK) return st;
-    const size_t need = apmm::kv_partial_bytes(plan, cache->kv_heads, cache->head_dim);
+    const size_t need = partial_bytes(plan, a.c);
     if (need && (!workspace || workspace_bytes < need)) return fail(APMM_ERR_WORKSPACE, "kv_attention: needs a workspace of apmm_kv_attention_workspace_bytes() bytes");
     if (need && !aligned(workspace, 16)) return fail(APMM_ERR_INVALID_ARG, "kv_attention: workspace must be 16-byte aligned");
     a.groups = q_heads / cache->kv_heads;

@@ -41,26 +41,28 @@ struct KvAttentionArgs {
     float *partial;    // results of pieces of sequences: see KvPlan
 };
 
-// How the work of an attention call is cut.  Rows are the queries of the heads that share a key/value head, `tile` of them to a workgroup; the keys that a tile sees are cut in
-// pieces of at least `least` steps so that there are about `target` workgroups for each key/value head whatever the lengths are, which the host does not know.
-struct KvPlan {
-    int tile;    // rows of a workgroup
+// How the work of an attention call is cut.  Rows are the queries of the heads that share a key/value head; a kernel takes the sequences with `from_rows` to `to_rows` of them, `tile` rows
+// to a workgroup.  The keys that a tile sees are cut in pieces of at least `least` steps so that there are about `target` workgroups for each key/value head whatever the lengths
+// are, which the host does not know.
+struct KvPart {
+    int tile;    // rows of a workgroup; 0: the kernel is not launched
     int waves;   // of a workgroup
     int target;  // 0: nothing is cut
     int least;
     int slots;   // most pieces there can be
+    int from_rows, to_rows;
+};
+struct KvPlan {
+    KvPart rows, tiles;  // kv_attention_rows_kernel's, kv_attention_tiles_kernel's
 };
 KvPlan kv_plan(const KvArgs &c, int groups);
-// Workspace of a call that cuts: for every piece and head the sums of `tile` rows, base and total of each row, and a KvPieceNote
-size_t kv_partial_bytes(const KvPlan &plan, int heads, int head_dim);
+size_t kv_partial_bytes(const KvPart &part, int heads, int head_dim);  // of the workspace that pieces take
 
 hipError_t launch_kv_write(const KvArgs &c, const KvTensor &k, const KvTensor &v, hipStream_t stream);
 hipError_t launch_kv_read(const KvArgs &c, const KvTensor &k, const KvTensor &v, hipStream_t stream);
 hipError_t launch_kv_attention(const KvAttentionArgs &a, const KvPlan &plan, hipStream_t stream);
 
 #ifdef __HIPCC__
-constexpr int kKvStep = 32;  // keys of one step of attention
-
 // Place of lane `lane` within its wave of a workgroup of whole waves
 __device__ __forceinline__ int kv_lane() { return threadIdx.x & 63; }
 

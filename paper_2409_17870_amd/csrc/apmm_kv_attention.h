@@ -26,8 +26,11 @@ namespace apmm {
 constexpr int kRowsTile = 16;    // rows of a workgroup of kv_attention_rows_kernel
 constexpr int kTilesTile = 128;  // and of kv_attention_tiles_kernel
 
-hipError_t launch_kv_attention_rows(const KvAttentionArgs &a, const KvPlan &plan, hipStream_t stream);
-hipError_t launch_kv_attention_tiles(const KvAttentionArgs &a, const KvPlan &plan, hipStream_t stream);
+constexpr int kRowsStep = 32;    // keys of one step
+constexpr int kTilesStep = 64;
+
+hipError_t launch_kv_attention_rows(const KvAttentionArgs &a, const KvPart &part, hipStream_t stream);
+hipError_t launch_kv_attention_tiles(const KvAttentionArgs &a, const KvPart &part, hipStream_t stream);
 
 #ifdef __HIPCC__
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
@@ -39,39 +42,27 @@ typedef float float16v __attribute__((ext_vector_type(16)));
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kSlack = 6.0f, kRoom = 9.0f;
 
-// A workgroup's part of the call: keys of steps `from` to `to` - 1 (of kKvStep keys, the hidden ones between the first tokens and the window left out) for rows of one sequence
+// A workgroup's part of the call: keys of steps `from` to `to` - 1 (of STEP keys, the hidden ones between the first tokens and the window left out) for rows of one sequence
+template <int STEP>
 struct KvItem {
     KvSequence s;
     int b, row0, rows;   // first row, rows that there are from there on (may be more than a tile)
     int from, to;
     int sink_steps, gap; // step v lies at v < sink_steps ? v : v + gap
-    int pieces, part, slot;
-    __device__ __forceinline__ int key_of(int v) const { return (v < sink_steps ? v : v + gap) * kKvStep; }
+    int pieces, part;    // of the tile; which this is
+    __device__ __forceinline__ int key_of(int v) const { return (v < sink_steps ? v : v + gap) * STEP; }
 };
-
-// Steps of one tile whose queries lie at positions first_pos to last_pos
-struct KvSteps {
-    int sink_steps, gap, count;
-};
-__device__ __forceinline__ KvSteps kv_steps(const KvAttentionArgs &a, const KvSequence &s, int first_pos, int last_pos)
-{
-    KvSteps r;
-    const int end = min(last_pos + 1, s.keys), steps = end > 0 ? (end + kKvStep - 1) / kKvStep : 0;
-    const int low = min(a.window ? max(first_pos - a.window + 1, 0) / kKvStep : 0, steps);
-    r.sink_steps = min((int)(((int64_t)a.sinks + kKvStep - 1) / kKvStep), low);
-    r.gap = low - r.sink_steps;
-    r.count = steps - r.gap;
-    return r;
-}
 
 // Tiles of a sequence, and steps of the one with most (or a few more)
-__device__ __forceinline__ void kv_extent(const KvAttentionArgs &a, const KvSequence &s, int tile, int &tiles, int &steps)
+template <int STEP>
+__device__ __forceinline__ void kv_extent(const KvAttentionArgs &a, const KvSequence &s, const KvPart &p, int &tiles, int &steps)
 {
-    tiles = (int)(((int64_t)s.n * a.groups + tile - 1) / tile);
-    steps = (s.keys + kKvStep - 1) / kKvStep;
+    const int rows = s.n * a.groups;
+    tiles = rows >= p.from_rows && rows <= p.to_rows ? (rows + p.tile - 1) / p.tile : 0;
+    steps = (s.keys + STEP - 1) / STEP;
     if (a.window) {
-        const int64_t span = (int64_t)a.window + (tile + a.groups - 2) / a.groups;  // positions that the queries of a tile see, without the first tokens
-        steps = (int)min((int64_t)steps, (span + kKvStep - 1) / kKvStep + 1 + ((int64_t)a.sinks + kKvStep - 1) / kKvStep);
+        const int64_t span = (int64_t)a.window + (p.tile + a.groups - 2) / a.groups;  // positions that the queries of a tile see, without the first tokens
+        steps = (int)min((int64_t)steps, (span + STEP - 1) / STEP + 1 + ((int64_t)a.sinks + STEP - 1) / STEP);
     }
     if (!tiles) steps = 0;
 }
@@ -79,24 +70,25 @@ __device__ __forceinline__ void kv_extent(const KvAttentionArgs &a, const KvSequ
 __device__ __forceinline__ int kv_pieces(int steps, int piece) { return steps > piece ? (steps + piece - 1) / piece : 1; }
 
 // Piece `slot` of the call; false: there is none
-__device__ __forceinline__ bool kv_item(const KvAttentionArgs &a, const KvPlan &plan, int slot, KvItem &it)
+template <int STEP>
+__device__ __forceinline__ bool kv_item(const KvAttentionArgs &a, const KvPart &p, int slot, KvItem<STEP> &it)
 {
     const int lane = kv_lane();
     int piece = 0x7fffffff, tiles, steps;
     KvSequence s = {};
     if (lane < a.c.sequences) s = kv_sequence(a.c, lane);  // the first 64 stay in registers
-    kv_extent(a, s, plan.tile, tiles, steps);
-    if (plan.target) {
+    kv_extent<STEP>(a, s, p, tiles, steps);
+    if (p.target) {
         float work = (float)tiles * (float)steps;
         for (int at = lane + 64; at < a.c.sequences; at += 64) {
             int t, n;
-            kv_extent(a, kv_sequence(a.c, at), plan.tile, t, n);
+            kv_extent<STEP>(a, kv_sequence(a.c, at), p, t, n);
             work += (float)t * (float)n;
         }
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) work += __shfl_xor(work, d);
         // (rounding: a piece may be 2^-20 shorter than the work asks for, for which there is one slot more)
-        piece = __builtin_amdgcn_readfirstlane(max((int)ceilf(fminf(work / (float)plan.target * (1.0f - 0x1p-20f), 0x1p30f)), plan.least));
+        piece = __builtin_amdgcn_readfirstlane(max((int)ceilf(fminf(work / (float)p.target * (1.0f - 0x1p-20f), 0x1p30f)), p.least));
     }
     int rest, l;
     const int own = tiles * kv_pieces(steps, piece), to = kv_scan(own);
@@ -114,26 +106,26 @@ __device__ __forceinline__ bool kv_item(const KvAttentionArgs &a, const KvPlan &
         auto count = [&](int at) {
             int t, n;
             if (at + 64 >= a.c.sequences) return 0;
-            kv_extent(a, kv_sequence(a.c, at + 64), plan.tile, t, n);
+            kv_extent<STEP>(a, kv_sequence(a.c, at + 64), p, t, n);
             return t * kv_pieces(n, piece);
         };
         if (a.c.sequences <= 64 || !kv_find(a.c.sequences - 64, slot - before, it.b, rest, count)) return false;
         it.b += 64;
         it.s = kv_sequence(a.c, it.b);
     }
-    kv_extent(a, it.s, plan.tile, tiles, steps);
-    it.slot = slot;
+    kv_extent<STEP>(a, it.s, p, tiles, steps);
     it.pieces = kv_pieces(steps, piece);
-    const int tile = tiles - 1 - rest / it.pieces, part = rest % it.pieces;  // (the last queries see the most keys: those first)
-    it.part = part;
-    it.row0 = tile * plan.tile;
+    const int tile = tiles - 1 - rest / it.pieces;  // (the last queries see the most keys: those first)
+    it.part = rest % it.pieces;
+    it.row0 = tile * p.tile;
     it.rows = it.s.n * a.groups - it.row0;
-    const int last = min(it.rows, plan.tile) - 1;
-    const KvSteps r = kv_steps(a, it.s, it.s.first + it.row0 / a.groups, it.s.first + (it.row0 + last) / a.groups);
-    it.sink_steps = r.sink_steps;
-    it.gap = r.gap;
-    it.from = min(part * (int64_t)piece, (int64_t)r.count);
-    it.to = min((part + 1) * (int64_t)piece, (int64_t)r.count);
+    const int last = min(it.rows, p.tile) - 1, first_pos = it.s.first + it.row0 / a.groups, last_pos = it.s.first + (it.row0 + last) / a.groups;
+    const int end = min(last_pos + 1, it.s.keys), all = end > 0 ? (end + STEP - 1) / STEP : 0;
+    const int low = min(a.window ? max(first_pos - a.window + 1, 0) / STEP : 0, all);
+    it.sink_steps = min((a.sinks + STEP - 1) / STEP, low);
+    it.gap = low - it.sink_steps;
+    it.from = min(it.part * (int64_t)piece, (int64_t)all - it.gap);
+    it.to = min((it.part + 1) * (int64_t)piece, (int64_t)all - it.gap);
     return true;
 }
 
@@ -146,21 +138,22 @@ struct KvPartial {
     float2 *row;        // [slot][head][tile row]: base and total; the row is sum_i 2^base_i sums_i / sum_i 2^base_i total_i over its pieces
     KvPieceNote *note;  // [slot][head]
 };
-__host__ __device__ inline KvPartial kv_partial(float *at, const KvPlan &plan, int heads, int head_dim)
+__host__ __device__ inline KvPartial kv_partial(float *at, const KvPart &part, int heads, int head_dim)
 {
-    const int64_t rows = (int64_t)plan.slots * heads * plan.tile;
+    const int64_t rows = (int64_t)part.slots * heads * part.tile;
     KvPartial p;
     p.sums = at;
     p.row = reinterpret_cast<float2 *>(at + rows * head_dim);
     p.note = reinterpret_cast<KvPieceNote *>(p.row + rows);
     return p;
 }
-__device__ __forceinline__ void kv_note(const KvAttentionArgs &a, const KvPlan &plan, int slot, int head, bool there, const KvItem &it)
+template <int STEP>
+__device__ __forceinline__ void kv_note(const KvAttentionArgs &a, const KvPart &p, int slot, int head, bool there, const KvItem<STEP> &it)
 {
-    if (!plan.target || threadIdx.x) return;
+    if (!p.target || threadIdx.x) return;
     KvPieceNote n = {};
-    if (there && it.part == 0 && it.pieces > 1) n = {it.s.start, it.row0, min(it.rows, plan.tile), it.pieces};
-    kv_partial(a.partial, plan, a.c.heads, a.c.head_dim).note[(int64_t)slot * a.c.heads + head] = n;
+    if (there && it.part == 0 && it.pieces > 1) n = {it.s.start, it.row0, min(it.rows, p.tile), it.pieces};
+    kv_partial(a.partial, p, a.c.heads, a.c.head_dim).note[(int64_t)slot * a.c.heads + head] = n;
 }
 
 // Four words of a matrix operand from one word of codes: nibbles 0 and 4, 1 and 5, 2 and 6, 3 and 7, those of even number as u 2^-24, of odd number as u 2^-20
@@ -221,12 +214,13 @@ __device__ __forceinline__ void kv_queries(const uint32_t (&x)[N], float scale, 
     factor = ldexpf(scale * 1.44269504088896341f, min(21 - e, 122));  // (queries of 2^115 and more: scores beyond any other's all the same)
 }
 
-// Page of half a step (16 keys); lane i of `ids` has that of half step i of the next 32 steps of a wave
-__device__ __forceinline__ int kv_page_ids(const KvAttentionArgs &a, const KvItem &it, int v, int stride)
+// Pages of 16 keys each: lane i of the result has that of the i-th sixteen of the next steps of a wave (v, v + stride, ...), -1 where there is none
+template <int STEP>
+__device__ __forceinline__ int kv_page_ids(const KvAttentionArgs &a, const KvItem<STEP> &it, int v, int stride)
 {
-    const int step = v + (kv_lane() >> 1) * stride;
+    const int step = v + kv_lane() / (STEP / 16) * stride;
     if (step >= it.to) return -1;
-    const int key = it.key_of(step) + 16 * (kv_lane() & 1);
+    const int key = it.key_of(step) + 16 * (kv_lane() % (STEP / 16));
     if (key >= it.s.keys) return -1;
     const int page = a.c.table[it.b * a.c.table_stride + (key >> a.c.page_shift)];
     return page < a.c.pages ? page : -1;

@@ -7,15 +7,17 @@ namespace apmm {
 
 namespace {
 
+constexpr int kFewRows = 32;  // of a sequence: those go to kv_attention_rows_kernel
+
 // A workgroup looks at one piece and head (blockIdx.x) and 16 rows of its tile (blockIdx.y), and has work where the piece is the first of several.  16 lanes to a row; what is left of
 // the 256 for fewer rows shares out the pieces, each with its own running base, and meets in LDS.
 template <int D, bool BF16>
-__global__ __launch_bounds__(256) void kv_attention_join_kernel(KvAttentionArgs a, KvPlan plan)
+__global__ __launch_bounds__(256) void kv_attention_join_kernel(KvAttentionArgs a, KvPart part)
 {
     constexpr int C = D / 16;  // channels of a lane
     __shared__ float bases[16][16], totals[16][16];  // by threadIdx.x / 16: share of the pieces, row
     __shared__ __align__(16) float sums[256][C];
-    const KvPartial partial = kv_partial(a.partial, plan, a.c.heads, D);
+    const KvPartial partial = kv_partial(a.partial, part, a.c.heads, D);
     const KvPieceNote note = partial.note[blockIdx.x];
     const int first_row = blockIdx.y * 16, rows = min(note.rows - first_row, 16);
     if (note.pieces == 0 || rows <= 0) return;
@@ -24,7 +26,7 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(KvAttentionArgs 
     const int head = blockIdx.x % a.c.heads;
     float base = kLowest, total = 0.0f, o[C] = {};
     if (row < rows) {
-        const int64_t place = (int64_t)blockIdx.x * plan.tile + first_row + row, step = (int64_t)a.c.heads * plan.tile;
+        const int64_t place = (int64_t)blockIdx.x * part.tile + first_row + row, step = (int64_t)a.c.heads * part.tile;
 #pragma unroll 4
         for (int i = share; i < note.pieces; i += shares) {
             const int64_t at = place + i * step;
@@ -67,48 +69,74 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(KvAttentionArgs 
 
 }  // namespace
 
+namespace {
+
+// The workgroups of one kernel for sequences of at most `tokens` new tokens in all
+void cut(KvPart &p, const KvArgs &c, int groups, int step, int wanted)
+{
+    const int64_t rows = (int64_t)c.tokens * groups;
+    const int64_t tiles = std::min<int64_t>((int64_t)c.tokens * ((groups + p.tile - 1) / p.tile), rows / p.tile + c.sequences);
+    const int64_t most_steps = (((int64_t)c.width << c.page_shift) + step - 1) / step;  // of a sequence, as far as the page table goes
+    p.target = tiles * c.heads >= 4 * (int64_t)wanted || most_steps <= p.least ? 0 : std::max(wanted / c.heads, 1);
+    p.slots = (int)(tiles + (p.target ? p.target + 1 : 0));
+}
+
+template <int D, bool BF16>
+void join(const KvAttentionArgs &a, const KvPart &part, hipStream_t stream)
+{
+    kv_attention_join_kernel<D, BF16><<<dim3((uint32_t)((int64_t)part.slots * a.c.heads), part.tile / 16), dim3(256), 0, stream>>>(a, part);
+}
+
+}  // namespace
+
 KvPlan kv_plan(const KvArgs &c, int groups)
 {
-    KvPlan p;
-    const int64_t rows = (int64_t)c.tokens * groups, sequences = c.sequences;
-    p.tile = rows <= 32 * sequences ? kRowsTile : kTilesTile;
-    const int64_t tiles = std::min<int64_t>((int64_t)c.tokens * ((groups + p.tile - 1) / p.tile), rows / p.tile + sequences), work = tiles * c.heads;
-    const int64_t most_steps = (((int64_t)c.width << c.page_shift) + kKvStep - 1) / kKvStep;  // of a sequence, as far as the page table goes
-    int64_t wanted;
-    if (p.tile == kRowsTile) {
-        p.waves = work >= 512 ? 4 : 8;
-        p.least = p.waves == 4 ? 32 : 64;
-        wanted = p.waves == 4 ? 2048 : 256;
-    } else {
-        p.waves = 4;
-        p.least = 16;
-        wanted = 512;
+    KvPlan p = {};
+    const int64_t rows = (int64_t)c.tokens * groups;
+    // A sequence's rows are as many as the call's where it is the only one, and no more than one token's where there is no other: else both kernels are launched
+    const bool few = rows <= kFewRows || c.tokens <= c.sequences, many = !few && c.sequences == 1;
+    if (!many) {
+        p.rows.tile = kRowsTile;
+        p.rows.to_rows = few ? INT32_MAX : kFewRows;
+        const int64_t groups_of = std::min<int64_t>((int64_t)c.sequences, c.tokens) * c.heads * ((std::min<int64_t>(groups, rows) + kRowsTile - 1) / kRowsTile);
+        p.rows.waves = groups_of >= 512 ? 4 : 8;
+        p.rows.least = 64;
+        cut(p.rows, c, groups, kRowsStep, p.rows.waves == 4 ? 2048 : 256);
     }
-    p.target = work >= 4 * wanted || most_steps <= p.least ? 0 : (int)std::max<int64_t>(wanted / c.heads, 1);
-    p.slots = (int)(tiles + (p.target ? p.target + 1 : 0));
+    if (!few) {
+        p.tiles.tile = kTilesTile;
+        p.tiles.waves = 4;
+        p.tiles.from_rows = many ? 0 : kFewRows + 1;
+        p.tiles.to_rows = INT32_MAX;
+        p.tiles.least = 8;
+        cut(p.tiles, c, groups, kTilesStep, 512);
+    }
     return p;
 }
 
-size_t kv_partial_bytes(const KvPlan &plan, int heads, int head_dim)
+size_t kv_partial_bytes(const KvPart &part, int heads, int head_dim)
 {
-    if (!plan.target) return 0;
-    const KvPartial p = kv_partial(nullptr, plan, heads, head_dim);
-    return reinterpret_cast<size_t>(p.note + (int64_t)plan.slots * heads);
+    if (!part.tile || !part.target) return 0;
+    const KvPartial p = kv_partial(nullptr, part, heads, head_dim);
+    return reinterpret_cast<size_t>(p.note + (int64_t)part.slots * heads);
 }
 
 hipError_t launch_kv_attention(const KvAttentionArgs &a, const KvPlan &plan, hipStream_t stream)
 {
-    const hipError_t e = plan.tile == kRowsTile ? launch_kv_attention_rows(a, plan, stream) : launch_kv_attention_tiles(a, plan, stream);
-    if (e != hipSuccess || !plan.target) return e;
-    const dim3 grid((uint32_t)((int64_t)plan.slots * a.c.heads), plan.tile / 16), block(256);
-    if (a.c.head_dim == 128) {
-        if (a.c.bf16) kv_attention_join_kernel<128, true><<<grid, block, 0, stream>>>(a, plan);
-        else kv_attention_join_kernel<128, false><<<grid, block, 0, stream>>>(a, plan);
-    } else {
-        if (a.c.bf16) kv_attention_join_kernel<64, true><<<grid, block, 0, stream>>>(a, plan);
-        else kv_attention_join_kernel<64, false><<<grid, block, 0, stream>>>(a, plan);
+    KvAttentionArgs b = a;
+    for (const KvPart *part : {&plan.rows, &plan.tiles}) {
+        if (!part->tile) continue;
+        const hipError_t e = part == &plan.rows ? launch_kv_attention_rows(b, *part, stream) : launch_kv_attention_tiles(b, *part, stream);
+        if (e != hipSuccess) return e;
+        if (part->target) {
+            if (a.c.head_dim == 128) a.c.bf16 ? join<128, true>(b, *part, stream) : join<128, false>(b, *part, stream);
+            else a.c.bf16 ? join<64, true>(b, *part, stream) : join<64, false>(b, *part, stream);
+            const hipError_t j = hipGetLastError();
+            if (j != hipSuccess) return j;
+        }
+        b.partial += kv_partial_bytes(*part, a.c.heads, a.c.head_dim) / sizeof(float);
     }
-    return hipGetLastError();
+    return hipSuccess;
 }
 
 }  // namespace apmm

@@ -18,7 +18,7 @@ struct Step {
 };
 
 template <int D, bool BF16, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 2) void kv_attention_rows_kernel(KvAttentionArgs a, KvPlan plan)
+__global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 2) void kv_attention_rows_kernel(KvAttentionArgs a, KvPart part)
 {
     constexpr int W = D / 32, V = D / 64, T = kRowsTile;
     constexpr int R = 4, kPitch = D + 4;  // rows that meet in LDS at a time
@@ -26,9 +26,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 2) void kv_attention_r
     __shared__ float bases[WAVES][T], totals[WAVES][T];
     const int head = blockIdx.x % a.c.heads, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = kv_lane(), n = lane & 15, g = lane >> 4;
     const int slot = blockIdx.x / a.c.heads;
-    KvItem it;
-    const bool there = kv_item(a, plan, slot, it);
-    kv_note(a, plan, slot, head, there, it);
+    KvItem<kRowsStep> it;
+    const bool there = kv_item(a, part, slot, it);
+    kv_note(a, part, slot, head, there, it);
     if (!there) return;
 
     const int rows = min(it.rows, T), row = it.row0 + min(n, rows - 1), at = row / a.groups;
@@ -108,8 +108,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 2) void kv_attention_r
         float x[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = fmaf(sc[i / 4][i % 4], i & 1 ? kv_high<BF16>(ks[i / 2]) : kv_low<BF16>(ks[i / 2]), 0.0f);
-        const bool all = key0 + kKvStep <= it.s.keys && key0 + kKvStep - 1 <= first_pos && page0 >= 0 && page1 >= 0 &&
-                         (!a.window || key0 > last_pos - a.window || key0 + kKvStep <= a.sinks);
+        const bool all = key0 + kRowsStep <= it.s.keys && key0 + kRowsStep - 1 <= first_pos && page0 >= 0 && page1 >= 0 &&
+                         (!a.window || key0 > last_pos - a.window || key0 + kRowsStep <= a.sinks);
         if (!all) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -181,7 +181,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 2) void kv_attention_r
     }
     constexpr int kThreads = 64 * WAVES, C = kThreads >= R * D ? 1 : R * D / kThreads;  // channels of a thread
     const int mine = threadIdx.x / (D / C), c0 = threadIdx.x % (D / C) * C;
-    const KvPartial partial = kv_partial(a.partial, plan, a.c.heads, D);
+    const KvPartial partial = kv_partial(a.partial, part, a.c.heads, D);
     for (int r0 = 0; r0 < rows; r0 += R) {
         if ((n & ~(R - 1)) == r0) {
 #pragma unroll
@@ -227,24 +227,24 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 2) void kv_attention_r
 }
 
 template <int WAVES>
-void launch(const KvAttentionArgs &a, const KvPlan &plan, hipStream_t stream)
+void launch(const KvAttentionArgs &a, const KvPart &part, hipStream_t stream)
 {
-    const dim3 grid((uint32_t)((int64_t)plan.slots * a.c.heads)), block(64 * WAVES);
+    const dim3 grid((uint32_t)((int64_t)part.slots * a.c.heads)), block(64 * WAVES);
     if (a.c.head_dim == 128) {
-        if (a.c.bf16) kv_attention_rows_kernel<128, true, WAVES><<<grid, block, 0, stream>>>(a, plan);
-        else kv_attention_rows_kernel<128, false, WAVES><<<grid, block, 0, stream>>>(a, plan);
+        if (a.c.bf16) kv_attention_rows_kernel<128, true, WAVES><<<grid, block, 0, stream>>>(a, part);
+        else kv_attention_rows_kernel<128, false, WAVES><<<grid, block, 0, stream>>>(a, part);
     } else {
-        if (a.c.bf16) kv_attention_rows_kernel<64, true, WAVES><<<grid, block, 0, stream>>>(a, plan);
-        else kv_attention_rows_kernel<64, false, WAVES><<<grid, block, 0, stream>>>(a, plan);
+        if (a.c.bf16) kv_attention_rows_kernel<64, true, WAVES><<<grid, block, 0, stream>>>(a, part);
+        else kv_attention_rows_kernel<64, false, WAVES><<<grid, block, 0, stream>>>(a, part);
     }
 }
 
 }  // namespace
 
-hipError_t launch_kv_attention_rows(const KvAttentionArgs &a, const KvPlan &plan, hipStream_t stream)
+hipError_t launch_kv_attention_rows(const KvAttentionArgs &a, const KvPart &part, hipStream_t stream)
 {
-    if (plan.waves == 4) launch<4>(a, plan, stream);
-    else launch<8>(a, plan, stream);
+    if (part.waves == 4) launch<4>(a, part, stream);
+    else launch<8>(a, part, stream);
     return hipGetLastError();
 }
 
