@@ -9,8 +9,8 @@
 //                       from, and 15 times the sum of the weights is taken off the second one's result.
 //   Queries             times a power of two for each row, so that its largest number is just below 2^11 (2^15 for the channels that meet u 2^-24): binary16 numbers as they are, bfloat16
 //                       ones exactly as far as 2^-35 of the row's largest.
-//   Weights             p_j b_j, rounded once to binary16 (bfloat16 would cost an output of binary16 numbers eight times its own rounding).  The value scales may lie anywhere, so a
-//                       wave holds a power of two 2^E above all that it has met, and weights carry the factor 2^(9 - E) until the end: at most 2^15, and 2^-21 of the largest without loss.
+//   Weights             p_j b_j, rounded once to binary16 (bfloat16 would cost an output of binary16 numbers eight times its own rounding).  The value scales may lie anywhere, so
+//                       each row holds a power of two 2^E above all that it has met, and weights carry the factor 2^(9 - E) until the end: at most 2^15, and 2^-21 of the largest without loss.
 //                       The sum of the rounded weights goes with them (dot products with ones).
 //   Running maximum     m (and E) are only moved where a score passes m + 6: until then weights are at most 2^6 times larger, for which there is room.  Then the accumulators are scaled;
 //                       -m + 9 - E is one number, `base`.
@@ -27,7 +27,7 @@ constexpr int kRowsTile = 16;    // rows of a workgroup of kv_attention_rows_ker
 constexpr int kTilesTile = 128;  // and of kv_attention_tiles_kernel
 
 constexpr int kRowsStep = 32;    // keys of one step
-constexpr int kTilesStep = 64;
+constexpr int kTilesStep = 32;
 
 hipError_t launch_kv_attention_rows(const KvAttentionArgs &a, const KvPart &part, hipStream_t stream);
 hipError_t launch_kv_attention_tiles(const KvAttentionArgs &a, const KvPart &part, hipStream_t stream);
@@ -40,7 +40,7 @@ typedef float float4v __attribute__((ext_vector_type(4)));
 typedef float float16v __attribute__((ext_vector_type(16)));
 
 constexpr float kLowest = -3.402823466e38f;
-constexpr float kSlack = 6.0f, kRoom = 9.0f;
+constexpr float kSlack = 11.0f, kRoom = 4.0f;
 
 // A workgroup's part of the call: keys of steps `from` to `to` - 1 (of STEP keys, the hidden ones between the first tokens and the window left out) for rows of one sequence
 template <int STEP>
@@ -178,38 +178,37 @@ __device__ __forceinline__ float kv_low(uint32_t w) { return BF16 ? __uint_as_fl
 template <bool BF16>
 __device__ __forceinline__ float kv_high(uint32_t w) { return BF16 ? __uint_as_float(w & 0xffff0000u) : (float)__builtin_bit_cast(half2v, w)[1]; }
 
-// The queries of a lane as operand words: x holds 8 channels to 4 words in their order.  `across` folds a value over the lanes that share the row.
+// The larger of m and a magnitude's bits, if that is finite
+template <bool BF16>
+__device__ __forceinline__ uint32_t kv_finite_max(uint32_t m, uint32_t bits)
+{
+    return bits < (BF16 ? 0x7f80u : 0x7c00u) ? max(m, bits) : m;
+}
+// The queries of a lane as operand words: x holds 8 channels to 4 words in their order.  max_across and sum_across fold a value over the lanes that share the row.
 template <int N, bool BF16, class Max, class Sum>
 __device__ __forceinline__ void kv_queries(const uint32_t (&x)[N], float scale, Max max_across, Sum sum_across, half8 (&q)[N / 4], float &init, float &factor)
 {
-    float top = 0.0f;
+    uint32_t bits = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const float a = fabsf(kv_low<BF16>(x[i])), b = fabsf(kv_high<BF16>(x[i]));
-        top = fmaxf(top, a <= -kLowest ? a : 0.0f);
-        top = fmaxf(top, b <= -kLowest ? b : 0.0f);
-    }
-    top = max_across(top);
+    for (int i = 0; i < N; ++i) bits = kv_finite_max<BF16>(kv_finite_max<BF16>(bits, x[i] & 0x7fffu), (x[i] >> 16) & 0x7fffu);
+    const float top = max_across(kv_scale_value(bits, BF16));
     int e = top > 0.0f ? 11 - (int)((__float_as_uint(top) >> 23) - 126u) : 0;  // top 2^e < 2^11
     e = min(e, 100);                                                         // (a row of subnormal numbers)
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < N / 4; ++i) {
-        float f[8];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            f[2 * j] = ldexpf(kv_low<BF16>(x[4 * i + j]), e);
-            f[2 * j + 1] = ldexpf(kv_high<BF16>(x[4 * i + j]), e);
-        }
+        __builtin_amdgcn_sched_barrier(0);  // a few registers at a time
         uint32_t w[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float by = j & 1 ? 1.0f : 16.0f, back = j & 1 ? 1.0f : 0.0625f;
-            w[j] = kv_half_pair(f[j] * by, f[j + 4] * by);
-            sum += (kv_low<false>(w[j]) + kv_high<false>(w[j])) * back;
+        for (int j = 0; j < 4; ++j) {  // channels j and j + 4
+            const uint32_t a = x[4 * i + j / 2], b = x[4 * i + j / 2 + 2];
+            const int by = j & 1 ? e : e + 4;
+            w[j] = kv_half_pair(ldexpf(j & 1 ? kv_high<BF16>(a) : kv_low<BF16>(a), by), ldexpf(j & 1 ? kv_high<BF16>(b) : kv_low<BF16>(b), by));
+            sum = fmaf(kv_low<false>(w[j]) + kv_high<false>(w[j]), j & 1 ? 1.0f : 0.0625f, sum);
         }
         q[i] = __builtin_bit_cast(half8, make_uint4(w[0], w[1], w[2], w[3]));
     }
+    __builtin_amdgcn_sched_barrier(0);
     init = -7.5f * 0x1p-20f * sum_across(sum);
     factor = ldexpf(scale * 1.44269504088896341f, min(21 - e, 122));  // (queries of 2^115 and more: scores beyond any other's all the same)
 }
@@ -231,11 +230,6 @@ __device__ __forceinline__ uint32_t kv_fold_max(uint32_t m, uint32_t w)
 {
     typedef unsigned short us2 __attribute__((ext_vector_type(2)));
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(us2, m), __builtin_bit_cast(us2, w)));
-}
-template <bool BF16>
-__device__ __forceinline__ uint32_t kv_finite_max(uint32_t m, uint32_t bits)
-{
-    return bits < (BF16 ? 0x7f80u : 0x7c00u) ? max(m, bits) : m;
 }
 // E of a largest scale: s < 2^E.  Held above -80, so that sums of 2^(9 - E) stay in range (scales below 2^-103 lose bits).
 template <bool BF16>

@@ -108,7 +108,7 @@ KvPlan kv_plan(const KvArgs &c, int groups)
         p.tiles.waves = 4;
         p.tiles.from_rows = many ? 0 : kFewRows + 1;
         p.tiles.to_rows = INT32_MAX;
-        p.tiles.least = 8;
+        p.tiles.least = 16;
         cut(p.tiles, c, groups, kTilesStep, 512);
     }
     return p;

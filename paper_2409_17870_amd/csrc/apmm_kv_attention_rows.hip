@@ -80,7 +80,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 2) void kv_attention_r
 #pragma unroll
         for (int i = 0; i < V; ++i) acc[e][i] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
     float top = kLowest, base = -kLowest, total = 0.0f, weights = 0.0f;
-    uint32_t limit = 0, met = 0;  // largest scale of values: where it is passed, met so far
+    uint32_t limit = 0, met = 0;  // scales of values that the row has met: the largest, and the largest that needs no other E
 
     auto step = [&](const Step<D> &cur, Step<D> &next) {
         const int key0 = it.key_of(v), page0 = __builtin_amdgcn_readlane(ids, id), page1 = __builtin_amdgcn_readlane(ids, id + 1);
@@ -126,8 +126,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 2) void kv_attention_r
             uint32_t m = met;
 #pragma unroll
             for (int i = 0; i < 4; ++i) m = kv_finite_max<BF16>(kv_finite_max<BF16>(m, vs[i] & 0xffffu), vs[i] >> 16);
-#pragma unroll
-            for (int d = 1; d < 64; d *= 2) m = max(m, (uint32_t)__shfl_xor((int)m, d));  // (rows see different keys where some are hidden)
+            m = max(m, (uint32_t)__shfl_xor((int)m, 16));
+            m = max(m, (uint32_t)__shfl_xor((int)m, 32));
             met = m;
             limit = kv_limit<BF16>(met);
             const float to = -top + (kRoom - (float)kv_exponent<BF16>(met));

@@ -1,7 +1,13 @@
 // Attention of many rows over the four-bit cache (apmm_kv_attention.h): prompts and pieces of prompts.
 //
-// A workgroup has 128 rows, 32 to each of its four waves, and goes through the keys in steps of 64 with matrix instructions 32 x 32 x 16.  Codes become operands once for all four waves:
-// each wave loads a quarter of a step one step ahead, makes its operands and leaves them in LDS, in the order in which lanes take them (no bank is asked twice).  Two buffers, one barrier a step.
+// A workgroup has 128 rows, 32 to each of its four waves, which go through the keys by themselves in steps of 32 with matrix instructions 32 x 32 x 16: codes come from memory (L1 and L2: the
+// waves and the workgroups of a head read the same) into registers and become operands there, no barrier anywhere.  Only the scales, which lanes need sixteen of, go through a little LDS of the wave.
+//
+// What bounds it is the vector unit: of a step's about 190 instructions 80 unpack codes and 92 are the weights of 16 keys a lane (product with the scale, exponent, power, sum, product with the
+// value's scale and rounding, sum of the rounded ones).  Hence a step that has no hidden keys does not look for the maximum of its scores either: its sums tell afterwards whether a weight was too
+// large for the running maximum.  Every other step (the first, those at the diagonal and at the window's edge, those whose sums are too large) goes the general way.
+#include <type_traits>
+
 #include "apmm_kv_attention.h"
 
 namespace apmm {
@@ -10,19 +16,37 @@ namespace {
 
 constexpr int kWaves = 4, kRows = kTilesTile / kWaves;
 
-// 32 keys and values as matrix operands, 64 lanes x 16 bytes each, and their scales
-template <int D>
-struct Operands {
-    uint4 k[D / 16][64];
-    uint4 v[2][D / 32][64];
-    uint4 ks[4], vs[4];
+// Scales of the 16 keys of a lane: binary16 numbers two to a word, or bfloat16 ones as 32-bit numbers
+template <bool BF16>
+struct Scales {
+    uint32_t w[BF16 ? 16 : 8];
+    __device__ __forceinline__ void take(const void *from)
+    {
+#pragma unroll
+        for (int i = 0; i < (BF16 ? 4 : 2); ++i) {
+            const uint4 x = static_cast<const uint4 *>(from)[i];
+            w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
+        }
+    }
+    __device__ __forceinline__ float at(int i) const
+    {
+        if constexpr (BF16) return __uint_as_float(w[i]);
+        else return i & 1 ? kv_high<false>(w[i / 2]) : kv_low<false>(w[i / 2]);
+    }
+    __device__ __forceinline__ void hide(int i, bool hidden)
+    {
+        if constexpr (BF16) w[i] = hidden ? 0u : w[i];
+        else w[i / 2] &= hidden ? (i & 1 ? 0x0000ffffu : 0xffff0000u) : 0xffffffffu;
+    }
 };
 
-template <int D, bool BF16>
+// SMALL: pages of 16 keys, two to a step
+template <int D, bool BF16, bool SMALL>
 __global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAttentionArgs a, KvPart part)
 {
-    constexpr int W = D / 16, E = D / 32;  // operands of 32 keys, blocks of 32 channels of the result
-    __shared__ Operands<D> shared[2][2];
+    constexpr int W = D / 16, E = D / 32;  // words of a lane's key, blocks of 32 channels of the result
+    typedef typename std::conditional<BF16, uint32_t, uint16_t>::type Scale;
+    __shared__ __align__(16) Scale scales[kWaves][64];  // of a step: keys, values
     const int head = blockIdx.x % a.c.heads, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = kv_lane(), n = lane & 31, h = lane >> 5;
     KvItem<kTilesStep> it;
     const int slot = blockIdx.x / a.c.heads;
@@ -30,190 +54,225 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAt
     kv_note(a, part, slot, head, there, it);
     if (!there) return;
 
-    // what this wave makes ready of each step: keys (waves 0 and 1) or values (2 and 3) of one of its two 32s, with their scales
-    const int shift = a.c.page_shift, mask = (1 << shift) - 1, sub = wave & 1;
-    const bool values = wave >= 2;
-    // operand row 8 i + 4 h' + j of the keys is key 16 h' + 4 i + j; half h of the values' operand s has keys 16 h + 8 s to 16 h + 8 s + 7
-    const bool second = values ? h : (n & 4) != 0;
-    const uint32_t lane_at = values ? (n & (D / 4 - 1)) * 16 + ((uint32_t)(D / 2) << shift) : (uint32_t)(4 * (n >> 3) + (n & 3)) * (D / 2) + h * (D / 4);
-    constexpr int kParts = D == 128 ? 2 : 1;
-    uint4 codes[2], scales = {};
-    auto load = [&](int key, int page0, int page1) {
-        const int64_t place0 = ((((int64_t)max(page0, 0) * a.c.heads + head) * 2) << shift) + (key & mask);
-        const int64_t place1 = ((((int64_t)max(page1, 0) * a.c.heads + head) * 2) << shift) + ((key + 16) & mask);
-        const uint8_t *at = a.c.codes + (second ? place1 : place0) * (D / 2) + lane_at;
-        codes[0] = *reinterpret_cast<const uint4 *>(at);
-        if (values) codes[1] = *reinterpret_cast<const uint4 *>(at + D * 4);
-        else if (D == 128) codes[1] = *reinterpret_cast<const uint4 *>(at + 16);
-        if (lane < 4) scales = *reinterpret_cast<const uint4 *>(a.c.scales + (lane & 2 ? place1 : place0) + (values ? (int64_t)1 << shift : 0) + 8 * (lane & 1));
-    };
-    auto store = [&](Operands<D> &to) {
-        if (values) {
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                uint32_t c[4] = {codes[s].x, codes[s].y, codes[s].z, codes[s].w};
-                if (D == 64) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) c[j] >>= 8 * (n >> 4);  // operand rows 16 and up: channels 4 m + 2 and 4 m + 3
-                }
-                constexpr uint32_t L = 0x000f000fu, H = 0x00f000f0u;
-                to.v[s][0][lane] = make_uint4(c[0] & L, c[1] & L, c[2] & L, c[3] & L);
-                to.v[s][1][lane] = make_uint4(c[0] & H, c[1] & H, c[2] & H, c[3] & H);
-                if constexpr (D == 128) {
-                    to.v[s][2][lane] = make_uint4((c[0] >> 8) & L, (c[1] >> 8) & L, (c[2] >> 8) & L, (c[3] >> 8) & L);
-                    to.v[s][3][lane] = make_uint4((c[0] >> 8) & H, (c[1] >> 8) & H, (c[2] >> 8) & H, (c[3] >> 8) & H);
-                }
-            }
-        } else {
-#pragma unroll
-            for (int s = 0; s < kParts; ++s) {
-                const uint32_t c[4] = {codes[s].x, codes[s].y, codes[s].z, codes[s].w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) to.k[4 * s + j][lane] = __builtin_bit_cast(uint4, kv_operand(c[j]));
-            }
-        }
-        if (lane < 4) (values ? to.vs : to.ks)[lane] = scales;
-    };
-
-    const int row0 = it.row0 + wave * kRows, rows = min(it.rows - wave * kRows, kRows);  // (may be none: such a wave helps the others)
-    const int row = row0 + max(min(n, rows - 1), 0), at = min(row / a.groups, it.s.n - 1);
-    const int pos = it.s.first + at, first_pos = it.s.first + row0 / a.groups, last_pos = rows > 0 ? it.s.first + (row0 + rows - 1) / a.groups : -1;
+    const int row0 = it.row0 + wave * kRows, rows = min(it.rows - wave * kRows, kRows);
+    if (rows <= 0) return;
+    const int row = row0 + min(n, rows - 1), at = row / a.groups;
+    const int pos = it.s.first + at, first_pos = it.s.first + row0 / a.groups, last_pos = it.s.first + (row0 + rows - 1) / a.groups;
     auto over_row = [](float v, auto f) { return f(v, __shfl_xor(v, 32)); };
     auto larger = [](float x, float y) { return fmaxf(x, y); };
     auto plus = [](float x, float y) { return x + y; };
 
-    int v = it.from, ids = kv_page_ids(a, it, v, 1), next_ids = -1, id = 0;
+    // the steps of this wave: those of the workgroup's that some row of it sees
+    auto seen = [&](int key) { return key <= last_pos && (!a.window || key + kTilesStep > first_pos - a.window + 1 || key < a.sinks); };
+    int to = it.to, t = it.from;
+    while (to > t && !seen(it.key_of(to - 1))) --to;
+    while (t < to && !seen(it.key_of(t))) ++t;
+
+    // Where a step's codes and scales are.  Operand row 8 i + 4 h' + j of the keys is key 16 h' + 4 i + j; half h of the values' operand s has keys 16 h + 8 s to 16 h + 8 s + 7.
+    const int shift = a.c.page_shift, mask = (1 << shift) - 1;
+    const int64_t page_scales = (int64_t)a.c.heads << (shift + 2), page_codes = page_scales / 4 * D;  // bytes of a page (a scale is 2 for D / 2 of codes)
+    const uint8_t *const codes_head = a.c.codes + (((int64_t)head * D) << shift), *const scales_head = reinterpret_cast<const uint8_t *>(a.c.scales) + ((int64_t)head << (shift + 2));
+    const bool key_half = n & 4;
+    const uint32_t key_lane = (uint32_t)(4 * (n >> 3) + (n & 3) + (!SMALL && key_half ? 16 : 0)) * (D / 2) + h * (D / 4);
+    const uint32_t value_lane = (uint32_t)(n & (D / 4 - 1)) * 16 + ((uint32_t)(D / 2) << shift) + (!SMALL ? h * 8 * D : 0);
+    const uint32_t scale_lane = ((uint32_t)(lane & (SMALL ? 15 : 31)) + (h ? 1u << shift : 0u)) * 2;
+    struct Place {
+        const uint8_t *codes, *scales;
+        int64_t codes_on, scales_on;  // in small pages: from there to the second half of the step
+    };
+    auto place_of = [&](int t, int ids, int i) {  // lanes 2 i and 2 i + 1 of ids are its pages
+        Place p = {};
+        const int key = it.key_of(t), page = max(__builtin_amdgcn_readlane(ids, 2 * i), 0), in = key & mask;
+        p.codes = codes_head + page * page_codes + in * (D / 2);
+        p.scales = scales_head + page * page_scales + in * 2;
+        if (SMALL) {
+            const int page1 = max(__builtin_amdgcn_readlane(ids, 2 * i + 1), 0), in1 = (key + 16) & mask;
+            p.codes_on = (page1 - page) * page_codes + (in1 - in) * (D / 2);
+            p.scales_on = (page1 - page) * page_scales + (in1 - in) * 2;
+        }
+        return p;
+    };
+    auto load_keys = [&](const Place &p, uint4 (&k)[D / 64]) {
+        const uint8_t *from = p.codes + (SMALL && key_half ? p.codes_on : 0) + key_lane;
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) k[i] = reinterpret_cast<const uint4 *>(from)[i];
+    };
+    auto load_values = [&](const Place &p, uint4 (&v)[2]) {
+        const uint8_t *from = p.codes + (SMALL && h ? p.codes_on : 0) + value_lane;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) v[i] = *reinterpret_cast<const uint4 *>(from + i * (D * 4));
+    };
+    auto load_scales = [&](const Place &p) -> uint32_t { return *reinterpret_cast<const uint16_t *>(p.scales + (SMALL && (lane & 16) ? p.scales_on : 0) + scale_lane); };
+    // Pages of steps t to t + 31, and whether one of their keys has none
+    auto pages_from = [&](int t, bool &bad) {
+        const int ids = kv_page_ids(a, it, t, 1), step = t + (lane >> 1);
+        bad = __any(ids < 0 && step < it.to && it.key_of(step) + 16 * (lane & 1) < it.s.keys);
+        return ids;
+    };
+
     half8 q[W];
     float init, factor;
+    uint4 k[D / 64] = {}, v[2] = {};  // of step t, on their way
+    uint32_t scale = 0;
+    int ids;              // pages of the 32 steps behind `block`
+    int block = t;
+    const int begin = t;
+    bool bad, bad_before; // whether keys of those, of the 32 up to `block`, have none
     {
         uint32_t x[4 * W];
         kv_load(a.q.data + (int64_t)(it.s.start + at) * a.q.token_stride + (int64_t)(head * a.groups + row % a.groups) * a.q.head_stride + h * (D / 2), a.q.aligned, x);
-        if (v < it.to) {
-            load(it.key_of(v) + 32 * sub, __builtin_amdgcn_readlane(ids, 2 * sub), __builtin_amdgcn_readlane(ids, 2 * sub + 1));
-            store(shared[0][sub]);
+        const Place p = place_of(t, pages_from(t, bad_before), 0);
+        ids = pages_from(t + 1, bad);
+        if (t < to) {
+            load_keys(p, k);
+            scale = load_scales(p);
+            load_values(p, v);
         }
         kv_queries<4 * W, BF16>(x, a.scale, [&](float v) { return over_row(v, larger); }, [&](float v) { return over_row(v, plus); }, q, init, factor);
     }
 
-    float16v acc[E];
+    float16v acc[E], init16;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) init16[i] = init;
+    asm volatile("" : "+v"(init16));  // stays in registers: made anew it would be 16 moves a step
 #pragma unroll
     for (int e = 0; e < E; ++e)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[e][i] = 0.0f;
     float top = kLowest, base = -kLowest, total = 0.0f, weights = 0.0f;
-    uint32_t limit = 0, met = 0;  // largest scale of values: where it is passed, met so far
-    bool moved = false;           // the step at hand has moved the maximum (scales that are not finite would do so again)
-    bool loaded = false;
-    int buffer = 0;
+    float met = 0.0f, limit = 0.0f, most = 0.0f;  // largest scale of values that the row has met, the power of two above it; largest sum that a step may add
 
-    __syncthreads();
-    while (v < it.to) {
-        float high, x[2][16];
-        uint32_t vs[2][8];
-        do {  // steps that leave the maximum where it is; one that does not ends the loop before it has added anything, and is done again
-            const int key0 = it.key_of(v);
-            if (!loaded && v + 1 < it.to) {
-                int after = id + 4;
-                if (after == 64) {
-                    next_ids = kv_page_ids(a, it, v + 1, 1);
-                    after = 0;
-                }
-                const int from = after ? ids : next_ids;
-                load(it.key_of(v + 1) + 32 * sub, __builtin_amdgcn_readlane(from, after + 2 * sub), __builtin_amdgcn_readlane(from, after + 2 * sub + 1));
-                loaded = true;
+    auto scores = [&]() {
+        float16v s = init16;
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            const uint4 x = k[i / 4];
+            s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kv_operand(i % 4 == 0 ? x.x : i % 4 == 1 ? x.y : i % 4 == 2 ? x.z : x.w), q[i], s, 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        return s;
+    };
+    auto add = [&](const uint32_t (&w)[8]) {
+#pragma unroll
+        for (int i = 0; i < 2 * E; ++i) {
+            const int j = i / E, e = i % E;
+            uint32_t c[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                if (D == 64) c[x] >>= 8 * (n >> 4);  // operand rows 16 and up: channels 4 m + 2 and 4 m + 3
+                if (e & 2) c[x] >>= 8;
+                c[x] &= e & 1 ? 0x00f000f0u : 0x000f000fu;
             }
-            const uint32_t pages = (uint32_t)(__ballot(ids >= 0) >> id) & 15u;
-            const bool all = key0 + kTilesStep <= it.s.keys && key0 + kTilesStep - 1 <= first_pos && pages == 15u &&
-                             (!a.window || key0 > last_pos - a.window || key0 + kTilesStep <= a.sinks);
-            uint32_t most2 = 0;
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const Operands<D> &cur = shared[buffer][t];
-                float16v sc;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) sc[i] = init;
-#pragma unroll
-                for (int i = 0; i < W; ++i) sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, cur.k[i][lane]), q[i], sc, 0, 0, 0);
-                const uint4 ks0 = cur.ks[2 * h], ks1 = cur.ks[2 * h + 1], vs0 = cur.vs[2 * h], vs1 = cur.vs[2 * h + 1];
-                const uint32_t ks[8] = {ks0.x, ks0.y, ks0.z, ks0.w, ks1.x, ks1.y, ks1.z, ks1.w};
-                vs[t][0] = vs0.x; vs[t][1] = vs0.y; vs[t][2] = vs0.z; vs[t][3] = vs0.w; vs[t][4] = vs1.x; vs[t][5] = vs1.y; vs[t][6] = vs1.z; vs[t][7] = vs1.w;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[t][i] = fmaf(sc[i], i & 1 ? kv_high<BF16>(ks[i / 2]) : kv_low<BF16>(ks[i / 2]), 0.0f);
-            }
-            if (!all) {
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const int end = pages >> (2 * t + h) & 1 ? min(it.s.keys, pos + 1) : 0, first = key0 + 32 * t + 16 * h;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int key = first + i;
-                        const bool hidden = (key >= end) | ((a.window != 0) & (key <= pos - a.window) & (key >= a.sinks));
-                        x[t][i] = hidden ? -__builtin_inff() : x[t][i];
-                        vs[t][i / 2] &= hidden ? (i & 1 ? 0x0000ffffu : 0xffff0000u) : 0xffffffffu;  // weights of hidden keys are zero whatever their scale is
-                    }
-                }
-            }
-            high = x[0][0];
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) most2 = kv_fold_max(most2, vs[t][i]);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) high = fmaxf(high, x[t][i]);
-            }
-            const uint32_t most = max(most2 & 0xffffu, most2 >> 16);
-            high *= factor;
-            if (!moved && __any((high > top + kSlack) | (most > limit))) break;
-            moved = false;
+            acc[e] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, make_uint4(c[0], c[1], c[2], c[3])),
+                                                            __builtin_bit_cast(half8, make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3])), acc[e], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    auto weigh = [&](int i, float x0, float x1, const Scales<BF16> &vs, uint32_t (&w)[8], float &sum, float &weight_sum) {  // two keys
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(x0, factor, base)), p1 = __builtin_amdgcn_exp2f(fmaf(x1, factor, base));
+        sum += p0 + p1;
+        half2v pair;
+        pair[0] = (_Float16)fmaf(p0, vs.at(2 * i), 0.0f);
+        pair[1] = (_Float16)fmaf(p1, vs.at(2 * i + 1), 0.0f);
+        w[i] = __builtin_bit_cast(uint32_t, pair);
+        weight_sum = __builtin_amdgcn_fdot2(pair, (half2v){1, 1}, weight_sum, false);
+    };
+    auto take_scales = [&](Scales<BF16> &ks, Scales<BF16> &vs) {
+        scales[wave][lane] = (Scale)(BF16 ? scale << 16 : scale);
+        const Scale *from = scales[wave] + 16 * h;
+        ks.take(from);
+        vs.take(from + 32);
+    };
+    // Steps from t on that every row of the wave sees all keys of, as far as the places of keys go
+    auto plain_until = [&]() {
+        const int key0 = it.key_of(t);
+        if (key0 + 32 > it.s.keys || key0 + 31 > first_pos || t == begin) return t;
+        if (a.window && key0 <= last_pos - a.window) return min(it.sink_steps, a.sinks / 32);
+        return min(it.s.keys, first_pos + 1) / 32 - it.gap;
+    };
 
+    while (t < to) {
+        if (t == block + 32) {
+            block = t;
+            bad_before = bad;
+            ids = pages_from(t + 1, bad);
+        }
+        const int stop = bad || bad_before ? t : min(min(plain_until(), block + 32), to);
+        bool again = false;
+        while (t < stop) {
+            Scales<BF16> ks, vs;
+            take_scales(ks, vs);
+            const float16v s = scores();
+            const Place next = place_of(min(t + 1, to - 1), ids, min(t + 1, to - 1) - block - 1);
+            load_keys(next, k);
+            scale = load_scales(next);
+            float sum = 0.0f, weight_sum = 0.0f;
+            uint32_t w[8];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const Operands<D> &cur = shared[buffer][t];
-                uint32_t w[8];
+            for (int i = 0; i < 8; ++i) weigh(i, fmaf(s[2 * i], ks.at(2 * i), 0.0f), fmaf(s[2 * i + 1], ks.at(2 * i + 1), 0.0f), vs, w, sum, weight_sum);
+            again = __any((sum > most) | (weight_sum > 60000.0f));
+            if (again) break;
+            total += sum;
+            weights += weight_sum;
+            add(w);
+            load_values(next, v);
+            ++t;
+        }
+        if (!again && (t == to || t == block + 32)) continue;
+        // step t in general
+        if (again) {  // its keys and scales once more
+            const Place now = place_of(t, t == block ? kv_page_ids(a, it, t, 1) : ids, t == block ? 0 : t - block - 1);
+            load_keys(now, k);
+            scale = load_scales(now);
+        }
+        Scales<BF16> ks, vs;
+        take_scales(ks, vs);
+        const float16v s = scores();
+        const Place next = place_of(min(t + 1, to - 1), ids, max(min(t + 1, to - 1) - block - 1, 0));
+        load_keys(next, k);
+        scale = load_scales(next);
+        const int first = it.key_of(t) + 16 * h;
+        int end = min(it.s.keys, pos + 1);
+        if ((bad || bad_before) && first < it.s.keys) {
+            const int page = a.c.table[it.b * a.c.table_stride + (first >> shift)];
+            if (page < 0 || page >= a.c.pages) end = 0;
+        }
+        float x[16], high = -__builtin_inff(), largest = met;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float p0 = __builtin_amdgcn_exp2f(fmaf(x[t][2 * i], factor, base)), p1 = __builtin_amdgcn_exp2f(fmaf(x[t][2 * i + 1], factor, base));
-                    total += p0 + p1;
-                    w[i] = kv_half_pair(fmaf(p0, kv_low<BF16>(vs[t][i]), 0.0f), fmaf(p1, kv_high<BF16>(vs[t][i]), 0.0f));
-                    weights = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, w[i]), (half2v){1, 1}, weights, false);
-                }
+        for (int i = 0; i < 16; ++i) {
+            const int key = first + i;
+            const bool hidden = (key >= end) | ((a.window != 0) & (key <= pos - a.window) & (key >= a.sinks));
+            x[i] = hidden ? -__builtin_inff() : fmaf(s[i], ks.at(i), 0.0f);
+            vs.hide(i, hidden);  // weights of hidden keys are zero whatever their scale is
+            high = fmaxf(high, x[i]);
+            largest = fmaxf(largest, vs.at(i) <= -kLowest ? vs.at(i) : 0.0f);
+        }
+        high *= factor;
+        if (__any((high > top + kSlack) | (largest > limit))) {
+            top = fmaxf(top, over_row(high, larger));
+            met = over_row(largest, larger);
+            // 2^E above it, E from -80 (sums of 2^(4 - E) stay in range; scales below 2^-98 lose bits) to 127
+            const int e = min(max((int)(__float_as_uint(met) >> 23) - 126, -80), 127);
+            limit = ldexpf(1.0f, e);
+            const float moved = -top + (kRoom - (float)e), by = __builtin_amdgcn_exp2f(moved - base);
+            base = moved;
+            most = ldexpf(1.0f, (int)(kRoom + kSlack) - e);
+            total *= by;
+            weights *= by;
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const half8 p = __builtin_bit_cast(half8, make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
+            for (int e = 0; e < E; ++e)
 #pragma unroll
-                    for (int e = 0; e < E; ++e) acc[e] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, cur.v[i][e][lane]), p, acc[e], 0, 0, 0);
-                }
-            }
-            buffer ^= 1;
-            if (loaded) store(shared[buffer][sub]);
-            __syncthreads();
-            loaded = false;
-            ++v;
-            id += 4;
-            if (id == 64) {
-                ids = next_ids;
-                id = 0;
-            }
-        } while (v < it.to);
-        if (v >= it.to) break;
-        top = fmaxf(top, over_row(high, larger));
-        uint32_t m = met;
+                for (int i = 0; i < 16; ++i) acc[e][i] *= by;
+        }
+        float sum = 0.0f, weight_sum = 0.0f;
+        uint32_t w[8];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) m = kv_finite_max<BF16>(kv_finite_max<BF16>(m, vs[i / 8][i % 8] & 0xffffu), vs[i / 8][i % 8] >> 16);
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) m = max(m, (uint32_t)__shfl_xor((int)m, d));
-        met = m;
-        limit = kv_limit<BF16>(met);
-        const float to = -top + (kRoom - (float)kv_exponent<BF16>(met));
-        const float by = __builtin_amdgcn_exp2f(to - base);
-        base = to;
-        total *= by;
-        weights *= by;
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[e][i] *= by;
-        moved = true;
+        for (int i = 0; i < 8; ++i) weigh(i, x[2 * i], x[2 * i + 1], vs, w, sum, weight_sum);
+        total += sum;
+        weights += weight_sum;
+        add(w);
+        load_values(next, v);
+        ++t;
     }
 
     // row n's channels of this lane, 16 at a time: 32 i + 16 h + 4 j + e of acc[e][4 i + j] (64 channels: 32 i + 16 h + 4 j + e of acc[e & 1][4 (i + (e & 2)) + j])
@@ -249,18 +308,20 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAt
     if (!whole && h == 0) partial.row[place] = make_float2(-base, total);
 }
 
+template <int D, bool BF16>
+void launch(const KvAttentionArgs &a, const KvPart &part, hipStream_t stream)
+{
+    const dim3 grid((uint32_t)((int64_t)part.slots * a.c.heads)), block(64 * kWaves);
+    if (a.c.page_shift == 4) kv_attention_tiles_kernel<D, BF16, true><<<grid, block, 0, stream>>>(a, part);
+    else kv_attention_tiles_kernel<D, BF16, false><<<grid, block, 0, stream>>>(a, part);
+}
+
 }  // namespace
 
 hipError_t launch_kv_attention_tiles(const KvAttentionArgs &a, const KvPart &part, hipStream_t stream)
 {
-    const dim3 grid((uint32_t)((int64_t)part.slots * a.c.heads)), block(64 * kWaves);
-    if (a.c.head_dim == 128) {
-        if (a.c.bf16) kv_attention_tiles_kernel<128, true><<<grid, block, 0, stream>>>(a, part);
-        else kv_attention_tiles_kernel<128, false><<<grid, block, 0, stream>>>(a, part);
-    } else {
-        if (a.c.bf16) kv_attention_tiles_kernel<64, true><<<grid, block, 0, stream>>>(a, part);
-        else kv_attention_tiles_kernel<64, false><<<grid, block, 0, stream>>>(a, part);
-    }
+    if (a.c.head_dim == 128) a.c.bf16 ? launch<128, true>(a, part, stream) : launch<128, false>(a, part, stream);
+    else a.c.bf16 ? launch<64, true>(a, part, stream) : launch<64, false>(a, part, stream);
     return hipGetLastError();
 }
 

@@ -278,6 +278,29 @@ def test_not_a_number_stays_in_its_row(gpu, new):
             close(torch, got[~bad], exact[~bad.cpu()], near[~bad.cpu()])
 
 
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("new, heads, groups", [(16, 2, 1), (5, 1, 3), (90, 2, 2)])
+def test_each_row_has_its_own_range(gpu, dtype, new, heads, groups):
+    """Very large queries, and keys and values with very large scales that later queries see: the results of the others are as exact as without."""
+    torch, binding = gpu
+    dt = getattr(torch, dtype)
+    D, length = 128, 140
+    x = Batch(torch, dt, D, heads, groups, 16, [length], [new], seed=13, fused=False)
+    late = length - new // 2
+    big = 2.0 ** 11 if dt == torch.float16 else 2.0 ** 100
+    exact, near = x.attention(x.q, 0, 0, D ** -0.5)
+    before = late - (length - new)  # queries that do not see the key at `late`
+    for which in (0, 1):
+        scales = x.scales.clone()
+        scales[int(x.table[0, late // 16]), :, which, late % 16] = big
+        got = binding.apmm_kv_attention(x.q, x.codes, scales, *x.args[2:], x.starts_gpu)
+        close(torch, got[:before], exact[:before], near[:before])
+    q = x.q.clone()
+    q[1::2] *= big / 2 ** 4
+    got = binding.apmm_kv_attention(q, *x.args, x.starts_gpu)
+    close(torch, got[0::2], exact[0::2], near[0::2])
+
+
 def test_pages_that_are_none(gpu):
     """Page numbers outside of the cache: their tokens are not written, read as zeros and are not seen.  Lengths beyond the table, starts that do not fit: nothing outside of the buffers."""
     torch, binding = gpu
