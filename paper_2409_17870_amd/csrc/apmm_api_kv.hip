@@ -147,6 +147,8 @@ apmm_status apmm_kv_attention(const apmm_kv_cache *cache, const apmm_kv_batch *b
     if (need && (!workspace || workspace_bytes < need)) return fail(APMM_ERR_WORKSPACE, "kv_attention: needs a workspace of apmm_kv_attention_workspace_bytes() bytes");
     if (need && !aligned(workspace, 16)) return fail(APMM_ERR_INVALID_ARG, "kv_attention: workspace must be 16-byte aligned");
     a.groups = q_heads / cache->kv_heads;
+    a.by_groups = apmm::kv_divisor(a.groups);
+    a.by_heads = apmm::kv_divisor(cache->kv_heads);
     a.window = (int)window;
     a.sinks = window ? (int)sinks : 0;
     a.scale = scale;

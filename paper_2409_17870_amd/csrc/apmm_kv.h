@@ -36,6 +36,7 @@ struct KvAttentionArgs {
     KvArgs c;
     KvTensor q, out;
     int groups;        // query heads to a key/value head
+    uint64_t by_groups, by_heads;  // what kv_divide divides by groups and by key/value heads with
     int window, sinks; // window 0: none
     float scale;
     float *partial;    // results of pieces of sequences: see KvPlan
@@ -48,6 +49,7 @@ struct KvPart {
     int tile;    // rows of a workgroup; 0: the kernel is not launched
     int waves;   // of a workgroup
     int target;  // 0: nothing is cut
+    float over_target;
     int least;
     int slots;   // most pieces there can be
     int from_rows, to_rows;
@@ -62,7 +64,15 @@ hipError_t launch_kv_write(const KvArgs &c, const KvTensor &k, const KvTensor &v
 hipError_t launch_kv_read(const KvArgs &c, const KvTensor &k, const KvTensor &v, hipStream_t stream);
 hipError_t launch_kv_attention(const KvAttentionArgs &a, const KvPlan &plan, hipStream_t stream);
 
+// x / d as (x m) >> 40 with m = 2^40 / d, rounded up: exact for x < 2^30 and d <= 1024, since x (m - 2^40 / d) < 2^30 = 2^40 / 1024
+inline uint64_t kv_divisor(int d) { return ((1ull << 40) + d - 1) / d; }
+
 #ifdef __HIPCC__
+typedef uint16_t __attribute__((may_alias)) kv_u16;  // what is written in these and read in words, or the other way round
+typedef uint32_t __attribute__((may_alias)) kv_u32;
+
+__device__ __forceinline__ int kv_divide(int x, uint64_t m) { return (int)(((uint64_t)(uint32_t)x * m) >> 40); }
+
 // Place of lane `lane` within its wave of a workgroup of whole waves
 __device__ __forceinline__ int kv_lane() { return threadIdx.x & 63; }
 

@@ -40,7 +40,7 @@ typedef float float4v __attribute__((ext_vector_type(4)));
 typedef float float16v __attribute__((ext_vector_type(16)));
 
 constexpr float kLowest = -3.402823466e38f;
-constexpr float kSlack = 11.0f, kRoom = 4.0f;
+constexpr float kSlack = 13.0f, kRoom = 2.0f;
 
 // A workgroup's part of the call: keys of steps `from` to `to` - 1 (of STEP keys, the hidden ones between the first tokens and the window left out) for rows of one sequence
 template <int STEP>
@@ -54,44 +54,49 @@ struct KvItem {
 };
 
 // Tiles of a sequence, and steps of the one with most (or a few more)
-template <int STEP>
+template <int STEP, int TILE>
 __device__ __forceinline__ void kv_extent(const KvAttentionArgs &a, const KvSequence &s, const KvPart &p, int &tiles, int &steps)
 {
     const int rows = s.n * a.groups;
-    tiles = rows >= p.from_rows && rows <= p.to_rows ? (rows + p.tile - 1) / p.tile : 0;
+    tiles = rows >= p.from_rows && rows <= p.to_rows ? (rows + TILE - 1) / TILE : 0;
     steps = (s.keys + STEP - 1) / STEP;
     if (a.window) {
-        const int64_t span = (int64_t)a.window + (p.tile + a.groups - 2) / a.groups;  // positions that the queries of a tile see, without the first tokens
-        steps = (int)min((int64_t)steps, (span + STEP - 1) / STEP + 1 + ((int64_t)a.sinks + STEP - 1) / STEP);
+        const int span = a.window + kv_divide(TILE + a.groups - 2, a.by_groups);  // positions that the queries of a tile see, without the first tokens
+        steps = min(steps, (span + STEP - 1) / STEP + 1 + (a.sinks + STEP - 1) / STEP);
     }
     if (!tiles) steps = 0;
 }
 
-__device__ __forceinline__ int kv_pieces(int steps, int piece) { return steps > piece ? (steps + piece - 1) / piece : 1; }
+__device__ __forceinline__ int kv_pieces(int steps, int piece)
+{
+    if (steps <= piece) return 1;
+    const int n = (int)((float)steps / (float)piece);  // steps < 2^25; within one of the quotient
+    return n * (int64_t)piece >= steps ? ((n - 1) * (int64_t)piece >= steps ? n - 1 : n) : ((n + 1) * (int64_t)piece >= steps ? n + 1 : n + 2);
+}
 
 // Piece `slot` of the call; false: there is none
-template <int STEP>
+template <int STEP, int TILE>
 __device__ __forceinline__ bool kv_item(const KvAttentionArgs &a, const KvPart &p, int slot, KvItem<STEP> &it)
 {
     const int lane = kv_lane();
     int piece = 0x7fffffff, tiles, steps;
     KvSequence s = {};
     if (lane < a.c.sequences) s = kv_sequence(a.c, lane);  // the first 64 stay in registers
-    kv_extent<STEP>(a, s, p, tiles, steps);
+    kv_extent<STEP, TILE>(a, s, p, tiles, steps);
     if (p.target) {
         float work = (float)tiles * (float)steps;
         for (int at = lane + 64; at < a.c.sequences; at += 64) {
             int t, n;
-            kv_extent<STEP>(a, kv_sequence(a.c, at), p, t, n);
+            kv_extent<STEP, TILE>(a, kv_sequence(a.c, at), p, t, n);
             work += (float)t * (float)n;
         }
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) work += __shfl_xor(work, d);
         // (rounding: a piece may be 2^-20 shorter than the work asks for, for which there is one slot more)
-        piece = __builtin_amdgcn_readfirstlane(max((int)ceilf(fminf(work / (float)p.target * (1.0f - 0x1p-20f), 0x1p30f)), p.least));
+        piece = __builtin_amdgcn_readfirstlane(max((int)ceilf(fminf(work * p.over_target * (1.0f - 0x1p-20f), 0x1p30f)), p.least));
     }
     int rest, l;
-    const int own = tiles * kv_pieces(steps, piece), to = kv_scan(own);
+    const int pieces = kv_pieces(steps, piece), own = tiles * pieces, to = kv_scan(own);
     const uint64_t past = __ballot(to > slot);
     if (past) {
         l = __ffsll((long long)past) - 1;
@@ -101,31 +106,42 @@ __device__ __forceinline__ bool kv_item(const KvAttentionArgs &a, const KvPart &
         it.s.n = __builtin_amdgcn_readlane(s.n, l);
         it.s.first = __builtin_amdgcn_readlane(s.first, l);
         it.s.keys = __builtin_amdgcn_readlane(s.keys, l);
+        it.pieces = __builtin_amdgcn_readlane(pieces, l);
+        tiles = __builtin_amdgcn_readlane(tiles, l);
     } else {
         const int before = __builtin_amdgcn_readlane(to, 63);
         auto count = [&](int at) {
             int t, n;
             if (at + 64 >= a.c.sequences) return 0;
-            kv_extent<STEP>(a, kv_sequence(a.c, at + 64), p, t, n);
+            kv_extent<STEP, TILE>(a, kv_sequence(a.c, at + 64), p, t, n);
             return t * kv_pieces(n, piece);
         };
         if (a.c.sequences <= 64 || !kv_find(a.c.sequences - 64, slot - before, it.b, rest, count)) return false;
         it.b += 64;
         it.s = kv_sequence(a.c, it.b);
+        kv_extent<STEP, TILE>(a, it.s, p, tiles, steps);
+        it.pieces = kv_pieces(steps, piece);
     }
-    kv_extent<STEP>(a, it.s, p, tiles, steps);
-    it.pieces = kv_pieces(steps, piece);
-    const int tile = tiles - 1 - rest / it.pieces;  // (the last queries see the most keys: those first)
-    it.part = rest % it.pieces;
-    it.row0 = tile * p.tile;
+    int tile = rest;
+    it.part = 0;
+    if (it.pieces > 1) {
+        tile = rest / it.pieces;
+        it.part = rest % it.pieces;
+    }
+    tile = tiles - 1 - tile;  // (the last queries see the most keys: those first)
+    it.row0 = tile * TILE;
     it.rows = it.s.n * a.groups - it.row0;
-    const int last = min(it.rows, p.tile) - 1, first_pos = it.s.first + it.row0 / a.groups, last_pos = it.s.first + (it.row0 + last) / a.groups;
+    const int last = min(it.rows, TILE) - 1, first_pos = it.s.first + kv_divide(it.row0, a.by_groups), last_pos = it.s.first + kv_divide(it.row0 + last, a.by_groups);
     const int end = min(last_pos + 1, it.s.keys), all = end > 0 ? (end + STEP - 1) / STEP : 0;
     const int low = min(a.window ? max(first_pos - a.window + 1, 0) / STEP : 0, all);
     it.sink_steps = min((a.sinks + STEP - 1) / STEP, low);
     it.gap = low - it.sink_steps;
-    it.from = min(it.part * (int64_t)piece, (int64_t)all - it.gap);
-    it.to = min((it.part + 1) * (int64_t)piece, (int64_t)all - it.gap);
+    it.from = 0;
+    it.to = all - it.gap;
+    if (it.pieces > 1) {
+        it.from = min(it.part * (int64_t)piece, (int64_t)it.to);
+        it.to = min((it.part + 1) * (int64_t)piece, (int64_t)it.to);
+    }
     return true;
 }
 
@@ -178,6 +194,12 @@ __device__ __forceinline__ float kv_low(uint32_t w) { return BF16 ? __uint_as_fl
 template <bool BF16>
 __device__ __forceinline__ float kv_high(uint32_t w) { return BF16 ? __uint_as_float(w & 0xffff0000u) : (float)__builtin_bit_cast(half2v, w)[1]; }
 
+// The larger of two 16-bit numbers each
+__device__ __forceinline__ uint32_t kv_fold_max(uint32_t m, uint32_t w)
+{
+    typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(us2, m), __builtin_bit_cast(us2, w)));
+}
 // The larger of m and a magnitude's bits, if that is finite
 template <bool BF16>
 __device__ __forceinline__ uint32_t kv_finite_max(uint32_t m, uint32_t bits)
@@ -188,23 +210,40 @@ __device__ __forceinline__ uint32_t kv_finite_max(uint32_t m, uint32_t bits)
 template <int N, bool BF16, class Max, class Sum>
 __device__ __forceinline__ void kv_queries(const uint32_t (&x)[N], float scale, Max max_across, Sum sum_across, half8 (&q)[N / 4], float &init, float &factor)
 {
-    uint32_t bits = 0;
+    uint32_t bits2 = 0, bits;  // of the largest magnitude
 #pragma unroll
-    for (int i = 0; i < N; ++i) bits = kv_finite_max<BF16>(kv_finite_max<BF16>(bits, x[i] & 0x7fffu), (x[i] >> 16) & 0x7fffu);
+    for (int i = 0; i < N; ++i) bits2 = kv_fold_max(bits2, x[i] & 0x7fff7fffu);
+    bits = max(bits2 & 0xffffu, bits2 >> 16);
+    if (bits >= (BF16 ? 0x7f80u : 0x7c00u)) {  // not finite: of those that are
+        bits = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) bits = kv_finite_max<BF16>(kv_finite_max<BF16>(bits, x[i] & 0x7fffu), (x[i] >> 16) & 0x7fffu);
+    }
     const float top = max_across(kv_scale_value(bits, BF16));
     int e = top > 0.0f ? 11 - (int)((__float_as_uint(top) >> 23) - 126u) : 0;  // top 2^e < 2^11
-    e = min(e, 100);                                                         // (a row of subnormal numbers)
+    e = min(e, BF16 ? 100 : 26);                                             // (rows of the smallest numbers)
     float sum = 0.0f;
+    // binary16 numbers are multiplied as they are, by 2^e or 2^(e + 4) in two steps where one factor has no room for it; channels j and j + 4 make a word
+    const float first = BF16 ? 1.0f : ldexpf(1.0f, min(e, 11)), second = BF16 ? 1.0f : ldexpf(1.0f, e - min(e, 11));
+    const half2v by0 = {(_Float16)first, (_Float16)first}, by1 = {(_Float16)second, (_Float16)second}, by16 = {(_Float16)16.0f, (_Float16)16.0f};
+    const float even = ldexpf(1.0f, e + 4), odd = ldexpf(1.0f, e);
 #pragma unroll
     for (int i = 0; i < N / 4; ++i) {
         __builtin_amdgcn_sched_barrier(0);  // a few registers at a time
         uint32_t w[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {  // channels j and j + 4
+        for (int j = 0; j < 4; ++j) {
             const uint32_t a = x[4 * i + j / 2], b = x[4 * i + j / 2 + 2];
-            const int by = j & 1 ? e : e + 4;
-            w[j] = kv_half_pair(ldexpf(j & 1 ? kv_high<BF16>(a) : kv_low<BF16>(a), by), ldexpf(j & 1 ? kv_high<BF16>(b) : kv_low<BF16>(b), by));
-            sum = fmaf(kv_low<false>(w[j]) + kv_high<false>(w[j]), j & 1 ? 1.0f : 0.0625f, sum);
+            half2v pair;
+            if (BF16) {
+                const float by = j & 1 ? odd : even;
+                pair = __builtin_bit_cast(half2v, kv_half_pair((j & 1 ? kv_high<true>(a) : kv_low<true>(a)) * by, (j & 1 ? kv_high<true>(b) : kv_low<true>(b)) * by));
+            } else {
+                pair = __builtin_bit_cast(half2v, __builtin_amdgcn_perm(b, a, j & 1 ? 0x07060302u : 0x05040100u)) * by0 * by1;
+                if (!(j & 1)) pair *= by16;
+            }
+            w[j] = __builtin_bit_cast(uint32_t, pair);
+            sum = __builtin_amdgcn_fdot2(pair, j & 1 ? half2v{(_Float16)1.0f, (_Float16)1.0f} : half2v{(_Float16)0.0625f, (_Float16)0.0625f}, sum, false);
         }
         q[i] = __builtin_bit_cast(half8, make_uint4(w[0], w[1], w[2], w[3]));
     }
@@ -225,12 +264,6 @@ __device__ __forceinline__ int kv_page_ids(const KvAttentionArgs &a, const KvIte
     return page < a.c.pages ? page : -1;
 }
 
-// Largest finite scale of two to a word
-__device__ __forceinline__ uint32_t kv_fold_max(uint32_t m, uint32_t w)
-{
-    typedef unsigned short us2 __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(us2, m), __builtin_bit_cast(us2, w)));
-}
 // E of a largest scale: s < 2^E.  Held above -80, so that sums of 2^(9 - E) stay in range (scales below 2^-103 lose bits).
 template <bool BF16>
 __device__ __forceinline__ int kv_exponent(uint32_t bits) { return BF16 ? max((int)(bits >> 7) - 126, -80) : (int)(bits >> 10) - 14; }

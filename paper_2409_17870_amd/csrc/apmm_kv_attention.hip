@@ -23,7 +23,7 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(KvAttentionArgs 
     if (note.pieces == 0 || rows <= 0) return;
     const int row_slots = rows > 8 ? 16 : rows > 4 ? 8 : rows > 2 ? 4 : rows, shares = 16 / row_slots;
     const int group = threadIdx.x >> 4, row = group % row_slots, share = group / row_slots, c0 = (threadIdx.x & 15) * C;
-    const int head = blockIdx.x % a.c.heads;
+    const int head = blockIdx.x - kv_divide(blockIdx.x, a.by_heads) * a.c.heads;
     float base = kLowest, total = 0.0f, o[C] = {};
     if (row < rows) {
         const int64_t place = (int64_t)blockIdx.x * part.tile + first_row + row, step = (int64_t)a.c.heads * part.tile;
@@ -63,8 +63,8 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(KvAttentionArgs 
     uint32_t w[C / 2];
 #pragma unroll
     for (int j = 0; j < C / 2; ++j) w[j] = kv_round(o[2 * j] * over, BF16) | (uint32_t)kv_round(o[2 * j + 1] * over, BF16) << 16;
-    const int r = note.row0 + first_row + row;
-    kv_store(a.out.data + (int64_t)(note.start + r / a.groups) * a.out.token_stride + (int64_t)(head * a.groups + r % a.groups) * a.out.head_stride + c0, a.out.aligned, w);
+    const int r = note.row0 + first_row + row, at = kv_divide(r, a.by_groups);
+    kv_store(a.out.data + (int64_t)(note.start + at) * a.out.token_stride + (int64_t)(head * a.groups + r - at * a.groups) * a.out.head_stride + c0, a.out.aligned, w);
 }
 
 }  // namespace
@@ -78,6 +78,7 @@ void cut(KvPart &p, const KvArgs &c, int groups, int step, int wanted)
     const int64_t tiles = std::min<int64_t>((int64_t)c.tokens * ((groups + p.tile - 1) / p.tile), rows / p.tile + c.sequences);
     const int64_t most_steps = (((int64_t)c.width << c.page_shift) + step - 1) / step;  // of a sequence, as far as the page table goes
     p.target = tiles * c.heads >= 4 * (int64_t)wanted || most_steps <= p.least ? 0 : std::max(wanted / c.heads, 1);
+    p.over_target = p.target ? 1.0f / p.target : 0.0f;
     p.slots = (int)(tiles + (p.target ? p.target + 1 : 0));
 }
 

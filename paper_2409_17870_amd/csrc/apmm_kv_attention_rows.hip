@@ -24,15 +24,14 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 2) void kv_attention_r
     constexpr int R = 4, kPitch = D + 4;  // rows that meet in LDS at a time
     __shared__ __align__(16) float sums[WAVES][R][kPitch];
     __shared__ float bases[WAVES][T], totals[WAVES][T];
-    const int head = blockIdx.x % a.c.heads, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = kv_lane(), n = lane & 15, g = lane >> 4;
-    const int slot = blockIdx.x / a.c.heads;
+    const int slot = kv_divide(blockIdx.x, a.by_heads), head = blockIdx.x - slot * a.c.heads, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = kv_lane(), n = lane & 15, g = lane >> 4;
     KvItem<kRowsStep> it;
-    const bool there = kv_item(a, part, slot, it);
+    const bool there = kv_item<kRowsStep, kRowsTile>(a, part, slot, it);
     kv_note(a, part, slot, head, there, it);
     if (!there) return;
 
-    const int rows = min(it.rows, T), row = it.row0 + min(n, rows - 1), at = row / a.groups;
-    const int pos = it.s.first + at, first_pos = it.s.first + it.row0 / a.groups, last_pos = it.s.first + (it.row0 + rows - 1) / a.groups;
+    const int rows = min(it.rows, T), row = it.row0 + min(n, rows - 1), at = kv_divide(row, a.by_groups);
+    const int pos = it.s.first + at, first_pos = it.s.first + kv_divide(it.row0, a.by_groups), last_pos = it.s.first + kv_divide(it.row0 + rows - 1, a.by_groups);
     auto over_row = [](float v, auto f) {
         v = f(v, __shfl_xor(v, 16));
         return f(v, __shfl_xor(v, 32));
@@ -68,7 +67,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 2) void kv_attention_r
     Step<D> s0, s1;
     {
         uint32_t x[4 * W];
-        kv_load(a.q.data + (int64_t)(it.s.start + at) * a.q.token_stride + (int64_t)(head * a.groups + row % a.groups) * a.q.head_stride + g * (D / 4), a.q.aligned, x);
+        kv_load(a.q.data + (int64_t)(it.s.start + at) * a.q.token_stride + (int64_t)(head * a.groups + row - at * a.groups) * a.q.head_stride + g * (D / 4), a.q.aligned, x);
         if (v < it.to) load(it.key_of(v), __builtin_amdgcn_readlane(ids, 0), __builtin_amdgcn_readlane(ids, 1), s0);
         kv_queries<4 * W, BF16>(x, a.scale, [&](float v) { return over_row(v, larger); }, [&](float v) { return over_row(v, plus); }, q, init, factor);
     }
@@ -209,10 +208,10 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 2) void kv_attention_r
                 for (int j = 0; j < C; ++j) o[j] = fmaf(sums[i][mine][c0 + j], by, o[j]);
             }
             if (it.pieces == 1) {
-                const int to_row = it.row0 + r;
+                const int to_row = it.row0 + r, to_at = kv_divide(to_row, a.by_groups);
                 const float over = sum == 0.0f ? 0.0f : 1.0f / sum;
-                uint16_t *out = a.out.data + (int64_t)(it.s.start + to_row / a.groups) * a.out.token_stride +
-                                (int64_t)(head * a.groups + to_row % a.groups) * a.out.head_stride + c0;
+                uint16_t *out = a.out.data + (int64_t)(it.s.start + to_at) * a.out.token_stride +
+                                (int64_t)(head * a.groups + to_row - to_at * a.groups) * a.out.head_stride + c0;
 #pragma unroll
                 for (int j = 0; j < C; ++j) out[j] = kv_round(o[j] * over, BF16);
             } else {

@@ -45,28 +45,26 @@ template <int D, bool BF16, bool SMALL>
 __global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAttentionArgs a, KvPart part)
 {
     constexpr int W = D / 16, E = D / 32;  // words of a lane's key, blocks of 32 channels of the result
-    typedef typename std::conditional<BF16, uint32_t, uint16_t>::type Scale;
+    typedef typename std::conditional<BF16, kv_u32, kv_u16>::type Scale;
     __shared__ __align__(16) Scale scales[kWaves][64];  // of a step: keys, values
-    const int head = blockIdx.x % a.c.heads, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = kv_lane(), n = lane & 31, h = lane >> 5;
+    const int slot = kv_divide(blockIdx.x, a.by_heads), head = blockIdx.x - slot * a.c.heads, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = kv_lane(), n = lane & 31, h = lane >> 5;
     KvItem<kTilesStep> it;
-    const int slot = blockIdx.x / a.c.heads;
-    const bool there = kv_item(a, part, slot, it);
+    const bool there = kv_item<kTilesStep, kTilesTile>(a, part, slot, it);
     kv_note(a, part, slot, head, there, it);
     if (!there) return;
 
     const int row0 = it.row0 + wave * kRows, rows = min(it.rows - wave * kRows, kRows);
     if (rows <= 0) return;
-    const int row = row0 + min(n, rows - 1), at = row / a.groups;
-    const int pos = it.s.first + at, first_pos = it.s.first + row0 / a.groups, last_pos = it.s.first + (row0 + rows - 1) / a.groups;
+    const int row = row0 + min(n, rows - 1), at = kv_divide(row, a.by_groups);
+    const int pos = it.s.first + at, first_pos = it.s.first + kv_divide(row0, a.by_groups), last_pos = it.s.first + kv_divide(row0 + rows - 1, a.by_groups);
     auto over_row = [](float v, auto f) { return f(v, __shfl_xor(v, 32)); };
     auto larger = [](float x, float y) { return fmaxf(x, y); };
     auto plus = [](float x, float y) { return x + y; };
 
-    // the steps of this wave: those of the workgroup's that some row of it sees
-    auto seen = [&](int key) { return key <= last_pos && (!a.window || key + kTilesStep > first_pos - a.window + 1 || key < a.sinks); };
-    int to = it.to, t = it.from;
-    while (to > t && !seen(it.key_of(to - 1))) --to;
-    while (t < to && !seen(it.key_of(t))) ++t;
+    // the steps of this wave: those of the workgroup's up to its last query (a workgroup's window begins with its first wave: the others' steps before theirs are few)
+    const int ends = last_pos < 0 ? 0 : last_pos / kTilesStep + 1;
+    const int to = min(it.to, ends <= it.sink_steps ? ends : max(ends - it.gap, it.sink_steps));
+    int t = it.from;
 
     // Where a step's codes and scales are.  Operand row 8 i + 4 h' + j of the keys is key 16 h' + 4 i + j; half h of the values' operand s has keys 16 h + 8 s to 16 h + 8 s + 7.
     const int shift = a.c.page_shift, mask = (1 << shift) - 1;
@@ -120,7 +118,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAt
     bool bad, bad_before; // whether keys of those, of the 32 up to `block`, have none
     {
         uint32_t x[4 * W];
-        kv_load(a.q.data + (int64_t)(it.s.start + at) * a.q.token_stride + (int64_t)(head * a.groups + row % a.groups) * a.q.head_stride + h * (D / 2), a.q.aligned, x);
+        kv_load(a.q.data + (int64_t)(it.s.start + at) * a.q.token_stride + (int64_t)(head * a.groups + row - at * a.groups) * a.q.head_stride + h * (D / 2), a.q.aligned, x);
         const Place p = place_of(t, pages_from(t, bad_before), 0);
         ids = pages_from(t + 1, bad);
         if (t < to) {
@@ -199,18 +197,21 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAt
         }
         const int stop = bad || bad_before ? t : min(min(plain_until(), block + 32), to);
         bool again = false;
+        float16v s;
+        Place next;
         while (t < stop) {
             Scales<BF16> ks, vs;
             take_scales(ks, vs);
-            const float16v s = scores();
-            const Place next = place_of(min(t + 1, to - 1), ids, min(t + 1, to - 1) - block - 1);
+            s = scores();
+            next = place_of(min(t + 1, to - 1), ids, min(t + 1, to - 1) - block - 1);
             load_keys(next, k);
-            scale = load_scales(next);
+            const uint32_t scale_after = load_scales(next);
             float sum = 0.0f, weight_sum = 0.0f;
             uint32_t w[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) weigh(i, fmaf(s[2 * i], ks.at(2 * i), 0.0f), fmaf(s[2 * i + 1], ks.at(2 * i + 1), 0.0f), vs, w, sum, weight_sum);
             again = __any((sum > most) | (weight_sum > 60000.0f));
+            scale = scale_after;
             if (again) break;
             total += sum;
             weights += weight_sum;
@@ -220,17 +221,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAt
         }
         if (!again && (t == to || t == block + 32)) continue;
         // step t in general
-        if (again) {  // its keys and scales once more
-            const Place now = place_of(t, t == block ? kv_page_ids(a, it, t, 1) : ids, t == block ? 0 : t - block - 1);
-            load_keys(now, k);
-            scale = load_scales(now);
+        if (!again) {
+            scales[wave][lane] = (Scale)(BF16 ? scale << 16 : scale);
+            s = scores();
+            next = place_of(min(t + 1, to - 1), ids, max(min(t + 1, to - 1) - block - 1, 0));
+            load_keys(next, k);
+            scale = load_scales(next);
         }
         Scales<BF16> ks, vs;
-        take_scales(ks, vs);
-        const float16v s = scores();
-        const Place next = place_of(min(t + 1, to - 1), ids, max(min(t + 1, to - 1) - block - 1, 0));
-        load_keys(next, k);
-        scale = load_scales(next);
+        ks.take(scales[wave] + 16 * h);
+        vs.take(scales[wave] + 16 * h + 32);
         const int first = it.key_of(t) + 16 * h;
         int end = min(it.s.keys, pos + 1);
         if ((bad || bad_before) && first < it.s.keys) {
@@ -251,7 +251,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAt
         if (__any((high > top + kSlack) | (largest > limit))) {
             top = fmaxf(top, over_row(high, larger));
             met = over_row(largest, larger);
-            // 2^E above it, E from -80 (sums of 2^(4 - E) stay in range; scales below 2^-98 lose bits) to 127
+            // 2^E above it, E from -80 (sums of 2^(2 - E) stay in range; scales below 2^-96 lose bits) to 127
             const int e = min(max((int)(__float_as_uint(met) >> 23) - 126, -80), 127);
             limit = ldexpf(1.0f, e);
             const float moved = -top + (kRoom - (float)e), by = __builtin_amdgcn_exp2f(moved - base);
@@ -281,7 +281,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAt
     if (n >= rows) return;
     const bool whole = it.pieces == 1;
     const float over = whole ? (total == 0.0f ? 0.0f : 1.0f / total) : 1.0f;
-    uint16_t *out = a.out.data + (int64_t)(it.s.start + at) * a.out.token_stride + (int64_t)(head * a.groups + row % a.groups) * a.out.head_stride;
+    uint16_t *out = a.out.data + (int64_t)(it.s.start + at) * a.out.token_stride + (int64_t)(head * a.groups + row - at * a.groups) * a.out.head_stride;
     const int64_t place = ((int64_t)slot * a.c.heads + head) * kTilesTile + wave * kRows + n;
     const KvPartial partial = kv_partial(a.partial, part, a.c.heads, D);
 #pragma unroll

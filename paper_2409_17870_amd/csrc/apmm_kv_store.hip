@@ -97,7 +97,7 @@ __global__ __launch_bounds__(64 * kWaves) void kv_write_kernel(KvArgs c, KvTenso
 {
     constexpr int N = D / 16;  // words of a lane's channels, two to a word
     constexpr int P = D / 32;  // 16-bit pieces of a lane
-    __shared__ __align__(16) uint16_t turn[kWaves][D / 4 * 8];
+    __shared__ __align__(16) kv_u16 turn[kWaves][D / 4 * 8];
     Eight e;
     if (!find_eight(c, e) || e.page < 0) return;
     const int lane = kv_lane(), token = lane >> 3, part = lane & 7;
@@ -122,7 +122,7 @@ __global__ __launch_bounds__(64 * kWaves) void kv_write_kernel(KvArgs c, KvTenso
         }
     }
     if (e.whole) {
-        uint16_t *t = turn[threadIdx.x >> 6];
+        kv_u16 *t = turn[threadIdx.x >> 6];
 #pragma unroll
         for (int i = 0; i < P; ++i) t[(part * P + i) * 8 + token] = (uint16_t)(uv[i / 2] >> (16 * (i & 1)));
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -166,7 +166,7 @@ template <int D, bool BF16>
 __global__ __launch_bounds__(64 * kWaves) void kv_read_kernel(KvArgs c, KvTensor k, KvTensor v)
 {
     constexpr int N = D / 16, P = D / 32;
-    __shared__ __align__(16) uint16_t turn[kWaves][D / 4 * 8];
+    __shared__ __align__(16) kv_u16 turn[kWaves][D / 4 * 8];
     Eight e;
     if (!find_eight(c, e)) return;
     const int lane = kv_lane(), token = lane >> 3, part = lane & 7;
@@ -175,7 +175,7 @@ __global__ __launch_bounds__(64 * kWaves) void kv_read_kernel(KvArgs c, KvTensor
     const uint16_t *scales = c.scales + (block << c.page_shift) + e.in_page;
     const uint8_t *keys = c.codes + (block << c.page_shift) * (D / 2) + (int64_t)e.in_page * (D / 2);
     const uint8_t *values = keys + ((int64_t)(D / 2) << c.page_shift);
-    uint16_t *t = turn[threadIdx.x >> 6];
+    kv_u16 *t = turn[threadIdx.x >> 6];
     uint32_t uk[N / 4], uv[N / 4], xk[N], xv[N];
     const uint32_t *from = reinterpret_cast<const uint32_t *>(keys + token * (D / 2)) + part * (N / 4);
     if constexpr (N == 8) {
