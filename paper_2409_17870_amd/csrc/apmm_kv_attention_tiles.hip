@@ -101,6 +101,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAt
         for (int i = 0; i < 2; ++i) v[i] = *reinterpret_cast<const uint4 *>(from + i * (D * 4));
     };
     auto load_scales = [&](const Place &p) -> uint32_t { return *reinterpret_cast<const uint16_t *>(p.scales + (SMALL && (lane & 16) ? p.scales_on : 0) + scale_lane); };
+    // Wherever a step begins, keys, scales and values have been asked for in this order: the wait for the keys is none for the values
+    auto in_order = [] { __builtin_amdgcn_sched_barrier(0); };
     // Pages of steps t to t + 31, and whether one of their keys has none
     auto pages_from = [&](int t, bool &bad) {
         const int ids = kv_page_ids(a, it, t, 1), step = t + (lane >> 1);
@@ -119,12 +121,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAt
     {
         uint32_t x[4 * W];
         kv_load(a.q.data + (int64_t)(it.s.start + at) * a.q.token_stride + (int64_t)(head * a.groups + row - at * a.groups) * a.q.head_stride + h * (D / 2), a.q.aligned, x);
-        const Place p = place_of(t, pages_from(t, bad_before), 0);
+        const Place here = place_of(t, pages_from(t, bad_before), 0);
         ids = pages_from(t + 1, bad);
         if (t < to) {
-            load_keys(p, k);
-            scale = load_scales(p);
-            load_values(p, v);
+            load_keys(here, k);
+            in_order();
+            scale = load_scales(here);
+            in_order();
+            load_values(here, v);
+            in_order();
         }
         kv_queries<4 * W, BF16>(x, a.scale, [&](float v) { return over_row(v, larger); }, [&](float v) { return over_row(v, plus); }, q, init, factor);
     }
@@ -195,42 +200,56 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAt
             bad_before = bad;
             ids = pages_from(t + 1, bad);
         }
-        const int stop = bad || bad_before ? t : min(min(plain_until(), block + 32), to);
+        const int stop = __builtin_amdgcn_readfirstlane(bad || bad_before ? t : min(min(plain_until(), block + 32), to));
         bool again = false;
-        float16v s;
-        Place next;
-        while (t < stop) {
+        if (t < stop) __builtin_amdgcn_s_waitcnt(0x0f70);  // nothing under way here, so that in the loop only its own loads are waited for, and each where it is needed
+        while (t < stop && !again) {
             Scales<BF16> ks, vs;
             take_scales(ks, vs);
-            s = scores();
-            next = place_of(min(t + 1, to - 1), ids, min(t + 1, to - 1) - block - 1);
+            const float16v s = scores();
+            const Place next = place_of(min(t + 1, to - 1), ids, min(t + 1, to - 1) - block - 1);
             load_keys(next, k);
-            const uint32_t scale_after = load_scales(next);
+            in_order();
+            scale = load_scales(next);
+            in_order();
             float sum = 0.0f, weight_sum = 0.0f;
             uint32_t w[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) weigh(i, fmaf(s[2 * i], ks.at(2 * i), 0.0f), fmaf(s[2 * i + 1], ks.at(2 * i + 1), 0.0f), vs, w, sum, weight_sum);
             again = __any((sum > most) | (weight_sum > 60000.0f));
-            scale = scale_after;
-            if (again) break;
+            if (again) {
+                sum = weight_sum = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i] = 0;
+            }
             total += sum;
             weights += weight_sum;
             add(w);
             load_values(next, v);
+            in_order();
             ++t;
         }
-        if (!again && (t == to || t == block + 32)) continue;
-        // step t in general
-        if (!again) {
-            scales[wave][lane] = (Scale)(BF16 ? scale << 16 : scale);
-            s = scores();
-            next = place_of(min(t + 1, to - 1), ids, max(min(t + 1, to - 1) - block - 1, 0));
-            load_keys(next, k);
-            scale = load_scales(next);
+        if (again) {  // back to the step
+            --t;
+            const Place here = place_of(t, t == block ? kv_page_ids(a, it, t, 1) : ids, t == block ? 0 : t - block - 1);
+            load_keys(here, k);
+            in_order();
+            scale = load_scales(here);
+            in_order();
+            load_values(here, v);
+            in_order();
+        } else if (t == to || t == block + 32) {
+            continue;
         }
+        // step t in general
         Scales<BF16> ks, vs;
-        ks.take(scales[wave] + 16 * h);
-        vs.take(scales[wave] + 16 * h + 32);
+        take_scales(ks, vs);
+        const float16v s = scores();
+        const Place next = place_of(min(t + 1, to - 1), ids, max(min(t + 1, to - 1) - block - 1, 0));
+        load_keys(next, k);
+        in_order();
+        scale = load_scales(next);
+        in_order();
         const int first = it.key_of(t) + 16 * h;
         int end = min(it.s.keys, pos + 1);
         if ((bad || bad_before) && first < it.s.keys) {
@@ -272,6 +291,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAt
         weights += weight_sum;
         add(w);
         load_values(next, v);
+        in_order();
         ++t;
     }
 
