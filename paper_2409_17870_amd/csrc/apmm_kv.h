@@ -55,7 +55,8 @@ struct KvPart {
     int from_rows, to_rows;
 };
 struct KvPlan {
-    KvPart rows, tiles;  // kv_attention_rows_kernel's, kv_attention_tiles_kernel's
+    KvPart rows, tiles;     // kv_attention_rows_kernel's, kv_attention_tiles_kernel's
+    int64_t tiles_partial;  // where the latter's pieces begin in the workspace
 };
 KvPlan kv_plan(const KvArgs &c, int groups);
 size_t kv_partial_bytes(const KvPart &part, int heads, int head_dim);  // of the workspace that pieces take

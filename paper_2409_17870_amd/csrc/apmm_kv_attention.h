@@ -139,8 +139,9 @@ __device__ __forceinline__ bool kv_item(const KvAttentionArgs &a, const KvPart &
     it.from = 0;
     it.to = all - it.gap;
     if (it.pieces > 1) {
-        it.from = min(it.part * (int64_t)piece, (int64_t)it.to);
-        it.to = min((it.part + 1) * (int64_t)piece, (int64_t)it.to);
+        const int even = max(kv_pieces(it.to, it.pieces), min(piece, p.least));
+        it.from = min(it.part * (int64_t)even, (int64_t)it.to);
+        it.to = min((it.part + 1) * (int64_t)even, (int64_t)it.to);
     }
     return true;
 }

@@ -9,24 +9,27 @@ namespace {
 
 constexpr int kFewRows = 32;  // of a sequence: those go to kv_attention_rows_kernel
 
-// A workgroup looks at one piece and head (blockIdx.x) and 16 rows of its tile (blockIdx.y), and has work where the piece is the first of several.  16 lanes to a row; what is left of
-// the 256 for fewer rows shares out the pieces, each with its own running base, and meets in LDS.
+// A workgroup looks at one piece and head and 16 rows of its tile, and has work where the piece is the first of several.  16 lanes to a row; what is left of the 256 for fewer rows shares
+// out the pieces, each with its own running base, and meets in LDS.  One launch for both kernels' pieces: those of kv_attention_rows_kernel first.
 template <int D, bool BF16>
-__global__ __launch_bounds__(256) void kv_attention_join_kernel(KvAttentionArgs a, KvPart part)
+__global__ __launch_bounds__(256) void kv_attention_join_kernel(KvAttentionArgs a, KvPlan plan, int of_rows)
 {
+    const bool tiles = (int)blockIdx.x >= of_rows;
+    const KvPart &part = tiles ? plan.tiles : plan.rows;
+    const int in_tile = tiles ? (int)(blockIdx.x - of_rows) % (kTilesTile / 16) : 0, item = tiles ? (int)(blockIdx.x - of_rows) / (kTilesTile / 16) : blockIdx.x;
     constexpr int C = D / 16;  // channels of a lane
     __shared__ float bases[16][16], totals[16][16];  // by threadIdx.x / 16: share of the pieces, row
     __shared__ __align__(16) float sums[256][C];
-    const KvPartial partial = kv_partial(a.partial, part, a.c.heads, D);
-    const KvPieceNote note = partial.note[blockIdx.x];
-    const int first_row = blockIdx.y * 16, rows = min(note.rows - first_row, 16);
+    const KvPartial partial = kv_partial(a.partial + (tiles ? plan.tiles_partial : 0), part, a.c.heads, D);
+    const KvPieceNote note = partial.note[item];
+    const int first_row = in_tile * 16, rows = min(note.rows - first_row, 16);
     if (note.pieces == 0 || rows <= 0) return;
     const int row_slots = rows > 8 ? 16 : rows > 4 ? 8 : rows > 2 ? 4 : rows, shares = 16 / row_slots;
     const int group = threadIdx.x >> 4, row = group % row_slots, share = group / row_slots, c0 = (threadIdx.x & 15) * C;
-    const int head = blockIdx.x - kv_divide(blockIdx.x, a.by_heads) * a.c.heads;
+    const int head = item - kv_divide(item, a.by_heads) * a.c.heads;
     float base = kLowest, total = 0.0f, o[C] = {};
     if (row < rows) {
-        const int64_t place = (int64_t)blockIdx.x * part.tile + first_row + row, step = (int64_t)a.c.heads * part.tile;
+        const int64_t place = (int64_t)item * part.tile + first_row + row, step = (int64_t)a.c.heads * part.tile;
 #pragma unroll 4
         for (int i = share; i < note.pieces; i += shares) {
             const int64_t at = place + i * step;
@@ -71,21 +74,20 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(KvAttentionArgs 
 
 namespace {
 
-// The workgroups of one kernel for sequences of at most `tokens` new tokens in all
-void cut(KvPart &p, const KvArgs &c, int groups, int step, int wanted)
+// How many workgroups one kernel has for sequences of at most `tokens` new tokens in all: `tiles` for a head where nothing is cut.  Nothing is where there are `plenty` anyway.
+void cut(KvPart &p, const KvArgs &c, int64_t tiles, int step, int wanted, int plenty)
 {
-    const int64_t rows = (int64_t)c.tokens * groups;
-    const int64_t tiles = std::min<int64_t>((int64_t)c.tokens * ((groups + p.tile - 1) / p.tile), rows / p.tile + c.sequences);
     const int64_t most_steps = (((int64_t)c.width << c.page_shift) + step - 1) / step;  // of a sequence, as far as the page table goes
-    p.target = tiles * c.heads >= 4 * (int64_t)wanted || most_steps <= p.least ? 0 : std::max(wanted / c.heads, 1);
+    p.target = tiles * c.heads >= plenty || most_steps <= p.least ? 0 : std::max(wanted / c.heads, 1);
     p.over_target = p.target ? 1.0f / p.target : 0.0f;
     p.slots = (int)(tiles + (p.target ? p.target + 1 : 0));
 }
 
 template <int D, bool BF16>
-void join(const KvAttentionArgs &a, const KvPart &part, hipStream_t stream)
+void join(const KvAttentionArgs &a, const KvPlan &plan, hipStream_t stream)
 {
-    kv_attention_join_kernel<D, BF16><<<dim3((uint32_t)((int64_t)part.slots * a.c.heads), part.tile / 16), dim3(256), 0, stream>>>(a, part);
+    const int64_t of_rows = plan.rows.target ? (int64_t)plan.rows.slots * a.c.heads : 0, of_tiles = plan.tiles.target ? (int64_t)plan.tiles.slots * a.c.heads * (kTilesTile / 16) : 0;
+    kv_attention_join_kernel<D, BF16><<<dim3((uint32_t)(of_rows + of_tiles)), dim3(256), 0, stream>>>(a, plan, (int)of_rows);
 }
 
 }  // namespace
@@ -93,25 +95,29 @@ void join(const KvAttentionArgs &a, const KvPart &part, hipStream_t stream)
 KvPlan kv_plan(const KvArgs &c, int groups)
 {
     KvPlan p = {};
-    const int64_t rows = (int64_t)c.tokens * groups;
+    const int64_t rows = (int64_t)c.tokens * groups, sequences = std::min(c.sequences, c.tokens);  // (with new tokens)
     // A sequence's rows are as many as the call's where it is the only one, and no more than one token's where there is no other: else both kernels are launched
     const bool few = rows <= kFewRows || c.tokens <= c.sequences, many = !few && c.sequences == 1;
+    auto tiles = [&](int tile) { return std::min(c.tokens * (int64_t)((groups + tile - 1) / tile), rows / tile + sequences); };
     if (!many) {
         p.rows.tile = kRowsTile;
         p.rows.to_rows = few ? INT32_MAX : kFewRows;
-        const int64_t groups_of = std::min<int64_t>((int64_t)c.sequences, c.tokens) * c.heads * ((std::min<int64_t>(groups, rows) + kRowsTile - 1) / kRowsTile);
+        const int64_t most = std::min(tiles(kRowsTile), few ? INT64_MAX : sequences * (kFewRows / kRowsTile));
+        const int64_t groups_of = sequences * c.heads * ((std::min<int64_t>(groups, rows) + kRowsTile - 1) / kRowsTile);
         p.rows.waves = groups_of >= 512 ? 4 : 8;
         p.rows.least = 64;
-        cut(p.rows, c, groups, kRowsStep, p.rows.waves == 4 ? 2048 : 256);
+        const int wanted = p.rows.waves == 4 ? 2048 : 256;
+        cut(p.rows, c, most, kRowsStep, wanted, 4 * wanted);
     }
     if (!few) {
         p.tiles.tile = kTilesTile;
         p.tiles.waves = 4;
         p.tiles.from_rows = many ? 0 : kFewRows + 1;
         p.tiles.to_rows = INT32_MAX;
-        p.tiles.least = 16;
-        cut(p.tiles, c, groups, kTilesStep, 512);
+        p.tiles.least = 32;
+        cut(p.tiles, c, tiles(kTilesTile), kTilesStep, 512, many ? 1024 : 2048);
     }
+    p.tiles_partial = (int64_t)(kv_partial_bytes(p.rows, c.heads, c.head_dim) / sizeof(float));
     return p;
 }
 
@@ -124,18 +130,20 @@ size_t kv_partial_bytes(const KvPart &part, int heads, int head_dim)
 
 hipError_t launch_kv_attention(const KvAttentionArgs &a, const KvPlan &plan, hipStream_t stream)
 {
-    KvAttentionArgs b = a;
-    for (const KvPart *part : {&plan.rows, &plan.tiles}) {
-        if (!part->tile) continue;
-        const hipError_t e = part == &plan.rows ? launch_kv_attention_rows(b, *part, stream) : launch_kv_attention_tiles(b, *part, stream);
+    if (plan.rows.tile) {
+        const hipError_t e = launch_kv_attention_rows(a, plan.rows, stream);
         if (e != hipSuccess) return e;
-        if (part->target) {
-            if (a.c.head_dim == 128) a.c.bf16 ? join<128, true>(b, *part, stream) : join<128, false>(b, *part, stream);
-            else a.c.bf16 ? join<64, true>(b, *part, stream) : join<64, false>(b, *part, stream);
-            const hipError_t j = hipGetLastError();
-            if (j != hipSuccess) return j;
-        }
-        b.partial += kv_partial_bytes(*part, a.c.heads, a.c.head_dim) / sizeof(float);
+    }
+    if (plan.tiles.tile) {
+        KvAttentionArgs b = a;
+        b.partial += plan.tiles_partial;
+        const hipError_t e = launch_kv_attention_tiles(b, plan.tiles, stream);
+        if (e != hipSuccess) return e;
+    }
+    if (plan.rows.target || plan.tiles.target) {
+        if (a.c.head_dim == 128) a.c.bf16 ? join<128, true>(a, plan, stream) : join<128, false>(a, plan, stream);
+        else a.c.bf16 ? join<64, true>(a, plan, stream) : join<64, false>(a, plan, stream);
+        return hipGetLastError();
     }
     return hipSuccess;
 }

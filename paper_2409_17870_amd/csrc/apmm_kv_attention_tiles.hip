@@ -6,8 +6,6 @@
 // What bounds it is the vector unit: of a step's about 190 instructions 80 unpack codes and 92 are the weights of 16 keys a lane (product with the scale, exponent, power, sum, product with the
 // value's scale and rounding, sum of the rounded ones).  Hence a step that has no hidden keys does not look for the maximum of its scores either: its sums tell afterwards whether a weight was too
 // large for the running maximum.  Every other step (the first, those at the diagonal and at the window's edge, those whose sums are too large) goes the general way.
-#include <type_traits>
-
 #include "apmm_kv_attention.h"
 
 namespace apmm {
@@ -16,37 +14,12 @@ namespace {
 
 constexpr int kWaves = 4, kRows = kTilesTile / kWaves;
 
-// Scales of the 16 keys of a lane: binary16 numbers two to a word, or bfloat16 ones as 32-bit numbers
-template <bool BF16>
-struct Scales {
-    uint32_t w[BF16 ? 16 : 8];
-    __device__ __forceinline__ void take(const void *from)
-    {
-#pragma unroll
-        for (int i = 0; i < (BF16 ? 4 : 2); ++i) {
-            const uint4 x = static_cast<const uint4 *>(from)[i];
-            w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
-        }
-    }
-    __device__ __forceinline__ float at(int i) const
-    {
-        if constexpr (BF16) return __uint_as_float(w[i]);
-        else return i & 1 ? kv_high<false>(w[i / 2]) : kv_low<false>(w[i / 2]);
-    }
-    __device__ __forceinline__ void hide(int i, bool hidden)
-    {
-        if constexpr (BF16) w[i] = hidden ? 0u : w[i];
-        else w[i / 2] &= hidden ? (i & 1 ? 0x0000ffffu : 0xffff0000u) : 0xffffffffu;
-    }
-};
-
 // SMALL: pages of 16 keys, two to a step
 template <int D, bool BF16, bool SMALL>
 __global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAttentionArgs a, KvPart part)
 {
     constexpr int W = D / 16, E = D / 32;  // words of a lane's key, blocks of 32 channels of the result
-    typedef typename std::conditional<BF16, kv_u32, kv_u16>::type Scale;
-    __shared__ __align__(16) Scale scales[kWaves][64];  // of a step: keys, values
+    __shared__ __align__(16) float scales[kWaves][64];  // of a step: keys, values
     const int slot = kv_divide(blockIdx.x, a.by_heads), head = blockIdx.x - slot * a.c.heads, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = kv_lane(), n = lane & 31, h = lane >> 5;
     KvItem<kTilesStep> it;
     const bool there = kv_item<kTilesStep, kTilesTile>(a, part, slot, it);
@@ -110,6 +83,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAt
         return ids;
     };
 
+    // The rows of a wave share the factor of its largest query unless some row's are so small (2^-10 of that) that they would lose bits of it
+    bool one_factor;
     half8 q[W];
     float init, factor;
     uint4 k[D / 64] = {}, v[2] = {};  // of step t, on their way
@@ -131,8 +106,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAt
             load_values(here, v);
             in_order();
         }
-        kv_queries<4 * W, BF16>(x, a.scale, [&](float v) { return over_row(v, larger); }, [&](float v) { return over_row(v, plus); }, q, init, factor);
+        kv_queries<4 * W, BF16>(x, a.scale, [&](float v) {
+            v = over_row(v, larger);
+            float all = v;
+#pragma unroll
+            for (int i = 1; i < 32; i *= 2) all = fmaxf(all, __shfl_xor(all, i));
+            one_factor = !__any(v > 0.0f && v < 0x1p-10f * all);
+            return one_factor ? all : v;
+        }, [&](float v) { return over_row(v, plus); }, q, init, factor);
     }
+
+    const float scale_by = h ? 1.0f : factor;  // of the scale that a lane loads: a key's or a value's
 
     float16v acc[E], init16;
 #pragma unroll
@@ -171,20 +155,24 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAt
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    auto weigh = [&](int i, float x0, float x1, const Scales<BF16> &vs, uint32_t (&w)[8], float &sum, float &weight_sum) {  // two keys
-        const float p0 = __builtin_amdgcn_exp2f(fmaf(x0, factor, base)), p1 = __builtin_amdgcn_exp2f(fmaf(x1, factor, base));
+    auto weigh = [&](int i, float x0, float by0, float x1, float by1, const float (&vs)[16], uint32_t (&w)[8], float &sum, float &weight_sum) {  // two keys
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(x0, by0, base)), p1 = __builtin_amdgcn_exp2f(fmaf(x1, by1, base));
         sum += p0 + p1;
-        half2v pair;
-        pair[0] = (_Float16)fmaf(p0, vs.at(2 * i), 0.0f);
-        pair[1] = (_Float16)fmaf(p1, vs.at(2 * i + 1), 0.0f);
+        const half2v pair = {(_Float16)(p0 * vs[2 * i]), (_Float16)(p1 * vs[2 * i + 1])};
         w[i] = __builtin_bit_cast(uint32_t, pair);
         weight_sum = __builtin_amdgcn_fdot2(pair, (half2v){1, 1}, weight_sum, false);
     };
-    auto take_scales = [&](Scales<BF16> &ks, Scales<BF16> &vs) {
-        scales[wave][lane] = (Scale)(BF16 ? scale << 16 : scale);
-        const Scale *from = scales[wave] + 16 * h;
-        ks.take(from);
-        vs.take(from + 32);
+    auto take_scales = [&](float own, float (&ks)[16], float (&vs)[16]) {
+        scales[wave][lane] = own;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float4v x = *reinterpret_cast<const float4v *>(&scales[wave][16 * h + 4 * i]), y = *reinterpret_cast<const float4v *>(&scales[wave][32 + 16 * h + 4 * i]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                ks[4 * i + j] = x[j];
+                vs[4 * i + j] = y[j];
+            }
+        }
     };
     // Steps from t on that every row of the wave sees all keys of, as far as the places of keys go
     auto plain_until = [&]() {
@@ -200,12 +188,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAt
             bad_before = bad;
             ids = pages_from(t + 1, bad);
         }
-        const int stop = __builtin_amdgcn_readfirstlane(bad || bad_before ? t : min(min(plain_until(), block + 32), to));
+        const int stop = __builtin_amdgcn_readfirstlane(bad || bad_before || !one_factor ? t : min(min(plain_until(), block + 32), to));
         bool again = false;
         if (t < stop) __builtin_amdgcn_s_waitcnt(0x0f70);  // nothing under way here, so that in the loop only its own loads are waited for, and each where it is needed
         while (t < stop && !again) {
-            Scales<BF16> ks, vs;
-            take_scales(ks, vs);
+            float ks[16], vs[16];
+            const float own = kv_scale_value(scale, BF16) * scale_by;
+            take_scales(own, ks, vs);
             const float16v s = scores();
             const Place next = place_of(min(t + 1, to - 1), ids, min(t + 1, to - 1) - block - 1);
             load_keys(next, k);
@@ -215,16 +204,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAt
             float sum = 0.0f, weight_sum = 0.0f;
             uint32_t w[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) weigh(i, fmaf(s[2 * i], ks.at(2 * i), 0.0f), fmaf(s[2 * i + 1], ks.at(2 * i + 1), 0.0f), vs, w, sum, weight_sum);
-            again = __any((sum > most) | (weight_sum > 60000.0f));
-            if (again) {
-                sum = weight_sum = 0.0f;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) w[i] = 0;
+            for (int i = 0; i < 8; ++i) weigh(i, s[2 * i], ks[2 * i], s[2 * i + 1], ks[2 * i + 1], vs, w, sum, weight_sum);
+            again = __any((sum > most) | (weight_sum > 60000.0f) | (own > -kLowest));
+            if (!again) {
+                total += sum;
+                weights += weight_sum;
+                add(w);
             }
-            total += sum;
-            weights += weight_sum;
-            add(w);
             load_values(next, v);
             in_order();
             ++t;
@@ -242,8 +228,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAt
             continue;
         }
         // step t in general
-        Scales<BF16> ks, vs;
-        take_scales(ks, vs);
+        float ks[16], vs[16];
+        take_scales(kv_scale_value(scale, BF16), ks, vs);
         const float16v s = scores();
         const Place next = place_of(min(t + 1, to - 1), ids, max(min(t + 1, to - 1) - block - 1, 0));
         load_keys(next, k);
@@ -261,10 +247,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAt
         for (int i = 0; i < 16; ++i) {
             const int key = first + i;
             const bool hidden = (key >= end) | ((a.window != 0) & (key <= pos - a.window) & (key >= a.sinks));
-            x[i] = hidden ? -__builtin_inff() : fmaf(s[i], ks.at(i), 0.0f);
-            vs.hide(i, hidden);  // weights of hidden keys are zero whatever their scale is
+            x[i] = hidden ? -__builtin_inff() : s[i] * ks[i];
+            vs[i] = hidden ? 0.0f : vs[i];  // weights of hidden keys are zero whatever their scale is
             high = fmaxf(high, x[i]);
-            largest = fmaxf(largest, vs.at(i) <= -kLowest ? vs.at(i) : 0.0f);
+            largest = fmaxf(largest, vs[i] <= -kLowest ? vs[i] : 0.0f);
         }
         high *= factor;
         if (__any((high > top + kSlack) | (largest > limit))) {
@@ -286,7 +272,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAt
         float sum = 0.0f, weight_sum = 0.0f;
         uint32_t w[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) weigh(i, x[2 * i], x[2 * i + 1], vs, w, sum, weight_sum);
+        for (int i = 0; i < 8; ++i) weigh(i, x[2 * i], factor, x[2 * i + 1], factor, vs, w, sum, weight_sum);
         total += sum;
         weights += weight_sum;
         add(w);

@@ -301,6 +301,35 @@ def test_each_row_has_its_own_range(gpu, dtype, new, heads, groups):
     close(torch, got[0::2], exact[0::2], near[0::2])
 
 
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("smaller", [4, 9, 14])
+def test_queries_of_different_sizes(gpu, dtype, smaller):
+    """Rows of a tile whose queries are 2^-smaller of the others': the scores of neither lose bits."""
+    torch, binding = gpu
+    dt = getattr(torch, dtype)
+    x = Batch(torch, dt, 128, 2, 2, 16, [300], [100], seed=17, fused=False)
+    q = x.q.clone()
+    q[1::3] *= 2.0 ** -smaller
+    scale = 128 ** -0.5 * 2.0 ** (smaller // 2)
+    got = binding.apmm_kv_attention(q, *x.args, x.starts_gpu, scale=scale)
+    close(torch, got, *ref.attention(q, x.codes, x.scales, x.table, x.lengths, x.starts, 0, 0, scale))
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_scales_near_the_largest_number(gpu, new):
+    """A key scale whose product with the factor of the queries is beyond 32-bit numbers: queries that are zero weigh its key like the others."""
+    torch, binding = gpu
+    x = Batch(torch, torch.bfloat16, 128, 2, 2, 16, [200], [new], seed=19, fused=False)
+    scales = x.scales.clone()
+    for at in (3, 45, 77, 140):
+        scales[int(x.table[0, at // 16]), :, 0, at % 16] = 2.0 ** 122
+    q = x.q.clone()
+    q[::2] = 0.0
+    got = binding.apmm_kv_attention(q, x.codes, scales, *x.args[2:], x.starts_gpu)
+    want, near = ref.attention(q, x.codes, scales, x.table, x.lengths, x.starts, 0, 0, 128 ** -0.5)
+    close(torch, got[::2], want[::2], near[::2])
+
+
 def test_pages_that_are_none(gpu):
     """Page numbers outside of the cache: their tokens are not written, read as zeros and are not seen.  Lengths beyond the table, starts that do not fit: nothing outside of the buffers."""
     torch, binding = gpu
