@@ -49,7 +49,6 @@ struct KvPart {
     int tile;    // rows of a workgroup; 0: the kernel is not launched
     int waves;   // of a workgroup
     int target;  // 0: nothing is cut
-    float over_target;
     int least;
     int slots;   // most pieces there can be
     int from_rows, to_rows;

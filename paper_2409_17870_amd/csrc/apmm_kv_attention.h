@@ -30,7 +30,7 @@ constexpr int kRowsStep = 32;    // keys of one step
 constexpr int kTilesStep = 32;
 
 hipError_t launch_kv_attention_rows(const KvAttentionArgs &a, const KvPart &part, hipStream_t stream);
-hipError_t launch_kv_attention_tiles(const KvAttentionArgs &a, const KvPart &part, hipStream_t stream);
+hipError_t launch_kv_attention_tiles(const KvAttentionArgs &a, const KvPlan &plan, hipStream_t stream);
 
 #ifdef __HIPCC__
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
@@ -84,16 +84,26 @@ __device__ __forceinline__ bool kv_item(const KvAttentionArgs &a, const KvPart &
     if (lane < a.c.sequences) s = kv_sequence(a.c, lane);  // the first 64 stay in registers
     kv_extent<STEP, TILE>(a, s, p, tiles, steps);
     if (p.target) {
-        float work = (float)tiles * (float)steps;
+        float work = (float)tiles * (float)steps, all = (float)tiles;
         for (int at = lane + 64; at < a.c.sequences; at += 64) {
             int t, n;
             kv_extent<STEP, TILE>(a, kv_sequence(a.c, at), p, t, n);
             work += (float)t * (float)n;
+            all += (float)t;
         }
+        auto sum = [](float v) {
 #pragma unroll
-        for (int d = 1; d < 64; d *= 2) work += __shfl_xor(work, d);
+            for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
+            return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v)));  // (and what follows from it is the same for the wave)
+        };
+        work = sum(work);
+        all = sum(all);
+        // A tile's last piece is half a piece too many on average: so much less than `target` is asked for, and, where the pieces are more than that nevertheless, a whole one
         // (rounding: a piece may be 2^-20 shorter than the work asks for, for which there is one slot more)
-        piece = __builtin_amdgcn_readfirstlane(max((int)ceilf(fminf(work * p.over_target * (1.0f - 0x1p-20f), 0x1p30f)), p.least));
+        auto length = [&](float pieces) { return __builtin_amdgcn_readfirstlane(max((int)ceilf(fminf(work / pieces * (1.0f - 0x1p-20f), 0x1p30f)), p.least)); };
+        const float target = (float)p.target;
+        piece = length(fmaxf(target - 0.5f * all, 0.5f * target));
+        if (a.c.sequences <= 64 && all < target && sum((float)(tiles * kv_pieces(steps, piece))) > target) piece = length(target - all);
     }
     int rest, l;
     const int pieces = kv_pieces(steps, piece), own = tiles * pieces, to = kv_scan(own);
@@ -165,12 +175,12 @@ __host__ __device__ inline KvPartial kv_partial(float *at, const KvPart &part, i
     return p;
 }
 template <int STEP>
-__device__ __forceinline__ void kv_note(const KvAttentionArgs &a, const KvPart &p, int slot, int head, bool there, const KvItem<STEP> &it)
+__device__ __forceinline__ void kv_note(const KvAttentionArgs &a, const KvPart &p, float *partials, int slot, int head, bool there, const KvItem<STEP> &it)
 {
     if (!p.target || threadIdx.x) return;
     KvPieceNote n = {};
     if (there && it.part == 0 && it.pieces > 1) n = {it.s.start, it.row0, min(it.rows, p.tile), it.pieces};
-    kv_partial(a.partial, p, a.c.heads, a.c.head_dim).note[(int64_t)slot * a.c.heads + head] = n;
+    kv_partial(partials, p, a.c.heads, a.c.head_dim).note[(int64_t)slot * a.c.heads + head] = n;
 }
 
 // Four words of a matrix operand from one word of codes: nibbles 0 and 4, 1 and 5, 2 and 6, 3 and 7, those of even number as u 2^-24, of odd number as u 2^-20

@@ -79,7 +79,6 @@ void cut(KvPart &p, const KvArgs &c, int64_t tiles, int step, int wanted, int pl
 {
     const int64_t most_steps = (((int64_t)c.width << c.page_shift) + step - 1) / step;  // of a sequence, as far as the page table goes
     p.target = tiles * c.heads >= plenty || most_steps <= p.least ? 0 : std::max(wanted / c.heads, 1);
-    p.over_target = p.target ? 1.0f / p.target : 0.0f;
     p.slots = (int)(tiles + (p.target ? p.target + 1 : 0));
 }
 
@@ -96,7 +95,7 @@ KvPlan kv_plan(const KvArgs &c, int groups)
 {
     KvPlan p = {};
     const int64_t rows = (int64_t)c.tokens * groups, sequences = std::min(c.sequences, c.tokens);  // (with new tokens)
-    // A sequence's rows are as many as the call's where it is the only one, and no more than one token's where there is no other: else both kernels are launched
+    // A sequence's rows are as many as the call's where it is the only one, and no more than one token's where there is no other: else workgroups of both kinds
     const bool few = rows <= kFewRows || c.tokens <= c.sequences, many = !few && c.sequences == 1;
     auto tiles = [&](int tile) { return std::min(c.tokens * (int64_t)((groups + tile - 1) / tile), rows / tile + sequences); };
     if (!many) {
@@ -104,8 +103,8 @@ KvPlan kv_plan(const KvArgs &c, int groups)
         p.rows.to_rows = few ? INT32_MAX : kFewRows;
         const int64_t most = std::min(tiles(kRowsTile), few ? INT64_MAX : sequences * (kFewRows / kRowsTile));
         const int64_t groups_of = sequences * c.heads * ((std::min<int64_t>(groups, rows) + kRowsTile - 1) / kRowsTile);
-        p.rows.waves = groups_of >= 512 ? 4 : 8;
-        p.rows.least = 64;
+        p.rows.waves = !few || groups_of >= 512 ? 4 : 8;
+        p.rows.least = p.rows.waves == 4 ? 64 : 48;
         const int wanted = p.rows.waves == 4 ? 2048 : 256;
         cut(p.rows, c, most, kRowsStep, wanted, 4 * wanted);
     }
@@ -130,16 +129,8 @@ size_t kv_partial_bytes(const KvPart &part, int heads, int head_dim)
 
 hipError_t launch_kv_attention(const KvAttentionArgs &a, const KvPlan &plan, hipStream_t stream)
 {
-    if (plan.rows.tile) {
-        const hipError_t e = launch_kv_attention_rows(a, plan.rows, stream);
-        if (e != hipSuccess) return e;
-    }
-    if (plan.tiles.tile) {
-        KvAttentionArgs b = a;
-        b.partial += plan.tiles_partial;
-        const hipError_t e = launch_kv_attention_tiles(b, plan.tiles, stream);
-        if (e != hipSuccess) return e;
-    }
+    const hipError_t e = plan.tiles.tile ? launch_kv_attention_tiles(a, plan, stream) : launch_kv_attention_rows(a, plan.rows, stream);
+    if (e != hipSuccess) return e;
     if (plan.rows.target || plan.tiles.target) {
         if (a.c.head_dim == 128) a.c.bf16 ? join<128, true>(a, plan, stream) : join<128, false>(a, plan, stream);
         else a.c.bf16 ? join<64, true>(a, plan, stream) : join<64, false>(a, plan, stream);

@@ -6,7 +6,7 @@
 // What bounds it is the vector unit: of a step's about 190 instructions 80 unpack codes and 92 are the weights of 16 keys a lane (product with the scale, exponent, power, sum, product with the
 // value's scale and rounding, sum of the rounded ones).  Hence a step that has no hidden keys does not look for the maximum of its scores either: its sums tell afterwards whether a weight was too
 // large for the running maximum.  Every other step (the first, those at the diagonal and at the window's edge, those whose sums are too large) goes the general way.
-#include "apmm_kv_attention.h"
+#include "apmm_kv_attention_rows.h"
 
 namespace apmm {
 
@@ -16,14 +16,14 @@ constexpr int kWaves = 4, kRows = kTilesTile / kWaves;
 
 // SMALL: pages of 16 keys, two to a step
 template <int D, bool BF16, bool SMALL>
-__global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAttentionArgs a, KvPart part)
+__device__ __forceinline__ void kv_attention_tiles(const KvAttentionArgs &a, const KvPart &part, float *partials, int block_id)
 {
     constexpr int W = D / 16, E = D / 32;  // words of a lane's key, blocks of 32 channels of the result
     __shared__ __align__(16) float scales[kWaves][64];  // of a step: keys, values
-    const int slot = kv_divide(blockIdx.x, a.by_heads), head = blockIdx.x - slot * a.c.heads, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = kv_lane(), n = lane & 31, h = lane >> 5;
+    const int slot = kv_divide(block_id, a.by_heads), head = block_id - slot * a.c.heads, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = kv_lane(), n = lane & 31, h = lane >> 5;
     KvItem<kTilesStep> it;
     const bool there = kv_item<kTilesStep, kTilesTile>(a, part, slot, it);
-    kv_note(a, part, slot, head, there, it);
+    kv_note(a, part, partials, slot, head, there, it);
     if (!there) return;
 
     const int row0 = it.row0 + wave * kRows, rows = min(it.rows - wave * kRows, kRows);
@@ -289,7 +289,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAt
     const float over = whole ? (total == 0.0f ? 0.0f : 1.0f / total) : 1.0f;
     uint16_t *out = a.out.data + (int64_t)(it.s.start + at) * a.out.token_stride + (int64_t)(head * a.groups + row - at * a.groups) * a.out.head_stride;
     const int64_t place = ((int64_t)slot * a.c.heads + head) * kTilesTile + wave * kRows + n;
-    const KvPartial partial = kv_partial(a.partial, part, a.c.heads, D);
+    const KvPartial partial = kv_partial(partials, part, a.c.heads, D);
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
         float o[16];
@@ -314,20 +314,30 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAt
     if (!whole && h == 0) partial.row[place] = make_float2(-base, total);
 }
 
-template <int D, bool BF16>
-void launch(const KvAttentionArgs &a, const KvPart &part, hipStream_t stream)
+// Workgroups of both kinds in one launch: those of tiles first, which take long; those of sequences with few rows come in where the others leave room (two launches one after the other took
+// 15 us more of a batch of 5 pieces of prompts and 19 sequences with a new token each, 3000 tokens at most).
+template <int D, bool BF16, bool SMALL>
+__global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAttentionArgs a, KvPlan plan, int of_tiles)
 {
-    const dim3 grid((uint32_t)((int64_t)part.slots * a.c.heads)), block(64 * kWaves);
-    if (a.c.page_shift == 4) kv_attention_tiles_kernel<D, BF16, true><<<grid, block, 0, stream>>>(a, part);
-    else kv_attention_tiles_kernel<D, BF16, false><<<grid, block, 0, stream>>>(a, part);
+    if ((int)blockIdx.x < of_tiles) kv_attention_tiles<D, BF16, SMALL>(a, plan.tiles, a.partial + plan.tiles_partial, blockIdx.x);
+    else kv_attention_rows<D, BF16, kWaves>(a, plan.rows, blockIdx.x - of_tiles);
+}
+
+template <int D, bool BF16>
+void launch(const KvAttentionArgs &a, const KvPlan &plan, hipStream_t stream)
+{
+    const int of_tiles = plan.tiles.slots * a.c.heads, of_rows = plan.rows.tile ? plan.rows.slots * a.c.heads : 0;
+    const dim3 grid((uint32_t)(of_tiles + of_rows)), block(64 * kWaves);
+    if (a.c.page_shift == 4) kv_attention_tiles_kernel<D, BF16, true><<<grid, block, 0, stream>>>(a, plan, of_tiles);
+    else kv_attention_tiles_kernel<D, BF16, false><<<grid, block, 0, stream>>>(a, plan, of_tiles);
 }
 
 }  // namespace
 
-hipError_t launch_kv_attention_tiles(const KvAttentionArgs &a, const KvPart &part, hipStream_t stream)
+hipError_t launch_kv_attention_tiles(const KvAttentionArgs &a, const KvPlan &plan, hipStream_t stream)
 {
-    if (a.c.head_dim == 128) a.c.bf16 ? launch<128, true>(a, part, stream) : launch<128, false>(a, part, stream);
-    else a.c.bf16 ? launch<64, true>(a, part, stream) : launch<64, false>(a, part, stream);
+    if (a.c.head_dim == 128) a.c.bf16 ? launch<128, true>(a, plan, stream) : launch<128, false>(a, plan, stream);
+    else a.c.bf16 ? launch<64, true>(a, plan, stream) : launch<64, false>(a, plan, stream);
     return hipGetLastError();
 }
 
