@@ -40,6 +40,7 @@ apmm_status check_sizes(const apmm_kv_cache *c, const apmm_kv_batch *b, apmm::Kv
     a.page_shift = __builtin_ctz((unsigned)c->page_size);
     a.head_dim = c->head_dim;
     a.bf16 = c->dtype == APMM_BF16;
+    a.by_heads = apmm::kv_divisor(c->kv_heads);
     return APMM_OK;
 }
 
@@ -148,7 +149,6 @@ apmm_status apmm_kv_attention(const apmm_kv_cache *cache, const apmm_kv_batch *b
     if (need && !aligned(workspace, 16)) return fail(APMM_ERR_INVALID_ARG, "kv_attention: workspace must be 16-byte aligned");
     a.groups = q_heads / cache->kv_heads;
     a.by_groups = apmm::kv_divisor(a.groups);
-    a.by_heads = apmm::kv_divisor(cache->kv_heads);
     a.window = (int)window;
     a.sinks = window ? (int)sinks : 0;
     a.scale = scale;

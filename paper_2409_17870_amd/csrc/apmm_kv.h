@@ -24,6 +24,7 @@ struct KvArgs {
     int64_t pages, table_stride;
     int sequences, tokens, width, heads, page_shift, head_dim;
     bool bf16;
+    uint64_t by_heads;       // what kv_divide divides by heads with
 };
 
 struct KvTensor {  // rows of head_dim contiguous elements
@@ -36,7 +37,7 @@ struct KvAttentionArgs {
     KvArgs c;
     KvTensor q, out;
     int groups;        // query heads to a key/value head
-    uint64_t by_groups, by_heads;  // what kv_divide divides by groups and by key/value heads with
+    uint64_t by_groups;  // what kv_divide divides by groups with
     int window, sinks; // window 0: none
     float scale;
     float *partial;    // results of pieces of sequences: see KvPlan
@@ -131,6 +132,13 @@ __device__ __forceinline__ bool kv_find(int sequences, int unit, int &b, int &re
         before = __builtin_amdgcn_readlane(to, 63);
     }
     return false;
+}
+
+// The larger of two 16-bit numbers each
+__device__ __forceinline__ uint32_t kv_fold_max(uint32_t m, uint32_t w)
+{
+    typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(us2, m), __builtin_bit_cast(us2, w)));
 }
 
 __device__ __forceinline__ float kv_scale_value(uint32_t bits, bool bf16)

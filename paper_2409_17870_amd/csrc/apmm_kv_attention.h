@@ -205,12 +205,6 @@ __device__ __forceinline__ float kv_low(uint32_t w) { return BF16 ? __uint_as_fl
 template <bool BF16>
 __device__ __forceinline__ float kv_high(uint32_t w) { return BF16 ? __uint_as_float(w & 0xffff0000u) : (float)__builtin_bit_cast(half2v, w)[1]; }
 
-// The larger of two 16-bit numbers each
-__device__ __forceinline__ uint32_t kv_fold_max(uint32_t m, uint32_t w)
-{
-    typedef unsigned short us2 __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(us2, m), __builtin_bit_cast(us2, w)));
-}
 // The larger of m and a magnitude's bits, if that is finite
 template <bool BF16>
 __device__ __forceinline__ uint32_t kv_finite_max(uint32_t m, uint32_t bits)

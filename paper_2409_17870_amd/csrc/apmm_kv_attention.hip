@@ -26,7 +26,7 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(KvAttentionArgs 
     if (note.pieces == 0 || rows <= 0) return;
     const int row_slots = rows > 8 ? 16 : rows > 4 ? 8 : rows > 2 ? 4 : rows, shares = 16 / row_slots;
     const int group = threadIdx.x >> 4, row = group % row_slots, share = group / row_slots, c0 = (threadIdx.x & 15) * C;
-    const int head = item - kv_divide(item, a.by_heads) * a.c.heads;
+    const int head = item - kv_divide(item, a.c.by_heads) * a.c.heads;
     float base = kLowest, total = 0.0f, o[C] = {};
     if (row < rows) {
         const int64_t place = (int64_t)item * part.tile + first_row + row, step = (int64_t)a.c.heads * part.tile;

@@ -24,7 +24,7 @@ __device__ __forceinline__ void kv_attention_rows(const KvAttentionArgs &a, cons
     constexpr int R = 4, kPitch = D + 4;  // rows that meet in LDS at a time
     __shared__ __align__(16) float sums[WAVES][R][kPitch];
     __shared__ float bases[WAVES][T], totals[WAVES][T];
-    const int slot = kv_divide(block, a.by_heads), head = block - slot * a.c.heads, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = kv_lane(), n = lane & 15, g = lane >> 4;
+    const int slot = kv_divide(block, a.c.by_heads), head = block - slot * a.c.heads, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = kv_lane(), n = lane & 15, g = lane >> 4;
     KvItem<kRowsStep> it;
     const bool there = kv_item<kRowsStep, kRowsTile>(a, part, slot, it);
     kv_note(a, part, a.partial, slot, head, there, it);

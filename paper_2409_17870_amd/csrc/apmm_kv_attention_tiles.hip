@@ -20,7 +20,7 @@ __device__ __forceinline__ void kv_attention_tiles(const KvAttentionArgs &a, con
 {
     constexpr int W = D / 16, E = D / 32;  // words of a lane's key, blocks of 32 channels of the result
     __shared__ __align__(16) float scales[kWaves][64];  // of a step: keys, values
-    const int slot = kv_divide(block_id, a.by_heads), head = block_id - slot * a.c.heads, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = kv_lane(), n = lane & 31, h = lane >> 5;
+    const int slot = kv_divide(block_id, a.c.by_heads), head = block_id - slot * a.c.heads, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = kv_lane(), n = lane & 31, h = lane >> 5;
     KvItem<kTilesStep> it;
     const bool there = kv_item<kTilesStep, kTilesTile>(a, part, slot, it);
     kv_note(a, part, partials, slot, head, there, it);

@@ -3,10 +3,11 @@
 // A row x (head_dim numbers of a token and head) becomes s = max |x| / 15 rounded to its type and codes u = clamp(floor(x / (2 s)) + 8, 0, 15): the nearest odd
 // multiple 2 u - 15 of s, ties upward, as apmm_quantize_pack_activations has it.
 //
-// One wave takes the up to eight tokens of an aligned eight of positions, one head, keys and values: eight lanes to a token, head_dim / 8 channels to a lane.  The eight tokens of
+// One wave takes the up to eight tokens of an aligned eight of positions, one head, keys and values: eight lanes to a token.  The eight tokens of
 // a channel are neighbours in the cache's values, so they are turned in LDS and written whole (an eight that is not all new is written in pieces of 16 bits, what is there
 // of earlier tokens stays).  Bound by HBM: 4 bytes a channel in or out, one and a bit in the cache.
 #include <algorithm>
+#include <type_traits>
 
 #include "apmm_kv.h"
 
@@ -28,14 +29,14 @@ struct Eight {  // of one wave
 __device__ __forceinline__ bool find_eight(const KvArgs &c, Eight &e)
 {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t unit = (int64_t)blockIdx.x * kWaves + wave;
-    e.head = (int)(unit % c.heads);
+    const int unit = blockIdx.x * kWaves + wave, eight = kv_divide(unit, c.by_heads);  // (fewer than 2^30 units: 2^28 for tokens, 2^27 for sequences at most)
+    e.head = unit - eight * c.heads;
     int b, rest;
     auto count = [&](int at) {
         const KvSequence s = kv_sequence(c, at);
         return s.n ? ((s.first + s.n - 1) >> 3) - (s.first >> 3) + 1 : 0;
     };
-    if (!kv_find(c.sequences, (int)(unit / c.heads), b, rest, count)) return false;
+    if (!kv_find(c.sequences, eight, b, rest, count)) return false;
     e.s = kv_sequence(c, b);
     e.first = ((e.s.first >> 3) + rest) * 8;
     e.page = e.first >= 0 && e.first < e.s.keys ? c.table[b * c.table_stride + (e.first >> c.page_shift)] : -1;
@@ -47,6 +48,31 @@ __device__ __forceinline__ bool find_eight(const KvArgs &c, Eight &e)
     return true;
 }
 
+// A lane's channels: eight that follow each other, and with head_dim 128 eight more 64 behind them, so that eight lanes move 128 bytes at a time
+template <int N>
+__device__ __forceinline__ void load_row(const uint16_t *row, bool aligned, int part, uint32_t (&x)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+        uint32_t w[4];
+        kv_load(row + 64 * i + 8 * part, aligned, w);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[4 * i + j] = w[j];
+    }
+}
+template <int N>
+__device__ __forceinline__ void store_row(uint16_t *row, bool aligned, int part, const uint32_t (&x)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+        const uint32_t w[4] = {x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
+        kv_store(row + 64 * i + 8 * part, aligned, w);
+    }
+}
+
+// The i-th four of a lane's channels among all of them
+__device__ __forceinline__ int four_of(int part, int i) { return i / 2 * 16 + part * 2 + (i & 1); }
+
 // Largest of the eight lanes of a token
 __device__ __forceinline__ uint32_t max_over_eight(uint32_t v)
 {
@@ -55,40 +81,46 @@ __device__ __forceinline__ uint32_t max_over_eight(uint32_t v)
     return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, true));  // eight lanes mirrored
 }
 
+__device__ __forceinline__ int floor_of(float x)
+{
+    int i;
+    asm("v_cvt_flr_i32_f32 %0, %1" : "=v"(i) : "v"(x));  // (0 for NaN)
+    return i;
+}
+
 // Scale bits and the codes of a lane's channels, eight to a word, channel order from the low bits
 template <int N, bool BF16>
 __device__ __forceinline__ uint32_t quantise(const uint32_t (&x)[N], uint32_t (&u)[N / 4])
 {
-    uint32_t top = 0;
+    uint32_t top2 = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i) top = max(top, max(x[i] & 0x7fffu, (x[i] >> 16) & 0x7fffu));  // |x| orders like its bit pattern
-    top = max_over_eight(top);
+    for (int i = 0; i < N; ++i) top2 = kv_fold_max(top2, x[i] & 0x7fff7fffu);  // |x| orders like its bit pattern
+    const uint32_t top = max_over_eight(max(top2 & 0xffffu, top2 >> 16));
     constexpr uint32_t kInfinity = BF16 ? 0x7f80u : 0x7c00u;
     uint32_t scale = kv_round(kv_scale_value(top, BF16) / 15.0f, BF16);
     if (top >= kInfinity) scale = kInfinity | (kInfinity >> 1);  // a number that is not finite: no scale, the row reads back as NaN
-    float s = kv_scale_value(scale, BF16), by = 1.0f;
-    if (BF16 && s < 0x1p-64f) {  // 1 / s stays in range
-        by = 0x1p64f;
-        s *= by;
-    }
-    // t = x / (2 s) up to 2^-23 of itself.  What is not an integer is 2^-12 from every one but zero (numbers of 11 bits and |t| <= 8.01), so moving t up by 2^-21 |t|
-    // gives the floor of the exact quotient.
-    const float half_r = s > 0.0f ? 1.0f / s * 0.5f : 0.0f;  // (no scale, or one that rounds to zero: every code is that of +1)
+    const float s = kv_scale_value(scale, BF16);
+    const bool small = s < (BF16 ? 0x1p-64f : 0x1p-18f);  // 1 / s could leave the range, or s has been rounded by so much that |t| passes 8
+    const float by = BF16 && small ? 0x1p64f : 1.0f, r = 0.5f / (s * by);
+    // t = x / (2 s) up to 2^-23 of itself.  What is not an integer is 2^-12 from every one but zero (numbers of 11 bits and |t| <= 8, or a few bits and |t| <= 12), so moving t up by
+    // 2^-21 |t| gives the floor of the exact quotient.  Codes less 8, which the sum puts on all eight of a word.
+    auto codes = [&](auto general) {
 #pragma unroll
-    for (int i = 0; i < N / 4; ++i) {
-        uint32_t w = 0;
+        for (int i = 0; i < N / 4; ++i) {
+            uint32_t w = 0x88888888u;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const uint32_t bits = j & 1 ? x[4 * i + j / 2] >> 16 : x[4 * i + j / 2] & 0xffffu;
-            float v = kv_scale_value(bits, BF16);
-            if (BF16) v *= by;
-            if (!(s > 0.0f)) v = 0.0f;
-            const float t = fmaf(v, half_r, 0.0f);
-            const float code = __builtin_amdgcn_fmed3f(floorf(fmaf(fabsf(t), 0x1p-21f, t)) + 8.0f, 0.0f, 15.0f);
-            w |= (uint32_t)code << (4 * j);
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t bits = j & 1 ? x[4 * i + j / 2] >> 16 : x[4 * i + j / 2] & 0xffffu;
+                const float v = kv_scale_value(bits, BF16), t = (general ? v * by : v) * r;
+                int code = floor_of(fmaf(fabsf(t), 0x1p-21f, t));
+                if (general) code = min(max(code, -8), 7);
+                w += (uint32_t)code << (4 * j);
+            }
+            u[i] = s > 0.0f ? w : 0x88888888u;  // (no scale, or one that rounds to zero: every code is that of +1)
         }
-        u[i] = w;
-    }
+    };
+    if (__any(small)) codes(std::true_type());
+    else codes(std::false_type());
     return scale;
 }
 
@@ -103,8 +135,8 @@ __global__ __launch_bounds__(64 * kWaves) void kv_write_kernel(KvArgs c, KvTenso
     const int lane = kv_lane(), token = lane >> 3, part = lane & 7;
     const int64_t row = e.s.start + (e.is_new ? e.first + token - e.s.first : 0);  // (a lane without one reads the first)
     uint32_t xk[N], xv[N];
-    kv_load(k.data + row * k.token_stride + e.head * k.head_stride + part * 2 * N, k.aligned, xk);
-    kv_load(v.data + row * v.token_stride + e.head * v.head_stride + part * 2 * N, v.aligned, xv);
+    load_row(k.data + row * k.token_stride + e.head * k.head_stride, k.aligned, part, xk);
+    load_row(v.data + row * v.token_stride + e.head * v.head_stride, v.aligned, part, xv);
     uint32_t uk[N / 4], uv[N / 4];
     const uint32_t sk = quantise<N, BF16>(xk, uk), sv = quantise<N, BF16>(xv, uv);
 
@@ -113,9 +145,9 @@ __global__ __launch_bounds__(64 * kWaves) void kv_write_kernel(KvArgs c, KvTenso
     uint8_t *keys = c.codes + (block << c.page_shift) * (D / 2) + (int64_t)e.in_page * (D / 2);
     uint16_t *values = reinterpret_cast<uint16_t *>(keys + ((int64_t)(D / 2) << c.page_shift));  // (an eight of tokens has its place at the same byte)
     if (e.is_new) {
-        uint32_t *to = reinterpret_cast<uint32_t *>(keys + token * (D / 2)) + part * (N / 4);
-        if constexpr (N == 8) *reinterpret_cast<uint2 *>(to) = make_uint2(uk[0], uk[1]);
-        else to[0] = uk[0];
+        uint32_t *to = reinterpret_cast<uint32_t *>(keys + token * (D / 2)) + part;
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) to[8 * i] = uk[i];
         if (part == 0) {
             scales[token] = (uint16_t)sk;
             scales[((int64_t)1 << c.page_shift) + token] = (uint16_t)sv;
@@ -124,13 +156,13 @@ __global__ __launch_bounds__(64 * kWaves) void kv_write_kernel(KvArgs c, KvTenso
     if (e.whole) {
         kv_u16 *t = turn[threadIdx.x >> 6];
 #pragma unroll
-        for (int i = 0; i < P; ++i) t[(part * P + i) * 8 + token] = (uint16_t)(uv[i / 2] >> (16 * (i & 1)));
+        for (int i = 0; i < P; ++i) t[four_of(part, i) * 8 + token] = (uint16_t)(uv[i / 2] >> (16 * (i & 1)));
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         if constexpr (P == 4) reinterpret_cast<uint2 *>(values)[lane] = reinterpret_cast<const uint2 *>(t)[lane];
         else reinterpret_cast<uint32_t *>(values)[lane] = reinterpret_cast<const uint32_t *>(t)[lane];
     } else if (e.is_new) {
 #pragma unroll
-        for (int i = 0; i < P; ++i) values[(part * P + i) * 8 + token] = (uint16_t)(uv[i / 2] >> (16 * (i & 1)));
+        for (int i = 0; i < P; ++i) values[four_of(part, i) * 8 + token] = (uint16_t)(uv[i / 2] >> (16 * (i & 1)));
     }
 }
 
@@ -165,7 +197,7 @@ __device__ __forceinline__ void values_of(const uint32_t (&u)[N / 4], uint32_t s
 template <int D, bool BF16>
 __global__ __launch_bounds__(64 * kWaves) void kv_read_kernel(KvArgs c, KvTensor k, KvTensor v)
 {
-    constexpr int N = D / 16, P = D / 32;
+    constexpr int N = D / 16;
     __shared__ __align__(16) kv_u16 turn[kWaves][D / 4 * 8];
     Eight e;
     if (!find_eight(c, e)) return;
@@ -177,19 +209,15 @@ __global__ __launch_bounds__(64 * kWaves) void kv_read_kernel(KvArgs c, KvTensor
     const uint8_t *values = keys + ((int64_t)(D / 2) << c.page_shift);
     kv_u16 *t = turn[threadIdx.x >> 6];
     uint32_t uk[N / 4], uv[N / 4], xk[N], xv[N];
-    const uint32_t *from = reinterpret_cast<const uint32_t *>(keys + token * (D / 2)) + part * (N / 4);
-    if constexpr (N == 8) {
-        const uint2 w = *reinterpret_cast<const uint2 *>(from);
-        uk[0] = w.x; uk[1] = w.y;
-        reinterpret_cast<uint2 *>(t)[lane] = reinterpret_cast<const uint2 *>(values)[lane];
-    } else {
-        uk[0] = from[0];
-        reinterpret_cast<uint32_t *>(t)[lane] = reinterpret_cast<const uint32_t *>(values)[lane];
-    }
+    const uint32_t *from = reinterpret_cast<const uint32_t *>(keys + token * (D / 2)) + part;
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) uk[i] = from[8 * i];
+    if constexpr (N == 8) reinterpret_cast<uint2 *>(t)[lane] = reinterpret_cast<const uint2 *>(values)[lane];
+    else reinterpret_cast<uint32_t *>(t)[lane] = reinterpret_cast<const uint32_t *>(values)[lane];
     const uint32_t sk = scales[token], sv = scales[((int64_t)1 << c.page_shift) + token];
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-    for (int i = 0; i < N / 4; ++i) uv[i] = t[(part * P + 2 * i) * 8 + token] | (uint32_t)t[(part * P + 2 * i + 1) * 8 + token] << 16;
+    for (int i = 0; i < N / 4; ++i) uv[i] = t[four_of(part, 2 * i) * 8 + token] | (uint32_t)t[four_of(part, 2 * i + 1) * 8 + token] << 16;
     values_of<N, BF16>(uk, sk, xk);
     values_of<N, BF16>(uv, sv, xv);
     if (!there) {  // a position before the first token, or without a page: zeros
@@ -198,8 +226,8 @@ __global__ __launch_bounds__(64 * kWaves) void kv_read_kernel(KvArgs c, KvTensor
     }
     if (!e.is_new) return;
     const int64_t row = e.s.start + e.first + token - e.s.first;
-    kv_store(k.data + row * k.token_stride + e.head * k.head_stride + part * 2 * N, k.aligned, xk);
-    kv_store(v.data + row * v.token_stride + e.head * v.head_stride + part * 2 * N, v.aligned, xv);
+    store_row(k.data + row * k.token_stride + e.head * k.head_stride, k.aligned, part, xk);
+    store_row(v.data + row * v.token_stride + e.head * v.head_stride, v.aligned, part, xv);
 }
 
 // Waves for the most eights that `tokens` new ones can touch: n tokens of a sequence lie in n of them at most, and in (n + 14) / 8
