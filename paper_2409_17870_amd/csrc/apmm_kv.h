@@ -52,6 +52,7 @@ struct KvPart {
     int target;  // 0: nothing is cut
     int least;
     int slots;   // most pieces there can be
+    int turn;    // of a sequence's tiles, longest first, the second `turn` come in reverse order; 0: none
     int from_rows, to_rows;
 };
 struct KvPlan {

@@ -138,6 +138,7 @@ __device__ __forceinline__ bool kv_item(const KvAttentionArgs &a, const KvPart &
         tile = rest / it.pieces;
         it.part = rest % it.pieces;
     }
+    if (tile >= p.turn && tile < 2 * p.turn) tile = p.turn + min(2 * p.turn, tiles) - 1 - tile;
     tile = tiles - 1 - tile;  // (the last queries see the most keys: those first)
     it.row0 = tile * TILE;
     it.rows = it.s.n * a.groups - it.row0;

@@ -114,6 +114,9 @@ KvPlan kv_plan(const KvArgs &c, int groups)
         p.tiles.from_rows = many ? 0 : kFewRows + 1;
         p.tiles.to_rows = INT32_MAX;
         p.tiles.least = 32;
+        // Two workgroups run on each of the 256 compute units at a time, and the second set comes to them in the order of the first: shortest of these first, each unit gets one long and one
+        // short tile and all are done with both at about the same time (2048 tokens of 32 heads: 72.9 us without, 69.5 so; 4096: 199 and 191; from 8192 on no difference).
+        p.tiles.turn = many ? 256 / c.heads : 0;
         cut(p.tiles, c, tiles(kTilesTile), kTilesStep, 512, many ? 1024 : 2048);
     }
     p.tiles_partial = (int64_t)(kv_partial_bytes(p.rows, c.heads, c.head_dim) / sizeof(float));
