@@ -330,6 +330,32 @@ def test_scales_near_the_largest_number(gpu, new):
     close(torch, got[::2], want[::2], near[::2])
 
 
+@pytest.mark.parametrize("heads, groups, new", [(64, 1, 700), (100, 1, 1000), (40, 2, 900)])
+def test_every_tile_of_a_prompt(gpu, heads, groups, new):
+    """Prompts of more tiles of rows than a head has compute units: some rows of each tile and some heads."""
+    torch, binding = gpu
+    x = Batch(torch, torch.float16, 64, heads, groups, 16, [new + 9], [new], seed=23, fused=False)
+    got = binding.apmm_kv_attention(x.q, *x.args, x.starts_gpu)
+    for h in (0, heads - 1):
+        for row in range(0, new, 128 // groups):
+            for a in (row, min(row + 128 // groups, new) - 1):
+                want, near = ref.attention(x.q[a:a + 1, h * groups:(h + 1) * groups], x.codes[:, h:h + 1], x.scales[:, h:h + 1], x.table, [a + 10], [0, 1], 0, 0, 64 ** -0.5)
+                close(torch, got[a:a + 1, h * groups:(h + 1) * groups], want, near)
+
+
+def test_more_sequences_than_lanes(gpu):
+    """Pieces of prompts, single tokens and nothing, in turn, for 150 sequences, some of them long enough to be cut."""
+    torch, binding = gpu
+    lengths = [(37 * i) % 200 for i in range(150)]
+    lengths[7], lengths[100], lengths[149] = 3100, 2500, 2900
+    new = [min((1, 40, 0, 1, 1, 3)[i % 6], n) for i, n in enumerate(lengths)]
+    x = Batch(torch, torch.float16, 64, 2, 2, 16, lengths, new, seed=29, fused=False)
+    got = binding.apmm_kv_attention(x.q, *x.args, x.starts_gpu)
+    close(torch, got, *x.attention(x.q, 0, 0, 64 ** -0.5))
+    got = binding.apmm_kv_attention(x.q, *x.args, x.starts_gpu, window=300, sinks=5)
+    close(torch, got, *x.attention(x.q, 300, 5, 64 ** -0.5))
+
+
 def test_pages_that_are_none(gpu):
     """Page numbers outside of the cache: their tokens are not written, read as zeros and are not seen.  Lengths beyond the table, starts that do not fit: nothing outside of the buffers."""
     torch, binding = gpu
