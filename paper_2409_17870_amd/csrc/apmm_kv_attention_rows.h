@@ -139,15 +139,20 @@ __device__ __forceinline__ void kv_attention_rows(const KvAttentionArgs &a, cons
 #pragma unroll
                 for (int i = 0; i < V; ++i) acc[e][i] *= by;
         }
-        uint32_t w[4];
+        uint32_t w[4], rest[4] = {};  // rounded weights and, for results of binary16, what that left: two numbers of 11 bits
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float p0 = __builtin_amdgcn_exp2f(fmaf(x[2 * i], factor, base)), p1 = __builtin_amdgcn_exp2f(fmaf(x[2 * i + 1], factor, base));
             total += p0 + p1;
-            w[i] = kv_half_pair(fmaf(p0, kv_low<BF16>(vs[i]), 0.0f), fmaf(p1, kv_high<BF16>(vs[i]), 0.0f));
+            const float w0 = fmaf(p0, kv_low<BF16>(vs[i]), 0.0f), w1 = fmaf(p1, kv_high<BF16>(vs[i]), 0.0f);
+            w[i] = kv_half_pair(w0, w1);
             weights = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, w[i]), (half2v){1, 1}, weights, false);
+            if (!BF16) {
+                rest[i] = kv_half_pair(w0 - kv_low<false>(w[i]), w1 - kv_high<false>(w[i]));
+                weights = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, rest[i]), (half2v){1, 1}, weights, false);
+            }
         }
-        const half8 p = __builtin_bit_cast(half8, make_uint4(w[0], w[1], w[2], w[3]));
+        const half8 p = __builtin_bit_cast(half8, make_uint4(w[0], w[1], w[2], w[3])), p_rest = __builtin_bit_cast(half8, make_uint4(rest[0], rest[1], rest[2], rest[3]));
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const uint32_t c[4] = {cur.v[0][i].x, cur.v[0][i].y, cur.v[1][i].x, cur.v[1][i].y};
@@ -161,8 +166,11 @@ __device__ __forceinline__ void kv_attention_rows(const KvAttentionArgs &a, cons
                 o[3][j] = h & 0x00f000f0u;
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                acc[e][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, make_uint4(o[e][0], o[e][1], o[e][2], o[e][3])), p, acc[e][i], 0, 0, 0);
+            for (int e = 0; e < 4; ++e) {
+                const half8 codes = __builtin_bit_cast(half8, make_uint4(o[e][0], o[e][1], o[e][2], o[e][3]));
+                acc[e][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes, p, acc[e][i], 0, 0, 0);
+                if (!BF16) acc[e][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes, p_rest, acc[e][i], 0, 0, 0);
+            }
         }
     };
     while (v < it.to) {
