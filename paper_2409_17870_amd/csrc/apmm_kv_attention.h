@@ -9,11 +9,12 @@
 //                       from, and 15 times the sum of the weights is taken off the second one's result.
 //   Queries             times a power of two for each row, so that its largest number is just below 2^11 (2^15 for the channels that meet u 2^-24): binary16 numbers as they are, bfloat16
 //                       ones exactly as far as 2^-35 of the row's largest.
-//   Weights             p_j b_j, rounded once to binary16 (bfloat16 would cost an output of binary16 numbers eight times its own rounding).  The value scales may lie anywhere, so
-//                       each row holds a power of two 2^E above all that it has met, and weights carry the factor 2^(9 - E) until the end: at most 2^15, and 2^-21 of the largest without loss.
+//   Weights             p_j b_j, rounded once to binary16 (bfloat16 would cost an output of binary16 numbers eight times its own rounding; kv_attention_rows, which waits for memory, adds what
+//                       the rounding left as a second number for them).  The value scales may lie anywhere, so each row holds a power of two 2^E above all that it has met, and weights carry the
+//                       factor 2^(2 - E) until the end: at most 2^15, full precision down to 2^-16 of that for p = 1 and b = 2^E, and 2^-27 of it is the least that counts.
 //                       The sum of the rounded weights goes with them (dot products with ones).
-//   Running maximum     m (and E) are only moved where a score passes m + 6: until then weights are at most 2^6 times larger, for which there is room.  Then the accumulators are scaled;
-//                       -m + 9 - E is one number, `base`.
+//   Running maximum     m (and E) are only moved where a score passes m + 13: until then weights are at most 2^13 times larger, for which there is room.  Then the accumulators are scaled;
+//                       -m + 2 - E is one number, `base`.  So large a slack is what lets kv_attention_tiles go without a maximum in most steps.
 //   Products transposed S^T = K Q^T and O^T = V^T P^T: the rows of S^T in a lane's accumulators are eight (or sixteen) keys that follow each other, if key rows are dealt to the operand's
 //                       rows in that order, and those are the lane's part of the operand P^T of the second product.  No weight passes through LDS.
 // A row that sees no key has the weight sum 0 and gets zeros.
@@ -40,7 +41,7 @@ typedef float float4v __attribute__((ext_vector_type(4)));
 typedef float float16v __attribute__((ext_vector_type(16)));
 
 constexpr float kLowest = -3.402823466e38f;
-constexpr float kSlack = 13.0f, kRoom = 2.0f;
+constexpr float kSlack = 13.0f, kRoom = 2.0f;  // 2^(kSlack + kRoom) is what binary16 has room for, but for the last octave
 
 // A workgroup's part of the call: keys of steps `from` to `to` - 1 (of STEP keys, the hidden ones between the first tokens and the window left out) for rows of one sequence
 template <int STEP>
@@ -270,7 +271,7 @@ __device__ __forceinline__ int kv_page_ids(const KvAttentionArgs &a, const KvIte
     return page < a.c.pages ? page : -1;
 }
 
-// E of a largest scale: s < 2^E.  Held above -80, so that sums of 2^(9 - E) stay in range (scales below 2^-103 lose bits).
+// E of a largest scale: s < 2^E.  Held above -80, so that sums of 2^(2 - E) stay in range (scales below 2^-96 lose bits).
 template <bool BF16>
 __device__ __forceinline__ int kv_exponent(uint32_t bits) { return BF16 ? max((int)(bits >> 7) - 126, -80) : (int)(bits >> 10) - 14; }
 template <bool BF16>

