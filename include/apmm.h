@@ -273,7 +273,7 @@ apmm_status apmm_kv_read(const apmm_kv_cache *cache, const apmm_kv_batch *batch,
  * may count as nothing.  Accuracy holds for value scales from 2^-96 on (bfloat16; below, values lose bits).
  *   scale     > 0 and finite, 1 / sqrt(head_dim) in most models
  *   window    0 (all keys) to 2^30;  sinks  0 to 2^30, without effect where window is 0
- *   workspace device, 16-byte aligned, apmm_kv_attention_workspace_bytes() bytes of the same arguments (0 for most large calls); calls that may overlap need one each */
+ *   workspace device, 16-byte aligned, apmm_kv_attention_workspace_bytes() bytes of the same arguments (0 for most large calls; a call with a window needs no more); calls that may overlap need one each */
 size_t apmm_kv_attention_workspace_bytes(const apmm_kv_cache *cache, const apmm_kv_batch *batch, int q_heads);
 apmm_status apmm_kv_attention(const apmm_kv_cache *cache, const apmm_kv_batch *batch, int q_heads,
                               const void *q, int64_t q_token_stride, int64_t q_head_stride,

@@ -78,13 +78,13 @@ apmm_status check_pair(const apmm_kv_cache *cache, const apmm_kv_batch *batch, c
     return APMM_OK;
 }
 
-apmm_status check_heads(const apmm_kv_cache *cache, const apmm_kv_batch *batch, const apmm::KvArgs &a, int q_heads, apmm::KvPlan &plan)
+apmm_status check_heads(const apmm_kv_cache *cache, const apmm_kv_batch *batch, const apmm::KvArgs &a, int q_heads, int window, int sinks, apmm::KvPlan &plan)
 {
     if (q_heads < 1 || q_heads % cache->kv_heads) return fail(APMM_ERR_INVALID_ARG, "kv_attention: q_heads must be a multiple of kv_heads");
     const int groups = q_heads / cache->kv_heads;
     if (groups > 1024 || (batch->tokens + batch->sequences) * q_heads > INT32_MAX / 4)
         return fail(APMM_ERR_UNSUPPORTED, "kv_attention: more than 1024 query heads to a key/value head, or tokens * q_heads is more than one launch takes");
-    plan = apmm::kv_plan(a, groups);
+    plan = apmm::kv_plan(a, groups, window, sinks);
     return APMM_OK;
 }
 
@@ -121,11 +121,12 @@ apmm_status apmm_kv_read(const apmm_kv_cache *cache, const apmm_kv_batch *batch,
     return e == hipSuccess ? APMM_OK : fail_hip(e, "apmm_kv_read");
 }
 
+// (without a window: under one as much is needed or less)
 size_t apmm_kv_attention_workspace_bytes(const apmm_kv_cache *cache, const apmm_kv_batch *batch, int q_heads)
 {
     apmm::KvArgs a;
     apmm::KvPlan plan;
-    if (check_sizes(cache, batch, a) != APMM_OK || batch->sequences == 0 || batch->tokens == 0 || check_heads(cache, batch, a, q_heads, plan) != APMM_OK) return 0;
+    if (check_sizes(cache, batch, a) != APMM_OK || batch->sequences == 0 || batch->tokens == 0 || check_heads(cache, batch, a, q_heads, 0, 0, plan) != APMM_OK) return 0;
     return partial_bytes(plan, a);
 }
 
@@ -138,11 +139,10 @@ apmm_status apmm_kv_attention(const apmm_kv_cache *cache, const apmm_kv_batch *b
     bool empty;
     apmm_status st = check_batch(cache, batch, a.c, empty);
     if (st != APMM_OK) return st;
-    if ((st = check_heads(cache, batch, a.c, q_heads, plan)) != APMM_OK) return st;
     if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(APMM_ERR_INVALID_ARG, "kv_attention: scale must be positive and finite");
     if (window < 0 || sinks < 0) return fail(APMM_ERR_INVALID_ARG, "kv_attention: window < 0 or sinks < 0");
     if (window > apmm::kKvMost || sinks > apmm::kKvMost) return fail(APMM_ERR_UNSUPPORTED, "kv_attention: window or sinks > 2^30");
-    if (empty) return APMM_OK;
+    if ((st = check_heads(cache, batch, a.c, q_heads, (int)window, (int)sinks, plan)) != APMM_OK || empty) return st;
     if ((st = check_tensor(q, q_token_stride, q_head_stride, a.q)) != APMM_OK || (st = check_tensor(out, out_token_stride, out_head_stride, a.out)) != APMM_OK) return st;
     const size_t need = partial_bytes(plan, a.c);
     if (need && (!workspace || workspace_bytes < need)) return fail(APMM_ERR_WORKSPACE, "kv_attention: needs a workspace of apmm_kv_attention_workspace_bytes() bytes");

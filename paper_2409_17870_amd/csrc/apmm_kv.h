@@ -59,7 +59,7 @@ struct KvPlan {
     KvPart rows, tiles;     // kv_attention_rows_kernel's, kv_attention_tiles_kernel's
     int64_t tiles_partial;  // where the latter's pieces begin in the workspace
 };
-KvPlan kv_plan(const KvArgs &c, int groups);
+KvPlan kv_plan(const KvArgs &c, int groups, int window, int sinks);
 size_t kv_partial_bytes(const KvPart &part, int heads, int head_dim);  // of the workspace that pieces take
 
 hipError_t launch_kv_write(const KvArgs &c, const KvTensor &k, const KvTensor &v, hipStream_t stream);

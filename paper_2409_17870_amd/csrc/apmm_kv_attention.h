@@ -33,6 +33,9 @@ constexpr int kTilesStep = 32;
 hipError_t launch_kv_attention_rows(const KvAttentionArgs &a, const KvPart &part, hipStream_t stream);
 hipError_t launch_kv_attention_tiles(const KvAttentionArgs &a, const KvPlan &plan, hipStream_t stream);
 
+// Most steps of a tile under a window, whose queries are at most `later` positions behind the first one's
+__host__ __device__ inline int kv_window_steps(int window, int sinks, int later, int step) { return (int)(((int64_t)window + later + step - 1) / step) + 1 + (sinks + step - 1) / step; }
+
 #ifdef __HIPCC__
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
@@ -61,10 +64,7 @@ __device__ __forceinline__ void kv_extent(const KvAttentionArgs &a, const KvSequ
     const int rows = s.n * a.groups;
     tiles = rows >= p.from_rows && rows <= p.to_rows ? (rows + TILE - 1) / TILE : 0;
     steps = (s.keys + STEP - 1) / STEP;
-    if (a.window) {
-        const int span = a.window + kv_divide(TILE + a.groups - 2, a.by_groups);  // positions that the queries of a tile see, without the first tokens
-        steps = min(steps, (span + STEP - 1) / STEP + 1 + (a.sinks + STEP - 1) / STEP);
-    }
+    if (a.window) steps = min(steps, kv_window_steps(a.window, a.sinks, kv_divide(TILE + a.groups - 2, a.by_groups), STEP));
     if (!tiles) steps = 0;
 }
 

@@ -76,9 +76,10 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(KvAttentionArgs 
 namespace {
 
 // How many workgroups one kernel has for sequences of at most `tokens` new tokens in all: `tiles` for a head where nothing is cut.  Nothing is where there are `plenty` anyway.
-void cut(KvPart &p, const KvArgs &c, int64_t tiles, int step, int wanted, int plenty)
+void cut(KvPart &p, const KvArgs &c, int groups, int window, int sinks, int64_t tiles, int step, int wanted, int plenty)
 {
-    const int64_t most_steps = (((int64_t)c.width << c.page_shift) + step - 1) / step;  // of a sequence, as far as the page table goes
+    int64_t most_steps = (((int64_t)c.width << c.page_shift) + step - 1) / step;  // of a sequence, as far as the page table goes
+    if (window) most_steps = std::min<int64_t>(most_steps, kv_window_steps(window, sinks, (p.tile + groups - 2) / groups, step));
     p.target = tiles * c.heads >= plenty || most_steps <= p.least ? 0 : std::max(wanted / c.heads, 1);
     p.slots = (int)(tiles + (p.target ? p.target + 1 : 0));
 }
@@ -92,7 +93,7 @@ void join(const KvAttentionArgs &a, const KvPlan &plan, hipStream_t stream)
 
 }  // namespace
 
-KvPlan kv_plan(const KvArgs &c, int groups)
+KvPlan kv_plan(const KvArgs &c, int groups, int window, int sinks)
 {
     KvPlan p = {};
     const int64_t rows = (int64_t)c.tokens * groups, sequences = std::min(c.sequences, c.tokens);  // (with new tokens)
@@ -107,10 +108,10 @@ KvPlan kv_plan(const KvArgs &c, int groups)
         p.rows.waves = !few || groups_of >= 512 ? 4 : 8;
         // Few workgroups (less than two for each compute unit): eight waves, one workgroup to a unit at a time, pieces for one round.  Else four waves, three workgroups to a unit.
         // (8 x 65536 tokens, 8 heads: 102 us in one round of 256, 106 in 512; 32 sequences of up to 4096, 40 heads: 73 us with 2048 wanted, 75 with 768 and 77 with 1536.)  Shorter
-        // pieces do not pay for the join: 1203 tokens uncut 11 us, in pieces of 32 steps 15.
-        p.rows.least = p.rows.waves == 4 ? 64 : 48;
+        // pieces do not pay for the join: 1203 tokens uncut 11 us, in pieces of 32 steps 15.  Beside tiles, which take longer, there is time for longer ones.
+        p.rows.least = !few ? 128 : p.rows.waves == 4 ? 64 : 48;
         const int wanted = p.rows.waves == 4 ? 2048 : 256;
-        cut(p.rows, c, most, kRowsStep, wanted, 4 * wanted);
+        cut(p.rows, c, groups, window, sinks, most, kRowsStep, wanted, 4 * wanted);
     }
     if (!few) {
         p.tiles.tile = kTilesTile;
@@ -119,11 +120,12 @@ KvPlan kv_plan(const KvArgs &c, int groups)
         p.tiles.to_rows = INT32_MAX;
         // Two workgroups to a compute unit at a time.  A piece costs its beginning (5 us) and 64 KiB written and read, so no more of them than fit at once: a batch of 5 pieces of prompts took
         // 131 us with 512 wanted, 138 with 1024 and 150 with 2048; a prompt of 2048 tokens 77, 93 and 117.  Pieces of 32 steps at least: 1000 tokens 36 us, with 16 46.
+        // How many are enough without: of one sequence and under a window tiles are known to be alike, those of several may be few long ones among short ones.
         p.tiles.least = 32;
         // Two workgroups run on each of the 256 compute units at a time, and the second set comes to them in the order of the first: shortest of these first, each unit gets one long and one
         // short tile and all are done with both at about the same time (2048 tokens of 32 heads: 72.9 us without, 69.5 so; 4096: 199 and 191; from 8192 on no difference).
         p.tiles.turn = many ? 256 / c.heads : 0;
-        cut(p.tiles, c, tiles(kTilesTile), kTilesStep, 512, many ? 1024 : 2048);
+        cut(p.tiles, c, groups, window, sinks, tiles(kTilesTile), kTilesStep, 512, window ? 512 : many ? 1024 : 2048);
     }
     p.tiles_partial = (int64_t)(kv_partial_bytes(p.rows, c.heads, c.head_dim) / sizeof(float));
     return p;
