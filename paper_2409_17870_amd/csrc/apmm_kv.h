@@ -44,7 +44,7 @@ struct KvAttentionArgs {
 };
 
 // How the work of an attention call is cut.  Rows are the queries of the heads that share a key/value head; a kernel takes the sequences with `from_rows` to `to_rows` of them, `tile` rows
-// to a workgroup.  The keys that a tile sees are cut in pieces of at least `least` steps so that there are about `target` workgroups for each key/value head whatever the lengths
+// to a tile.  The keys that a tile sees are cut in pieces of at least `least` steps so that there are about `target` workgroups for each key/value head whatever the lengths
 // are, which the host does not know.
 struct KvPart {
     int tile;    // rows of a workgroup; 0: the kernel is not launched

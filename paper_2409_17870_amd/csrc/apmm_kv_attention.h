@@ -25,7 +25,7 @@
 namespace apmm {
 
 constexpr int kRowsTile = 16;    // rows of a workgroup of kv_attention_rows_kernel
-constexpr int kTilesTile = 128;  // and of kv_attention_tiles_kernel
+constexpr int kTilesTile = 64;   // and of half a workgroup of kv_attention_tiles_kernel
 
 constexpr int kRowsStep = 32;    // keys of one step
 constexpr int kTilesStep = 32;
@@ -177,9 +177,9 @@ __host__ __device__ inline KvPartial kv_partial(float *at, const KvPart &part, i
     return p;
 }
 template <int STEP>
-__device__ __forceinline__ void kv_note(const KvAttentionArgs &a, const KvPart &p, float *partials, int slot, int head, bool there, const KvItem<STEP> &it)
+__device__ __forceinline__ void kv_note(const KvAttentionArgs &a, const KvPart &p, float *partials, int slot, int head, bool there, const KvItem<STEP> &it, bool first)
 {
-    if (!p.target || threadIdx.x) return;
+    if (!p.target || !first) return;
     KvPieceNote n = {};
     if (there && it.part == 0 && it.pieces > 1) n = {it.s.start, it.row0, min(it.rows, p.tile), it.pieces};
     kv_partial(partials, p, a.c.heads, a.c.head_dim).note[(int64_t)slot * a.c.heads + head] = n;

@@ -118,14 +118,14 @@ KvPlan kv_plan(const KvArgs &c, int groups, int window, int sinks)
         p.tiles.waves = 4;
         p.tiles.from_rows = many ? 0 : kFewRows + 1;
         p.tiles.to_rows = INT32_MAX;
-        // Two workgroups to a compute unit at a time.  A piece costs its beginning (5 us) and 64 KiB written and read, so no more of them than fit at once: a batch of 5 pieces of prompts took
-        // 131 us with 512 wanted, 138 with 1024 and 150 with 2048; a prompt of 2048 tokens 77, 93 and 117.  Pieces of 32 steps at least: 1000 tokens 36 us, with 16 46.
+        // Two workgroups of two tiles to a compute unit at a time.  A piece costs its beginning (5 us) and 32 KiB written and read, so no more of them than fit at once, 1024: with twice as many a
+        // batch of 5 pieces of prompts took 5 % longer and a prompt of 2048 tokens 20 %, with three quarters the batch 10 %.  Pieces of 32 steps at least: 1000 tokens 36 us, with 16 46.
         // How many are enough without: of one sequence and under a window tiles are known to be alike, those of several may be few long ones among short ones.
         p.tiles.least = 32;
         // Two workgroups run on each of the 256 compute units at a time, and the second set comes to them in the order of the first: shortest of these first, each unit gets one long and one
-        // short tile and all are done with both at about the same time (2048 tokens of 32 heads: 72.9 us without, 69.5 so; 4096: 199 and 191; from 8192 on no difference).
-        p.tiles.turn = many ? 256 / c.heads : 0;
-        cut(p.tiles, c, groups, window, sinks, tiles(kTilesTile), kTilesStep, 512, window ? 512 : many ? 1024 : 2048);
+        // short pair of tiles and all are done with both at about the same time (2048 tokens of 32 heads: 72.9 us without, 69.5 so; 4096: 199 and 191; from 8192 on no difference).
+        p.tiles.turn = many ? 512 / c.heads : 0;
+        cut(p.tiles, c, groups, window, sinks, tiles(kTilesTile), kTilesStep, 1024, window ? 896 : many ? 2048 : 4096);
     }
     p.tiles_partial = (int64_t)(kv_partial_bytes(p.rows, c.heads, c.head_dim) / sizeof(float));
     return p;

@@ -30,7 +30,7 @@ __device__ __forceinline__ void kv_attention_rows(const KvAttentionArgs &a, cons
     const int slot = kv_divide(block, a.c.by_heads), head = block - slot * a.c.heads, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = kv_lane(), n = lane & 15, g = lane >> 4;
     KvItem<kRowsStep> it;
     const bool there = kv_item<kRowsStep, kRowsTile>(a, part, slot, it);
-    kv_note(a, part, a.partial, slot, head, there, it);
+    kv_note(a, part, a.partial, slot, head, there, it, threadIdx.x == 0);
     if (!there) return;
 
     const int rows = min(it.rows, T), row = it.row0 + min(n, rows - 1), at = kv_divide(row, a.by_groups);

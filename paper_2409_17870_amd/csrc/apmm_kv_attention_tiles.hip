@@ -1,7 +1,8 @@
 // Attention of many rows over the four-bit cache (apmm_kv_attention.h): prompts and pieces of prompts.
 //
-// A workgroup has 128 rows, 32 to each of its four waves, which go through the keys by themselves in steps of 32 with matrix instructions 32 x 32 x 16: codes come from memory (L1 and L2: the
-// waves and the workgroups of a head read the same) into registers and become operands there, no barrier anywhere.  Only the scales, which lanes need sixteen of, go through a little LDS of the wave.
+// A workgroup has two tiles of 64 rows of a head, 32 rows to each of its four waves, which go through the keys by themselves in steps of 32 with matrix instructions 32 x 32 x 16: codes come
+// from memory (L1 and L2: the waves and the workgroups of a head read the same) into registers and become operands there, no barrier anywhere.  (One tile of 128 rows leaves two waves idle
+// where a sequence has 33 to 64: 30 sequences of 4000 tokens with 50 new ones, 32 heads, 280 us in place of 200; long prompts take the same time.  Workgroups of one tile of 64: 5 % longer.)  Only the scales, which lanes need sixteen of, go through a little LDS of the wave.
 // (Operands made once for the workgroup and shared through LDS save three quarters of the unpacking, and lost more than that in barriers: 280 us where this takes 190.)
 //
 // What bounds it is the vector unit, then the power of the card: of a step's about 200 instructions 80 unpack codes and 96 are the weights of 16 keys a lane (product with the key's scale and
@@ -17,7 +18,7 @@ namespace apmm {
 
 namespace {
 
-constexpr int kWaves = 4, kRows = kTilesTile / kWaves;
+constexpr int kWaves = 4, kRows = 32, kTileWaves = kTilesTile / kRows;
 
 // SMALL: pages of 16 keys, two to a step
 template <int D, bool BF16, bool SMALL>
@@ -25,13 +26,15 @@ __device__ __forceinline__ void kv_attention_tiles(const KvAttentionArgs &a, con
 {
     constexpr int W = D / 16, E = D / 32;  // words of a lane's key, blocks of 32 channels of the result
     __shared__ __align__(16) float scales[kWaves][64];  // of a step: keys, values
-    const int slot = kv_divide(block_id, a.c.by_heads), head = block_id - slot * a.c.heads, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = kv_lane(), n = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tile_wave = wave % kTileWaves, lane = kv_lane(), n = lane & 31, h = lane >> 5;
+    const int at_block = kv_divide(block_id, a.c.by_heads), slot = at_block * (kWaves / kTileWaves) + wave / kTileWaves, head = block_id - at_block * a.c.heads;
+    if (slot >= part.slots) return;
     KvItem<kTilesStep> it;
     const bool there = kv_item<kTilesStep, kTilesTile>(a, part, slot, it);
-    kv_note(a, part, partials, slot, head, there, it);
+    kv_note(a, part, partials, slot, head, there, it, tile_wave == 0 && lane == 0);
     if (!there) return;
 
-    const int row0 = it.row0 + wave * kRows, rows = min(it.rows - wave * kRows, kRows);
+    const int row0 = it.row0 + tile_wave * kRows, rows = min(it.rows - tile_wave * kRows, kRows);
     if (rows <= 0) return;
     const int row = row0 + min(n, rows - 1), at = kv_divide(row, a.by_groups);
     const int pos = it.s.first + at, first_pos = it.s.first + kv_divide(row0, a.by_groups), last_pos = it.s.first + kv_divide(row0 + rows - 1, a.by_groups);
@@ -293,7 +296,7 @@ __device__ __forceinline__ void kv_attention_tiles(const KvAttentionArgs &a, con
     const bool whole = it.pieces == 1;
     const float over = whole ? (total == 0.0f ? 0.0f : 1.0f / total) : 1.0f;
     uint16_t *out = a.out.data + (int64_t)(it.s.start + at) * a.out.token_stride + (int64_t)(head * a.groups + row - at * a.groups) * a.out.head_stride;
-    const int64_t place = ((int64_t)slot * a.c.heads + head) * kTilesTile + wave * kRows + n;
+    const int64_t place = ((int64_t)slot * a.c.heads + head) * kTilesTile + tile_wave * kRows + n;
     const KvPartial partial = kv_partial(partials, part, a.c.heads, D);
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
@@ -331,7 +334,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAt
 template <int D, bool BF16>
 void launch(const KvAttentionArgs &a, const KvPlan &plan, hipStream_t stream)
 {
-    const int of_tiles = plan.tiles.slots * a.c.heads, of_rows = plan.rows.tile ? plan.rows.slots * a.c.heads : 0;
+    const int of_tiles = (plan.tiles.slots + kWaves / kTileWaves - 1) / (kWaves / kTileWaves) * a.c.heads, of_rows = plan.rows.tile ? plan.rows.slots * a.c.heads : 0;
     const dim3 grid((uint32_t)(of_tiles + of_rows)), block(64 * kWaves);
     if (a.c.page_shift == 4) kv_attention_tiles_kernel<D, BF16, true><<<grid, block, 0, stream>>>(a, plan, of_tiles);
     else kv_attention_tiles_kernel<D, BF16, false><<<grid, block, 0, stream>>>(a, plan, of_tiles);
