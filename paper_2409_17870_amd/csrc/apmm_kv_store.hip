@@ -3,7 +3,7 @@
 // A row x (head_dim numbers of a token and head) becomes s = max |x| / 15 rounded to its type and codes u = clamp(floor(x / (2 s)) + 8, 0, 15): the nearest odd
 // multiple 2 u - 15 of s, ties upward, as apmm_quantize_pack_activations has it.
 //
-// One wave takes the up to eight tokens of an aligned eight of positions, one head, keys and values: eight lanes to a token.  The eight tokens of
+// One wave takes the up to eight tokens of an aligned eight of positions, one head (or two of 64 channels), keys and values: eight lanes to a token.  The eight tokens of
 // a channel are neighbours in the cache's values, so they are turned in LDS and written whole (an eight that is not all new is written in pieces of 16 bits, what is there
 // of earlier tokens stays).  Bound by HBM: 4 bytes a channel in or out,
 // one and a bit in the cache.  Reading 16384 tokens of 32 heads of 128: 338 MB in 61 us, 5.5 TB/s (a large copy: 5.1); writing 2048 of 40 heads: 53 MB in 13 us, some 4 of them the launch and
@@ -18,21 +18,25 @@ namespace apmm {
 namespace {
 
 constexpr int kWaves = 4;
+// Heads of a wave: two of 64 channels, or finding its eight costs as much as moving it (3 sequences of 37000 tokens, 16 heads of 64, read back: 147 us with one, 120 with two)
+template <int D>
+constexpr int kHeads = 128 / D;
 
 struct Eight {  // of one wave
     KvSequence s;
-    int head, first, in_page;  // position of its first token (a multiple of eight, may be negative), its place in the page
+    int head, first, in_page;  // the first of its heads; position of its first token (a multiple of eight, may be negative), its place in the page
     int page;                  // -1: none
     bool is_new;               // this lane's token is one of the call's
     bool whole;                // all eight are
 };
 
-// false: nothing for this wave
+// false: nothing for this wave.  (by_heads is that of the heads' groups of H)
+template <int H>
 __device__ __forceinline__ bool find_eight(const KvArgs &c, Eight &e)
 {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int unit = blockIdx.x * kWaves + wave, eight = kv_divide(unit, c.by_heads);  // (fewer than 2^30 units: 2^28 for tokens, 2^27 for sequences at most)
-    e.head = unit - eight * c.heads;
+    e.head = (unit - eight * ((c.heads + H - 1) / H)) * H;
     int b, rest;
     auto count = [&](int at) {
         const KvSequence s = kv_sequence(c, at);
@@ -133,38 +137,40 @@ __global__ __launch_bounds__(64 * kWaves) void kv_write_kernel(KvArgs c, KvTenso
     constexpr int P = D / 32;  // 16-bit pieces of a lane
     __shared__ __align__(16) kv_u16 turn[kWaves][D / 4 * 8];
     Eight e;
-    if (!find_eight(c, e) || e.page < 0) return;
+    if (!find_eight<kHeads<D>>(c, e) || e.page < 0) return;
     const int lane = kv_lane(), token = lane >> 3, part = lane & 7;
     const int64_t row = e.s.start + (e.is_new ? e.first + token - e.s.first : 0);  // (a lane without one reads the first)
-    uint32_t xk[N], xv[N];
-    load_row(k.data + row * k.token_stride + e.head * k.head_stride, k.aligned, part, xk);
-    load_row(v.data + row * v.token_stride + e.head * v.head_stride, v.aligned, part, xv);
-    uint32_t uk[N / 4], uv[N / 4];
-    const uint32_t sk = quantise<N, BF16>(xk, uk), sv = quantise<N, BF16>(xv, uv);
+    for (int head = e.head; head < min(e.head + kHeads<D>, c.heads); ++head) {
+        uint32_t xk[N], xv[N];
+        load_row(k.data + row * k.token_stride + head * k.head_stride, k.aligned, part, xk);
+        load_row(v.data + row * v.token_stride + head * v.head_stride, v.aligned, part, xv);
+        uint32_t uk[N / 4], uv[N / 4];
+        const uint32_t sk = quantise<N, BF16>(xk, uk), sv = quantise<N, BF16>(xv, uv);
 
-    const int64_t block = ((int64_t)e.page * c.heads + e.head) * 2;
-    uint16_t *scales = c.scales + (block << c.page_shift) + e.in_page;
-    uint8_t *keys = c.codes + (block << c.page_shift) * (D / 2) + (int64_t)e.in_page * (D / 2);
-    uint16_t *values = reinterpret_cast<uint16_t *>(keys + ((int64_t)(D / 2) << c.page_shift));  // (an eight of tokens has its place at the same byte)
-    if (e.is_new) {
-        uint32_t *to = reinterpret_cast<uint32_t *>(keys + token * (D / 2)) + part;
+        const int64_t block = ((int64_t)e.page * c.heads + head) * 2;
+        uint16_t *scales = c.scales + (block << c.page_shift) + e.in_page;
+        uint8_t *keys = c.codes + (block << c.page_shift) * (D / 2) + (int64_t)e.in_page * (D / 2);
+        uint16_t *values = reinterpret_cast<uint16_t *>(keys + ((int64_t)(D / 2) << c.page_shift));  // (an eight of tokens has its place at the same byte)
+        if (e.is_new) {
+            uint32_t *to = reinterpret_cast<uint32_t *>(keys + token * (D / 2)) + part;
 #pragma unroll
-        for (int i = 0; i < N / 4; ++i) to[8 * i] = uk[i];
-        if (part == 0) {
-            scales[token] = (uint16_t)sk;
-            scales[((int64_t)1 << c.page_shift) + token] = (uint16_t)sv;
+            for (int i = 0; i < N / 4; ++i) to[8 * i] = uk[i];
+            if (part == 0) {
+                scales[token] = (uint16_t)sk;
+                scales[((int64_t)1 << c.page_shift) + token] = (uint16_t)sv;
+            }
         }
-    }
-    if (e.whole) {
-        kv_u16 *t = turn[threadIdx.x >> 6];
+        if (e.whole) {
+            kv_u16 *t = turn[threadIdx.x >> 6];
 #pragma unroll
-        for (int i = 0; i < P; ++i) t[four_of(part, i) * 8 + token] = (uint16_t)(uv[i / 2] >> (16 * (i & 1)));
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if constexpr (P == 4) reinterpret_cast<uint2 *>(values)[lane] = reinterpret_cast<const uint2 *>(t)[lane];
-        else reinterpret_cast<uint32_t *>(values)[lane] = reinterpret_cast<const uint32_t *>(t)[lane];
-    } else if (e.is_new) {
+            for (int i = 0; i < P; ++i) t[four_of(part, i) * 8 + token] = (uint16_t)(uv[i / 2] >> (16 * (i & 1)));
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            if constexpr (P == 4) reinterpret_cast<uint2 *>(values)[lane] = reinterpret_cast<const uint2 *>(t)[lane];
+            else reinterpret_cast<uint32_t *>(values)[lane] = reinterpret_cast<const uint32_t *>(t)[lane];
+        } else if (e.is_new) {
 #pragma unroll
-        for (int i = 0; i < P; ++i) values[four_of(part, i) * 8 + token] = (uint16_t)(uv[i / 2] >> (16 * (i & 1)));
+            for (int i = 0; i < P; ++i) values[four_of(part, i) * 8 + token] = (uint16_t)(uv[i / 2] >> (16 * (i & 1)));
+        }
     }
 }
 
@@ -202,34 +208,36 @@ __global__ __launch_bounds__(64 * kWaves) void kv_read_kernel(KvArgs c, KvTensor
     constexpr int N = D / 16;
     __shared__ __align__(16) kv_u16 turn[kWaves][D / 4 * 8];
     Eight e;
-    if (!find_eight(c, e)) return;
+    if (!find_eight<kHeads<D>>(c, e)) return;
     const int lane = kv_lane(), token = lane >> 3, part = lane & 7;
     const bool there = e.page >= 0;
-    const int64_t block = ((int64_t)(there ? e.page : 0) * c.heads + e.head) * 2;
-    const uint16_t *scales = c.scales + (block << c.page_shift) + e.in_page;
-    const uint8_t *keys = c.codes + (block << c.page_shift) * (D / 2) + (int64_t)e.in_page * (D / 2);
-    const uint8_t *values = keys + ((int64_t)(D / 2) << c.page_shift);
-    kv_u16 *t = turn[threadIdx.x >> 6];
-    uint32_t uk[N / 4], uv[N / 4], xk[N], xv[N];
-    const uint32_t *from = reinterpret_cast<const uint32_t *>(keys + token * (D / 2)) + part;
+    for (int head = e.head; head < min(e.head + kHeads<D>, c.heads); ++head) {
+        const int64_t block = ((int64_t)(there ? e.page : 0) * c.heads + head) * 2;
+        const uint16_t *scales = c.scales + (block << c.page_shift) + e.in_page;
+        const uint8_t *keys = c.codes + (block << c.page_shift) * (D / 2) + (int64_t)e.in_page * (D / 2);
+        const uint8_t *values = keys + ((int64_t)(D / 2) << c.page_shift);
+        kv_u16 *t = turn[threadIdx.x >> 6];
+        uint32_t uk[N / 4], uv[N / 4], xk[N], xv[N];
+        const uint32_t *from = reinterpret_cast<const uint32_t *>(keys + token * (D / 2)) + part;
 #pragma unroll
-    for (int i = 0; i < N / 4; ++i) uk[i] = from[8 * i];
-    if constexpr (N == 8) reinterpret_cast<uint2 *>(t)[lane] = reinterpret_cast<const uint2 *>(values)[lane];
-    else reinterpret_cast<uint32_t *>(t)[lane] = reinterpret_cast<const uint32_t *>(values)[lane];
-    const uint32_t sk = scales[token], sv = scales[((int64_t)1 << c.page_shift) + token];
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        for (int i = 0; i < N / 4; ++i) uk[i] = from[8 * i];
+        if constexpr (N == 8) reinterpret_cast<uint2 *>(t)[lane] = reinterpret_cast<const uint2 *>(values)[lane];
+        else reinterpret_cast<uint32_t *>(t)[lane] = reinterpret_cast<const uint32_t *>(values)[lane];
+        const uint32_t sk = scales[token], sv = scales[((int64_t)1 << c.page_shift) + token];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-    for (int i = 0; i < N / 4; ++i) uv[i] = t[four_of(part, 2 * i) * 8 + token] | (uint32_t)t[four_of(part, 2 * i + 1) * 8 + token] << 16;
-    values_of<N, BF16>(uk, sk, xk);
-    values_of<N, BF16>(uv, sv, xv);
-    if (!there) {  // a position before the first token, or without a page: zeros
+        for (int i = 0; i < N / 4; ++i) uv[i] = t[four_of(part, 2 * i) * 8 + token] | (uint32_t)t[four_of(part, 2 * i + 1) * 8 + token] << 16;
+        values_of<N, BF16>(uk, sk, xk);
+        values_of<N, BF16>(uv, sv, xv);
+        if (!there) {  // a position before the first token, or without a page: zeros
 #pragma unroll
-        for (int i = 0; i < N; ++i) xk[i] = xv[i] = 0;
+            for (int i = 0; i < N; ++i) xk[i] = xv[i] = 0;
+        }
+        if (!e.is_new) continue;
+        const int64_t row = e.s.start + e.first + token - e.s.first;
+        store_row(k.data + row * k.token_stride + head * k.head_stride, k.aligned, part, xk);
+        store_row(v.data + row * v.token_stride + head * v.head_stride, v.aligned, part, xv);
     }
-    if (!e.is_new) return;
-    const int64_t row = e.s.start + e.first + token - e.s.first;
-    store_row(k.data + row * k.token_stride + e.head * k.head_stride, k.aligned, part, xk);
-    store_row(v.data + row * v.token_stride + e.head * v.head_stride, v.aligned, part, xv);
 }
 
 // Waves for the most eights that `tokens` new ones can touch: n tokens of a sequence lie in n of them at most, and in (n + 14) / 8
@@ -238,9 +246,12 @@ int64_t eights(const KvArgs &c) { return std::min<int64_t>(c.tokens, c.tokens / 
 template <int D, bool BF16>
 hipError_t launch(bool write, const KvArgs &c, const KvTensor &k, const KvTensor &v, hipStream_t stream)
 {
-    const int64_t groups = (eights(c) * c.heads + kWaves - 1) / kWaves;
-    if (write) kv_write_kernel<D, BF16><<<dim3((uint32_t)groups), dim3(64 * kWaves), 0, stream>>>(c, k, v);
-    else kv_read_kernel<D, BF16><<<dim3((uint32_t)groups), dim3(64 * kWaves), 0, stream>>>(c, k, v);
+    const int groups_of = (c.heads + kHeads<D> - 1) / kHeads<D>;
+    KvArgs a = c;
+    a.by_heads = kv_divisor(groups_of);
+    const int64_t groups = (eights(c) * groups_of + kWaves - 1) / kWaves;
+    if (write) kv_write_kernel<D, BF16><<<dim3((uint32_t)groups), dim3(64 * kWaves), 0, stream>>>(a, k, v);
+    else kv_read_kernel<D, BF16><<<dim3((uint32_t)groups), dim3(64 * kWaves), 0, stream>>>(a, k, v);
     return hipGetLastError();
 }
 
