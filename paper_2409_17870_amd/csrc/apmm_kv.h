@@ -25,6 +25,7 @@ struct KvArgs {
     int sequences, tokens, width, heads, page_shift, head_dim;
     bool bf16;
     uint64_t by_heads;       // what kv_divide divides by heads with
+    int per_wave;            // writing and reading: heads of a wave
 };
 
 struct KvTensor {  // rows of head_dim contiguous elements

@@ -18,9 +18,11 @@ namespace apmm {
 namespace {
 
 constexpr int kWaves = 4;
-// Heads of a wave: two of 64 channels, or finding its eight costs as much as moving it (3 sequences of 37000 tokens, 16 heads of 64, read back: 147 us with one, 120 with two)
+// Heads of a wave: two of 64 channels where there is enough for two rounds of waves, or finding its eight costs as much as moving it (3 sequences of 37000 tokens, 16 heads of 64, read
+// back: 147 us with one, 120 with two; pieces of 333 tokens and single ones of 23 sequences, 8 heads: 4.2 and 4.7)
+constexpr int kManyUnits = 16384;
 template <int D>
-constexpr int kHeads = 128 / D;
+__device__ __forceinline__ int heads_of_wave(const KvArgs &c) { return D == 64 ? c.per_wave : 1; }
 
 struct Eight {  // of one wave
     KvSequence s;
@@ -30,13 +32,12 @@ struct Eight {  // of one wave
     bool whole;                // all eight are
 };
 
-// false: nothing for this wave.  (by_heads is that of the heads' groups of H)
-template <int H>
-__device__ __forceinline__ bool find_eight(const KvArgs &c, Eight &e)
+// false: nothing for this wave.  (by_heads is that of the heads' groups of `per`, 1 or 2)
+__device__ __forceinline__ bool find_eight(const KvArgs &c, int per, Eight &e)
 {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int unit = blockIdx.x * kWaves + wave, eight = kv_divide(unit, c.by_heads);  // (fewer than 2^30 units: 2^28 for tokens, 2^27 for sequences at most)
-    e.head = (unit - eight * ((c.heads + H - 1) / H)) * H;
+    e.head = (unit - eight * (per == 1 ? c.heads : (c.heads + 1) >> 1)) * per;
     int b, rest;
     auto count = [&](int at) {
         const KvSequence s = kv_sequence(c, at);
@@ -137,10 +138,11 @@ __global__ __launch_bounds__(64 * kWaves) void kv_write_kernel(KvArgs c, KvTenso
     constexpr int P = D / 32;  // 16-bit pieces of a lane
     __shared__ __align__(16) kv_u16 turn[kWaves][D / 4 * 8];
     Eight e;
-    if (!find_eight<kHeads<D>>(c, e) || e.page < 0) return;
+    const int per = heads_of_wave<D>(c);
+    if (!find_eight(c, per, e) || e.page < 0) return;
     const int lane = kv_lane(), token = lane >> 3, part = lane & 7;
     const int64_t row = e.s.start + (e.is_new ? e.first + token - e.s.first : 0);  // (a lane without one reads the first)
-    for (int head = e.head; head < min(e.head + kHeads<D>, c.heads); ++head) {
+    for (int head = e.head; head < min(e.head + per, c.heads); ++head) {
         uint32_t xk[N], xv[N];
         load_row(k.data + row * k.token_stride + head * k.head_stride, k.aligned, part, xk);
         load_row(v.data + row * v.token_stride + head * v.head_stride, v.aligned, part, xv);
@@ -208,10 +210,11 @@ __global__ __launch_bounds__(64 * kWaves) void kv_read_kernel(KvArgs c, KvTensor
     constexpr int N = D / 16;
     __shared__ __align__(16) kv_u16 turn[kWaves][D / 4 * 8];
     Eight e;
-    if (!find_eight<kHeads<D>>(c, e)) return;
+    const int per = heads_of_wave<D>(c);
+    if (!find_eight(c, per, e)) return;
     const int lane = kv_lane(), token = lane >> 3, part = lane & 7;
     const bool there = e.page >= 0;
-    for (int head = e.head; head < min(e.head + kHeads<D>, c.heads); ++head) {
+    for (int head = e.head; head < min(e.head + per, c.heads); ++head) {
         const int64_t block = ((int64_t)(there ? e.page : 0) * c.heads + head) * 2;
         const uint16_t *scales = c.scales + (block << c.page_shift) + e.in_page;
         const uint8_t *keys = c.codes + (block << c.page_shift) * (D / 2) + (int64_t)e.in_page * (D / 2);
@@ -246,8 +249,9 @@ int64_t eights(const KvArgs &c) { return std::min<int64_t>(c.tokens, c.tokens / 
 template <int D, bool BF16>
 hipError_t launch(bool write, const KvArgs &c, const KvTensor &k, const KvTensor &v, hipStream_t stream)
 {
-    const int groups_of = (c.heads + kHeads<D> - 1) / kHeads<D>;
     KvArgs a = c;
+    a.per_wave = D == 64 && eights(c) * c.heads >= kManyUnits ? 2 : 1;
+    const int groups_of = (c.heads + a.per_wave - 1) / a.per_wave;
     a.by_heads = kv_divisor(groups_of);
     const int64_t groups = (eights(c) * groups_of + kWaves - 1) / kWaves;
     if (write) kv_write_kernel<D, BF16><<<dim3((uint32_t)groups), dim3(64 * kWaves), 0, stream>>>(a, k, v);

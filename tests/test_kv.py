@@ -104,6 +104,26 @@ def test_write_and_read_are_exact(gpu, dtype, case):
     assert torch.equal(k.cpu(), rk) and torch.equal(v.cpu(), rv)
 
 
+@pytest.mark.parametrize("heads", [32, 33])
+def test_large_writes_and_reads_are_the_small_ones(gpu, heads):
+    """Heads of 64 channels go two to a wave in large calls: the same cache and rows as from calls of one sequence."""
+    torch, binding = gpu
+    lengths, new = [1500, 777, 1800, 9], [1490, 777, 1793, 0]
+    x = Batch(torch, torch.float16, 64, heads, 1, 16, lengths, new, seed=31)
+    assert (sum(new) // 8) * heads >= 16384 > (max(new) // 8 + 2) * heads
+    large, small = [(x.codes.clone(), x.scales.clone()) for _ in range(2)]
+    binding.apmm_kv_write(x.k, x.v, *large, *x.args[2:], x.starts_gpu)
+    k, v = binding.apmm_kv_read(*large, *x.args[2:], x.tokens, x.starts_gpu)
+    for b, n in enumerate(new):
+        rows = slice(x.starts[b], x.starts[b + 1])
+        one = (x.args[2][b:b + 1], x.args[3][b:b + 1])
+        starts = torch.tensor([0, n], dtype=torch.int32).cuda()
+        binding.apmm_kv_write(x.k[rows], x.v[rows], *small, *one, starts)
+        k1, v1 = binding.apmm_kv_read(*small, *one, n, starts)
+        assert torch.equal(k1, k[rows]) and torch.equal(v1, v[rows])
+    assert torch.equal(large[0], small[0]) and torch.equal(large[1], small[1])
+
+
 @pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
 def test_borders_of_the_grid(gpu, dtype):
     """Numbers on and beside the cells' borders, zeros, the smallest and the largest numbers, and rows that are not finite."""
