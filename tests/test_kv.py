@@ -110,7 +110,7 @@ def test_large_writes_and_reads_are_the_small_ones(gpu, heads):
     torch, binding = gpu
     lengths, new = [1500, 777, 1800, 9], [1490, 777, 1793, 0]
     x = Batch(torch, torch.float16, 64, heads, 1, 16, lengths, new, seed=31)
-    assert (sum(new) // 8) * heads >= 16384 > (max(new) // 8 + 2) * heads
+    assert (sum(new) // 8 + 2 * len(new)) * heads >= 16384 > (max(new) // 8 + 2) * heads  # the eights that a call may touch, as the launch counts them
     large, small = [(x.codes.clone(), x.scales.clone()) for _ in range(2)]
     binding.apmm_kv_write(x.k, x.v, *large, *x.args[2:], x.starts_gpu)
     k, v = binding.apmm_kv_read(*large, *x.args[2:], x.tokens, x.starts_gpu)
