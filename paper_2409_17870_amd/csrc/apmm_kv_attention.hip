@@ -7,7 +7,6 @@ namespace apmm {
 
 namespace {
 
-constexpr int kFewRows = 32;  // of a sequence: those go to kv_attention_rows_kernel
 
 // Reads what the pieces wrote, 4 (head_dim + 2) bytes a row and piece; a launch of it takes 4 to 7 us, nearly all of it the launch and the notes' way from memory.
 // A workgroup looks at one piece and head and 16 rows of its tile, and has work where the piece is the first of several.  16 lanes to a row; what is left of the 256 for fewer rows shares
@@ -98,12 +97,15 @@ KvPlan kv_plan(const KvArgs &c, int groups, int window, int sinks)
     KvPlan p = {};
     const int64_t rows = (int64_t)c.tokens * groups, sequences = std::min(c.sequences, c.tokens);  // (with new tokens)
     // A sequence's rows are as many as the call's where it is the only one, and no more than one token's where there is no other: else workgroups of both kinds
-    const bool few = rows <= kFewRows || c.tokens <= c.sequences, many = !few && c.sequences == 1;
+    // Few rows of a sequence go to kv_attention_rows: up to 32, where keys are cut for the sake of enough workgroups; where there are enough a tile reads the keys of 17 to 32 rows once, not twice
+    // (20 new ones of 1000 tokens, 40 sequences, 32 heads: 81 us with 32 as the border, 60 with 16; 28 rows of 30 sequences of 2000, 8 heads: 36 and 42; 30 rows of one of 56000: 36 and 48)
+    const int few_rows = sequences * c.heads >= 512 ? 16 : 32;
+    const bool few = rows <= few_rows || c.tokens <= c.sequences, many = !few && c.sequences == 1;
     auto tiles = [&](int tile) { return std::min(c.tokens * (int64_t)((groups + tile - 1) / tile), rows / tile + sequences); };
     if (!many) {
         p.rows.tile = kRowsTile;
-        p.rows.to_rows = few ? INT32_MAX : kFewRows;
-        const int64_t most = std::min(tiles(kRowsTile), few ? INT64_MAX : sequences * (kFewRows / kRowsTile));
+        p.rows.to_rows = few ? INT32_MAX : few_rows;
+        const int64_t most = std::min(tiles(kRowsTile), few ? INT64_MAX : sequences * (few_rows / kRowsTile));
         const int64_t groups_of = sequences * c.heads * ((std::min<int64_t>(groups, rows) + kRowsTile - 1) / kRowsTile);
         p.rows.waves = !few || groups_of >= 512 ? 4 : 8;
         // Few workgroups (less than two for each compute unit): eight waves, one workgroup to a unit at a time, pieces for one round.  Else four waves, three workgroups to a unit.
@@ -116,7 +118,7 @@ KvPlan kv_plan(const KvArgs &c, int groups, int window, int sinks)
     if (!few) {
         p.tiles.tile = kTilesTile;
         p.tiles.waves = 4;
-        p.tiles.from_rows = many ? 0 : kFewRows + 1;
+        p.tiles.from_rows = many ? 0 : few_rows + 1;
         p.tiles.to_rows = INT32_MAX;
         // Two workgroups of two tiles to a compute unit at a time.  A piece costs its beginning (5 us) and 32 KiB written and read, so no more of them than fit at once, 1024: with twice as many a
         // batch of 5 pieces of prompts took 5 % longer and a prompt of 2048 tokens 20 %, with three quarters the batch 10 %.  Pieces of 32 steps at least: 1000 tokens 36 us, with 16 46.
