@@ -49,7 +49,7 @@ struct KvAttentionArgs {
 // are, which the host does not know.
 struct KvPart {
     int tile;    // rows of a workgroup; 0: the kernel is not launched
-    int waves;   // of a workgroup
+    int waves;   // of a workgroup of kv_attention_rows_kernel
     int target;  // 0: nothing is cut
     int least;
     int slots;   // most pieces there can be

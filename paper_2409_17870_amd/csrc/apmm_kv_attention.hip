@@ -117,7 +117,6 @@ KvPlan kv_plan(const KvArgs &c, int groups, int window, int sinks)
     }
     if (!few) {
         p.tiles.tile = kTilesTile;
-        p.tiles.waves = 4;
         p.tiles.from_rows = many ? 0 : few_rows + 1;
         p.tiles.to_rows = INT32_MAX;
         // Two workgroups of two tiles to a compute unit at a time.  A piece costs its beginning (5 us) and 32 KiB written and read, so no more of them than fit at once, 1024: with twice as many a
