@@ -160,7 +160,7 @@ __device__ __forceinline__ bool kv_item(const KvAttentionArgs &a, const KvPart &
 
 // For the joining of pieces: what lies at a slot and head
 struct KvPieceNote {
-    int start, row0, rows, pieces;  // pieces: of the tile, 0 where this is not the first of several
+    int start, row0, rows, pieces;  // pieces: of the tile, no more than there are slots from this one on; 0 where this is not the first of several
 };
 struct KvPartial {
     float *sums;        // [slot][head][tile row][channel]
@@ -181,7 +181,8 @@ __device__ __forceinline__ void kv_note(const KvAttentionArgs &a, const KvPart &
 {
     if (!p.target || !first) return;
     KvPieceNote n = {};
-    if (there && it.part == 0 && it.pieces > 1) n = {it.s.start, it.row0, min(it.rows, p.tile), it.pieces};
+    // (there are slots for all pieces but where starts do not ascend: sequences that share rows may then have more tiles than the host counted)
+    if (there && it.part == 0 && it.pieces > 1) n = {it.s.start, it.row0, min(it.rows, p.tile), min(it.pieces, p.slots - slot)};
     kv_partial(partials, p, a.c.heads, a.c.head_dim).note[(int64_t)slot * a.c.heads + head] = n;
 }
 
