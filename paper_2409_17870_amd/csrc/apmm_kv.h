@@ -67,14 +67,19 @@ hipError_t launch_kv_write(const KvArgs &c, const KvTensor &k, const KvTensor &v
 hipError_t launch_kv_read(const KvArgs &c, const KvTensor &k, const KvTensor &v, hipStream_t stream);
 hipError_t launch_kv_attention(const KvAttentionArgs &a, const KvPlan &plan, hipStream_t stream);
 
-// x / d as (x m) >> 40 with m = 2^40 / d, rounded up: exact for x < 2^30 and d <= 1024, since x (m - 2^40 / d) < 2^30 = 2^40 / 1024
-inline uint64_t kv_divisor(int d) { return ((1ull << 40) + d - 1) / d; }
+// x / d as (x m) >> 63 with m = 2^63 / d, rounded up: exact for 0 <= x < 2^31 and d <= 1024, since x (m - 2^63 / d) < 2^31 is less than 2^63 / 1024
+inline uint64_t kv_divisor(int d) { return ((1ull << 63) + d - 1) / d; }
 
 #ifdef __HIPCC__
 typedef uint16_t __attribute__((may_alias)) kv_u16;  // what is written in these and read in words, or the other way round
 typedef uint32_t __attribute__((may_alias)) kv_u32;
 
-__device__ __forceinline__ int kv_divide(int x, uint64_t m) { return (int)(((uint64_t)(uint32_t)x * m) >> 40); }
+// (the high half of 2 x m, a product of up to 95 bits; 2 x is one of 32)
+__device__ __forceinline__ int kv_divide(int x, uint64_t m)
+{
+    const uint64_t y = 2u * (uint32_t)x;
+    return (int)((y * (m >> 32) + ((y * (uint32_t)m) >> 32)) >> 32);
+}
 
 // Place of lane `lane` within its wave of a workgroup of whole waves
 __device__ __forceinline__ int kv_lane() { return threadIdx.x & 63; }
