@@ -84,6 +84,10 @@ __device__ __forceinline__ int kv_divide(int x, uint64_t m)
 // Place of lane `lane` within its wave of a workgroup of whole waves
 __device__ __forceinline__ int kv_lane() { return threadIdx.x & 63; }
 
+// What lanes of a wave have written to LDS before this the others read behind it, and the other way round.  No instruction: a wave's LDS accesses are done in their order, which is
+// kept by the compiler only where it is told that one lane's are another's.
+__device__ __forceinline__ void kv_wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local"); }
+
 // A sequence of the batch.  Whatever lies in lengths and starts, rows start .. start + n - 1 are rows of the tensors and keys below `keys` have a place in the table.
 struct KvSequence {
     int start, n;  // new tokens

@@ -172,6 +172,7 @@ __device__ __forceinline__ void kv_attention_tiles(const KvAttentionArgs &a, con
     };
     auto take_scales = [&](float own, float (&ks)[16], float (&vs)[16]) {
         scales[wave][lane] = own;
+        kv_wave_fence();
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float4v x = *reinterpret_cast<const float4v *>(&scales[wave][16 * h + 4 * i]), y = *reinterpret_cast<const float4v *>(&scales[wave][32 + 16 * h + 4 * i]);
@@ -181,6 +182,7 @@ __device__ __forceinline__ void kv_attention_tiles(const KvAttentionArgs &a, con
                 vs[4 * i + j] = y[j];
             }
         }
+        kv_wave_fence();
     };
     // Steps from t on that every row of the wave sees all keys of, as far as the places of keys go
     auto plain_until = [&]() {

@@ -166,9 +166,10 @@ __global__ __launch_bounds__(64 * kWaves) void kv_write_kernel(KvArgs c, KvTenso
             kv_u16 *t = turn[threadIdx.x >> 6];
 #pragma unroll
             for (int i = 0; i < P; ++i) t[four_of(part, i) * 8 + token] = (uint16_t)(uv[i / 2] >> (16 * (i & 1)));
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            kv_wave_fence();
             if constexpr (P == 4) reinterpret_cast<uint2 *>(values)[lane] = reinterpret_cast<const uint2 *>(t)[lane];
             else reinterpret_cast<uint32_t *>(values)[lane] = reinterpret_cast<const uint32_t *>(t)[lane];
+            kv_wave_fence();  // (the next head's go to the same place)
         } else if (e.is_new) {
 #pragma unroll
             for (int i = 0; i < P; ++i) values[four_of(part, i) * 8 + token] = (uint16_t)(uv[i / 2] >> (16 * (i & 1)));
@@ -227,9 +228,10 @@ __global__ __launch_bounds__(64 * kWaves) void kv_read_kernel(KvArgs c, KvTensor
         if constexpr (N == 8) reinterpret_cast<uint2 *>(t)[lane] = reinterpret_cast<const uint2 *>(values)[lane];
         else reinterpret_cast<uint32_t *>(t)[lane] = reinterpret_cast<const uint32_t *>(values)[lane];
         const uint32_t sk = scales[token], sv = scales[((int64_t)1 << c.page_shift) + token];
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        kv_wave_fence();
 #pragma unroll
         for (int i = 0; i < N / 4; ++i) uv[i] = t[four_of(part, 2 * i) * 8 + token] | (uint32_t)t[four_of(part, 2 * i + 1) * 8 + token] << 16;
+        kv_wave_fence();
         values_of<N, BF16>(uk, sk, xk);
         values_of<N, BF16>(uv, sv, xv);
         if (!there) {  // a position before the first token, or without a page: zeros
