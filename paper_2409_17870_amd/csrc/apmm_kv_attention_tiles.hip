@@ -188,7 +188,7 @@ __device__ __forceinline__ void kv_attention_tiles(const KvAttentionArgs &a, con
     auto plain_until = [&]() {
         const int key0 = it.key_of(t);
         if (key0 + 32 > it.s.keys || key0 + 31 > first_pos || t == begin) return t;
-        if (a.window && key0 <= last_pos - a.window) return min(it.sink_steps, a.sinks / 32);
+        if (a.window && key0 <= last_pos - a.window) return min(min(it.sink_steps, a.sinks / 32), it.s.keys / 32);  // (the last of these may end behind the page table)
         return min(it.s.keys, first_pos + 1) / 32 - it.gap;
     };
 
