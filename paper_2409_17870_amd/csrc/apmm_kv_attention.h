@@ -11,7 +11,7 @@
 //                       ones exactly as far as 2^-35 of the row's largest.
 //   Weights             p_j b_j, rounded once to binary16 (bfloat16 would cost an output of binary16 numbers eight times its own rounding; kv_attention_rows, which waits for memory, adds what
 //                       the rounding left as a second number for them).  The value scales may lie anywhere, so each row holds a power of two 2^E above all that it has met, and weights carry the
-//                       factor 2^(2 - E) until the end: at most 2^15, full precision down to 2^-16 of that for p = 1 and b = 2^E, and 2^-27 of it is the least that counts.
+//                       factor 2^(2 - E) until the end (in p as far as it has the range, kv_rest): at most 2^15, full precision down to 2^-16 of that for p = 1 and b = 2^E, and 2^-27 of it is the least that counts.
 //                       The sum of the rounded weights goes with them (dot products with ones).
 //   Running maximum     m (and E) are only moved where a score passes m + 13: until then weights are at most 2^13 times larger, for which there is room.  Then the accumulators are scaled;
 //                       -m + 2 - E is one number, `base`.  So large a slack is what lets kv_attention_tiles go without a maximum in most steps.
@@ -272,7 +272,10 @@ __device__ __forceinline__ int kv_page_ids(const KvAttentionArgs &a, const KvIte
     return page < a.c.pages ? page : -1;
 }
 
-// E of a largest scale: s < 2^E.  Held above -80, so that sums of 2^(2 - E) stay in range (scales below 2^-96 lose bits).
+// E of a largest scale: s < 2^E.  Held above -80, so that sums of 2^(2 - E) stay in range (scales below 2^-96 lose bits).  Of an E above kMostExponent the rest goes into the value scales
+// (kv_rest, a power of two of the row), or weights would be subnormal numbers, which the exponent's instruction does not make.
+constexpr int kMostExponent = 64;
+__device__ __forceinline__ int kv_rest(int e) { return max(e - kMostExponent, 0); }
 template <bool BF16>
 __device__ __forceinline__ int kv_exponent(uint32_t bits) { return BF16 ? max((int)(bits >> 7) - 126, -80) : (int)(bits >> 10) - 14; }
 template <bool BF16>

@@ -83,6 +83,7 @@ __device__ __forceinline__ void kv_attention_rows(const KvAttentionArgs &a, cons
         for (int i = 0; i < V; ++i) acc[e][i] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
     float top = kLowest, base = -kLowest, total = 0.0f, weights = 0.0f;
     uint32_t limit = 0, met = 0;  // scales of values that the row has met: the largest, and the largest that needs no other E
+    bool large = false;           // whether some row's E is more than kMostExponent
 
     auto step = [&](const KvRowsStep<D> &cur, KvRowsStep<D> &next) {
         const int key0 = it.key_of(v), page0 = __builtin_amdgcn_readlane(ids, id), page1 = __builtin_amdgcn_readlane(ids, id + 1);
@@ -130,12 +131,17 @@ __device__ __forceinline__ void kv_attention_rows(const KvAttentionArgs &a, cons
             for (int i = 0; i < 4; ++i) m = kv_finite_max<BF16>(kv_finite_max<BF16>(m, vs[i] & 0xffffu), vs[i] >> 16);
             m = max(m, (uint32_t)__shfl_xor((int)m, 16));
             m = max(m, (uint32_t)__shfl_xor((int)m, 32));
-            met = m;
-            limit = kv_limit<BF16>(met);
-            const float to = -top + (kRoom - (float)kv_exponent<BF16>(met));
-            const float by = __builtin_amdgcn_exp2f(to - base);
+            const int e = kv_exponent<BF16>(m);
+            const float to = -top + (kRoom - (float)min(e, kMostExponent));
+            float by = __builtin_amdgcn_exp2f(to - base);
             base = to;
             total *= by;
+            if (BF16) {
+                by *= ldexpf(1.0f, kv_rest(kv_exponent<true>(met)) - kv_rest(e));
+                large = __any(e > kMostExponent);
+            }
+            met = m;
+            limit = kv_limit<BF16>(met);
             weights *= by;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
@@ -143,11 +149,22 @@ __device__ __forceinline__ void kv_attention_rows(const KvAttentionArgs &a, cons
                 for (int i = 0; i < V; ++i) acc[e][i] *= by;
         }
         uint32_t w[4], rest[4] = {};  // rounded weights and, for results of binary16, what that left: two numbers of 11 bits
+        float weight[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float p0 = __builtin_amdgcn_exp2f(fmaf(x[2 * i], factor, base)), p1 = __builtin_amdgcn_exp2f(fmaf(x[2 * i + 1], factor, base));
             total += p0 + p1;
-            const float w0 = fmaf(p0, kv_low<BF16>(vs[i]), 0.0f), w1 = fmaf(p1, kv_high<BF16>(vs[i]), 0.0f);
+            weight[2 * i] = fmaf(p0, kv_low<BF16>(vs[i]), 0.0f);
+            weight[2 * i + 1] = fmaf(p1, kv_high<BF16>(vs[i]), 0.0f);
+        }
+        if (BF16 && large) {
+            const float by = ldexpf(1.0f, -kv_rest(kv_exponent<BF16>(met)));
+#pragma unroll
+            for (int i = 0; i < 8; ++i) weight[i] *= by;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float w0 = weight[2 * i], w1 = weight[2 * i + 1];
             w[i] = kv_half_pair(w0, w1);
             weights = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, w[i]), (half2v){1, 1}, weights, false);
             if (!BF16) {
@@ -185,6 +202,7 @@ __device__ __forceinline__ void kv_attention_rows(const KvAttentionArgs &a, cons
     // the waves' sums, four rows at a time: channel 64 i + 16 g + 4 j + e of row n is acc[e][i][j]
     total = over_row(total, plus);
     weights = over_row(weights, plus);
+    const float lift = BF16 ? ldexpf(1.0f, kv_rest(kv_exponent<BF16>(met))) : 1.0f;
     if (g == 0) {
         bases[wave][n] = -base;
         totals[wave][n] = total;
@@ -200,7 +218,7 @@ __device__ __forceinline__ void kv_attention_rows(const KvAttentionArgs &a, cons
                 for (int j = 0; j < 4; ++j) {
                     float4v o;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) o[e] = fmaf(acc[e][i][j], e & 1 ? 0x1p21f : 0x1p25f, -15.0f * weights);
+                    for (int e = 0; e < 4; ++e) o[e] = fmaf(acc[e][i][j], e & 1 ? 0x1p21f : 0x1p25f, -15.0f * weights) * lift;
                     *reinterpret_cast<float4v *>(&sums[wave][n & (R - 1)][64 * i + 16 * g + 4 * j]) = o;
                 }
         }

@@ -137,6 +137,9 @@ __device__ __forceinline__ void kv_attention_tiles(const KvAttentionArgs &a, con
     float top = kLowest, base = -kLowest, total = 0.0f, weights = 0.0f;
     float met = 0.0f, limit = 0.0f, most = 0.0f;  // largest scale of values that the row has met, the power of two above it; largest sum that a step may add
 
+    bool large = false;  // whether some row's E is more than kMostExponent
+    auto exponent_of = [](float s) { return max((int)(__float_as_uint(s) >> 23) - 126, -80); };  // E: 2^E above s, from -80 (sums of 2^(2 - E) stay in range; scales below 2^-96 lose bits)
+
     auto scores = [&]() {
         float16v s = init16;
 #pragma unroll
@@ -198,7 +201,7 @@ __device__ __forceinline__ void kv_attention_tiles(const KvAttentionArgs &a, con
             bad_before = bad;
             ids = pages_from(t + 1, bad);
         }
-        const int stop = __builtin_amdgcn_readfirstlane(bad || bad_before || !one_factor ? t : min(min(plain_until(), block + 32), to));
+        const int stop = __builtin_amdgcn_readfirstlane(bad || bad_before || !one_factor || large ? t : min(min(plain_until(), block + 32), to));
         bool again = false;
         if (t < stop) __builtin_amdgcn_s_waitcnt(0x0f70);  // nothing under way here, so that in the loop only its own loads are waited for, and each where it is needed
         while (t < stop && !again) {
@@ -265,19 +268,29 @@ __device__ __forceinline__ void kv_attention_tiles(const KvAttentionArgs &a, con
         high *= factor;
         if (__any((high > top + kSlack) | (largest > limit))) {
             top = fmaxf(top, over_row(high, larger));
+            const int before = kv_rest(exponent_of(met));
             met = over_row(largest, larger);
-            // 2^E above it, E from -80 (sums of 2^(2 - E) stay in range; scales below 2^-96 lose bits) to 127
-            const int e = min(max((int)(__float_as_uint(met) >> 23) - 126, -80), 127);
+            const int e = exponent_of(met);
             limit = ldexpf(1.0f, e);
-            const float moved = -top + (kRoom - (float)e), by = __builtin_amdgcn_exp2f(moved - base);
+            const float moved = -top + (kRoom - (float)min(e, kMostExponent));
+            float by = __builtin_amdgcn_exp2f(moved - base);
             base = moved;
-            most = ldexpf(1.0f, (int)(kRoom + kSlack) - e);
+            most = ldexpf(1.0f, (int)(kRoom + kSlack) - min(e, kMostExponent));
             total *= by;
+            if (BF16) {
+                by *= ldexpf(1.0f, before - kv_rest(e));
+                large = __any(e > kMostExponent);
+            }
             weights *= by;
 #pragma unroll
             for (int e = 0; e < E; ++e)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[e][i] *= by;
+        }
+        if (BF16 && large) {
+            const float by = ldexpf(1.0f, -kv_rest(exponent_of(met)));
+#pragma unroll
+            for (int i = 0; i < 16; ++i) vs[i] *= by;
         }
         float sum = 0.0f, weight_sum = 0.0f;
         uint32_t w[8];
@@ -296,7 +309,7 @@ __device__ __forceinline__ void kv_attention_tiles(const KvAttentionArgs &a, con
     weights = over_row(weights, plus);
     if (n >= rows) return;
     const bool whole = it.pieces == 1;
-    const float over = whole ? (total == 0.0f ? 0.0f : 1.0f / total) : 1.0f;
+    const float over = whole ? (total == 0.0f ? 0.0f : 1.0f / total) : 1.0f, lift = BF16 ? ldexpf(1.0f, kv_rest(exponent_of(met))) : 1.0f;
     uint16_t *out = a.out.data + (int64_t)(it.s.start + at) * a.out.token_stride + (int64_t)(head * a.groups + row - at * a.groups) * a.out.head_stride;
     const int64_t place = ((int64_t)slot * a.c.heads + head) * kTilesTile + tile_wave * kRows + n;
     const KvPartial partial = kv_partial(partials, part, a.c.heads, D);
@@ -308,7 +321,7 @@ __device__ __forceinline__ void kv_attention_tiles(const KvAttentionArgs &a, con
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float x = D == 128 ? acc[e & (E - 1)][4 * i + j] : acc[e & 1][4 * ((i + (e & 2)) & 3) + j];
-                o[4 * j + e] = fmaf(x, e & 1 ? 0x1p21f : 0x1p25f, -15.0f * weights) * over;
+                o[4 * j + e] = fmaf(x, e & 1 ? 0x1p21f : 0x1p25f, -15.0f * weights) * lift * over;
             }
         const int c0 = 32 * i + 16 * h;
         if (whole) {

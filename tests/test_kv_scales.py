@@ -1,0 +1,48 @@
+"""Attention over value scales of all sizes that bfloat16 has, on the CPU (host_wave.py) and the GPU against 64 bits."""
+import pytest
+import torch
+
+import host_wave
+import kv_reference as ref
+from paper_2409_17870_amd import binding
+from test_kv import close
+from test_kv_bounds import cache, host, rows  # noqa: F401  (host: the fixture)
+
+CASES = [(1, 190, 2), (5, 190, 2), (90, 190, 2), (1, 3300, 1), (40, 1100, 1)]  # new tokens, length (the last two are cut in pieces), heads
+
+
+def inputs(new, length, heads, by, some):
+    """Value scales times 2^by, all of them or those of every seventh token behind the first hundred."""
+    codes, scales, table, lengths = cache([length], heads, 64, 16, torch.bfloat16, seed=new)
+    tokens = torch.arange(length)
+    if some:
+        tokens = tokens[100::7]
+    page, at = table[0].long()[tokens // 16], tokens % 16
+    scales[page, :, 1, at] = (scales[page, :, 1, at].float() * 2.0 ** by).bfloat16()
+    q = rows(new, 2 * heads, 64, torch.bfloat16, seed=by)
+    q[::2] *= 0.25  # broad rows, whose many small weights count
+    return q, (codes, scales, table), [length], [0, new]
+
+
+def want(q, c, lengths, starts):
+    return ref.attention(q, *c, lengths, starts, 0, 0, 64 ** -0.5)
+
+
+@pytest.mark.parametrize("some", [False, True])
+@pytest.mark.parametrize("by", [-90, 60, 70, 104, 120, 126])
+@pytest.mark.parametrize("new, length, heads", CASES[:3])
+def test_on_the_host(host, new, length, heads, by, some):  # noqa: F811
+    q, c, lengths, starts = inputs(new, length, heads, by, some)
+    m = host_wave.Memory()
+    got = host.attention(m.copy(q), *[m.copy(t) for t in c], *[torch.tensor(x, dtype=torch.int32) for x in (lengths, starts)])
+    close(torch, got, *want(q, c, lengths, starts))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("some", [False, True])
+@pytest.mark.parametrize("by", [-90, 60, 70, 104, 120, 126])
+@pytest.mark.parametrize("new, length, heads", CASES)
+def test_on_the_gpu(new, length, heads, by, some):
+    q, c, lengths, starts = inputs(new, length, heads, by, some)
+    got = binding.apmm_kv_attention(q.cuda(), *[t.cuda() for t in c], *[torch.tensor(x, dtype=torch.int32).cuda() for x in (lengths, starts)])
+    close(torch, got, *want(q, c, lengths, starts))
