@@ -257,7 +257,8 @@ __device__ __forceinline__ void kv_queries(const uint32_t (&x)[N], float scale, 
     }
     __builtin_amdgcn_sched_barrier(0);
     init = -7.5f * 0x1p-20f * sum_across(sum);
-    factor = ldexpf(scale * 1.44269504088896341f, min(21 - e, 122));  // (queries of 2^115 and more: scores beyond any other's all the same)
+    // (queries of 2^115 and more: scores beyond any other's all the same.  Neither zero nor infinite: scores of hidden keys are -infinity, those of queries that are zero are zero)
+    factor = fminf(fmaxf(ldexpf(scale * 1.44269504088896341f, min(21 - e, 122)), 0x1p-149f), -kLowest);
 }
 
 // Pages of 16 keys each: lane i of the result has that of the i-th sixteen of the next steps of a wave (v, v + stride, ...), -1 where there is none

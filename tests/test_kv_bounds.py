@@ -5,6 +5,7 @@ import torch
 
 import host_wave
 from paper_2409_17870_amd import binding
+from test_kv import close
 
 
 @pytest.fixture(scope="module")
@@ -29,6 +30,12 @@ def cache(lengths, heads, D, ps, dtype=torch.float16, seed=1, width=0, spare=1):
 
 def rows(tokens, heads, D, dtype=torch.float16, seed=2):
     return torch.randn((tokens, heads, D), generator=torch.Generator().manual_seed(seed)).to(dtype)
+
+
+def agree(got, want, near):
+    """Finite, and as close as test_kv.py asks of its results (a difference that is no number passes its comparison)."""
+    assert bool(torch.isfinite(got).all())
+    close(torch, got, want, near)
 
 
 # Sequences whose rows overlap have more tiles (12 + 8 + 1) than the host makes slots for from 12 tokens of 12 sequences; the last one is long and cut.

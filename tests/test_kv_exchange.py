@@ -4,8 +4,7 @@ import pytest
 import torch
 
 import kv_reference as ref
-from test_kv import close
-from test_kv_bounds import cache, host, rows  # noqa: F401  (host: the fixture)
+from test_kv_bounds import agree, cache, host, rows  # noqa: F401  (host: the fixture)
 
 
 @pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
@@ -14,7 +13,7 @@ def test_scales_of_a_step_of_keys(host, dtype):  # noqa: F811
     lengths, starts = [100, 40], [0, 70, 110]
     args, q = cache(lengths, 2, 64, 16, dtype), rows(110, 4, 64, dtype)
     got = host.attention(q, *args, torch.tensor(starts, dtype=torch.int32))
-    close(torch, got, *ref.attention(q, *args[:3], lengths, starts, 0, 0, 64 ** -0.5))
+    agree(got, *ref.attention(q, *args[:3], lengths, starts, 0, 0, 64 ** -0.5))
 
 
 def test_codes_of_two_heads(host):  # noqa: F811

@@ -1,12 +1,11 @@
-"""Attention over value scales of all sizes that bfloat16 has, on the CPU (host_wave.py) and the GPU against 64 bits."""
+"""Attention over value scales of all sizes that bfloat16 has, and with softmax scales of all sizes, on the CPU (host_wave.py) and the GPU against 64 bits."""
 import pytest
 import torch
 
 import host_wave
 import kv_reference as ref
 from paper_2409_17870_amd import binding
-from test_kv import close
-from test_kv_bounds import cache, host, rows  # noqa: F401  (host: the fixture)
+from test_kv_bounds import agree, cache, host, rows  # noqa: F401  (host: the fixture)
 
 CASES = [(1, 190, 2), (5, 190, 2), (90, 190, 2), (1, 3300, 1), (40, 1100, 1)]  # new tokens, length (the last two are cut in pieces), heads
 
@@ -35,7 +34,7 @@ def test_on_the_host(host, new, length, heads, by, some):  # noqa: F811
     q, c, lengths, starts = inputs(new, length, heads, by, some)
     m = host_wave.Memory()
     got = host.attention(m.copy(q), *[m.copy(t) for t in c], *[torch.tensor(x, dtype=torch.int32) for x in (lengths, starts)])
-    close(torch, got, *want(q, c, lengths, starts))
+    agree(got, *want(q, c, lengths, starts))
 
 
 @pytest.mark.gpu
@@ -45,4 +44,39 @@ def test_on_the_host(host, new, length, heads, by, some):  # noqa: F811
 def test_on_the_gpu(new, length, heads, by, some):
     q, c, lengths, starts = inputs(new, length, heads, by, some)
     got = binding.apmm_kv_attention(q.cuda(), *[t.cuda() for t in c], *[torch.tensor(x, dtype=torch.int32).cuda() for x in (lengths, starts)])
-    close(torch, got, *want(q, c, lengths, starts))
+    agree(got, *want(q, c, lengths, starts))
+
+
+SOFTMAX = [1.5e-45, 1e-39, 2.0 ** -100, 2.0 ** 110, 3.4e38]
+
+
+def softmax_inputs(new, dtype, scale):
+    """Queries of many sizes; where the scale is large zeros, whose keys all weigh the same."""
+    codes, scales, table, _ = cache([130], 2, 64, 16, dtype, seed=7)
+    q = rows(new, 4, 64, dtype, seed=8)
+    q[1::3] *= 2.0 ** -12
+    if dtype == torch.bfloat16:
+        q[2::3] *= 2.0 ** -100
+    if scale > 1:
+        q.zero_()
+    return q, (codes, scales, table), [130], [0, new]
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("scale", SOFTMAX)
+@pytest.mark.parametrize("new", [1, 3, 70])
+def test_softmax_scales_on_the_host(host, new, scale, dtype):  # noqa: F811
+    q, c, lengths, starts = softmax_inputs(new, dtype, scale)
+    m = host_wave.Memory()
+    got = host.attention(m.copy(q), *[m.copy(t) for t in c], *[torch.tensor(x, dtype=torch.int32) for x in (lengths, starts)], scale=scale, window=60, sinks=5)
+    agree(got, *ref.attention(q, *c, lengths, starts, 60, 5, scale))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("scale", SOFTMAX)
+@pytest.mark.parametrize("new", [1, 3, 70])
+def test_softmax_scales_on_the_gpu(new, scale, dtype):
+    q, c, lengths, starts = softmax_inputs(new, dtype, scale)
+    got = binding.apmm_kv_attention(q.cuda(), *[t.cuda() for t in c], *[torch.tensor(x, dtype=torch.int32).cuda() for x in (lengths, starts)], scale=scale, window=60, sinks=5)
+    agree(got, *ref.attention(q, *c, lengths, starts, 60, 5, scale))

@@ -5,8 +5,7 @@ import torch
 import host_wave
 import kv_reference as ref
 from paper_2409_17870_amd import binding
-from test_kv import close
-from test_kv_bounds import cache, host, rows  # noqa: F401  (host: the fixture)
+from test_kv_bounds import agree, cache, host, rows  # noqa: F401  (host: the fixture)
 
 CASES = [  # page, pages of the table, length, new, window, sinks
     (16, 5, 10000, 100, 60, 96),     # all keys are first tokens, the last step of 32 has a page and none
@@ -40,7 +39,7 @@ def test_on_the_host(host, case, dtype):  # noqa: F811
     c, q, lengths, starts, window, sinks = inputs(case, dtype)
     m = host_wave.Memory()
     got = host.attention(m.copy(q), *[m.copy(t) for t in c], torch.tensor(lengths, dtype=torch.int32), torch.tensor(starts, dtype=torch.int32), window, sinks)
-    close(torch, got, *ref.attention(q, *c, lengths, starts, window, sinks, 64 ** -0.5))
+    agree(got, *ref.attention(q, *c, lengths, starts, window, sinks, 64 ** -0.5))
 
 
 @pytest.mark.gpu
@@ -50,4 +49,4 @@ def test_on_the_gpu(case, dtype):
     c, q, lengths, starts, window, sinks = inputs(case, dtype)
     on = [torch.tensor(x, dtype=torch.int32).cuda() for x in (lengths, starts)]
     got = binding.apmm_kv_attention(q.cuda(), *[t.cuda() for t in c], *on, window=window, sinks=sinks)
-    close(torch, got, *ref.attention(q, *c, lengths, starts, window, sinks, 64 ** -0.5))
+    agree(got, *ref.attention(q, *c, lengths, starts, window, sinks, 64 ** -0.5))
