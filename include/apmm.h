@@ -245,7 +245,9 @@ typedef struct apmm_kv_batch {
     int64_t table_stride;       /* elements between rows of the table, >= table_width */
     int64_t table_width;        /* pages of a row, 1 to 2^26; tokens beyond table_width * page_size have no place */
 } apmm_kv_batch;
-/* Lengths, starts and page numbers are read on the device and cannot be refused; whatever they are, nothing outside of the buffers is
+/* A call whose launch would have 2^32 work items or more is refused (APMM_ERR_UNSUPPORTED): writing and reading from tokens x kv_heads of about 2^29 on (sequences of
+ * one token: 2^26), attention from sequences x kv_heads of 2^24 on where each has a token.
+ * Lengths, starts and page numbers are read on the device and cannot be refused; whatever they are, nothing outside of the buffers is
  * read or written.  A token whose position is negative (more new tokens than the length says), beyond the table or in a page outside of 0 to pages - 1 has no place: it is not written,
  * reads as zeros and is seen by no query.
  * Tensors are tokens x heads x head_dim with head_dim contiguous elements and strides in elements, at any address of their type's

@@ -74,7 +74,7 @@ apmm_status check_pair(const apmm_kv_cache *cache, const apmm_kv_batch *batch, c
     apmm_status st = check_batch(cache, batch, a, empty);
     if (st != APMM_OK || empty) return st;
     if ((st = check_tensor(k, kt, kh, tk)) != APMM_OK || (st = check_tensor(v, vt, vh, tv)) != APMM_OK) return st;
-    if ((batch->tokens + 2 * (int64_t)batch->sequences) * cache->kv_heads > INT32_MAX) return fail(APMM_ERR_UNSUPPORTED, "kv: tokens * kv_heads is more than one launch takes");
+    if (apmm::kv_store_items(a) > apmm::kKvMostItems) return fail(APMM_ERR_UNSUPPORTED, "kv: tokens * kv_heads is more than one launch takes");
     return APMM_OK;
 }
 
@@ -85,6 +85,7 @@ apmm_status check_heads(const apmm_kv_cache *cache, const apmm_kv_batch *batch, 
     if (groups > 1024 || (batch->tokens + batch->sequences) * q_heads > INT32_MAX / 4)
         return fail(APMM_ERR_UNSUPPORTED, "kv_attention: more than 1024 query heads to a key/value head, or tokens * q_heads is more than one launch takes");
     plan = apmm::kv_plan(a, groups, window, sinks);
+    if (apmm::kv_attention_items(plan, a.heads) > apmm::kKvMostItems) return fail(APMM_ERR_UNSUPPORTED, "kv_attention: tokens * q_heads is more than one launch takes");
     return APMM_OK;
 }
 

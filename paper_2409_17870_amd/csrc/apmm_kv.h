@@ -63,6 +63,11 @@ struct KvPlan {
 KvPlan kv_plan(const KvArgs &c, int groups, int window, int sinks);
 size_t kv_partial_bytes(const KvPart &part, int heads, int head_dim);  // of the workspace that pieces take
 
+// Work items of the largest launch of a call; there may be fewer than 2^32
+constexpr int64_t kKvMostItems = UINT32_MAX;
+int64_t kv_store_items(const KvArgs &c);
+int64_t kv_attention_items(const KvPlan &plan, int heads);
+
 hipError_t launch_kv_write(const KvArgs &c, const KvTensor &k, const KvTensor &v, hipStream_t stream);
 hipError_t launch_kv_read(const KvArgs &c, const KvTensor &k, const KvTensor &v, hipStream_t stream);
 hipError_t launch_kv_attention(const KvAttentionArgs &a, const KvPlan &plan, hipStream_t stream);

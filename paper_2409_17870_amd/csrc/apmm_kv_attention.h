@@ -30,6 +30,9 @@ constexpr int kTilesTile = 64;   // and of half a workgroup of kv_attention_tile
 constexpr int kRowsStep = 32;    // keys of one step
 constexpr int kTilesStep = 32;
 
+// Workgroups of kv_attention_tiles_kernel for tiles
+inline int64_t kv_tiles_groups(const KvPart &part, int heads) { return (int64_t)((part.slots + 1) / 2) * heads; }
+
 hipError_t launch_kv_attention_rows(const KvAttentionArgs &a, const KvPart &part, hipStream_t stream);
 hipError_t launch_kv_attention_tiles(const KvAttentionArgs &a, const KvPlan &plan, hipStream_t stream);
 

@@ -83,11 +83,17 @@ void cut(KvPart &p, const KvArgs &c, int groups, int window, int sinks, int64_t 
     p.slots = (int)(tiles + (p.target ? p.target + 1 : 0));
 }
 
+int64_t join_groups_of_rows(const KvPlan &plan, int heads) { return plan.rows.target ? (int64_t)plan.rows.slots * heads : 0; }
+int64_t join_groups(const KvPlan &plan, int heads)
+{
+    return join_groups_of_rows(plan, heads) + (plan.tiles.target ? (int64_t)plan.tiles.slots * heads * (kTilesTile / 16) : 0);
+}
+
 template <int D, bool BF16>
 void join(const KvAttentionArgs &a, const KvPlan &plan, hipStream_t stream)
 {
-    const int64_t of_rows = plan.rows.target ? (int64_t)plan.rows.slots * a.c.heads : 0, of_tiles = plan.tiles.target ? (int64_t)plan.tiles.slots * a.c.heads * (kTilesTile / 16) : 0;
-    kv_attention_join_kernel<D, BF16><<<dim3((uint32_t)(of_rows + of_tiles)), dim3(256), 0, stream>>>(a, plan, (int)of_rows);
+    const int64_t of_rows = join_groups_of_rows(plan, a.c.heads), groups = join_groups(plan, a.c.heads);
+    kv_attention_join_kernel<D, BF16><<<dim3((uint32_t)groups), dim3(256), 0, stream>>>(a, plan, (int)of_rows);
 }
 
 }  // namespace
@@ -137,6 +143,13 @@ size_t kv_partial_bytes(const KvPart &part, int heads, int head_dim)
     if (!part.tile || !part.target) return 0;
     const KvPartial p = kv_partial(nullptr, part, heads, head_dim);
     return reinterpret_cast<size_t>(p.note + (int64_t)part.slots * heads);
+}
+
+int64_t kv_attention_items(const KvPlan &plan, int heads)
+{
+    const int64_t rows = plan.rows.tile ? (int64_t)plan.rows.slots * heads : 0;
+    const int64_t first = plan.tiles.tile ? (kv_tiles_groups(plan.tiles, heads) + rows) * 256 : rows * 64 * plan.rows.waves;
+    return std::max(first, join_groups(plan, heads) * 256);
 }
 
 hipError_t launch_kv_attention(const KvAttentionArgs &a, const KvPlan &plan, hipStream_t stream)

@@ -349,7 +349,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_attention_tiles_kernel(KvAt
 template <int D, bool BF16>
 void launch(const KvAttentionArgs &a, const KvPlan &plan, hipStream_t stream)
 {
-    const int of_tiles = (plan.tiles.slots + kWaves / kTileWaves - 1) / (kWaves / kTileWaves) * a.c.heads, of_rows = plan.rows.tile ? plan.rows.slots * a.c.heads : 0;
+    static_assert(kWaves / kTileWaves == 2 && kWaves == 4, "two tiles to a workgroup of 256 lanes");
+    const int of_tiles = (int)kv_tiles_groups(plan.tiles, a.c.heads), of_rows = plan.rows.tile ? plan.rows.slots * a.c.heads : 0;
     const dim3 grid((uint32_t)(of_tiles + of_rows)), block(64 * kWaves);
     if (a.c.page_shift == 4) kv_attention_tiles_kernel<D, BF16, true><<<grid, block, 0, stream>>>(a, plan, of_tiles);
     else kv_attention_tiles_kernel<D, BF16, false><<<grid, block, 0, stream>>>(a, plan, of_tiles);

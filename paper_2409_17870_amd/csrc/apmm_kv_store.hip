@@ -36,7 +36,7 @@ struct Eight {  // of one wave
 __device__ __forceinline__ bool find_eight(const KvArgs &c, int per, Eight &e)
 {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int unit = blockIdx.x * kWaves + wave, eight = kv_divide(unit, c.by_heads);  // (fewer than 2^30 units: 2^28 for tokens, 2^27 for sequences at most)
+    const int unit = blockIdx.x * kWaves + wave, eight = kv_divide(unit, c.by_heads);  // (fewer than 2^26 units, kv_store_items)
     e.head = (unit - eight * (per == 1 ? c.heads : (c.heads + 1) >> 1)) * per;
     int b, rest;
     auto count = [&](int at) {
@@ -248,14 +248,20 @@ __global__ __launch_bounds__(64 * kWaves) void kv_read_kernel(KvArgs c, KvTensor
 // Waves for the most eights that `tokens` new ones can touch: n tokens of a sequence lie in n of them at most, and in (n + 14) / 8
 int64_t eights(const KvArgs &c) { return std::min<int64_t>(c.tokens, c.tokens / 8 + 2 * (int64_t)c.sequences); }
 
+int heads_of_a_wave(const KvArgs &c) { return c.head_dim == 64 && eights(c) * c.heads >= kManyUnits ? 2 : 1; }
+int64_t workgroups(const KvArgs &c)
+{
+    const int per_wave = heads_of_a_wave(c);
+    return (eights(c) * ((c.heads + per_wave - 1) / per_wave) + kWaves - 1) / kWaves;
+}
+
 template <int D, bool BF16>
 hipError_t launch(bool write, const KvArgs &c, const KvTensor &k, const KvTensor &v, hipStream_t stream)
 {
     KvArgs a = c;
-    a.per_wave = D == 64 && eights(c) * c.heads >= kManyUnits ? 2 : 1;
-    const int groups_of = (c.heads + a.per_wave - 1) / a.per_wave;
-    a.by_heads = kv_divisor(groups_of);
-    const int64_t groups = (eights(c) * groups_of + kWaves - 1) / kWaves;
+    a.per_wave = heads_of_a_wave(c);
+    a.by_heads = kv_divisor((c.heads + a.per_wave - 1) / a.per_wave);
+    const int64_t groups = workgroups(c);
     if (write) kv_write_kernel<D, BF16><<<dim3((uint32_t)groups), dim3(64 * kWaves), 0, stream>>>(a, k, v);
     else kv_read_kernel<D, BF16><<<dim3((uint32_t)groups), dim3(64 * kWaves), 0, stream>>>(a, k, v);
     return hipGetLastError();
@@ -269,6 +275,7 @@ hipError_t launch(bool write, const KvArgs &c, const KvTensor &k, const KvTensor
 
 }  // namespace
 
+int64_t kv_store_items(const KvArgs &c) { return workgroups(c) * 64 * kWaves; }
 hipError_t launch_kv_write(const KvArgs &c, const KvTensor &k, const KvTensor &v, hipStream_t stream) { return launch(true, c, k, v, stream); }
 hipError_t launch_kv_read(const KvArgs &c, const KvTensor &k, const KvTensor &v, hipStream_t stream) { return launch(false, c, k, v, stream); }
 
