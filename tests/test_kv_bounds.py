@@ -1,5 +1,7 @@
 """What lies in lengths, starts and page tables is read on the device: whatever it is, the key/value cache's kernels touch nothing outside of their buffers.  On the CPU, where the kernels run
 between pages that cannot be touched (host_wave.py), and on the GPU with NaN behind the workspace."""
+import random
+
 import pytest
 import torch
 
@@ -52,6 +54,28 @@ def test_pieces_beyond_the_slots(host):
     m = host_wave.Memory()
     out = host.attention(m.copy(q), *[m.copy(t) for t in args], m.copy(starts))
     assert bool(torch.isfinite(out).all())
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_wild_batches(host, seed):
+    """Lengths, starts and page numbers of any size and order, for writes, reads and attention of few rows and many."""
+    r = random.Random(seed)
+    D, heads, groups, ps = r.choice([64, 128]), r.choice([1, 3, 32]), r.choice([1, 2, 16]), r.choice([16, 64])
+    sequences, tokens, width = r.choice([1, 2, 6, 12, 70]), r.choice([1, 3, 12, 40]), r.choice([1, 4, 50])
+
+    def wild(most):
+        return r.choice([0, 1, -1, most, r.randint(0, most), r.randint(0, most), 2 ** 31 - 1, -2 ** 31, r.randint(-50, most + 50)])
+    lengths = [wild(width * ps) if i < 8 else wild(60) for i in range(sequences)]
+    starts = [r.choice([(0, tokens)[i % 2], r.randint(0, tokens), wild(tokens)]) for i in range(sequences + 1)]
+    dtype = r.choice([torch.float16, torch.bfloat16])
+    codes, scales, _, _ = cache([200], heads, D, ps, dtype, seed=seed)
+    table = torch.randint(-2, codes.shape[0] + 2, (sequences, width), generator=torch.Generator().manual_seed(seed), dtype=torch.int32)
+    m = host_wave.Memory()
+    args = [m.copy(t) for t in (codes, scales, table, torch.tensor(lengths, dtype=torch.int32))]
+    starts = m.copy(torch.tensor(starts, dtype=torch.int32))
+    host.attention(m.copy(rows(tokens, heads * groups, D, dtype)), *args, starts, window=r.choice([0, 0, 50]), sinks=7)
+    host.write(*[m.copy(rows(tokens, heads, D, dtype, seed=i)) for i in (3, 4)], *args, starts)
+    host.read(*args, tokens, starts)
 
 
 @pytest.mark.gpu
