@@ -209,7 +209,7 @@ __device__ __forceinline__ void kv_attention_tiles(const KvAttentionArgs &a, con
             const float own = kv_scale_value(scale, BF16) * scale_by;
             take_scales(own, ks, vs);
             const float16v s = scores();
-            const Place next = place_of(min(t + 1, to - 1), ids, min(t + 1, to - 1) - block - 1);
+            const Place next = place_of(min(t + 1, to - 1), ids, max(min(t + 1, to - 1) - block - 1, 0));
             load_keys(next, k);
             in_order();
             scale = load_scales(next);

@@ -175,7 +175,11 @@ inline uint64_t ballot(bool p)
         if (all.there(i) && all[i]) m |= 1ull << i;
     return m;
 }
-inline int readlane(int v, int l) { return exchange(v)[l]; }
+inline int readlane(int v, int l)
+{
+    if (l < 0 || l > 63) std::fprintf(stderr, "host_wave: lane %d of a wave is read\n", l), std::abort();
+    return exchange(v)[l];
+}
 inline int update_dpp(int old, int v, int ctrl, int row_mask, int bank_mask, bool zero)
 {
     const auto all = exchange(v);

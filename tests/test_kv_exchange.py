@@ -26,3 +26,15 @@ def test_codes_of_two_heads(host):  # noqa: F811
     host.write(k, v, *host_args, starts)
     for got, given in zip(host.read(*host_args, tokens, starts), (k, v)):
         assert torch.equal(got, ref.value(*ref.quantise(given)))
+
+
+def test_pages_of_a_last_step(host):  # noqa: F811
+    """A piece whose last step is the first one behind a request for page numbers, and a plain one: no lane is asked for the page of a step before it (host_wave.py ends a run that
+    reads a lane which there is not).  Two tokens of 340 heads of 33 queries, 33 steps in one piece; some heads against 64 bits."""
+    heads, groups, length = 340, 33, 33 * 32
+    args, q, starts = cache([length], heads, 64, 16), rows(2, heads * groups, 64), [0, 2]
+    got = host.attention(q, *args, torch.tensor(starts, dtype=torch.int32))
+    for h in (0, heads - 1):
+        of = slice(h * groups, h * groups + 2)
+        c, s = (t[:, h:h + 1] for t in args[:2])
+        agree(got[:, of], *ref.attention(q[:, of], c, s, args[2], [length], starts, 0, 0, 64 ** -0.5))
