@@ -104,7 +104,8 @@ KvPlan kv_plan(const KvArgs &c, int groups, int window, int sinks)
     const int64_t rows = (int64_t)c.tokens * groups, sequences = std::min(c.sequences, c.tokens);  // (with new tokens)
     // A sequence's rows are as many as the call's where it is the only one, and no more than one token's where there is no other: else workgroups of both kinds
     // Few rows of a sequence go to kv_attention_rows: up to 32, where keys are cut for the sake of enough workgroups; where there are enough a tile reads the keys of 17 to 32 rows once, not twice
-    // (20 new ones of 1000 tokens, 40 sequences, 32 heads: 81 us with 32 as the border, 60 with 16; 28 rows of 30 sequences of 2000, 8 heads: 36 and 42; 30 rows of one of 56000: 36 and 48)
+    // (20 new ones of 1000 tokens, 32 heads: 8 sequences 18 us with 32 as the border, 28 with 16, 12 27 and 28, 16 33 and 28, 40 74 and 50; 7 tokens of 4 query heads, 8 heads, sequences of 2000:
+    // 48 44 and 45, 64 52 and 48; 30 rows of one of 56000: 36 and 48.  Longer contexts cross earlier: 30 rows of 2 sequences of 8000, 32 heads, 52 and 36)
     const int few_rows = sequences * c.heads >= 512 ? 16 : 32;
     const bool few = rows <= few_rows || c.tokens <= c.sequences, many = !few && c.sequences == 1;
     auto tiles = [&](int tile) { return std::min(c.tokens * (int64_t)((groups + tile - 1) / tile), rows / tile + sequences); };
@@ -127,12 +128,17 @@ KvPlan kv_plan(const KvArgs &c, int groups, int window, int sinks)
         p.tiles.to_rows = INT32_MAX;
         // Two workgroups of two tiles to a compute unit at a time.  A piece costs its beginning (5 us) and 32 KiB written and read, so no more of them than fit at once, 1024: with twice as many a
         // batch of 5 pieces of prompts took 5 % longer and a prompt of 2048 tokens 20 %, with three quarters the batch 10 %.  Pieces of 32 steps at least: 1000 tokens 36 us, with 16 46.
-        // How many are enough without: of one sequence and under a window tiles are known to be alike, those of several may be few long ones among short ones.
+        // How many are enough without cutting.  Tiles of one sequence are enough where more than one workgroup of two comes to a compute unit; from there on cutting is the join's 4 to 7 us more
+        // (prompts of 4096 tokens: 520 tiles 93 us uncut and 71 cut, 585 90 and 94, 2080 151 and 158; 500 new tokens of 8000: 512 170 and 156, 528 235 and 240).  Those of several sequences may be
+        // few long ones among short ones (60 prompts of 64 tokens and 64 new ones of 8000, 3904 tiles: 188 us uncut, 71 cut), which cutting loses 2 to 5 % for where all are alike (8 pieces of 500
+        // behind 4000 tokens: 269 and 276); the line is there for the workspace, 136 MB at 4096 tiles of 128 channels.  A window of up to 80 steps bounds what the long ones cost (window 2048: 2 pieces
+        // of 1000, 1016 tiles, 80 us uncut and 85 cut; 14 prompts of 64 and 64 new of 9000, 960 tiles, 53 and 36; window 4096: 150 and 154, 96 and 39).
         p.tiles.least = 32;
         // Two workgroups run on each of the 256 compute units at a time, and the second set comes to them in the order of the first: shortest of these first, each unit gets one long and one
         // short pair of tiles and all are done with both at about the same time (2048 tokens of 32 heads: 72.9 us without, 69.5 so; 4096: 199 and 191; from 8192 on no difference).
         p.tiles.turn = many ? 512 / c.heads : 0;
-        cut(p.tiles, c, groups, window, sinks, tiles(kTilesTile), kTilesStep, 1024, window ? 896 : many ? 2048 : 4096);
+        const bool short_window = window && kv_window_steps(window, sinks, (kTilesTile + groups - 2) / groups, kTilesStep) <= 80;
+        cut(p.tiles, c, groups, window, sinks, tiles(kTilesTile), kTilesStep, 1024, many ? 576 : short_window ? 896 : 4096);
     }
     p.tiles_partial = (int64_t)(kv_partial_bytes(p.rows, c.heads, c.head_dim) / sizeof(float));
     return p;
