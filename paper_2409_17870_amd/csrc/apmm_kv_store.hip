@@ -108,6 +108,7 @@ __device__ __forceinline__ uint32_t quantise(const uint32_t (&x)[N], uint32_t (&
     if (top >= kInfinity) scale = kInfinity | (kInfinity >> 1);  // a number that is not finite: no scale, the row reads back as NaN
     const float s = kv_scale_value(scale, BF16);
     const bool small = s < (BF16 ? 0x1p-64f : 0x1p-18f);  // 1 / s could leave the range, or s has been rounded by so much that |t| passes 8
+    const bool large = BF16 && s > 0x1p15f;               // the smallest numbers could become zero
     const float by = BF16 && small ? 0x1p64f : 1.0f, r = 0.5f / (s * by);
     // t = x / (2 s) up to 2^-23 of itself.  What is not an integer is 2^-12 from every one but zero (numbers of 11 bits and |t| <= 8, or a few bits and |t| <= 12), so moving t up by
     // 2^-21 |t| gives the floor of the exact quotient.  Codes less 8, which the sum puts on all eight of a word.
@@ -120,13 +121,16 @@ __device__ __forceinline__ uint32_t quantise(const uint32_t (&x)[N], uint32_t (&
                 const uint32_t bits = j & 1 ? x[4 * i + j / 2] >> 16 : x[4 * i + j / 2] & 0xffffu;
                 const float v = kv_scale_value(bits, BF16), t = (general ? v * by : v) * r;
                 int code = floor_of(fmaf(fabsf(t), 0x1p-21f, t));
-                if (general) code = min(max(code, -8), 7);
+                if (general) {
+                    code = min(max(code, -8), 7);
+                    if (BF16 && t == 0.0f && v < 0.0f) code = -1;
+                }
                 w += (uint32_t)code << (4 * j);
             }
             u[i] = s > 0.0f ? w : 0x88888888u;  // (no scale, or one that rounds to zero: every code is that of +1)
         }
     };
-    if (__any(small)) codes(std::true_type());
+    if (__any(small || large)) codes(std::true_type());
     else codes(std::false_type());
     return scale;
 }
