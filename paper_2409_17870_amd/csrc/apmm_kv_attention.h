@@ -280,6 +280,14 @@ __device__ __forceinline__ int kv_page_ids(const KvAttentionArgs &a, const KvIte
 // (kv_rest, a power of two of the row), or weights would be subnormal numbers, which the exponent's instruction does not make.
 constexpr int kMostExponent = 64;
 __device__ __forceinline__ int kv_rest(int e) { return max(e - kMostExponent, 0); }
+// total 2^x + plus for x <= 0.  With bfloat16 scales also where 2^x alone has no room: sums of weights begin between 2^(2 - kMostExponent) and 2^82, and those of a row's tiny values count like
+// those of its largest (sums of weights times values that far below the others' do not).
+template <bool BF16>
+__device__ __forceinline__ float kv_moved(float total, float x, float plus = 0.0f)
+{
+    if (!BF16) return fmaf(total, __builtin_amdgcn_exp2f(x), plus);
+    return fmaf(total * __builtin_amdgcn_exp2f(fminf(x + 100.0f, 0.0f)), __builtin_amdgcn_exp2f(fmaxf(x, -100.0f)), plus);
+}
 template <bool BF16>
 __device__ __forceinline__ int kv_exponent(uint32_t bits) { return BF16 ? max((int)(bits >> 7) - 126, -80) : (int)(bits >> 10) - 14; }
 template <bool BF16>

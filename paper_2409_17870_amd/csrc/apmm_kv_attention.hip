@@ -42,8 +42,8 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(KvAttentionArgs 
                 for (int k = 0; k < 4; ++k) x[j + k] = v[k];
             }
             const float top = fmaxf(base, r.x), old = __builtin_amdgcn_exp2f(base - top), by = __builtin_amdgcn_exp2f(r.x - top);
+            total = kv_moved<BF16>(total, base - top, kv_moved<BF16>(r.y, r.x - top));
             base = top;
-            total = fmaf(total, old, r.y * by);
 #pragma unroll
             for (int j = 0; j < C; ++j) o[j] = fmaf(o[j], old, x[j] * by);
         }
@@ -57,8 +57,8 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(KvAttentionArgs 
     for (int i = 1; i < shares; ++i) {
         const int other = group + i * row_slots;
         const float b = bases[other][0], top = fmaxf(base, b), old = __builtin_amdgcn_exp2f(base - top), by = __builtin_amdgcn_exp2f(b - top);
+        total = kv_moved<BF16>(total, base - top, kv_moved<BF16>(totals[other][0], b - top));
         base = top;
-        total = fmaf(total, old, totals[other][0] * by);
 #pragma unroll
         for (int j = 0; j < C; ++j) o[j] = fmaf(o[j], old, sums[threadIdx.x + 16 * i * row_slots][j] * by);
     }

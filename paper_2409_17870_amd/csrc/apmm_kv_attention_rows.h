@@ -134,8 +134,8 @@ __device__ __forceinline__ void kv_attention_rows(const KvAttentionArgs &a, cons
             const int e = kv_exponent<BF16>(m);
             const float to = -top + (kRoom - (float)min(e, kMostExponent));
             float by = __builtin_amdgcn_exp2f(to - base);
+            total = kv_moved<BF16>(total, to - base);
             base = to;
-            total *= by;
             if (BF16) {
                 by *= ldexpf(1.0f, kv_rest(kv_exponent<true>(met)) - kv_rest(e));
                 large = __any(e > kMostExponent);
@@ -232,7 +232,7 @@ __device__ __forceinline__ void kv_attention_rows(const KvAttentionArgs &a, cons
 #pragma unroll
             for (int i = 0; i < WAVES; ++i) {
                 const float by = __builtin_amdgcn_exp2f(bases[i][r] - most);
-                sum = fmaf(totals[i][r], by, sum);
+                sum = kv_moved<BF16>(totals[i][r], bases[i][r] - most, sum);
 #pragma unroll
                 for (int j = 0; j < C; ++j) o[j] = fmaf(sums[i][mine][c0 + j], by, o[j]);
             }

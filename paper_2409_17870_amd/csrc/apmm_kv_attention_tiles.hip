@@ -274,9 +274,9 @@ __device__ __forceinline__ void kv_attention_tiles(const KvAttentionArgs &a, con
             limit = ldexpf(1.0f, e);
             const float moved = -top + (kRoom - (float)min(e, kMostExponent));
             float by = __builtin_amdgcn_exp2f(moved - base);
+            total = kv_moved<BF16>(total, moved - base);
             base = moved;
             most = ldexpf(1.0f, (int)(kRoom + kSlack) - min(e, kMostExponent));
-            total *= by;
             if (BF16) {
                 by *= ldexpf(1.0f, before - kv_rest(e));
                 large = __any(e > kMostExponent);

@@ -80,3 +80,36 @@ def test_softmax_scales_on_the_gpu(new, scale, dtype):
     q, c, lengths, starts = softmax_inputs(new, dtype, scale)
     got = binding.apmm_kv_attention(q.cuda(), *[t.cuda() for t in c], *[torch.tensor(x, dtype=torch.int32).cuda() for x in (lengths, starts)], scale=scale, window=60, sinks=5)
     agree(got, *ref.attention(q, *c, lengths, starts, 60, 5, scale))
+
+
+# value scales of 2^-85 and 2^80 within a row: where the large ones are, of the tokens' numbers
+APART = {"later": lambda t, n: t >= n // 2, "earlier": lambda t, n: t < n // 3, "in turn": lambda t, n: t % 2 == 1, "steps in turn": lambda t, n: t // 32 % 2 == 1, "the last": lambda t, n: t == n - 1}
+
+
+def apart(new, length, heads, where):
+    codes, scales, table, _ = cache([length], heads, 64, 16, torch.bfloat16, seed=new)
+    t = torch.arange(length)
+    by = torch.where(APART[where](t, length), torch.tensor(2.0 ** 80), torch.tensor(2.0 ** -85))
+    page, at = table[0].long()[t // 16], t % 16
+    scales[page, :, 1, at] = (scales[page, :, 1, at].float() * by[:, None]).bfloat16()
+    return rows(new, 2 * heads, 64, torch.bfloat16, seed=3) * 0.25, (codes, scales, table), [length], [0, new]
+
+
+@pytest.mark.parametrize("window", [0, 7])
+@pytest.mark.parametrize("where", list(APART))
+@pytest.mark.parametrize("new, length, heads", CASES[:3])
+def test_far_apart_on_the_host(host, new, length, heads, where, window):  # noqa: F811
+    q, c, lengths, starts = apart(new, length, heads, where)
+    m = host_wave.Memory()
+    got = host.attention(m.copy(q), *[m.copy(t) for t in c], *[torch.tensor(x, dtype=torch.int32) for x in (lengths, starts)], window=window)
+    agree(got, *ref.attention(q, *c, lengths, starts, window, 0, 64 ** -0.5))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("window", [0, 7])
+@pytest.mark.parametrize("where", list(APART))
+@pytest.mark.parametrize("new, length, heads", CASES)
+def test_far_apart_on_the_gpu(new, length, heads, where, window):
+    q, c, lengths, starts = apart(new, length, heads, where)
+    got = binding.apmm_kv_attention(q.cuda(), *[t.cuda() for t in c], *[torch.tensor(x, dtype=torch.int32).cuda() for x in (lengths, starts)], window=window)
+    agree(got, *ref.attention(q, *c, lengths, starts, window, 0, 64 ** -0.5))
