@@ -311,8 +311,8 @@ def _kv_cache(codes, scales):
     if codes.get_device() != torch.cuda.current_device():
         raise ValueError("the cache must be on the current device, whose stream the call goes to")
     pages, heads, _, page_size = scales.shape
-    if page_size < 1 or codes.shape[3] * 2 % page_size:
-        raise ValueError("codes must hold a whole number of channels a token")
+    if page_size < 1 or codes.shape[3] < 1 or codes.shape[3] * 2 % page_size:
+        raise ValueError("codes must hold a whole number of channels a token, one at least")
     return ApmmKvCache(codes.data_ptr(), scales.data_ptr(), pages, page_size, heads, codes.shape[3] * 2 // page_size, _KV_DTYPES[scales.dtype])
 
 

@@ -262,7 +262,7 @@ bool kv_cache(PyObject *codes_arg, PyObject *scales_arg, apmm_kv_cache &c)
         codes->get_device() != c10::hip::getCurrentHIPStream().device_index())
         return false;
     const int64_t pages = codes->size(0), heads = codes->size(1), page_size = scales->size(3);
-    if (scales->size(0) != pages || scales->size(1) != heads || codes->size(2) != 2 || scales->size(2) != 2 || page_size < 1 || codes->size(3) * 2 % page_size) return false;
+    if (scales->size(0) != pages || scales->size(1) != heads || codes->size(2) != 2 || scales->size(2) != 2 || page_size < 1 || codes->size(3) < 1 || codes->size(3) * 2 % page_size) return false;
     const int64_t head_dim = codes->size(3) * 2 / page_size;
     if (heads > INT32_MAX || page_size > INT32_MAX || head_dim > INT32_MAX) return false;
     c = {codes->data_ptr(), scales->data_ptr(), pages, (int)page_size, (int)heads, (int)head_dim, scales->scalar_type() == at::kHalf ? APMM_F16 : APMM_BF16};
