@@ -271,8 +271,8 @@ apmm_status apmm_kv_read(const apmm_kv_cache *cache, const apmm_kv_batch *batch,
  * sequence's length less its new tokens, plus its place among them) sees key j of its sequence where
  *   j <= p, and where window > 0 also j > p - window or j < sinks
  * and its result is sum_j softmax_j(scale * q . k_j) v_j over these, zeros where there is none.  Statistics and sums are of 32 bits, the weights of the values are
- * rounded to 11 significant bits (where a sequence has few rows of binary16 numbers, 22), the result once; a weight times value scale below 2^-27 of the largest scale that its row sees
- * may count as nothing.  Accuracy holds for value scales from 2^-96 on (bfloat16; below, values lose bits).
+ * rounded to 11 significant bits (where a sequence has few rows of binary16 numbers, 22), the result once; a weight times value scale below 2^-26 of the largest scale that its row sees
+ * may count as nothing, and one below 2^-15 of it may be off by as much.  Accuracy holds for value scales from 2^-96 on (bfloat16; below, values lose bits).
  *   scale     > 0 and finite, 1 / sqrt(head_dim) in most models
  *   window    0 (all keys) to 2^30;  sinks  0 to 2^30, without effect where window is 0
  *   workspace device, 16-byte aligned, apmm_kv_attention_workspace_bytes() bytes of the same arguments (0 for most large calls; a call with a window needs no more); calls that may overlap need one each */

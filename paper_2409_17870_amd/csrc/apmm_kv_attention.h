@@ -7,8 +7,9 @@
 //   Codes as operands   A code in the low mantissa bits of a binary16 number is the subnormal u 2^-24 (bits 0 to 3) or u 2^-20 (bits 4 to 7), which the matrix unit takes exactly:
 //                       five operations make four operand words of one word of eight codes.  The -15 is added outside: -15 sum_d q_d is where the accumulators of the first product start
 //                       from, and 15 times the sum of the weights is taken off the second one's result.
-//   Queries             times a power of two for each row, so that its largest number is just below 2^11 (2^15 for the channels that meet u 2^-24): binary16 numbers as they are, bfloat16
-//                       ones exactly as far as 2^-35 of the row's largest.
+//   Queries             times a power of two for each row, so that its largest number is just below 2^11 (2^15 for the channels that meet u 2^-24).  Numbers below 2^-27 of the row's largest may
+//                       lose bits, 2^-35 of it at most (bfloat16, and binary16 rows beyond 2^11; other binary16 rows lose none); where the 32 rows of a wave share the power of the largest
+//                       one, rows down to 2^-10 of that, below 2^-17 of the row's largest and 2^-25 of it at most.
 //   Weights             p_j b_j, rounded once to binary16 (bfloat16 would cost an output of binary16 numbers eight times its own rounding; kv_attention_rows, which waits for memory, adds what
 //                       the rounding left as a second number for them).  The value scales may lie anywhere, so each row holds a power of two 2^E above all that it has met, and weights carry the
 //                       factor 2^(2 - E) until the end (in p as far as it has the range, kv_rest): at most 2^15, full precision down to 2^-16 of that for p = 1 and b = 2^E, and 2^-27 of it is the least that counts.

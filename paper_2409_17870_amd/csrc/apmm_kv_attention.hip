@@ -7,7 +7,6 @@ namespace apmm {
 
 namespace {
 
-
 // Reads what the pieces wrote, 4 (head_dim + 2) bytes a row and piece; a launch of it takes 4 to 7 us, nearly all of it the launch and the notes' way from memory.
 // A workgroup looks at one piece and head and 16 rows of its tile, and has work where the piece is the first of several.  16 lanes to a row; what is left of the 256 for fewer rows shares
 // out the pieces, each with its own running base, and meets in LDS.  One launch for both kernels' pieces: those of kv_attention_rows_kernel first.
@@ -70,10 +69,6 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(KvAttentionArgs 
     kv_store(a.out.data + (int64_t)(note.start + at) * a.out.token_stride + (int64_t)(head * a.groups + r - at * a.groups) * a.out.head_stride + c0, a.out.aligned, w);
 }
 
-}  // namespace
-
-namespace {
-
 // How many workgroups one kernel has for sequences of at most `tokens` new tokens in all: `tiles` for a head where nothing is cut.  Nothing is where there are `plenty` anyway.
 void cut(KvPart &p, const KvArgs &c, int groups, int window, int sinks, int64_t tiles, int step, int wanted, int plenty)
 {
@@ -102,7 +97,8 @@ KvPlan kv_plan(const KvArgs &c, int groups, int window, int sinks)
 {
     KvPlan p = {};
     const int64_t rows = (int64_t)c.tokens * groups, sequences = std::min(c.sequences, c.tokens);  // (with new tokens)
-    // A sequence's rows are as many as the call's where it is the only one, and no more than one token's where there is no other: else workgroups of both kinds
+    // A sequence's rows are as many as the call's where it is the only one: else workgroups of both kinds, but where there are no more tokens than sequences.  That is one token of each as a rule; a
+    // batch of many slots without new tokens has its few longer ones in tiles of 16 rows then (500 new tokens of 4000 beside 511 empty slots, 8 heads of 8: 146 us, beside 300 112).
     // Few rows of a sequence go to kv_attention_rows: up to 32, where keys are cut for the sake of enough workgroups; where there are enough a tile reads the keys of 17 to 32 rows once, not twice
     // (20 new ones of 1000 tokens, 32 heads: 8 sequences 18 us with 32 as the border, 28 with 16, 12 27 and 28, 16 33 and 28, 40 74 and 50; 7 tokens of 4 query heads, 8 heads, sequences of 2000:
     // 48 44 and 45, 64 52 and 48; 30 rows of one of 56000: 36 and 48.  Longer contexts cross earlier: 30 rows of 2 sequences of 8000, 32 heads, 52 and 36)

@@ -9,8 +9,9 @@
 // exponent in one, power, sum, product with the value's scale and rounding, sum of the rounded ones), beside 16 matrix instructions that take half as long.  Hence
 //   - the factor of a query's row is the same for the 32 of a wave in nearly all calls and goes into the keys' scales, one product a lane instead of one a key and row;
 //   - a step that has no hidden keys does not look for the maximum of its scores: its sums tell afterwards whether a weight was too large for the running maximum.
-// Every other step (the first, those at the diagonal and at the window's edge, those whose sums are too large, all of a wave whose queries differ by 2^10) goes the general way.
-// 16384 tokens of 32 heads of 128, binary16: 2.27 ms, 969 TFLOP/s; 4096 tokens: 191 us, 720 TFLOP/s (the vector units issue for 65 % of the kernel, for 76 % of the time that a compute unit
+// Every other step (the first, those at the diagonal and at the window's edge, those whose sums are too large, all of a wave whose queries differ by 2^10, all behind a value scale of 2^64) goes
+// the general way.
+// 16384 tokens of 32 heads of 128, binary16: 2.26 ms, 972 TFLOP/s; 4096 tokens: 191 us, 720 TFLOP/s (the vector units issue for 65 % of the kernel, for 76 % of the time that a compute unit
 // has work; the rest is the uneven end).  8192-cubed products of a library reach 1194 TFLOP/s here.
 #include "apmm_kv_attention_rows.h"
 
