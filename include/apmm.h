@@ -282,6 +282,67 @@ apmm_status apmm_kv_attention(const apmm_kv_cache *cache, const apmm_kv_batch *b
                               void *out, int64_t out_token_stride, int64_t out_head_stride,
                               float scale, int64_t window, int64_t sinks, void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- Rotary positions: pairs of a row's channels turned by an angle that its position gives.
+ * Of head_dim channels the first 2 * pairs are turned: pair i is channels 2 i and 2 i + 1 (interleaved) or i and i + pairs, and with t = position * frequencies[i] its (a, b) becomes
+ *   magnitude * (a cos t - b sin t), magnitude * (b cos t + a sin t);
+ * the other channels stay as they are.  The angle is a product of 64 bits, so far positions lose nothing; the rest is of 32 bits, rounded once to the rows' type.  Scaling for long contexts lies in
+ * the frequencies and the magnitude. */
+typedef struct apmm_rotation {
+    const double *frequencies; /* device, pairs: radians a position */
+    int64_t pairs;             /* 1 to head_dim / 2 */
+    int interleaved;
+    float magnitude;           /* > 0 and finite, 1 in most models */
+} apmm_rotation;
+
+/* tokens x heads rows of head_dim (1 to 1024) channels; positions: device, one of each token, of any sign.  `inverse`: by -t.  That is also the gradient: of y = apmm_rotary(x) the gradient of x is
+ * apmm_rotary, inverse, of y's.  `out` may be x with the same strides, else they must not overlap. */
+apmm_status apmm_rotary(int64_t tokens, int heads, int head_dim, int dtype, const void *x, int64_t x_token_stride, int64_t x_head_stride, const int32_t *positions, const apmm_rotation *rotation,
+                        int inverse, void *out, int64_t out_token_stride, int64_t out_head_stride, void *stream);
+
+/* apmm_rotary of queries (into q_out, which may be q with the same strides) and of keys, and apmm_kv_write of these keys and of the values, in one launch, with the results of the calls one by one.
+ *   q_heads    0 to 2048; 0: no queries, q and q_out may be NULL
+ *   positions  device, one of each new token; or NULL: its place in its sequence.  (After apmm_kv_evict places are not positions any more.)
+ * Rows of q that belong to no sequence are left as they are in q_out. */
+apmm_status apmm_kv_write_rotary(const apmm_kv_cache *cache, const apmm_kv_batch *batch, int q_heads, const int32_t *positions, const apmm_rotation *rotation,
+                                 const void *q, int64_t q_token_stride, int64_t q_head_stride, void *q_out, int64_t q_out_token_stride, int64_t q_out_head_stride,
+                                 const void *k, int64_t k_token_stride, int64_t k_head_stride, const void *v, int64_t v_token_stride, int64_t v_head_stride, void *stream);
+
+/* ---- Keeping the cache within a budget.
+ * What attention gives each cached token: for key j of sequence b and key/value head h
+ *   weights[b][h][j] = decay * weights[b][h][j] + sum over the sequence's new tokens i and the query heads of h of softmax_j(scale * q_i . k_j)
+ * over the keys that apmm_kv_attention with the same arguments lets query i see; a decay of 0 does not read what was there.  weights: device, sequences x kv_heads x capacity 32-bit floats with contiguous
+ * tokens; tokens from `capacity` on have none, tokens behind a sequence's length and sequences without new tokens keep what is there.  A query with a score that is NaN (a scale or a number of it is) gives NaN to
+ * the keys that it sees.  Results do not depend on the order of execution.
+ *   workspace  device, 16-byte aligned, apmm_kv_weights_workspace_bytes() bytes of the same arguments (a call with a window needs no more); calls that may overlap need one each */
+size_t apmm_kv_weights_workspace_bytes(const apmm_kv_cache *cache, const apmm_kv_batch *batch, int q_heads);
+apmm_status apmm_kv_weights(const apmm_kv_cache *cache, const apmm_kv_batch *batch, int q_heads, const void *q, int64_t q_token_stride, int64_t q_head_stride,
+                            float *weights, int64_t weights_sequence_stride, int64_t weights_head_stride, int64_t capacity, float decay, float scale, int64_t window, int64_t sinks,
+                            void *workspace, size_t workspace_bytes, void *stream);
+
+/* Of each sequence and key/value head the first `sinks` tokens, the last `recent` and of the others the heaviest, min(budget, length) in all, copied in their order to places 0, 1, ... of the pages that
+ * `to_table` names.  Of equal weights the token of the lower place stays; NaN, and a token from `capacity` on, is lighter than any number.  Tokens without a page never stay.  Heads of a sequence keep
+ * equally many tokens, as a rule different ones.
+ *   to_table    device, sequences x to_width (rows to_stride apart): pages that no sequence of the call has; a token without a place there is not copied.  The old pages stay as they are.
+ *   to_lengths  device, sequences: tokens that stay; not `lengths` itself
+ *   kept        device, sequences x kv_heads x budget: the places they had, ascending, then -1
+ *   to_weights  device, sequences x kv_heads x budget: their weights (0 for those that have none), then 0
+ * sinks + recent <= budget.  A call of 2^32 work items or more is refused: sequences x kv_heads from 2^22 on, sequences x kv_heads x budget from about 2^29 on. */
+apmm_status apmm_kv_evict(const apmm_kv_cache *cache, int sequences, const int32_t *lengths, const int32_t *page_table, int64_t table_stride, int64_t table_width,
+                          const float *weights, int64_t weights_sequence_stride, int64_t weights_head_stride, int64_t capacity, int64_t budget, int64_t sinks, int64_t recent,
+                          const int32_t *to_table, int64_t to_stride, int64_t to_width, int32_t *to_lengths, int32_t *kept, float *to_weights, void *stream);
+
+/* ---- Four-bit weights with group scales times activations of 16 bits: y = x * W^T with W[n][k] = (2 u[n][k] - 15) * scales[n][k / group], u bipolar-INT codes of four bits (paper Sec. 3.1, Eq. 1).
+ * For layers whose activations are not to be quantised.  The products of a group are exact and summed in 32 bits, its sum is multiplied with the scale in 32 bits, y is rounded once.  (Activations of
+ * 2^115 and more may overflow the sums.  Infinities and NaN reach the results of their own row alone.)
+ *   group     32, 64 or 128 inputs; the last one of a channel may be shorter
+ *   dtype     apmm_dtype of x, y and the scales; the packed form is made for one of them
+ *   codes     device, N x K uint8, row-major, the low four bits count;  scales  device, N x ceil(K / group)
+ *   packed    device, apmm_w4_packed_bytes(N, K, group) bytes, 16-byte aligned, opaque, of this version of the library
+ *   x, y      device, M x K and M x N, rows x_stride and y_stride elements apart, at any address of their type's alignment; M up to 2^20, N and K up to 2^24 */
+size_t apmm_w4_packed_bytes(int64_t N, int64_t K, int group);
+apmm_status apmm_w4_pack(const uint8_t *codes, const void *scales, int64_t N, int64_t K, int group, int dtype, void *packed, void *stream);
+apmm_status apmm_w4_gemm(int64_t M, int64_t N, int64_t K, int group, int dtype, const void *x, int64_t x_stride, const void *packed, void *y, int64_t y_stride, void *stream);
+
 /* Measurement aid.  The next apmm_gemm / apmm_gemm_ex / apmm_gemm_from_codes call of the calling thread, if it
  * runs the large-tile MFMA kernel or a small-M kernel in one launch, attaches the two hipEvent_t (created by the
  * caller; either may be NULL) to that kernel's dispatch itself (hipExtLaunchKernel): afterwards they hold the

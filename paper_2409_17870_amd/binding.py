@@ -6,6 +6,7 @@ no fallback: if the library is missing or a call fails, an exception is raised.
 """
 import ctypes
 import functools
+import math
 import os
 import warnings
 
@@ -20,7 +21,9 @@ ALGO_PLANE_PAIRS_GLOBAL, ALGO_PLANES_REGISTERS, ALGO_MFMA_KSPLIT = 6, 7, 8
 EXPORTS = [
     "apmm_packed_bytes", "apmm_packed_activation_bytes", "apmm_workspace_bytes", "apmm_pack_weights", "apmm_pack_activations",
     "apmm_quantize_pack_activations", "apmm_unpack", "apmm_unpack_activations", "apmm_gemm", "apmm_gemm_ex", "apmm_gemm_from_codes", "apmm_gemm_from_codes_noalloc", "apmm_gemm_grouped",
-    "apmm_kv_write", "apmm_kv_read", "apmm_kv_attention", "apmm_kv_attention_workspace_bytes", "apmm_time_next_gemm", "apmm_last_gemm_kernel", "apmm_status_string", "apmm_last_error", "apmm_version",
+    "apmm_kv_write", "apmm_kv_read", "apmm_kv_attention", "apmm_kv_attention_workspace_bytes",
+    "apmm_rotary", "apmm_kv_write_rotary", "apmm_kv_weights", "apmm_kv_weights_workspace_bytes", "apmm_kv_evict", "apmm_w4_packed_bytes", "apmm_w4_pack", "apmm_w4_gemm",
+    "apmm_time_next_gemm", "apmm_last_gemm_kernel", "apmm_status_string", "apmm_last_error", "apmm_version",
 ]
 
 
@@ -43,6 +46,11 @@ class ApmmKvBatch(ctypes.Structure):
     """struct apmm_kv_batch of include/apmm.h"""
     _fields_ = [("sequences", ctypes.c_int), ("tokens", ctypes.c_int64), ("lengths", ctypes.c_void_p), ("starts", ctypes.c_void_p),
                 ("page_table", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("table_width", ctypes.c_int64)]
+
+
+class ApmmRotation(ctypes.Structure):
+    """struct apmm_rotation of include/apmm.h"""
+    _fields_ = [("frequencies", ctypes.c_void_p), ("pairs", ctypes.c_int64), ("interleaved", ctypes.c_int), ("magnitude", ctypes.c_float)]
 
 
 _lib = None
@@ -108,6 +116,23 @@ def load():
     lib.apmm_kv_attention.argtypes = [cache, batch, ci] + rows + rows + [ctypes.c_float, i64, i64, vp, ctypes.c_size_t, vp]
     lib.apmm_kv_attention_workspace_bytes.restype = ctypes.c_size_t
     lib.apmm_kv_attention_workspace_bytes.argtypes = [cache, batch, ci]
+    rotation = ctypes.POINTER(ApmmRotation)
+    lib.apmm_rotary.restype = ci
+    lib.apmm_rotary.argtypes = [i64, ci, ci, ci] + rows + [vp, rotation, ci] + rows + [vp]
+    lib.apmm_kv_write_rotary.restype = ci
+    lib.apmm_kv_write_rotary.argtypes = [cache, batch, ci, vp, rotation] + rows * 4 + [vp]
+    lib.apmm_kv_weights.restype = ci
+    lib.apmm_kv_weights.argtypes = [cache, batch, ci] + rows + [vp, i64, i64, i64, ctypes.c_float, ctypes.c_float, i64, i64, vp, ctypes.c_size_t, vp]
+    lib.apmm_kv_weights_workspace_bytes.restype = ctypes.c_size_t
+    lib.apmm_kv_weights_workspace_bytes.argtypes = [cache, batch, ci]
+    lib.apmm_kv_evict.restype = ci
+    lib.apmm_kv_evict.argtypes = [cache, ci, vp, vp, i64, i64, vp, i64, i64, i64, i64, i64, i64, vp, i64, i64, vp, vp, vp, vp]
+    lib.apmm_w4_packed_bytes.restype = ctypes.c_size_t
+    lib.apmm_w4_packed_bytes.argtypes = [i64, i64, ci]
+    lib.apmm_w4_pack.restype = ci
+    lib.apmm_w4_pack.argtypes = [vp, vp, i64, i64, ci, ci, vp, vp]
+    lib.apmm_w4_gemm.restype = ci
+    lib.apmm_w4_gemm.argtypes = [i64, i64, i64, ci, ci, vp, i64, vp, vp, i64, vp]
     lib.apmm_time_next_gemm.restype = ci
     lib.apmm_time_next_gemm.argtypes = [vp, vp]
     lib.apmm_last_gemm_kernel.restype = ctypes.c_char_p
@@ -390,6 +415,177 @@ def apmm_kv_attention_workspace_bytes(tokens, q_heads, codes, scales, page_table
     batch = _kv_batch(codes, page_table, lengths, None, lengths.shape[0])
     batch.tokens = tokens
     return int(load().apmm_kv_attention_workspace_bytes(_kv_cache(codes, scales), batch, q_heads))
+
+
+# ---- rotary positions, the cache's budget, four-bit weights of groups
+def apmm_rotary_frequencies(rotary_dim, base=10000.0, factor=1.0, original=None, fast=32.0, slow=1.0, device="cuda"):
+    """Radians a position for the rotary_dim / 2 pairs, in 64 bits: base^(-2 i / rotary_dim), for contexts `factor` times longer than a model was trained for divided by factor.
+
+    With `original`, the positions that the model was trained for, frequencies of at least `fast` turns in them stay as they are, those of at most `slow` are divided, and between
+    the two a ramp over the turns mixes both.  (The magnitude that goes with it is 1 + 0.1 ln(factor) as a rule.)
+    """
+    if rotary_dim < 2 or rotary_dim % 2:
+        raise ValueError("rotary_dim must be even and at least 2")
+    f = base ** (torch.arange(0, rotary_dim, 2, dtype=torch.float64) / -rotary_dim)
+    if original is None:
+        return (f / factor).to(device)
+    keep = ((f * (original / (2.0 * math.pi)) - slow) / (fast - slow)).clamp(0.0, 1.0)
+    return (f * (keep + (1.0 - keep) / factor)).to(device)
+
+
+def _rotation(frequencies, interleaved, magnitude, device, what):
+    if frequencies.dtype != torch.float64 or frequencies.dim() != 1 or not frequencies.is_contiguous() or frequencies.device != device:
+        raise ValueError("frequencies must be a contiguous float64 vector on %s device" % what)
+    return ApmmRotation(frequencies.data_ptr(), frequencies.shape[0], bool(interleaved), magnitude)
+
+
+def _positions(positions, tokens, device):
+    if positions.dtype != torch.int32 or positions.dim() != 1 or positions.shape[0] != tokens or positions.device != device or (tokens > 1 and positions.stride(0) != 1):
+        raise ValueError("positions must be a contiguous int32 vector of one a token, on the rows' device")
+    return positions.data_ptr()
+
+
+def apmm_rotary(x, positions, frequencies, interleaved=False, magnitude=1.0, inverse=False, out=None):
+    """Turn the pairs of the first 2 * len(frequencies) channels of x (tokens x heads x head_dim, float16 or bfloat16) by position times frequency (float64, radians).
+
+    Pairs are neighbours (interleaved) or len(frequencies) apart.  inverse: turned back, which is also the gradient.  out: x itself, or rows that do not overlap it.
+    """
+    if x.dtype not in _KV_DTYPES or not x.is_cuda or x.dim() != 3 or (x.shape[2] > 1 and x.stride(2) != 1):
+        raise ValueError("x must be a float16 or bfloat16 CUDA tensor, tokens x heads x head_dim, contiguous in its last dimension")
+    if x.get_device() != torch.cuda.current_device():
+        raise ValueError("x must be on the current device, whose stream the call goes to")
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    elif out.dtype != x.dtype or out.device != x.device or out.shape != x.shape or (x.shape[2] > 1 and out.stride(2) != 1):
+        raise ValueError("out must be of x's shape, type and device, contiguous in its last dimension")
+    tokens, heads, head_dim = x.shape
+    _check(load().apmm_rotary(tokens, heads, head_dim, _KV_DTYPES[x.dtype], x.data_ptr(), x.stride(0), x.stride(1), _positions(positions, tokens, x.device),
+                              _rotation(frequencies, interleaved, magnitude, x.device, "x's"), bool(inverse), out.data_ptr(), out.stride(0), out.stride(1), _stream()))
+    return out
+
+
+def apmm_kv_write_rotary(q, k, v, codes, scales, page_table, lengths, frequencies, starts=None, positions=None, interleaved=False, magnitude=1.0, q_out=None):
+    """apmm_rotary of q and k and apmm_kv_write of these k and of v in one launch; the turned q (in q_out, which may be q).  positions: int32, one a new token, None: its place in its
+    sequence.  q may be None."""
+    cache = _kv_cache(codes, scales)
+    batch = _kv_batch(codes, page_table, lengths, starts, k.shape[0])
+    tokens, head_dim = batch.tokens, cache.head_dim
+    heads, q_rows = 0, (None, 0, 0) * 2
+    if q is not None:
+        if q.dim() != 3:
+            raise ValueError("q must be tokens x query heads x %d" % head_dim)
+        heads = q.shape[1]
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        q_rows = _kv_rows(q, codes, scales, heads, head_dim, tokens, "q") + _kv_rows(q_out, codes, scales, heads, head_dim, tokens, "q_out")
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    rotation = _rotation(frequencies, interleaved, magnitude, codes.device, "the cache's")
+    _check(load().apmm_kv_write_rotary(cache, batch, heads, None if positions is None else _positions(positions, tokens, codes.device), rotation, *q_rows,
+                                       *_kv_rows(k, codes, scales, cache.kv_heads, head_dim, tokens, "k"), *_kv_rows(v, codes, scales, cache.kv_heads, head_dim, tokens, "v"), _stream()))
+    return q_out
+
+
+def _kv_weights_rows(weights, codes, sequences, kv_heads):
+    if weights.dtype != torch.float32 or weights.device != codes.device or weights.dim() != 3 or weights.shape[0] != sequences or weights.shape[1] != kv_heads or             weights.shape[2] < 1 or (weights.shape[2] > 1 and weights.stride(2) != 1):
+        raise ValueError("weights must be a float32 tensor on the cache's device, sequences x %d x capacity, contiguous in its last dimension" % kv_heads)
+    return weights.data_ptr(), weights.stride(0), weights.stride(1), weights.shape[2]
+
+
+def apmm_kv_weights(q, codes, scales, page_table, lengths, weights, starts=None, window=0, sinks=0, scale=None, decay=1.0, workspace=None):
+    """What attention of the new tokens' queries gives each cached token, summed over the queries and the query heads of a key/value head, added to decay * weights (float32, sequences
+    x kv heads x capacity, changed and returned).  Arguments and the keys that a query sees as in apmm_kv_attention; workspace: uint8 tensor of
+    apmm_kv_weights_workspace_bytes(...) bytes, allocated if None.
+    """
+    cache = _kv_cache(codes, scales)
+    if q.dim() != 3 or q.shape[2] != cache.head_dim:
+        raise ValueError("q must be tokens x query heads x %d" % cache.head_dim)
+    tokens, heads, head_dim = q.shape
+    batch = _kv_batch(codes, page_table, lengths, starts, tokens)
+    rows = _kv_rows(q, codes, scales, heads, head_dim, tokens, "q")
+    to = _kv_weights_rows(weights, codes, batch.sequences, cache.kv_heads)
+    lib = load()
+    if workspace is None:
+        need = lib.apmm_kv_weights_workspace_bytes(cache, batch, heads)
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    elif workspace.device != codes.device or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the cache's device")
+    _check(lib.apmm_kv_weights(cache, batch, heads, *rows, *to, decay, head_dim ** -0.5 if scale is None else scale, window, sinks,
+                               _ptr(workspace), 0 if workspace is None else workspace.nbytes, _stream()))
+    return weights
+
+
+def apmm_kv_weights_workspace_bytes(tokens, q_heads, codes, scales, page_table, lengths):
+    """Bytes of workspace that apmm_kv_weights needs for `tokens` queries."""
+    batch = _kv_batch(codes, page_table, lengths, None, lengths.shape[0])
+    batch.tokens = tokens
+    return int(load().apmm_kv_weights_workspace_bytes(_kv_cache(codes, scales), batch, q_heads))
+
+
+def apmm_kv_evict(codes, scales, page_table, lengths, weights, budget, to_table, sinks=0, recent=0, kept=None, to_weights=None, to_lengths=None):
+    """Keep of each sequence and head the first `sinks` tokens, the last `recent` and the heaviest others, `budget` in all: copied in their order to the pages of to_table (int32, sequences
+    x pages, none of a sequence of the call).  (places they had, int32, sequences x kv heads x budget with -1 behind the last; their weights; the new lengths.)
+    """
+    cache = _kv_cache(codes, scales)
+    batch = _kv_batch(codes, page_table, lengths, None, lengths.shape[0])
+    _kv_batch(codes, to_table, lengths, None, lengths.shape[0])
+    sequences, shape = batch.sequences, (batch.sequences, cache.kv_heads, budget)
+    rows = _kv_weights_rows(weights, codes, sequences, cache.kv_heads)
+    if kept is None:
+        kept = torch.empty(shape, dtype=torch.int32, device=codes.device)
+    if to_weights is None:
+        to_weights = torch.empty(shape, dtype=torch.float32, device=codes.device)
+    if to_lengths is None:
+        to_lengths = torch.empty(sequences, dtype=torch.int32, device=codes.device)
+    for t, what, dtype, of in ((kept, "kept", torch.int32, shape), (to_weights, "to_weights", torch.float32, shape), (to_lengths, "to_lengths", torch.int32, (sequences,))):
+        if t.dtype != dtype or tuple(t.shape) != of or t.device != codes.device or not t.is_contiguous():
+            raise ValueError("%s must be a contiguous tensor of %s on the cache's device, %s" % (what, dtype, " x ".join(map(str, of))))
+    _check(load().apmm_kv_evict(cache, sequences, batch.lengths, batch.page_table, batch.table_stride, batch.table_width, *rows, budget, sinks, recent,
+                                to_table.data_ptr(), to_table.stride(0) if sequences > 1 else to_table.shape[1], to_table.shape[1], to_lengths.data_ptr(), kept.data_ptr(),
+                                to_weights.data_ptr(), _stream()))
+    return kept, to_weights, to_lengths
+
+
+@functools.lru_cache(maxsize=1024, typed=True)
+def apmm_w4_packed_bytes(N, K, group):
+    return int(load().apmm_w4_packed_bytes(N, K, group))
+
+
+def _on_current_device(t, what):
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise ValueError("%s must be on the current CUDA device, whose stream the call goes to" % what)
+
+
+def apmm_w4_pack(codes, scales, group, out=None):
+    """N x K uint8 codes of four bits and their N x ceil(K / group) scales (float16 or bfloat16, the type of the activations) -> packed weights of apmm_w4_gemm (uint8 tensor)."""
+    _dev_u8(codes, "codes")
+    _on_current_device(codes, "codes")
+    N, K = codes.shape
+    if group < 1 or scales.dtype not in _KV_DTYPES or scales.device != codes.device or tuple(scales.shape) != (N, -(-K // group)) or not scales.is_contiguous():
+        raise ValueError("scales must be a contiguous float16 or bfloat16 tensor on the codes' device, N x ceil(K / group)")
+    nbytes = apmm_w4_packed_bytes(N, K, group)
+    if out is None:
+        out = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=codes.device)
+    elif out.nbytes < nbytes or out.device != codes.device or not out.is_contiguous():
+        raise ValueError("packed buffer too small, or not contiguous on the codes' device")
+    _check(load().apmm_w4_pack(codes.data_ptr(), scales.data_ptr(), N, K, group, _KV_DTYPES[scales.dtype], out.data_ptr(), _stream()))
+    return out
+
+
+def apmm_w4_gemm(x, packed, N, group, out=None):
+    """x (M x K, float16 or bfloat16, rows at any distance) times packed weights of N channels: M x N of x's type."""
+    if x.dtype not in _KV_DTYPES or x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
+        raise ValueError("x must be a 2-D float16 or bfloat16 tensor, contiguous in its last dimension")
+    _on_current_device(x, "x")
+    M, K = x.shape
+    if packed.dtype != torch.uint8 or packed.device != x.device or not packed.is_contiguous() or packed.nbytes < apmm_w4_packed_bytes(N, K, group):
+        raise ValueError("packed must be what apmm_w4_pack gave for N channels, x's inputs and the group, on x's device")
+    if out is None:
+        out = torch.empty((M, N), dtype=x.dtype, device=x.device)
+    elif out.dtype != x.dtype or tuple(out.shape) != (M, N) or out.device != x.device or (N > 1 and out.stride(1) != 1):
+        raise ValueError("out must be M x N of x's type on x's device, contiguous in its last dimension")
+    _check(load().apmm_w4_gemm(M, N, K, group, _KV_DTYPES[x.dtype], x.data_ptr(), x.stride(0), packed.data_ptr(), out.data_ptr(), out.stride(0), _stream()))
+    return out
 
 
 def apmm_last_gemm_kernel():

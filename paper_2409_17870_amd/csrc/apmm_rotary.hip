@@ -1,0 +1,173 @@
+// Rotary positions (apmm_rotary.h): rows turned where they lie or into other ones, and queries, keys and values turned and written into the four-bit cache in one launch.
+#include <algorithm>
+
+#include "apmm_kv_store.h"
+#include "apmm_rotary.h"
+
+namespace apmm {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kTurns = 1024;  // cosines and sines that a workgroup holds
+
+// A workgroup has some tokens (those whose cosines and sines it holds) and a share of their heads.  A piece is what one lane reads and writes: both partners of its pairs are its own, so rows may be
+// turned where they lie.
+template <bool BF16, bool EIGHTS>
+__global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryRows a)
+{
+    __shared__ float2 turns[kTurns];
+    const int pairs = a.r.pairs, all = a.heads * a.items;
+    for (int64_t first = (int64_t)blockIdx.x * a.tokens_of_group; first < a.tokens; first += (int64_t)gridDim.x * a.tokens_of_group) {
+        const int tokens = (int)min((int64_t)a.tokens_of_group, a.tokens - first);
+        __syncthreads();
+        for (int i = threadIdx.x; i < tokens * pairs; i += kThreads) {
+            const int token = i / pairs;
+            turns[i] = rotary_turn(a.r, a.r.positions[first + token], i - token * pairs);
+        }
+        __syncthreads();
+        for (int token = 0; token < tokens; ++token) {
+            const uint16_t *x = a.x.data + (first + token) * a.x.token_stride;
+            uint16_t *out = a.out.data + (first + token) * a.out.token_stride;
+            const float2 *t = turns + token * pairs;
+            for (int i = blockIdx.y * kThreads + threadIdx.x; i < all; i += gridDim.y * kThreads) {
+                const int head = kv_divide(i, a.by_items), piece = i - head * a.items;
+                const uint16_t *from = x + head * a.x.head_stride;
+                uint16_t *to = out + head * a.out.head_stride;
+                if (EIGHTS) {
+                    // interleaved: the i-th eight of channels.  Halves: the i-th eight of first ones with that of second ones, behind these the eights that are not turned.
+                    const int of_pairs = a.r.interleaved ? pairs / 4 : pairs / 8;
+                    uint32_t w[4];
+                    if (piece >= of_pairs) {
+                        const int c0 = 2 * pairs + (piece - of_pairs) * 8;
+                        kv_load(from + c0, true, w);
+                        kv_store(to + c0, true, w);
+                    } else if (a.r.interleaved) {
+                        kv_load(from + piece * 8, true, w);
+                        rotary_eight<BF16>(from, true, piece * 8, w, t, pairs, true);
+                        kv_store(to + piece * 8, true, w);
+                    } else {
+                        uint32_t v[4];
+                        kv_load(from + piece * 8, true, w);
+                        kv_load(from + piece * 8 + pairs, true, v);
+    #pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float2 c1 = t[piece * 8 + 2 * j], c2 = t[piece * 8 + 2 * j + 1];
+                            const float a1 = kv_scale_value(w[j] & 0xffffu, BF16), a2 = kv_scale_value(w[j] >> 16, BF16), b1 = kv_scale_value(v[j] & 0xffffu, BF16), b2 = kv_scale_value(v[j] >> 16, BF16);
+                            w[j] = rotary_pair(rotary_one(a1, -b1, c1.x, c1.y), rotary_one(a2, -b2, c2.x, c2.y), BF16);
+                            v[j] = rotary_pair(rotary_one(b1, a1, c1.x, c1.y), rotary_one(b2, a2, c2.x, c2.y), BF16);
+                        }
+                        kv_store(to + piece * 8, true, w);
+                        kv_store(to + piece * 8 + pairs, true, v);
+                    }
+                } else if (piece >= pairs) {
+                    to[pairs + piece] = from[pairs + piece];
+                } else {
+                    const int c1 = a.r.interleaved ? 2 * piece : piece, c2 = a.r.interleaved ? c1 + 1 : piece + pairs;
+                    const float2 cs = t[piece];
+                    const float x1 = kv_scale_value(from[c1], BF16), x2 = kv_scale_value(from[c2], BF16);
+                    to[c1] = kv_round(rotary_one(x1, -x2, cs.x, cs.y), BF16);
+                    to[c2] = kv_round(rotary_one(x2, x1, cs.x, cs.y), BF16);
+                }
+            }
+        }
+    }
+}
+
+constexpr int kWaves = 4;
+
+// A workgroup has the up to eight tokens of an aligned eight of positions, as kv_write_kernel's waves have, and `per_wave` heads to each wave: those of keys and values first, then those of queries.
+// It makes the eight's cosines and sines once.
+template <int D, bool BF16>
+__global__ __launch_bounds__(64 * kWaves) void kv_rotary_write_kernel(KvRotaryArgs a)
+{
+    constexpr int N = D / 16;
+    __shared__ __align__(16) kv_u16 turn[kWaves][D / 4 * 8];
+    __shared__ float2 turns[8][D / 2];
+    const int eight = kv_divide(blockIdx.x, a.by_blocks), block = blockIdx.x - eight * a.blocks, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Eight e;
+    if (!find_eight(a.c, eight, e)) return;  // (all waves of the workgroup alike)
+    const int lane = kv_lane(), token = lane >> 3, part = lane & 7, pairs = a.r.pairs;
+    for (int i = threadIdx.x; i < 8 * pairs; i += 64 * kWaves) {
+        const int t = i / pairs, place = e.first + t;
+        if (place < e.s.first || place >= e.s.first + e.s.n) continue;
+        turns[t][i - t * pairs] = rotary_turn(a.r, a.r.positions ? a.r.positions[e.s.start + place - e.s.first] : place, i - t * pairs);
+    }
+    __syncthreads();
+    const int64_t row = e.s.start + (e.is_new ? e.first + token - e.s.first : 0);  // (a lane without one reads the first)
+    auto turned = [&](const uint16_t *from, bool aligned, uint32_t (&x)[N]) {
+        load_row(from, aligned, part, x);
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) {
+            uint32_t w[4] = {x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
+            rotary_eight<BF16>(from, aligned, 64 * i + 8 * part, w, turns[token], pairs, a.r.interleaved);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[4 * i + j] = w[j];
+        }
+    };
+    const int all = a.c.heads + a.q_heads;
+    for (int i = 0; i < a.per_wave; ++i) {
+        const int head = (block * a.per_wave + i) * kWaves + wave;
+        if (head >= all) break;
+        uint32_t x[N];
+        if (head >= a.c.heads) {
+            const int h = head - a.c.heads;
+            turned(a.q.data + row * a.q.token_stride + h * a.q.head_stride, a.q.aligned, x);
+            if (e.is_new) store_row(a.q_out.data + row * a.q_out.token_stride + h * a.q_out.head_stride, a.q_out.aligned, part, x);
+        } else if (e.page >= 0) {
+            uint32_t y[N], uk[N / 4], uv[N / 4];
+            turned(a.k.data + row * a.k.token_stride + head * a.k.head_stride, a.k.aligned, x);
+            load_row(a.v.data + row * a.v.token_stride + head * a.v.head_stride, a.v.aligned, part, y);
+            const uint32_t sk = quantise<N, BF16>(x, uk), sv = quantise<N, BF16>(y, uv);
+            write_codes<D>(a.c, e, head, uk, sk, uv, sv, turn[wave]);
+        }
+    }
+}
+
+int heads_of_a_wave(const KvArgs &c, int q_heads)
+{
+    return kv_eights(c) * (c.heads + q_heads) >= 16384 ? 4 : 1;
+}
+int blocks_of_an_eight(const KvArgs &c, int q_heads)
+{
+    const int of_block = kWaves * heads_of_a_wave(c, q_heads);
+    return (c.heads + q_heads + of_block - 1) / of_block;
+}
+
+}  // namespace
+
+hipError_t launch_rotary(const RotaryRows &in, hipStream_t stream)
+{
+    RotaryRows a = in;
+    const int pairs = a.r.pairs, rest = a.head_dim - 2 * pairs;
+    const bool copies = a.x.data != a.out.data;  // else what is not turned stays as it is
+    a.eights = a.x.aligned && a.out.aligned && pairs % (a.r.interleaved ? 4 : 8) == 0 && rest % 8 == 0;
+    a.items = a.eights ? pairs / (a.r.interleaved ? 4 : 8) + (copies ? rest / 8 : 0) : pairs + (copies ? rest : 0);
+    a.by_items = kv_divisor(a.items);
+    const int64_t pieces = (int64_t)a.heads * a.items;
+    // as many tokens to a workgroup as give its lanes a cosine and sine each, where there are workgroups enough without
+    const int most = std::max(1, kThreads / pairs);
+    a.tokens_of_group = (int)std::max<int64_t>(1, std::min<int64_t>(most, a.tokens / 1024));
+    const int64_t groups = std::min<int64_t>((a.tokens + a.tokens_of_group - 1) / a.tokens_of_group, 1 << 20);
+    const int64_t shares = std::max<int64_t>(1, std::min<int64_t>((pieces + kThreads - 1) / kThreads, 2048 / groups));
+    const dim3 grid((uint32_t)groups, (uint32_t)shares), block(kThreads);
+    if (a.bf16) a.eights ? rotary_kernel<true, true><<<grid, block, 0, stream>>>(a) : rotary_kernel<true, false><<<grid, block, 0, stream>>>(a);
+    else a.eights ? rotary_kernel<false, true><<<grid, block, 0, stream>>>(a) : rotary_kernel<false, false><<<grid, block, 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+int64_t kv_rotary_items(const KvArgs &c, int q_heads) { return kv_eights(c) * blocks_of_an_eight(c, q_heads) * 64 * kWaves; }
+
+hipError_t launch_kv_write_rotary(const KvRotaryArgs &in, hipStream_t stream)
+{
+    KvRotaryArgs a = in;
+    a.per_wave = heads_of_a_wave(a.c, a.q_heads);
+    a.blocks = blocks_of_an_eight(a.c, a.q_heads);
+    a.by_blocks = kv_divisor(a.blocks);
+    const dim3 grid((uint32_t)(kv_eights(a.c) * a.blocks)), block(64 * kWaves);
+    if (a.c.head_dim == 128) a.c.bf16 ? kv_rotary_write_kernel<128, true><<<grid, block, 0, stream>>>(a) : kv_rotary_write_kernel<128, false><<<grid, block, 0, stream>>>(a);
+    else a.c.bf16 ? kv_rotary_write_kernel<64, true><<<grid, block, 0, stream>>>(a) : kv_rotary_write_kernel<64, false><<<grid, block, 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace apmm
