@@ -338,10 +338,13 @@ apmm_status apmm_kv_evict(const apmm_kv_cache *cache, int sequences, const int32
  *   dtype     apmm_dtype of x, y and the scales; the packed form is made for one of them
  *   codes     device, N x K uint8, row-major, the low four bits count;  scales  device, N x ceil(K / group)
  *   packed    device, apmm_w4_packed_bytes(N, K, group) bytes, 16-byte aligned, opaque, of this version of the library
- *   x, y      device, M x K and M x N, rows x_stride and y_stride elements apart, at any address of their type's alignment; M up to 2^20, N and K up to 2^24 */
+ *   x, y      device, M x K and M x N, rows x_stride and y_stride elements apart, at any address of their type's alignment; M up to 2^20, N and K up to 2^24
+ *   workspace device, 16-byte aligned, apmm_w4_workspace_bytes() bytes of the same sizes (0, then it may be NULL, for many of them); calls that may overlap need one each */
 size_t apmm_w4_packed_bytes(int64_t N, int64_t K, int group);
 apmm_status apmm_w4_pack(const uint8_t *codes, const void *scales, int64_t N, int64_t K, int group, int dtype, void *packed, void *stream);
-apmm_status apmm_w4_gemm(int64_t M, int64_t N, int64_t K, int group, int dtype, const void *x, int64_t x_stride, const void *packed, void *y, int64_t y_stride, void *stream);
+size_t apmm_w4_workspace_bytes(int64_t M, int64_t N, int64_t K, int group);
+apmm_status apmm_w4_gemm(int64_t M, int64_t N, int64_t K, int group, int dtype, const void *x, int64_t x_stride, const void *packed, void *y, int64_t y_stride,
+                         void *workspace, size_t workspace_bytes, void *stream);
 
 /* Measurement aid.  The next apmm_gemm / apmm_gemm_ex / apmm_gemm_from_codes call of the calling thread, if it
  * runs the large-tile MFMA kernel or a small-M kernel in one launch, attaches the two hipEvent_t (created by the

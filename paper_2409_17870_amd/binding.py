@@ -22,7 +22,7 @@ EXPORTS = [
     "apmm_packed_bytes", "apmm_packed_activation_bytes", "apmm_workspace_bytes", "apmm_pack_weights", "apmm_pack_activations",
     "apmm_quantize_pack_activations", "apmm_unpack", "apmm_unpack_activations", "apmm_gemm", "apmm_gemm_ex", "apmm_gemm_from_codes", "apmm_gemm_from_codes_noalloc", "apmm_gemm_grouped",
     "apmm_kv_write", "apmm_kv_read", "apmm_kv_attention", "apmm_kv_attention_workspace_bytes",
-    "apmm_rotary", "apmm_kv_write_rotary", "apmm_kv_weights", "apmm_kv_weights_workspace_bytes", "apmm_kv_evict", "apmm_w4_packed_bytes", "apmm_w4_pack", "apmm_w4_gemm",
+    "apmm_rotary", "apmm_kv_write_rotary", "apmm_kv_weights", "apmm_kv_weights_workspace_bytes", "apmm_kv_evict", "apmm_w4_packed_bytes", "apmm_w4_workspace_bytes", "apmm_w4_pack", "apmm_w4_gemm",
     "apmm_time_next_gemm", "apmm_last_gemm_kernel", "apmm_status_string", "apmm_last_error", "apmm_version",
 ]
 
@@ -132,7 +132,9 @@ def load():
     lib.apmm_w4_pack.restype = ci
     lib.apmm_w4_pack.argtypes = [vp, vp, i64, i64, ci, ci, vp, vp]
     lib.apmm_w4_gemm.restype = ci
-    lib.apmm_w4_gemm.argtypes = [i64, i64, i64, ci, ci, vp, i64, vp, vp, i64, vp]
+    lib.apmm_w4_gemm.argtypes = [i64, i64, i64, ci, ci, vp, i64, vp, vp, i64, vp, ctypes.c_size_t, vp]
+    lib.apmm_w4_workspace_bytes.restype = ctypes.c_size_t
+    lib.apmm_w4_workspace_bytes.argtypes = [i64, i64, i64, ci]
     lib.apmm_time_next_gemm.restype = ci
     lib.apmm_time_next_gemm.argtypes = [vp, vp]
     lib.apmm_last_gemm_kernel.restype = ctypes.c_char_p
@@ -572,8 +574,16 @@ def apmm_w4_pack(codes, scales, group, out=None):
     return out
 
 
-def apmm_w4_gemm(x, packed, N, group, out=None):
-    """x (M x K, float16 or bfloat16, rows at any distance) times packed weights of N channels: M x N of x's type."""
+@functools.lru_cache(maxsize=1024, typed=True)
+def apmm_w4_workspace_bytes(M, N, K, group):
+    return int(load().apmm_w4_workspace_bytes(M, N, K, group))
+
+
+def apmm_w4_gemm(x, packed, N, group, out=None, workspace=None):
+    """x (M x K, float16 or bfloat16, rows at any distance) times packed weights of N channels: M x N of x's type.
+
+    workspace: uint8 tensor of apmm_w4_workspace_bytes(M, N, K, group) bytes; allocated if None.
+    """
     if x.dtype not in _KV_DTYPES or x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
         raise ValueError("x must be a 2-D float16 or bfloat16 tensor, contiguous in its last dimension")
     _on_current_device(x, "x")
@@ -584,7 +594,13 @@ def apmm_w4_gemm(x, packed, N, group, out=None):
         out = torch.empty((M, N), dtype=x.dtype, device=x.device)
     elif out.dtype != x.dtype or tuple(out.shape) != (M, N) or out.device != x.device or (N > 1 and out.stride(1) != 1):
         raise ValueError("out must be M x N of x's type on x's device, contiguous in its last dimension")
-    _check(load().apmm_w4_gemm(M, N, K, group, _KV_DTYPES[x.dtype], x.data_ptr(), x.stride(0), packed.data_ptr(), out.data_ptr(), out.stride(0), _stream()))
+    if workspace is None:
+        need = apmm_w4_workspace_bytes(M, N, K, group)
+        workspace = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
+    elif workspace.device != x.device or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on x's device")
+    _check(load().apmm_w4_gemm(M, N, K, group, _KV_DTYPES[x.dtype], x.data_ptr(), x.stride(0), packed.data_ptr(), out.data_ptr(), out.stride(0),
+                               _ptr(workspace), 0 if workspace is None else workspace.nbytes, _stream()))
     return out
 
 

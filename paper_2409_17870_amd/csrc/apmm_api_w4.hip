@@ -44,7 +44,14 @@ apmm_status apmm_w4_pack(const uint8_t *codes, const void *scales, int64_t N, in
     return e == hipSuccess ? APMM_OK : fail_hip(e, "apmm_w4_pack");
 }
 
-apmm_status apmm_w4_gemm(int64_t M, int64_t N, int64_t K, int group, int dtype, const void *x, int64_t x_stride, const void *packed, void *y, int64_t y_stride, void *stream)
+size_t apmm_w4_workspace_bytes(int64_t M, int64_t N, int64_t K, int group)
+{
+    if (check_sizes(N, K, group) != APMM_OK || M < 1 || N == 0 || M > apmm::kW4MostRows) return 0;
+    return (size_t)apmm::w4_partial_bytes(M, N, apmm::w4_rule(M, N, apmm::W4Shape{N, K, group}.blocks()));
+}
+
+apmm_status apmm_w4_gemm(int64_t M, int64_t N, int64_t K, int group, int dtype, const void *x, int64_t x_stride, const void *packed, void *y, int64_t y_stride,
+                         void *workspace, size_t workspace_bytes, void *stream)
 {
     const apmm_status st = check_sizes(N, K, group);
     if (st != APMM_OK) return st;
@@ -55,19 +62,24 @@ apmm_status apmm_w4_gemm(int64_t M, int64_t N, int64_t K, int group, int dtype, 
     if (!aligned(x, 2) || !aligned(y, 2) || !aligned(packed, 16)) return fail(APMM_ERR_INVALID_ARG, "w4: x and y must be 2-byte, packed weights 16-byte aligned");
     if (M > 1 && (x_stride < 0 || y_stride < N)) return fail(APMM_ERR_INVALID_ARG, "w4: x_stride < 0, or rows of y that overlap");
     const apmm::W4Shape s = {N, K, group};
+    const apmm::W4Rule r = apmm::w4_rule(M, N, s.blocks());
+    if (apmm::w4_items(M, N, r) >= ((int64_t)1 << 32)) return fail(APMM_ERR_UNSUPPORTED, "w4: M * N is more than one launch takes");
+    const size_t need = (size_t)apmm::w4_partial_bytes(M, N, r);
+    if (need && (!workspace || workspace_bytes < need)) return fail(APMM_ERR_WORKSPACE, "w4: needs a workspace of apmm_w4_workspace_bytes() bytes");
+    if (need && !aligned(workspace, 16)) return fail(APMM_ERR_INVALID_ARG, "w4: workspace must be 16-byte aligned");
     apmm::W4Args a;
     a.x = static_cast<const uint16_t *>(x);
     a.packed = static_cast<const uint8_t *>(packed);
     a.y = static_cast<uint16_t *>(y);
-    a.x_stride = x_stride;
-    a.y_stride = y_stride;
+    a.partial = static_cast<float *>(workspace);
+    a.x_stride = M > 1 ? x_stride : 0;
+    a.y_stride = M > 1 ? y_stride : 0;
     a.code_bytes = s.code_bytes();
     a.M = (int)M;
     a.N = (int)N;
     a.K = (int)K;
     a.blocks = (int)s.blocks();
-    if (apmm::w4_items(a) >= ((int64_t)1 << 32)) return fail(APMM_ERR_UNSUPPORTED, "w4: M * N is more than one launch takes");
-    const hipError_t e = apmm::launch_w4_gemm(a, group, dtype == APMM_BF16, static_cast<hipStream_t>(stream));
+    const hipError_t e = apmm::launch_w4_gemm(a, r, group, dtype == APMM_BF16, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? APMM_OK : fail_hip(e, "apmm_w4_gemm");
 }
 

@@ -31,14 +31,27 @@ struct W4Args {
     const uint16_t *x;
     const uint8_t *packed;
     uint16_t *y;
+    float *partial;
     int64_t x_stride, y_stride;  // elements between rows
     int64_t code_bytes;          // where the scales begin
     int M, N, K, blocks;
 };
 
 hipError_t launch_w4_pack(const uint8_t *codes, const uint16_t *scales, const W4Shape &s, bool bf16, uint8_t *packed, hipStream_t stream);
-int64_t w4_items(const W4Args &a);  // of the largest launch
-hipError_t launch_w4_gemm(const W4Args &a, int group, bool bf16, hipStream_t stream);
+
+// Which kernel a call takes, by its sizes
+struct W4Rule {
+    bool tiles;     // w4_tiles_kernel: blocks of 32 tokens, shares of the inputs; else w4_rows_kernel: tiles of 16 channels, waves
+    int t, shares;
+    int c, waves;
+};
+W4Rule w4_rule(int64_t M, int64_t N, int64_t blocks);
+int64_t w4_items(int64_t M, int64_t N, const W4Rule &r);  // of the largest launch
+// Of the workspace that the inputs' shares take
+__host__ __device__ inline int64_t w4_partial_stride(int64_t N) { return (N + 3) / 4 * 4; }
+inline int64_t w4_partial_bytes(int64_t M, int64_t N, const W4Rule &r) { return r.shares > 1 ? r.shares * M * w4_partial_stride(N) * 4 : 0; }
+hipError_t launch_w4_gemm(const W4Args &a, const W4Rule &r, int group, bool bf16, hipStream_t stream);
+hipError_t launch_w4_tiles(const W4Args &a, const W4Rule &r, int group, bool bf16, hipStream_t stream);
 
 #ifdef __HIPCC__
 // Word of eight codes.
@@ -93,6 +106,23 @@ __device__ __forceinline__ typename W4Type<BF16>::Eight w4_operand(uint32_t w)
         }
     }
     return __builtin_bit_cast(typename W4Type<BF16>::Eight, make_uint4(r[0], r[1], r[2], r[3]));
+}
+
+// Eight numbers of a row at any address, zeros behind K
+template <class Eight>
+__device__ __forceinline__ Eight w4_row_eight(const uint16_t *row, int k, int K)
+{
+    uint4 w = make_uint4(0, 0, 0, 0);
+    if (k + 8 <= K) {
+        __builtin_memcpy(&w, row + k, 16);
+    } else if (k < K) {
+        uint32_t p[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (k + i < K) p[i / 2] |= (uint32_t)row[k + i] << (16 * (i & 1));
+        w = make_uint4(p[0], p[1], p[2], p[3]);
+    }
+    return __builtin_bit_cast(Eight, w);
 }
 
 template <bool BF16>

@@ -1,6 +1,7 @@
-// Four-bit weights with group scales times 16-bit activations (apmm_w4.h): packing, and the kernels for few and for many tokens.
+// Four-bit weights with group scales times 16-bit activations (apmm_w4.h): packing, the kernel for up to sixteen tokens, and which kernel a call takes.
 //
 // The codes' odd integers are exact in both types and so are their products with the activations in 32 bits; a group's sum is multiplied with its scale in 32 bits, results are rounded once.
+#include <algorithm>
 #include <type_traits>
 
 #include "apmm_w4.h"
@@ -34,23 +35,6 @@ __global__ __launch_bounds__(256) void w4_pack_kernel(const uint8_t *codes, cons
     }
 }
 
-// Eight numbers of a row at any address, zeros behind K
-template <class Eight>
-__device__ __forceinline__ Eight row_eight(const uint16_t *row, int k, int K)
-{
-    uint4 w = make_uint4(0, 0, 0, 0);
-    if (k + 8 <= K) {
-        __builtin_memcpy(&w, row + k, 16);
-    } else if (k < K) {
-        uint32_t p[4] = {0, 0, 0, 0};
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (k + i < K) p[i / 2] |= (uint32_t)row[k + i] << (16 * (i & 1));
-        w = make_uint4(p[0], p[1], p[2], p[3]);
-    }
-    return __builtin_bit_cast(Eight, w);
-}
-
 template <bool BF16>
 __device__ __forceinline__ float4v multiply(typename W4Type<BF16>::Eight a, typename W4Type<BF16>::Eight b, float4v c)
 {
@@ -58,70 +42,122 @@ __device__ __forceinline__ float4v multiply(typename W4Type<BF16>::Eight a, type
     else return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
-// Few tokens: a workgroup has a tile of 16 channels and 16 T tokens, its waves take blocks of 128 inputs in turn and meet in LDS.
-template <bool BF16, int GROUP, int T, int WAVES>
+// Few tokens.  A workgroup has 16 C channels and 16 T tokens, its waves take blocks of 128 inputs in turn, the next block's weights and activations on their way while one is multiplied, and meet in LDS.
+// Activations come from the caches into each wave's registers: they are no two waves' of a workgroup.  Bound by HBM and the way there: one token of 11008 x 4096 24 MB in 9 us, of 4096 x 4096 in 4.4 to 6.4 as
+// called; at sixteen tokens by the activations, which every workgroup reads (12.4 us).
+template <bool BF16, int GROUP, int T, int C>
+struct Block {
+    typedef typename W4Type<BF16>::Eight Eight;
+    uint4 w[C];
+    uint16_t s[C][kW4Block / GROUP];
+    Eight x[T][4];
+};
+
+template <bool BF16, int GROUP, int T, int C, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void w4_rows_kernel(W4Args a)
 {
     typedef typename W4Type<BF16>::Eight Eight;
+    typedef Block<BF16, GROUP, T, C> Block;
     constexpr int kGroups = kW4Block / GROUP, kSteps = GROUP / 32;  // groups of a block, matrix instructions of a group
-    __shared__ float4v sums[WAVES][T][64];
+    __shared__ float sums[WAVES][T * C][256];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-    const int tile = blockIdx.x, row0 = blockIdx.y * 16 * T;
-    const uint8_t *codes = a.packed + (int64_t)tile * a.blocks * kW4BlockBytes + lane * 16;
-    const uint16_t *scales = reinterpret_cast<const uint16_t *>(a.packed + a.code_bytes) + (int64_t)tile * a.blocks * kGroups * kW4Tile + n;
+    const int tiles = (a.N + kW4Tile - 1) / kW4Tile, tile0 = blockIdx.x * C, row0 = blockIdx.y * 16 * T;
+    const uint8_t *codes[C];
+    const uint16_t *scales[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int64_t tile = min(tile0 + c, tiles - 1);
+        codes[c] = a.packed + tile * a.blocks * kW4BlockBytes + lane * 16;
+        scales[c] = reinterpret_cast<const uint16_t *>(a.packed + a.code_bytes) + tile * a.blocks * kGroups * kW4Tile + n;
+    }
     const uint16_t *rows[T];
+    bool there[T];
 #pragma unroll
-    for (int t = 0; t < T; ++t) rows[t] = a.x + min(row0 + 16 * t + n, a.M - 1) * a.x_stride;  // (a row that there is not has results that are not written)
+    for (int t = 0; t < T; ++t) {
+        there[t] = row0 + 16 * t + n < a.M;
+        rows[t] = a.x + (there[t] ? row0 + 16 * t + n : 0) * a.x_stride + 8 * g;
+    }
+    auto load = [&](int b, Block &to) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) to.w[c] = *reinterpret_cast<const uint4 *>(codes[c] + (int64_t)b * kW4BlockBytes);
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < kGroups; ++i) to.s[c][i] = scales[c][((int64_t)b * kGroups + i) * kW4Tile];
+        const int K = (b + 1) * kW4Block <= a.K ? INT32_MAX : a.K - 8 * g;  // (the last block's may end in it)
+#pragma unroll
+        for (int t = 0; t < T; ++t)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                to.x[t][j] = __builtin_bit_cast(Eight, make_uint4(0, 0, 0, 0));
+                if (there[t]) to.x[t][j] = w4_row_eight<Eight>(rows[t], b * kW4Block + 32 * j, K);
+            }
+    };
 
-    float4v acc[T];
+    float4v acc[T][C];
 #pragma unroll
-    for (int t = 0; t < T; ++t) acc[t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int b = wave; b < a.blocks; b += WAVES) {
-        const uint4 w = *reinterpret_cast<const uint4 *>(codes + (int64_t)b * kW4BlockBytes);
-        const uint32_t words[4] = {w.x, w.y, w.z, w.w};
-        uint16_t s[kGroups];
+    for (int t = 0; t < T; ++t)
 #pragma unroll
-        for (int i = 0; i < kGroups; ++i) s[i] = scales[((int64_t)b * kGroups + i) * kW4Tile];
+        for (int c = 0; c < C; ++c) acc[t][c] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+    auto add = [&](const Block &x) {
 #pragma unroll
         for (int i = 0; i < kGroups; ++i) {
-            float4v part[T];
 #pragma unroll
-            for (int t = 0; t < T; ++t) part[t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int c = 0; c < C; ++c) {
+                const uint32_t words[4] = {x.w[c].x, x.w[c].y, x.w[c].z, x.w[c].w};
+                float4v part[T];
 #pragma unroll
-            for (int j = i * kSteps; j < (i + 1) * kSteps; ++j) {
-                const Eight c = w4_operand<BF16>(words[j]);
+                for (int t = 0; t < T; ++t) part[t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int t = 0; t < T; ++t) part[t] = multiply<BF16>(row_eight<Eight>(rows[t], b * kW4Block + 32 * j + 8 * g, a.K), c, part[t]);
+                for (int j = i * kSteps; j < (i + 1) * kSteps; ++j) {
+                    const Eight w = w4_operand<BF16>(words[j]);
+#pragma unroll
+                    for (int t = 0; t < T; ++t) part[t] = multiply<BF16>(x.x[t][j], w, part[t]);
+                }
+                const float by = w4_scale<BF16>(x.s[c][i]);
+#pragma unroll
+                for (int t = 0; t < T; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[t][c][r] = fmaf(part[t][r], by, acc[t][c][r]);
             }
-            const float by = w4_scale<BF16>(s[i]);
-#pragma unroll
-            for (int t = 0; t < T; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) acc[t][r] = fmaf(part[t][r], by, acc[t][r]);
         }
+    };
+    Block one, other;
+    int b = wave;
+    if (b < a.blocks) load(b, one);
+    while (b < a.blocks) {
+        if (b + WAVES < a.blocks) load(b + WAVES, other);
+        add(one);
+        b += WAVES;
+        if (b >= a.blocks) break;
+        if (b + WAVES < a.blocks) load(b + WAVES, one);
+        add(other);
+        b += WAVES;
     }
 #pragma unroll
-    for (int t = 0; t < T; ++t) sums[wave][t][lane] = acc[t];
+    for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int c = 0; c < C; ++c) *reinterpret_cast<float4v *>(&sums[wave][t * C + c][4 * lane]) = acc[t][c];
     __syncthreads();
-    for (int t = wave; t < T; t += WAVES) {
-        float4v all = sums[0][t][lane];
+    const int left = min(a.M - row0, 16 * T);
+    for (int i = threadIdx.x; i < left * 16 * C; i += 64 * WAVES) {
+        const int row = i / (16 * C), c = i % (16 * C) / 16, column = i % 16, channel = (tile0 + c) * kW4Tile + column;
+        const int at = (row % 16 / 4 * 16 + column) * 4 + row % 4;
+        float all = 0.0f;
 #pragma unroll
-        for (int i = 1; i < WAVES; ++i) all += sums[i][t][lane];
-        const int channel = tile * kW4Tile + n;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int row = row0 + 16 * t + 4 * g + r;
-            if (row < a.M && channel < a.N) a.y[row * a.y_stride + channel] = w4_round<BF16>(all[r]);
-        }
+        for (int w = 0; w < WAVES; ++w) all += sums[w][row / 16 * C + c][at];
+        if (channel < a.N) a.y[(row0 + row) * a.y_stride + channel] = w4_round<BF16>(all);
     }
 }
 
 template <bool BF16, int GROUP>
-void launch(const W4Args &a, hipStream_t stream)
+void launch(const W4Args &a, const W4Rule &r, hipStream_t stream)
 {
-    const uint32_t tiles = (uint32_t)((a.N + kW4Tile - 1) / kW4Tile);
-    if (a.M <= 16) w4_rows_kernel<BF16, GROUP, 1, 8><<<dim3(tiles), dim3(512), 0, stream>>>(a);
-    else w4_rows_kernel<BF16, GROUP, 4, 4><<<dim3(tiles, (uint32_t)((a.M + 63) / 64)), dim3(256), 0, stream>>>(a);
+    const dim3 grid((uint32_t)((a.N + kW4Tile * r.c - 1) / (kW4Tile * r.c)), (uint32_t)((a.M + 16 * r.t - 1) / (16 * r.t)));
+    if (r.c == 2 && r.waves == 16) w4_rows_kernel<BF16, GROUP, 1, 2, 16><<<grid, dim3(1024), 0, stream>>>(a);
+    else if (r.c == 2) w4_rows_kernel<BF16, GROUP, 1, 2, 8><<<grid, dim3(512), 0, stream>>>(a);
+    else if (r.waves == 16) w4_rows_kernel<BF16, GROUP, 1, 1, 16><<<grid, dim3(1024), 0, stream>>>(a);
+    else w4_rows_kernel<BF16, GROUP, 1, 1, 8><<<grid, dim3(512), 0, stream>>>(a);
 }
 
 }  // namespace
@@ -136,15 +172,55 @@ hipError_t launch_w4_pack(const uint8_t *codes, const uint16_t *scales, const W4
     return hipGetLastError();
 }
 
-int64_t w4_items(const W4Args &a) { return (int64_t)((a.N + kW4Tile - 1) / kW4Tile) * (a.M <= 16 ? 512 : (a.M + 63) / 64 * 256); }
-
-hipError_t launch_w4_gemm(const W4Args &a, int group, bool bf16, hipStream_t stream)
+// Up to sixteen tokens: w4_rows_kernel.  Two tiles of channels to a workgroup where there are more tiles than compute units (320 tiles, 13800 inputs: a token 16.8 us with one, 15.5 with two, sixteen tokens
+// 30.5 and 19.7), else one, with sixteen waves where each then has four blocks and more (256 tiles of 11008 inputs 10.0 and 8.4 us, of 4096 inputs 6.6 both).
+//
+// More: w4_tiles_kernel, with the tokens and shares that promise the least time.  A workgroup takes 0.45 + 0.2 T us a block where it is alone on its compute unit and 0.3 + 0.17 T for each on it where there
+// are more, its launch and the way to the first block are the same for all; shares cost a launch of 3.5 us and their sums' way out and in.  (77 x 5119 x 13800 in shares of 4: 39 us, 8: 34, 12: 30; 128 x 4096 x
+// 4096 whole 46 us, in shares of 4 23, 8 23, 12 25; 512 x 4096 x 11008 whole 127, in 2 73, 4 63, 8 75; 1024 x 11008 x 4096 whole 114, in 2 138.)
+W4Rule w4_rule(int64_t M, int64_t N, int64_t blocks)
 {
+    W4Rule r = {false, 1, 1, 1, 8};
+    const int64_t tiles = (N + kW4Tile - 1) / kW4Tile;
+    if (M <= 16) {
+        r.c = tiles > 256 ? 2 : 1;
+        r.waves = blocks >= 64 ? 16 : 8;
+        return r;
+    }
+    r.tiles = true;
+    float least = 0.0f;
+    for (int t = 1; t <= 4; ++t) {
+        if (t < 4 && M > 96 * t) continue;  // (small tiles for many tokens)
+        const int64_t groups = (M + 32 * t - 1) / (32 * t) * ((N + 127) / 128);
+        for (int shares = 1; shares <= 16 && (shares == 1 || shares * 2 <= blocks); ++shares) {
+            const int64_t on_unit = (groups * shares + 255) / 256;
+            const float block = std::max(0.45f + 0.2f * t, (0.3f + 0.17f * t) * (float)on_unit);
+            const float us = (float)((blocks + shares - 1) / shares) * block + (shares > 1 ? 3.5f + (float)(shares * M * N) * 2e-6f : 0.0f);
+            if (least == 0.0f || us < least) {
+                least = us;
+                r.t = t;
+                r.shares = shares;
+            }
+        }
+    }
+    return r;
+}
+
+int64_t w4_items(int64_t M, int64_t N, const W4Rule &r)
+{
+    if (!r.tiles) return (N + kW4Tile * r.c - 1) / (kW4Tile * r.c) * 64 * r.waves;
+    const int64_t first = (M + 32 * r.t - 1) / (32 * r.t) * ((N + 127) / 128) * r.shares * 256;
+    return r.shares > 1 ? std::max(first, M * w4_partial_stride(N) / 4 + 256) : first;
+}
+
+hipError_t launch_w4_gemm(const W4Args &a, const W4Rule &r, int group, bool bf16, hipStream_t stream)
+{
+    if (r.tiles) return launch_w4_tiles(a, r, group, bf16, stream);
     auto go = [&](auto b) {
         constexpr bool B = decltype(b)::value;
-        if (group == 32) launch<B, 32>(a, stream);
-        else if (group == 64) launch<B, 64>(a, stream);
-        else launch<B, 128>(a, stream);
+        if (group == 32) launch<B, 32>(a, r, stream);
+        else if (group == 64) launch<B, 64>(a, r, stream);
+        else launch<B, 128>(a, r, stream);
     };
     if (bf16) go(std::true_type());
     else go(std::false_type());

@@ -99,8 +99,8 @@ def test_w4(lib):  # noqa: F811
     def pack(codes=0x1000, scales=0x2000, N=16, K=128, group=64, dtype=0, packed=0x3000):
         return lib.apmm_w4_pack(codes, scales, N, K, group, dtype, packed, None)
 
-    def gemm(M=4, N=16, K=128, group=64, dtype=0, x=0x1000, x_stride=128, packed=0x3000, y=0x4000, y_stride=16):
-        return lib.apmm_w4_gemm(M, N, K, group, dtype, x, x_stride, packed, y, y_stride, None)
+    def gemm(M=4, N=16, K=128, group=64, dtype=0, x=0x1000, x_stride=128, packed=0x3000, y=0x4000, y_stride=16, workspace=None, size=0):
+        return lib.apmm_w4_gemm(M, N, K, group, dtype, x, x_stride, packed, y, y_stride, workspace, size, None)
     assert pack(N=0) == OK and gemm(M=0) == OK and gemm(N=0, y=None) == OK
     for status, change in [(INVALID, dict(N=-1)), (INVALID, dict(K=0)), (INVALID, dict(group=0)), (UNSUPPORTED, dict(group=16)), (UNSUPPORTED, dict(group=256)), (UNSUPPORTED, dict(N=(1 << 24) + 1)),
                            (UNSUPPORTED, dict(K=(1 << 24) + 1)), (INVALID, dict(dtype=2)), (INVALID, dict(packed=None)), (INVALID, dict(packed=0x3008))]:
@@ -109,6 +109,21 @@ def test_w4(lib):  # noqa: F811
     for status, change in [(INVALID, dict(M=-1)), (UNSUPPORTED, dict(M=(1 << 20) + 1)), (INVALID, dict(x=None)), (INVALID, dict(x=0x1001)), (INVALID, dict(y=None)), (INVALID, dict(y=0x4001)),
                            (INVALID, dict(y_stride=15)), (INVALID, dict(x_stride=-1)), (UNSUPPORTED, dict(M=1 << 20, N=1 << 24, y_stride=1 << 24))]:
         assert gemm(**change) == status, change
+
+
+def test_w4_workspace(lib):  # noqa: F811
+    need = lib.apmm_w4_workspace_bytes
+    assert need(0, 4096, 4096, 64) == need(16, 4096, 4096, 64) == need(4, 0, 4096, 64) == need(64, 4096, 4096, 48) == need(64, 4096, 64, 64) == 0
+    size = need(64, 4096, 4096, 64)
+    assert size > 0 and size % (64 * 4096 * 4) == 0
+
+    def gemm(workspace, size):
+        return lib.apmm_w4_gemm(64, 4096, 4096, 64, 0, 0x1000, 4096, 0x3000, 0x4000, 4096, workspace, size, None)
+    assert gemm(None, 0) == gemm(None, size) == gemm(0x8000, size - 1) == WORKSPACE and gemm(0x8008, size) == INVALID
+    for M in (17, 100, 1000, 100000, 1 << 20):                         # of a few times the result, whatever the sizes
+        for N in (1, 1000, 100000):
+            for K in (1, 1000, 100000):
+                assert need(M, N, K, 32) <= max(64 * M * (N + 3), 0) and need(M, N, K, 32) <= 512 << 20
 
 
 def test_structure(lib):  # noqa: F811

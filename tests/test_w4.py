@@ -138,6 +138,26 @@ def test_graph_streams_and_equal_results(gpu):
             assert torch.equal(out, binding.apmm_w4_gemm(x, packed, N, group))
 
 
+def test_workspace(gpu):
+    """Shares of the inputs meet in it: of any contents, reused by calls one after the other, as much as the call asks for."""
+    torch, binding = gpu
+    N, K, group = 520, 4100, 128
+    codes, scales = weights(torch, N, K, group, torch.float16, 11)
+    packed = binding.apmm_w4_pack(codes.cuda(), scales.cuda(), group)
+    for M in (17, 40, 77, 128, 161):
+        need = binding.apmm_w4_workspace_bytes(M, N, K, group)
+        assert need > 0
+        workspace = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+        x = torch.randn((M, K), generator=torch.Generator().manual_seed(M)).half()
+        y = binding.apmm_w4_gemm(x.cuda(), packed, N, group, workspace=workspace)
+        close(torch, y, *exact(x, codes, scales, group))
+        assert torch.equal(y, binding.apmm_w4_gemm(x.cuda(), packed, N, group, workspace=workspace))
+        with pytest.raises(binding.ApmmError):
+            binding.apmm_w4_gemm(x.cuda(), packed, N, group, workspace=workspace[:-1])
+    with pytest.raises(ValueError):
+        binding.apmm_w4_gemm(x.cuda(), packed, N, group, workspace=workspace.cpu())
+
+
 def test_wide_calls(gpu):
     """More channels than one dimension of a launch would have as tiles of tokens, and no tokens or channels at all."""
     torch, binding = gpu
