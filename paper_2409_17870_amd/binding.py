@@ -61,7 +61,8 @@ except ImportError as _reason:  # not built, or built for another torch or Pytho
     warnings.warn("the calls' C++ marshalling is not used, each takes 2 to 3 us longer: %s" % _reason, RuntimeWarning)
 _CALL_FUNCTIONS = ("apmm_packed_bytes", "apmm_packed_activation_bytes", "apmm_pack_weights", "apmm_pack_activations",
                    "apmm_quantize_pack_activations", "apmm_gemm_ex", "apmm_gemm_from_codes", "apmm_kv_write", "apmm_kv_read", "apmm_kv_attention",
-                   "apmm_kv_attention_workspace_bytes")
+                   "apmm_kv_attention_workspace_bytes", "apmm_rotary", "apmm_kv_write_rotary", "apmm_kv_weights", "apmm_kv_weights_workspace_bytes", "apmm_kv_evict",
+                   "apmm_w4_packed_bytes", "apmm_w4_workspace_bytes", "apmm_w4_gemm")
 
 
 class ApmmError(RuntimeError):
@@ -618,7 +619,7 @@ def apmm_time_next_gemm(start_event, stop_event):
 _general = {}  # the Python functions behind the C++ calls
 if _call is not None:
     for _name in ("apmm_pack_weights", "apmm_pack_activations", "apmm_quantize_pack_activations", "apmm_gemm", "apmm_gemm_from_codes", "apmm_kv_write", "apmm_kv_read",
-                  "apmm_kv_attention"):
+                  "apmm_kv_attention", "apmm_rotary", "apmm_kv_write_rotary", "apmm_kv_weights", "apmm_kv_evict", "apmm_w4_gemm"):
         _general[_name] = globals()[_name]
         _call.set_general(_name, _general[_name])
         globals()[_name] = getattr(_call, _name)

@@ -19,30 +19,60 @@ __device__ __forceinline__ uint32_t order_of(float w)
 }
 
 struct Tokens {
-    const KvEvictArgs &a;
     const float *w;
     const int32_t *table;
-    int keys, length;
+    int64_t pages, capacity;
+    int keys, shift, sinks, recent_from;
+    // of any t from 0 on where there is a token (no branch: tokens behind the last are looked at in the last one's place)
     __device__ __forceinline__ uint32_t operator()(int t) const
     {
-        if (t >= keys) return 0;
-        const int page = table[t >> a.c.page_shift];
-        if (page < 0 || page >= a.c.pages) return 0;
-        if (t < a.sinks || t >= length - a.recent) return 0xffffffffu;
-        return t < a.w.capacity ? order_of(w[t]) : 1u;
+        const int at = min(t, keys - 1), page = table[at >> shift];
+        const uint32_t held = t < sinks || t >= recent_from ? 0xffffffffu : order_of(w[min((int64_t)at, capacity - 1)]);
+        return t >= keys || page < 0 || page >= pages ? 0u : held != 0xffffffffu && t >= capacity ? 1u : held;
     }
 };
 
-// A workgroup to a sequence and head.  Three passes find the budget-th largest number, digit by digit from the highest; then each wave takes a stretch of tokens, counts those that stay, and after the
-// counts have met writes them in their order.
+// A workgroup to a sequence and head, each of its waves has a stretch of tokens.  Three passes find the budget-th largest number, digit by digit from the highest; then each wave counts those of its stretch that
+// stay, and after the counts have met writes them in their order.  Sequences of up to 1024 HELD tokens are read once and held in registers, the second half of 64 to a lane in LDS: a pass over the weights of 65001 tokens is 10 us for the one compute
+// unit that works on them (five of them took 150 us, this takes 22).  What bounds it then: counting, LDS additions of which many meet in one digit.
+template <int HELD>
 __global__ __launch_bounds__(kThreads) void kv_select_kernel(KvEvictArgs a)
 {
     __shared__ uint32_t digits[kDigits];
+    __shared__ uint32_t totals[kWaves];
     __shared__ int above[kWaves], equal[kWaves];
     __shared__ uint32_t found_digit, found_rest;
     const int b = blockIdx.x, head = blockIdx.y, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = kv_lane();
     const int length = min(max(a.c.lengths[b], 0), kKvMost), keys = (int)min((int64_t)length, (int64_t)a.c.width << a.c.page_shift);
-    const Tokens order = {a, a.w.data + b * a.w.sequence_stride + head * a.w.head_stride, a.c.table + b * a.c.table_stride, keys, length};
+    const Tokens order = {a.w.data + b * a.w.sequence_stride + head * a.w.head_stride, a.c.table + b * a.c.table_stride, a.c.pages, a.w.capacity, keys, a.c.page_shift, a.sinks, length - a.recent};
+    const int stretch = ((keys + kThreads - 1) / kThreads) * 64, own_from = min(wave * stretch, keys), to = min(own_from + stretch, keys);
+    constexpr int kInRegisters = HELD < 32 ? HELD : 32;
+    uint32_t held[HELD ? kInRegisters : 1];
+    __shared__ uint32_t more[HELD > 32 ? HELD - 32 : 1][kThreads];
+    if (HELD) {
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) {
+            uint32_t v = 0;
+            if (own_from + 64 * i < to) v = own_from + 64 * i + lane < to ? order(own_from + 64 * i + lane) : 0u;
+            if (i < 32) held[i < 32 ? i : 0] = v;
+            else more[i < 32 ? 0 : i - 32][threadIdx.x] = v;
+            if (i % 8 == 7) __builtin_amdgcn_sched_barrier(0);  // (eight on their way at a time: of more there are no registers)
+        }
+    }
+    // f(token, number) of this lane's tokens, sixty-four to a wave at a time
+    auto each = [&](auto f) {
+        int from = own_from, lane = kv_lane();
+        asm volatile("" : "+s"(from), "+v"(lane));  // (places and borders of 64 tokens are not kept from one pass for the next: for those there are no registers)
+        if (HELD) {
+#pragma unroll
+            for (int i = 0; i < HELD; ++i) {
+                if (from + 64 * i < to) f(from + 64 * i + lane, i < 32 ? held[i < 32 ? i : 0] : more[i < 32 ? 0 : i - 32][threadIdx.x]);
+                if (i % 8 == 7) __builtin_amdgcn_sched_barrier(0);
+            }
+        } else {
+            for (int t = from; t < to; t += 64) f(t + lane, t + lane < to ? order(t + lane) : 0u);
+        }
+    };
     uint32_t least = 0, rest = (uint32_t)a.budget;  // what the digits so far say; how many are wanted of those that begin with them
     bool all = false;
 #pragma unroll
@@ -52,27 +82,21 @@ __global__ __launch_bounds__(kThreads) void kv_select_kernel(KvEvictArgs a)
         for (int i = threadIdx.x; i < kDigits; i += kThreads) digits[i] = 0;
         if (threadIdx.x == 0) found_digit = 0xffffffffu;
         __syncthreads();
-        for (int t = threadIdx.x; t < keys; t += kThreads) {
-            const uint32_t v = order(t);
+        each([&](int, uint32_t v) {
             if (v && (v & upper) == (least & upper)) atomicAdd(&digits[v >> shift & mask], 1u);
-        }
+        });
         __syncthreads();
-        if (wave == 0) {  // from the highest digit down: each lane has 32 that follow each other
-            uint32_t own = 0;
-            const int high = kDigits - 1 - 32 * lane;
-            for (int i = 0; i < 32; ++i) own += digits[high - i];
-            uint32_t before = (uint32_t)kv_scan((int)own) - own;
-            if (before < rest && before + own >= rest) {
-                for (int i = 0; i < 32; ++i) {
-                    const uint32_t n = digits[high - i];
-                    if (before + n >= rest) {
-                        found_digit = (uint32_t)(high - i);
-                        found_rest = rest - before;
-                        break;
-                    }
-                    before += n;
-                }
-            }
+        // from the highest digit down, two to a lane
+        const uint32_t high = digits[kDigits - 1 - 2 * threadIdx.x], low = digits[kDigits - 2 - 2 * threadIdx.x];
+        const uint32_t up_to = (uint32_t)kv_scan((int)(high + low));
+        if (lane == 63) totals[wave] = up_to;
+        __syncthreads();
+        uint32_t before = up_to - high - low;
+        for (int i = 0; i < wave; ++i) before += totals[i];
+        if (before < rest && before + high + low >= rest) {
+            const bool first = before + high >= rest;
+            found_digit = kDigits - 1 - 2 * threadIdx.x - (first ? 0 : 1);
+            found_rest = rest - before - (first ? 0 : high);
         }
         __syncthreads();
         if (found_digit == 0xffffffffu) {  // fewer than the budget (pass 0): all stay
@@ -87,13 +111,11 @@ __global__ __launch_bounds__(kThreads) void kv_select_kernel(KvEvictArgs a)
         least = 0;  // all above it
         rest = 0;
     }
-    const int stretch = ((keys + kThreads - 1) / kThreads) * 64, from = min(wave * stretch, keys), to = min(from + stretch, keys);
     int n_above = 0, n_equal = 0;
-    for (int t = from + lane; t < to; t += 64) {
-        const uint32_t v = order(t);
+    each([&](int t, uint32_t v) {
         n_above += v > least;
-        n_equal += v == least;
-    }
+        n_equal += t < to && v == least;
+    });
     n_above = __builtin_amdgcn_readlane(kv_scan(n_above), 63);
     n_equal = __builtin_amdgcn_readlane(kv_scan(n_equal), 63);
     if (lane == 0) {
@@ -112,21 +134,19 @@ __global__ __launch_bounds__(kThreads) void kv_select_kernel(KvEvictArgs a)
     }
     int32_t *kept_to = a.kept + ((int64_t)b * a.c.heads + head) * a.budget;
     float *weights_to = a.to_weights + ((int64_t)b * a.c.heads + head) * a.budget;
-    for (int t0 = from; t0 < to; t0 += 64) {
-        const int t = t0 + lane;
-        const uint32_t v = t < to ? order(t) : 0u;
+    each([&](int t, uint32_t v) {
         const bool is_equal = t < to && v == least;
-        const uint64_t equals = __ballot(is_equal);
-        const bool stays = (t < to && v > least) || (is_equal && equal_before + (int)__popcll(equals & ((1ull << lane) - 1)) < (int)rest);
+        const uint64_t equals = __ballot(is_equal), below = (1ull << lane) - 1;
+        const bool stays = v > least || (is_equal && equal_before + (int)__popcll(equals & below) < (int)rest);
         const uint64_t staying = __ballot(stays);
         if (stays) {
-            const int at = place + (int)__popcll(staying & ((1ull << lane) - 1));
+            const int at = place + (int)__popcll(staying & below);
             kept_to[at] = t;
             weights_to[at] = t < a.w.capacity ? order.w[t] : 0.0f;
         }
         place += (int)__popcll(staying);
         equal_before += (int)__popcll(equals);
-    }
+    });
     for (int i = kept + (int)threadIdx.x; i < a.budget; i += kThreads) {
         kept_to[i] = -1;
         weights_to[i] = 0.0f;
@@ -195,7 +215,12 @@ int64_t kv_evict_items(const KvEvictArgs &a)
 
 hipError_t launch_kv_evict(const KvEvictArgs &a, hipStream_t stream)
 {
-    kv_select_kernel<<<dim3((uint32_t)a.c.sequences, (uint32_t)a.c.heads), dim3(kThreads), 0, stream>>>(a);
+    const int64_t most = (int64_t)a.c.width << a.c.page_shift;  // tokens of a sequence, as far as the page table goes
+    const dim3 groups((uint32_t)a.c.sequences, (uint32_t)a.c.heads);
+    if (most <= 4 * kThreads) kv_select_kernel<4><<<groups, dim3(kThreads), 0, stream>>>(a);
+    else if (most <= 16 * kThreads) kv_select_kernel<16><<<groups, dim3(kThreads), 0, stream>>>(a);
+    else if (most <= 64 * kThreads) kv_select_kernel<64><<<groups, dim3(kThreads), 0, stream>>>(a);
+    else kv_select_kernel<0><<<groups, dim3(kThreads), 0, stream>>>(a);
     const int64_t units = move_units(a);
     const dim3 grid((uint32_t)((units + kMoveWaves - 1) / kMoveWaves)), block(64 * kMoveWaves);
     if (a.c.head_dim == 128) kv_move_kernel<128><<<grid, block, 0, stream>>>(a, kv_divisor(a.c.heads), (a.budget + 7) / 8, units);

@@ -37,14 +37,22 @@ struct Library {
     decltype(&apmm_kv_read) kv_read;
     decltype(&apmm_kv_attention) kv_attention;
     decltype(&apmm_kv_attention_workspace_bytes) kv_attention_workspace_bytes;
+    decltype(&apmm_rotary) rotary;
+    decltype(&apmm_kv_write_rotary) kv_write_rotary;
+    decltype(&apmm_kv_weights) kv_weights;
+    decltype(&apmm_kv_weights_workspace_bytes) kv_weights_workspace_bytes;
+    decltype(&apmm_kv_evict) kv_evict;
+    decltype(&apmm_w4_packed_bytes) w4_packed_bytes;
+    decltype(&apmm_w4_workspace_bytes) w4_workspace_bytes;
+    decltype(&apmm_w4_gemm) w4_gemm;
 };
-constexpr int kLibraryFunctions = 11;
+constexpr int kLibraryFunctions = 19;
 Library lib = {};
 bool loaded = false;
 PyObject *check = nullptr;  // binding.py's _check
 
 constexpr int kMaxArgs = 15;
-enum Function { kPackWeights, kPackActivations, kQuantize, kGemm, kFromCodes, kKvWrite, kKvRead, kKvAttention, kFunctions };
+enum Function { kPackWeights, kPackActivations, kQuantize, kGemm, kFromCodes, kKvWrite, kKvRead, kKvAttention, kRotary, kKvWriteRotary, kKvWeights, kKvEvict, kW4Gemm, kFunctions };
 struct Signature {
     const char *name;
     int count, required;
@@ -62,6 +70,13 @@ Signature signatures[kFunctions] = {
     {"apmm_kv_write", 7, 6, {"k", "v", "codes", "scales", "page_table", "lengths", "starts"}, {}, nullptr},
     {"apmm_kv_read", 8, 5, {"codes", "scales", "page_table", "lengths", "tokens", "starts", "k_out", "v_out"}, {}, nullptr},
     {"apmm_kv_attention", 11, 5, {"q", "codes", "scales", "page_table", "lengths", "starts", "window", "sinks", "scale", "out", "workspace"}, {}, nullptr},
+    {"apmm_rotary", 7, 3, {"x", "positions", "frequencies", "interleaved", "magnitude", "inverse", "out"}, {}, nullptr},
+    {"apmm_kv_write_rotary", 13, 8,
+     {"q", "k", "v", "codes", "scales", "page_table", "lengths", "frequencies", "starts", "positions", "interleaved", "magnitude", "q_out"}, {}, nullptr},
+    {"apmm_kv_weights", 12, 6, {"q", "codes", "scales", "page_table", "lengths", "weights", "starts", "window", "sinks", "scale", "decay", "workspace"}, {}, nullptr},
+    {"apmm_kv_evict", 12, 7,
+     {"codes", "scales", "page_table", "lengths", "weights", "budget", "to_table", "sinks", "recent", "kept", "to_weights", "to_lengths"}, {}, nullptr},
+    {"apmm_w4_gemm", 6, 4, {"x", "packed", "N", "group", "out", "workspace"}, {}, nullptr},
 };
 
 // Arguments by place, null where not given; false: not the plain case.
@@ -352,6 +367,183 @@ int kv_attention(PyObject **v, PyObject *&result)
     return result_of(done, out, nullptr, result);
 }
 
+bool half_type(const at::Tensor *t) { return t && (t->scalar_type() == at::kHalf || t->scalar_type() == at::kBFloat16); }
+int dtype_of(const at::Tensor &t) { return t.scalar_type() == at::kHalf ? APMM_F16 : APMM_BF16; }
+bool number(PyObject *o, double absent, float &v)
+{
+    if (o && !PyFloat_CheckExact(o)) return false;
+    v = (float)(o ? PyFloat_AS_DOUBLE(o) : absent);
+    return true;
+}
+bool dense_last(const at::Tensor &t) { return t.size(t.dim() - 1) <= 1 || t.stride(t.dim() - 1) == 1; }
+bool rotation(PyObject *frequencies_arg, PyObject *interleaved_arg, PyObject *magnitude_arg, int device, apmm_rotation &r)
+{
+    const at::Tensor *f = tensor(frequencies_arg);
+    bool interleaved;
+    if (!f || f->scalar_type() != at::kDouble || f->dim() != 1 || !f->is_contiguous() || f->get_device() != device || !flag(interleaved_arg, false, interleaved) ||
+        !number(magnitude_arg, 1.0, r.magnitude))
+        return false;
+    r.frequencies = static_cast<const double *>(f->data_ptr());
+    r.pairs = f->size(0);
+    r.interleaved = interleaved;
+    return true;
+}
+bool positions_ok(const at::Tensor *t, int64_t tokens, int device) { return kv_indices(t, 1, device) && t->size(0) == tokens; }
+
+int rotary(PyObject **v, PyObject *&result)
+{
+    apmm_rotation r;
+    bool inverse;
+    const at::Tensor *x = tensor(v[0]), *at = tensor(v[1]);
+    if (!half_type(x) || x->dim() != 3 || !dense_last(*x) || x->get_device() != c10::hip::current_device() || !positions_ok(at, x->size(0), x->get_device()) ||
+        !rotation(v[2], v[3], v[4], x->get_device(), r) || !flag(v[5], false, inverse) || x->size(1) > INT32_MAX || x->size(2) > INT32_MAX)
+        return 0;
+    if (given(v[6])) {
+        const at::Tensor *o = tensor(v[6]);
+        if (!o || o->scalar_type() != x->scalar_type() || o->get_device() != x->get_device() || o->sizes() != x->sizes() || !dense_last(*o)) return 0;
+    }
+    Output out;
+    if (!output(out, v[6], true, *x, x->sizes(), x->scalar_type())) return result_of(0, out, nullptr, result);
+    const at::Tensor &to = *tensor(out.object);
+    void *s = stream();
+    const bool went = called([&] {
+        return lib.rotary(x->size(0), (int)x->size(1), (int)x->size(2), dtype_of(*x), x->data_ptr(), x->stride(0), x->stride(1), static_cast<const int32_t *>(at->data_ptr()), &r, inverse, out.address,
+                          to.stride(0), to.stride(1), s);
+    });
+    return result_of(went ? 1 : -1, out, nullptr, result);
+}
+
+int kv_write_rotary(PyObject **v, PyObject *&result)
+{
+    apmm_kv_cache c;
+    apmm_kv_batch b;
+    apmm_rotation r;
+    const at::Tensor *q = tensor(v[0]), *k = tensor(v[1]), *x = tensor(v[2]);
+    if (!q || !k || !x || k->dim() != 3 || q->dim() != 3 || !kv_cache(v[3], v[4], c) || !kv_batch(v[3], v[5], v[6], v[8], k->size(0), b) || q->size(1) > INT32_MAX) return 0;
+    const int device = k->get_device();
+    if (!kv_rows(q, v[4], q->size(1), c.head_dim, b.tokens) || !kv_rows(k, v[4], c.kv_heads, c.head_dim, b.tokens) || !kv_rows(x, v[4], c.kv_heads, c.head_dim, b.tokens) ||
+        !rotation(v[7], v[10], v[11], device, r) || (given(v[9]) && !positions_ok(tensor(v[9]), b.tokens, device)) ||
+        (given(v[12]) && !kv_rows(tensor(v[12]), v[4], q->size(1), c.head_dim, b.tokens)))
+        return 0;
+    const int32_t *at = given(v[9]) ? static_cast<const int32_t *>(tensor(v[9])->data_ptr()) : nullptr;
+    Output out;
+    if (!output(out, v[12], true, *q, q->sizes(), q->scalar_type())) return result_of(0, out, nullptr, result);
+    const at::Tensor &to = *tensor(out.object);
+    void *s = stream();
+    const bool went = called([&] {
+        return lib.kv_write_rotary(&c, &b, (int)q->size(1), at, &r, q->data_ptr(), q->stride(0), q->stride(1), out.address, to.stride(0), to.stride(1), k->data_ptr(), k->stride(0), k->stride(1),
+                                   x->data_ptr(), x->stride(0), x->stride(1), s);
+    });
+    return result_of(went ? 1 : -1, out, nullptr, result);
+}
+
+bool kv_weight_rows(const at::Tensor *w, int64_t sequences, int64_t heads, int device)
+{
+    return w && w->scalar_type() == at::kFloat && w->get_device() == device && w->dim() == 3 && w->size(0) == sequences && w->size(1) == heads && w->size(2) >= 1 && dense_last(*w);
+}
+
+int kv_weights(PyObject **v, PyObject *&result)
+{
+    apmm_kv_cache c;
+    apmm_kv_batch b;
+    int64_t window = 0, sinks = 0;
+    float decay;
+    const at::Tensor *q = tensor(v[0]), *w = tensor(v[5]);
+    if (!q || q->dim() != 3 || !kv_cache(v[1], v[2], c) || !kv_batch(v[1], v[3], v[4], v[6], q->size(0), b) || q->size(1) > INT32_MAX || !kv_rows(q, v[2], q->size(1), c.head_dim, b.tokens) ||
+        !kv_weight_rows(w, b.sequences, c.kv_heads, q->get_device()) || (v[7] && !integer(v[7], -kAny, kAny, window)) || (v[8] && !integer(v[8], -kAny, kAny, sinks)) ||
+        (given(v[9]) && !PyFloat_CheckExact(v[9])) || !number(v[10], 1.0, decay) ||
+        (given(v[11]) && (!tensor(v[11]) || !tensor(v[11])->is_contiguous() || tensor(v[11])->get_device() != q->get_device())))
+        return 0;
+    const int heads = (int)q->size(1);
+    const float scale = (float)(given(v[9]) ? PyFloat_AS_DOUBLE(v[9]) : 1.0 / std::sqrt((double)c.head_dim));
+    const size_t need = given(v[11]) ? 0 : lib.kv_weights_workspace_bytes(&c, &b, heads);
+    Output work;
+    int done = output(work, v[11], need != 0, *q, {(int64_t)need}, at::kByte);
+    if (done) {
+        const size_t room = work.address ? bytes(*tensor(work.object)) : 0;
+        void *s = stream();
+        const bool went = called([&] {
+            return lib.kv_weights(&c, &b, heads, q->data_ptr(), q->stride(0), q->stride(1), static_cast<float *>(w->data_ptr()), w->stride(0), w->stride(1), w->size(2), decay, scale, window, sinks,
+                                  work.address, room, s);
+        });
+        done = went ? 1 : -1;
+    }
+    if (work.made) Py_DECREF(work.object);
+    if (done == 1) {
+        result = v[5];
+        Py_INCREF(result);
+    }
+    return done;
+}
+
+int kv_evict(PyObject **v, PyObject *&result)
+{
+    apmm_kv_cache c;
+    apmm_kv_batch b, to;
+    int64_t budget, sinks = 0, recent = 0;
+    const at::Tensor *lengths = tensor(v[3]), *w = tensor(v[4]);
+    if (!lengths || lengths->dim() != 1 || !kv_cache(v[0], v[1], c) || !kv_batch(v[0], v[2], v[3], nullptr, lengths->size(0), b) || !kv_batch(v[0], v[6], v[3], nullptr, lengths->size(0), to) ||
+        !kv_weight_rows(w, b.sequences, c.kv_heads, lengths->get_device()) || !integer(v[5], 1, INT32_MAX, budget) || (v[7] && !integer(v[7], -kAny, kAny, sinks)) ||
+        (v[8] && !integer(v[8], -kAny, kAny, recent)))
+        return 0;
+    const int64_t shape[3] = {b.sequences, c.kv_heads, budget};
+    for (int i = 9; i < 12; ++i) {
+        if (!given(v[i])) continue;
+        const at::Tensor *t = tensor(v[i]);
+        if (!t || t->scalar_type() != (i == 10 ? at::kFloat : at::kInt) || t->sizes() != at::IntArrayRef(shape, i == 11 ? 1 : 3) || t->get_device() != lengths->get_device() || !t->is_contiguous())
+            return 0;
+    }
+    Output out[3];
+    int done = 1;
+    for (int i = 0; i < 3 && done; ++i) done = output(out[i], v[9 + i], true, *lengths, at::IntArrayRef(shape, i == 2 ? 1 : 3), i == 1 ? at::kFloat : at::kInt);
+    if (done) {
+        void *s = stream();
+        const bool went = called([&] {
+            return lib.kv_evict(&c, b.sequences, b.lengths, b.page_table, b.table_stride, b.table_width, static_cast<const float *>(w->data_ptr()), w->stride(0), w->stride(1), w->size(2), budget, sinks,
+                                recent, to.page_table, to.table_stride, to.table_width, static_cast<int32_t *>(out[2].address), static_cast<int32_t *>(out[0].address),
+                                static_cast<float *>(out[1].address), s);
+        });
+        done = went ? 1 : -1;
+    }
+    if (done == 1) {
+        result = PyTuple_Pack(3, out[0].object, out[1].object, out[2].object);
+        if (!result) done = -1;
+    }
+    for (Output &o : out)
+        if (o.made) Py_DECREF(o.object);
+    return done;
+}
+
+int w4_gemm(PyObject **v, PyObject *&result)
+{
+    int64_t N, group;
+    const at::Tensor *x = tensor(v[0]), *packed = tensor(v[1]);
+    if (!half_type(x) || x->dim() != 2 || !dense_last(*x) || x->get_device() != c10::hip::current_device() || !packed || packed->scalar_type() != at::kByte || packed->get_device() != x->get_device() ||
+        !packed->is_contiguous() || !integer(v[2], 0, INT32_MAX, N) || !integer(v[3], 1, INT32_MAX, group))
+        return 0;
+    const int64_t M = x->size(0), K = x->size(1);
+    if (bytes(*packed) < lib.w4_packed_bytes(N, K, (int)group)) return 0;
+    if (given(v[4])) {
+        const at::Tensor *o = tensor(v[4]);
+        if (!o || o->scalar_type() != x->scalar_type() || o->dim() != 2 || o->size(0) != M || o->size(1) != N || o->get_device() != x->get_device() || !dense_last(*o)) return 0;
+    }
+    if (given(v[5]) && (!tensor(v[5]) || !tensor(v[5])->is_contiguous() || tensor(v[5])->get_device() != x->get_device())) return 0;
+    const size_t need = given(v[5]) ? 0 : lib.w4_workspace_bytes(M, N, K, (int)group);
+    Output out, work;
+    int done = output(out, v[4], true, *x, {M, N}, x->scalar_type()) && output(work, v[5], need != 0, *x, {(int64_t)need}, at::kByte);
+    if (done) {
+        const at::Tensor &to = *tensor(out.object);
+        const size_t room = work.address ? bytes(*tensor(work.object)) : 0;
+        void *s = stream();
+        const bool went = called([&] {
+            return lib.w4_gemm(M, N, K, (int)group, dtype_of(*x), x->data_ptr(), x->stride(0), packed->data_ptr(), out.address, to.stride(0), work.address, room, s);
+        });
+        done = went ? 1 : -1;
+    }
+    if (work.made) Py_DECREF(work.object);
+    return result_of(done, out, nullptr, result);
+}
+
 template <Function F>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *names)
 {
@@ -361,7 +553,8 @@ PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *n
         [&] {
             if (!place(s, args, nargs, names, v)) return 0;
             return F <= kPackActivations ? pack(F, v, result) : F == kQuantize ? quantize(v, result) : F == kGemm ? gemm(v, result) : F == kFromCodes ? from_codes(v, result) :
-                   F == kKvWrite ? kv_write(v, result) : F == kKvRead ? kv_read(v, result) : kv_attention(v, result);
+                   F == kKvWrite ? kv_write(v, result) : F == kKvRead ? kv_read(v, result) : F == kKvAttention ? kv_attention(v, result) : F == kRotary ? rotary(v, result) :
+                   F == kKvWriteRotary ? kv_write_rotary(v, result) : F == kKvWeights ? kv_weights(v, result) : F == kKvEvict ? kv_evict(v, result) : w4_gemm(v, result);
         },
         [] { return 0; });  // (torch's own refusal of a tensor: the general form meets the same one and reports it)
     if (done > 0) return result;
@@ -429,6 +622,20 @@ PyMethodDef methods[] = {
     {"apmm_kv_attention", ENTRY(kKvAttention),
      "apmm_kv_attention(q, codes, scales, page_table, lengths, starts=None, window=0, sinks=0, scale=None, out=None, workspace=None)\n--\n\n"
      "Causal attention of the new tokens' queries over the cache, which holds their keys and values already."},
+    {"apmm_rotary", ENTRY(kRotary),
+     "apmm_rotary(x, positions, frequencies, interleaved=False, magnitude=1.0, inverse=False, out=None)\n--\n\n"
+     "Turn the pairs of the first 2 * len(frequencies) channels of x by position times frequency."},
+    {"apmm_kv_write_rotary", ENTRY(kKvWriteRotary),
+     "apmm_kv_write_rotary(q, k, v, codes, scales, page_table, lengths, frequencies, starts=None, positions=None, interleaved=False, magnitude=1.0, q_out=None)\n--\n\n"
+     "apmm_rotary of q and k and apmm_kv_write of these k and of v in one launch; the turned q."},
+    {"apmm_kv_weights", ENTRY(kKvWeights),
+     "apmm_kv_weights(q, codes, scales, page_table, lengths, weights, starts=None, window=0, sinks=0, scale=None, decay=1.0, workspace=None)\n--\n\n"
+     "What attention of the new tokens' queries gives each cached token, added to decay * weights."},
+    {"apmm_kv_evict", ENTRY(kKvEvict),
+     "apmm_kv_evict(codes, scales, page_table, lengths, weights, budget, to_table, sinks=0, recent=0, kept=None, to_weights=None, to_lengths=None)\n--\n\n"
+     "Keep of each sequence and head the first tokens, the last and the heaviest others: (places they had, their weights, the new lengths)."},
+    {"apmm_w4_gemm", ENTRY(kW4Gemm),
+     "apmm_w4_gemm(x, packed, N, group, out=None, workspace=None)\n--\n\nx (M x K, float16 or bfloat16) times packed weights of N channels: M x N of x's type."},
     {"set_library", set_library, METH_VARARGS, nullptr},
     {"set_general", set_general, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr},
