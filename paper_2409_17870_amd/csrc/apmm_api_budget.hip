@@ -106,12 +106,15 @@ apmm_status apmm_kv_write_rotary(const apmm_kv_cache *cache, const apmm_kv_batch
     return e == hipSuccess ? APMM_OK : fail_hip(e, "apmm_kv_write_rotary");
 }
 
-// (without a window: under one as much is needed or less)
+// (without a window and with starts: under one and without them as much is needed or less)
 size_t apmm_kv_weights_workspace_bytes(const apmm_kv_cache *cache, const apmm_kv_batch *batch, int q_heads)
 {
+    static const int32_t any = 0;
     apmm::KvArgs a;
     apmm::KvWeightsPlan plan;
-    if (check_sizes(cache, batch, a) != APMM_OK || batch->sequences == 0 || batch->tokens == 0 || check_weighing(cache, batch, a, q_heads, 0, 0, plan) != APMM_OK) return 0;
+    if (check_sizes(cache, batch, a) != APMM_OK || batch->sequences == 0 || batch->tokens == 0) return 0;
+    a.starts = &any;
+    if (check_weighing(cache, batch, a, q_heads, 0, 0, plan) != APMM_OK) return 0;
     return apmm::kv_weights_bytes(plan);
 }
 

@@ -9,13 +9,14 @@ struct KvWeights {  // sequences x heads x capacity numbers
     int64_t sequence_stride, head_stride, capacity;
 };
 
-// What kv_weights' statistics of rows are cut into: the plan's one part (KvPart), and where in the workspace the rows' base and factor lie
+// How a call of kv_weights is cut: sequences of few rows, those of many, each with pieces of the keys for the first pass (KvPart).  The workspace has few's pieces, many's, and many's rows as operands with their factors.
 struct KvWeightsPlan {
-    KvPart part;
-    int row_tiles;        // tiles of 16 rows that a wave of the statistics has at a time: 1 or 4
-    int64_t rows;         // tokens * q_heads
-    size_t pieces_bytes;  // of the workspace that pieces take, in front of the rows'
-    int64_t groups;       // workgroups of the sums
+    KvPart few, many;              // tile 0: none of these
+    size_t few_bytes, many_bytes;  // of the workspace that pieces take
+    int64_t row_tiles;             // of 16 rows, of a head, whose operands and factors are in it
+    size_t rows_bytes;
+    int64_t units;                 // workgroups of many's second pass, for a head
+    int key_tiles;                 // of 16 keys, of a wave of it
 };
 KvWeightsPlan kv_weights_plan(const KvArgs &c, int groups, int window, int sinks);
 int64_t kv_weights_blocks(const KvArgs &c);
