@@ -33,8 +33,10 @@ struct Tokens {
 };
 
 // A workgroup to a sequence and head, each of its waves has a stretch of tokens.  Three passes find the budget-th largest number, digit by digit from the highest; then each wave counts those of its stretch that
-// stay, and after the counts have met writes them in their order.  Sequences of up to 1024 HELD tokens are read once and held in registers, the second half of 64 to a lane in LDS: a pass over the weights of 65001 tokens is 10 us for the one compute
-// unit that works on them (five of them took 150 us, this takes 22).  What bounds it then: counting, LDS additions of which many meet in one digit.
+// stay, and after the counts have met writes their places in order, whose weights are fetched at the end by all.  Sequences of up to 1024 HELD tokens are read once and held in registers, the second half of 64 to a
+// lane in LDS.  Bound by the instructions of the one compute unit that has a sequence and head: 65001 tokens take 102 000 cycles, 23 000 to read them, 46 000 for the three passes (a fifth of it LDS additions that
+// meet in one digit), 10 000 to count and 21 000 to write.  Reading every token with its own checks took 55 000, a weight fetched as its place is written 48 000 in place of 21 000; reading the weights anew in each of
+// five passes 150 us.  More workgroups to a head would need memory for their counts, and a launch more for calls of ordinary length, which take 31 us with the copy.
 template <int HELD>
 __global__ __launch_bounds__(kThreads) void kv_select_kernel(KvEvictArgs a)
 {
@@ -50,13 +52,34 @@ __global__ __launch_bounds__(kThreads) void kv_select_kernel(KvEvictArgs a)
     uint32_t held[HELD ? kInRegisters : 1];
     __shared__ uint32_t more[HELD > 32 ? HELD - 32 : 1][kThreads];
     if (HELD) {
-#pragma unroll
-        for (int i = 0; i < HELD; ++i) {
-            uint32_t v = 0;
-            if (own_from + 64 * i < to) v = own_from + 64 * i + lane < to ? order(own_from + 64 * i + lane) : 0u;
+        constexpr int kBatch = HELD < 16 ? HELD : 16;
+        auto hold = [&](int i, uint32_t v) {
             if (i < 32) held[i < 32 ? i : 0] = v;
             else more[i < 32 ? 0 : i - 32][threadIdx.x] = v;
-            if (i % 8 == 7) __builtin_amdgcn_sched_barrier(0);  // (eight on their way at a time: of more there are no registers)
+        };
+#pragma unroll
+        for (int first = 0; first < HELD; first += kBatch) {
+            // tokens that all have a weight and a page, and none of which stays whatever its weight, are read as they lie
+            const int begin = min(own_from + 64 * first, to), end = min(begin + 64 * kBatch, to), last = end - begin - 1;
+            bool plain = last >= 0 && begin >= order.sinks && end <= order.recent_from && end <= order.capacity;
+            if (plain)
+                for (int page = (begin >> order.shift) + lane; page <= (end - 1) >> order.shift; page += 64) plain &= order.table[page] >= 0 && order.table[page] < order.pages;
+            if (__ballot(!plain) == 0) {
+                const float *w = order.w + begin;
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) {
+                    const uint32_t v = order_of(w[min(64 * i + lane, last)]);
+                    hold(first + i, 64 * i + lane <= last ? v : 0u);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) {
+                    uint32_t v = 0;
+                    if (64 * i <= last) v = 64 * i + lane <= last ? order(begin + 64 * i + lane) : 0u;
+                    hold(first + i, v);
+                    if (i % 8 == 7) __builtin_amdgcn_sched_barrier(0);  // (eight on their way at a time: of more there are no registers)
+                }
+            }
         }
     }
     // f(token, number) of this lane's tokens, sixty-four to a wave at a time
@@ -134,22 +157,28 @@ __global__ __launch_bounds__(kThreads) void kv_select_kernel(KvEvictArgs a)
     }
     int32_t *kept_to = a.kept + ((int64_t)b * a.c.heads + head) * a.budget;
     float *weights_to = a.to_weights + ((int64_t)b * a.c.heads + head) * a.budget;
-    each([&](int t, uint32_t v) {
-        const bool is_equal = t < to && v == least;
-        const uint64_t equals = __ballot(is_equal), below = (1ull << lane) - 1;
-        const bool stays = v > least || (is_equal && equal_before + (int)__popcll(equals & below) < (int)rest);
+    auto put = [&](int t, bool stays) {
         const uint64_t staying = __ballot(stays);
-        if (stays) {
-            const int at = place + (int)__popcll(staying & below);
-            kept_to[at] = t;
-            weights_to[at] = t < a.w.capacity ? order.w[t] : 0.0f;
-        }
+        if (stays) kept_to[place + __builtin_amdgcn_mbcnt_hi((uint32_t)(staying >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)staying, 0))] = t;
         place += (int)__popcll(staying);
-        equal_before += (int)__popcll(equals);
-    });
-    for (int i = kept + (int)threadIdx.x; i < a.budget; i += kThreads) {
-        kept_to[i] = -1;
-        weights_to[i] = 0.0f;
+    };
+    const int equals_left = (int)rest - equal_before;  // of this stretch's tokens of the least number, so many stay
+    if (equals_left <= 0 || equals_left >= equal[wave]) {
+        const uint32_t over = equals_left <= 0 ? least : least - 1;  // (equals_left > 0: least > 0)
+        each([&](int t, uint32_t v) { put(t, v > over); });
+    } else {
+        each([&](int t, uint32_t v) {
+            const bool is_equal = t < to && v == least;
+            const uint64_t equals = __ballot(is_equal);
+            put(t, v > least || (is_equal && equal_before + (int)__popcll(equals & ((1ull << lane) - 1)) < (int)rest));
+            equal_before += (int)__popcll(equals);
+        });
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < a.budget; i += kThreads) {
+        const int t = i < kept ? kept_to[i] : -1;
+        if (t < 0) kept_to[i] = -1;
+        weights_to[i] = t >= 0 && t < a.w.capacity ? order.w[t] : 0.0f;
     }
     if (head == 0 && threadIdx.x == 0) a.to_lengths[b] = kept;
 }
