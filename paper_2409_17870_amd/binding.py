@@ -490,7 +490,8 @@ def apmm_kv_write_rotary(q, k, v, codes, scales, page_table, lengths, frequencie
 
 
 def _kv_weights_rows(weights, codes, sequences, kv_heads):
-    if weights.dtype != torch.float32 or weights.device != codes.device or weights.dim() != 3 or weights.shape[0] != sequences or weights.shape[1] != kv_heads or             weights.shape[2] < 1 or (weights.shape[2] > 1 and weights.stride(2) != 1):
+    if weights.dtype != torch.float32 or weights.device != codes.device or weights.dim() != 3 or weights.shape[0] != sequences or weights.shape[1] != kv_heads or \
+            weights.shape[2] < 1 or (weights.shape[2] > 1 and weights.stride(2) != 1):
         raise ValueError("weights must be a float32 tensor on the cache's device, sequences x %d x capacity, contiguous in its last dimension" % kv_heads)
     return weights.data_ptr(), weights.stride(0), weights.stride(1), weights.shape[2]
 

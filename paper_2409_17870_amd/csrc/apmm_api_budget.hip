@@ -1,5 +1,7 @@
 // C ABI of rotary positions and of what keeps the four-bit key/value cache within a budget (include/apmm.h): argument checks and launches.
+#include <algorithm>
 #include <cmath>
+#include <cstdint>
 
 #include "apmm_budget.h"
 #include "apmm_kv_checks.h"
@@ -33,8 +35,10 @@ apmm_status check_weights(const apmm_kv_cache *cache, const float *weights, int6
 {
     if (capacity < 1 || sequence_stride < 0 || head_stride < 0) return fail(APMM_ERR_INVALID_ARG, "kv: weights need capacity >= 1 and strides >= 0");
     if (capacity > ((int64_t)1 << 46) || sequence_stride > ((int64_t)1 << 46) || head_stride > ((int64_t)1 << 46)) return fail(APMM_ERR_UNSUPPORTED, "kv: capacity or a stride of weights > 2^46");
-    if ((sequences && cache->kv_heads > 1 && head_stride < capacity) || (sequences > 1 && sequence_stride < (cache->kv_heads - 1) * head_stride + capacity))
-        return fail(APMM_ERR_INVALID_ARG, "kv: weights' rows overlap");
+    // the shorter stride holds a row, the longer one all rows of the shorter; a stride of one sequence or head counts for nothing
+    const int64_t s = sequences > 1 ? sequence_stride : INT64_MAX, h = cache->kv_heads > 1 ? head_stride : INT64_MAX;
+    const int64_t inner = std::min(s, h), outer = std::max(s, h), rows = s < h ? sequences : cache->kv_heads;
+    if (sequences && (inner < capacity || (outer != INT64_MAX && outer < (rows - 1) * inner + capacity))) return fail(APMM_ERR_INVALID_ARG, "kv: weights' rows overlap");
     if (!weights || !aligned(weights, 4)) return fail(APMM_ERR_INVALID_ARG, "kv: null or misaligned weights");
     w.data = const_cast<float *>(weights);
     w.sequence_stride = sequence_stride;

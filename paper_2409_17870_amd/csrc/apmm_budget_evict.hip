@@ -44,7 +44,7 @@ __global__ __launch_bounds__(kThreads) void kv_select_kernel(KvEvictArgs a)
     __shared__ uint32_t totals[kWaves];
     __shared__ int above[kWaves], equal[kWaves];
     __shared__ uint32_t found_digit, found_rest;
-    const int b = blockIdx.x, head = blockIdx.y, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = kv_lane();
+    const int b = kv_divide(blockIdx.x, a.c.by_heads), head = blockIdx.x - b * a.c.heads, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = kv_lane();
     const int length = min(max(a.c.lengths[b], 0), kKvMost), keys = (int)min((int64_t)length, (int64_t)a.c.width << a.c.page_shift);
     const Tokens order = {a.w.data + b * a.w.sequence_stride + head * a.w.head_stride, a.c.table + b * a.c.table_stride, a.c.pages, a.w.capacity, keys, a.c.page_shift, a.sinks, length - a.recent};
     const int stretch = ((keys + kThreads - 1) / kThreads) * 64, own_from = min(wave * stretch, keys), to = min(own_from + stretch, keys);
@@ -245,15 +245,15 @@ int64_t kv_evict_items(const KvEvictArgs &a)
 hipError_t launch_kv_evict(const KvEvictArgs &a, hipStream_t stream)
 {
     const int64_t most = (int64_t)a.c.width << a.c.page_shift;  // tokens of a sequence, as far as the page table goes
-    const dim3 groups((uint32_t)a.c.sequences, (uint32_t)a.c.heads);
-    if (most <= 4 * kThreads) kv_select_kernel<4><<<groups, dim3(kThreads), 0, stream>>>(a);
-    else if (most <= 16 * kThreads) kv_select_kernel<16><<<groups, dim3(kThreads), 0, stream>>>(a);
-    else if (most <= 64 * kThreads) kv_select_kernel<64><<<groups, dim3(kThreads), 0, stream>>>(a);
-    else kv_select_kernel<0><<<groups, dim3(kThreads), 0, stream>>>(a);
+    const dim3 groups((uint32_t)a.c.sequences * (uint32_t)a.c.heads), block(kThreads);
+    if (most <= 4 * kThreads) kv_select_kernel<4><<<groups, block, 0, stream>>>(a);
+    else if (most <= 16 * kThreads) kv_select_kernel<16><<<groups, block, 0, stream>>>(a);
+    else if (most <= 64 * kThreads) kv_select_kernel<64><<<groups, block, 0, stream>>>(a);
+    else kv_select_kernel<0><<<groups, block, 0, stream>>>(a);
     const int64_t units = move_units(a);
-    const dim3 grid((uint32_t)((units + kMoveWaves - 1) / kMoveWaves)), block(64 * kMoveWaves);
-    if (a.c.head_dim == 128) kv_move_kernel<128><<<grid, block, 0, stream>>>(a, kv_divisor(a.c.heads), (a.budget + 7) / 8, units);
-    else kv_move_kernel<64><<<grid, block, 0, stream>>>(a, kv_divisor(a.c.heads), (a.budget + 7) / 8, units);
+    const dim3 grid((uint32_t)((units + kMoveWaves - 1) / kMoveWaves)), four(64 * kMoveWaves);
+    if (a.c.head_dim == 128) kv_move_kernel<128><<<grid, four, 0, stream>>>(a, kv_divisor(a.c.heads), (a.budget + 7) / 8, units);
+    else kv_move_kernel<64><<<grid, four, 0, stream>>>(a, kv_divisor(a.c.heads), (a.budget + 7) / 8, units);
     return hipGetLastError();
 }
 

@@ -50,7 +50,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryRows a)
                         uint32_t v[4];
                         kv_load(from + piece * 8, true, w);
                         kv_load(from + piece * 8 + pairs, true, v);
-    #pragma unroll
+#pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             const float2 c1 = t[piece * 8 + 2 * j], c2 = t[piece * 8 + 2 * j + 1];
                             const float a1 = kv_scale_value(w[j] & 0xffffu, BF16), a2 = kv_scale_value(w[j] >> 16, BF16), b1 = kv_scale_value(v[j] & 0xffffu, BF16), b2 = kv_scale_value(v[j] >> 16, BF16);

@@ -344,3 +344,31 @@ def test_generation_within_a_budget(gpu):
                     far = 2.0 ** -11 * D ** -0.5 * float((kk.abs() @ q[b, i].double().cpu().abs()).max())
                     assert bool(((o[b, i].double().cpu() - p @ vv).abs() <= (2 * far + 3 * 2.0 ** -11) * (p @ vv.abs()) + 2.0 ** -11 * (p @ vv).abs() + 1e-3 * 2.0 ** -10).all())
     assert bool((weights[:, :, :budget] >= heavy).all()) and bool((weights[:, :, budget:budget + 3] > 0).all())
+
+
+def test_offsets_beyond_32_bits(gpu):
+    """Pages beyond 4 GiB of codes, weights of sequences and heads 2^31 numbers apart and in the order of heads."""
+    torch, binding = gpu
+    D, heads, ps = 128, 8, 256
+    pages = (5 << 30) // (heads * ps * D)
+    codes, scales = binding.apmm_kv_cache(pages, ps, heads, D, torch.float16)
+    f = binding.apmm_rotary_frequencies(D)
+    for new, groups in (([300, 1], 1), ([1, 1], 4)):
+        x = Batch(torch, torch.float16, D, heads, groups, ps, [300, 520], new, seed=9, spare=4)
+        far = [pages - 1 - 7 * i for i in range(x.scales.shape[0])]
+        codes[far], scales[far] = x.codes, x.scales
+        where = torch.tensor(far, dtype=torch.int32)
+        table = torch.where(x.table >= 0, where[x.table.long()], x.table).cuda()
+        args = [codes, scales, table, x.args[3]]
+        a, b = (binding.apmm_kv_write_rotary(x.q, x.k, x.v, *to, f, x.starts_gpu) for to in (x.args, args))
+        assert torch.equal(a, b) and torch.equal(codes[far], x.codes) and torch.equal(scales[far], x.scales)
+        near = binding.apmm_kv_weights(a, *x.args, torch.zeros((2, heads, 700), device="cuda"), x.starts_gpu)
+        apart = torch.empty((1 << 31) + (8 << 20), device="cuda").as_strided((2, heads, 700), (1 << 31, 1 << 20, 1)).zero_()
+        turned = torch.zeros((heads, 2, 700), device="cuda").transpose(0, 1)
+        for w in (apart, turned):
+            assert torch.equal(binding.apmm_kv_weights(a, *args, w, x.starts_gpu), near)
+        used = set(int(p) for p in x.table.flatten() if p >= 0)
+        to = torch.tensor([p for p in range(len(far)) if p not in used][:4], dtype=torch.int32).view(2, 2)
+        one, other = binding.apmm_kv_evict(*x.args, near, 400, to.cuda(), recent=9), binding.apmm_kv_evict(*args, apart, 400, where[to.long()].cuda(), recent=9)
+        assert all(torch.equal(i, j) for i, j in zip(one, other)) and torch.equal(codes[far], x.codes) and torch.equal(scales[far], x.scales)
+        del apart

@@ -71,6 +71,13 @@ def test_weights(lib):  # noqa: F811
                            (UNSUPPORTED, dict(batch=dict(sequences=65536, tokens=65536, starts=None, table_width=1 << 26, table_stride=1 << 26), q_heads=8)), (WORKSPACE, {})]:
         assert weigh(lib, **change) == status, change
     need = lib.apmm_kv_weights_workspace_bytes(*structs(), 32)
+    # either order of sequences and heads, rows that follow each other or lie apart; 7 or 8 of them one capacity apart do not fit
+    s, h = structs()[1].sequences, structs()[0].kv_heads
+    for strides in ((h * 1000, 1000), (1000, s * 1000), (5000, 5000 * s), (h * 1234, 1234)):
+        assert weigh(lib, strides=strides) == WORKSPACE, strides
+    for strides in ((1000, s * 1000 - 1), (1000, 1000), (0, 1000), (1000, 0), (h * 1000 - 1, 1000)):
+        assert weigh(lib, strides=strides) == INVALID, strides
+    assert weigh(lib, strides=(0, 1000), batch=dict(sequences=1)) == WORKSPACE and weigh(lib, strides=(1000, 0), cache=dict(kv_heads=1), q_heads=4) == WORKSPACE
     assert need >= 7 * 32 * 8 and need % 8 == 0
     assert weigh(lib, workspace=0xc000, size=need - 1) == WORKSPACE and weigh(lib, workspace=0xc008, size=need) == INVALID
     assert lib.apmm_kv_weights_workspace_bytes(*structs(batch=dict(tokens=0)), 32) == 0 and lib.apmm_kv_weights_workspace_bytes(*structs(), 33) == 0

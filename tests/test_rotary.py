@@ -221,3 +221,14 @@ def test_refusals(gpu):
             bad()
     with pytest.raises(ValueError):
         binding.apmm_rotary_frequencies(7)
+
+
+def test_offsets_beyond_32_bits(gpu):
+    """Rows so far apart that the last ones begin beyond 2^32 elements."""
+    torch, binding = gpu
+    x = torch.randn((17, 3, 64), generator=torch.Generator().manual_seed(3)).half().cuda()
+    at, f = torch.arange(17, dtype=torch.int32, device="cuda"), binding.apmm_rotary_frequencies(64)
+    far = torch.empty((1 << 32) + (1 << 28), dtype=torch.float16, device="cuda").as_strided(x.shape, (1 << 28, 1 << 20, 1))
+    far.copy_(x)
+    want = binding.apmm_rotary(x, at, f)
+    assert torch.equal(binding.apmm_rotary(far, at, f), want) and torch.equal(binding.apmm_rotary(far, at, f, out=far), want)

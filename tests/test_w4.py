@@ -188,3 +188,18 @@ def test_refusals(gpu):
             bad()
     with pytest.raises(binding.ApmmError):
         binding.apmm_w4_pack(codes, torch.zeros((32, 3), dtype=torch.float16, device="cuda"), 48)
+
+
+def test_offsets_beyond_32_bits(gpu):
+    """Rows of x and y so far apart that the last ones begin beyond 2^32 elements."""
+    torch, binding = gpu
+    N, K, group = 40, 300, 64
+    codes, scales = weights(torch, N, K, group, torch.float16, 12)
+    packed = binding.apmm_w4_pack(codes.cuda(), scales.cuda(), group)
+    for M, stride in ((9, 1 << 29), (33, 1 << 27), (2100, 1 << 21)):
+        x = torch.randn((M, K), generator=torch.Generator().manual_seed(M)).half().cuda()
+        far = torch.empty((M - 1) * stride + 512, dtype=torch.float16, device="cuda")
+        rows, out = far.as_strided((M, K), (stride, 1)), far[400:].as_strided((M, N), (stride, 1))  # (results behind their row)
+        rows.copy_(x)
+        assert torch.equal(binding.apmm_w4_gemm(rows, packed, N, group, out=out), binding.apmm_w4_gemm(x, packed, N, group)) and torch.equal(rows, x)
+        del far, rows, out
