@@ -9,10 +9,12 @@ struct KvWeights {  // sequences x heads x capacity numbers
     int64_t sequence_stride, head_stride, capacity;
 };
 
-// How a call of kv_weights is cut: sequences of few rows, those of many, each with pieces of the keys for the first pass (KvPart).  The workspace has few's pieces, many's, and many's rows as operands with their factors.
+// How a call of kv_weights is cut: sequences of few rows, those of many, each with pieces of the keys for the first pass (KvPart).  The workspace has few's pieces, its scores where they are kept, many's pieces, and many's rows as operands with their factors.
 struct KvWeightsPlan {
     KvPart few, many;              // tile 0: none of these
     size_t few_bytes, many_bytes;  // of the workspace that pieces take
+    int64_t score_stride;          // few's scores, from one row to the next, and what they take of the workspace; 0: they are made twice
+    size_t score_bytes;
     int64_t row_tiles;             // of 16 rows, of a head, whose operands and factors are in it
     size_t rows_bytes;
     int64_t units;                 // workgroups of many's second pass, for a head

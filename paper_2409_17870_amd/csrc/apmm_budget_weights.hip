@@ -6,8 +6,10 @@
 // meet at the end, one that owns some keys and goes through the rows.  No sum's order depends on timing.  (m and 1 / l are kept apart: one number m + log2(l) would be rounded to 2^-24 of itself, which
 // is more than the sums' own error.)
 //
-// Few rows of a sequence (up to 16: token generation): both passes have the same workgroups, a piece of the keys each, and read the keys from memory; the second joins the pieces' m and l as it begins.  8 sequences of up
-// to 32768 tokens, 8 key/value heads of 128 and 4 query heads to one read 111 MB of keys twice, 34 and 40 us: more than HBM's time, since half of a step's instructions make operands of codes for 4 rows of 16.
+// Few rows of a sequence (up to 16: token generation): both passes have the same workgroups, a piece of the keys each; the second joins the pieces' m and l as it begins.  The first keeps its scores for the second, a
+// number for each row and key, where they are no more than 2^26; else, and for the sequences of few rows beside others of many, the second makes them again from the keys.  8 sequences of up to 32768 tokens, 8 key/value
+// heads of 128: 4 query heads to one 56 us with scores kept (38 and 14; 111 MB of keys, 26 MB of scores written and read) and 78 with scores made twice (34 and 40), 6 60 and 78; 4 sequences of 8 to one 39 and 49, 16 to one
+// of 4 heads 32 and 35; one sequence of 3000 tokens 19 and 24.  Bound by HBM and, at the beginnings, by the way from lengths to pages to codes.
 // Many: the second pass has blocks of 256 keys (fewer where there are few of them), as operands in registers, and every row that sees some of them comes by through LDS, as the first pass left it in the workspace (RowTiles).  Bound by
 // the vector unit: of a score's 7 issues the exponential takes four.  4096 tokens of 32 heads of 128: 122 us for each pass, the unit busy for 75 and 67 of them.  Half as many workgroups, each with a first and a
 // last block, took 257 us in all for 247; the next tile's operands read ahead, or its products made ahead, take registers that a fourth wave to a SIMD has (123 and 131 us for 121).
@@ -23,6 +25,7 @@ namespace {
 constexpr int kStep = 32;     // keys of a step of the first pass
 constexpr int kWaves = 4;
 constexpr int kFew = 16;      // rows of a sequence that are few
+constexpr int64_t kMostScores = 64 << 20;  // few rows' that are kept in the workspace
 constexpr int kChunk = 4;     // tiles of 16 rows that are in LDS at a time
 
 struct RowFactor { float base, by; };  // -m and 1 / l; zeros for a row that sees nothing
@@ -33,6 +36,12 @@ struct RowTiles {
     uint8_t *operands;    // [tile][head][operand][lane] of 16 bytes
     RowFactor *factors;   // [tile][head][16]
     float *scales;        // [tile][head][16]: what makes a score of a product and the key's scale
+};
+// Few rows' scores, in powers of two, by the first pass for the second: of each row of the call and head as many as the page table has tokens, of those keys that the row's tile visits
+struct RowScores {
+    float *data;
+    int64_t stride;
+    __device__ __forceinline__ float *of(const KvAttentionArgs &a, int row, int head) const { return data + ((int64_t)row * a.c.heads + head) * stride; }
 };
 // The first tile of sequence b: the tiles of the sequences before it end below
 __device__ __forceinline__ int first_tile(const KvAttentionArgs &a, const KvSequence &s, int b) { return (int)((int64_t)s.start * a.groups / 16) + b; }
@@ -161,8 +170,8 @@ __device__ __forceinline__ float max_of_three(float x, float y, float z)
 }
 
 // First pass.  A workgroup has R tiles of 16 rows and a piece of the keys that they see, its waves take steps in turn, the next step's codes on their way while one's scores are made.
-template <int D, bool BF16, int R>
-__global__ __launch_bounds__(64 * kWaves, R == 1 ? 4 : 2) void kv_statistics_kernel(KvAttentionArgs a, KvPart part, float *pieces, RowTiles out)
+template <int D, bool BF16, int R, bool SCORES>
+__global__ __launch_bounds__(64 * kWaves, R == 1 ? 4 : 2) void kv_statistics_kernel(KvAttentionArgs a, KvPart part, float *pieces, RowTiles out, RowScores scores)
 {
     constexpr int W = D / 32, T = 16 * R;
     __shared__ float bases[kWaves][T], totals[kWaves][T];
@@ -246,6 +255,11 @@ __global__ __launch_bounds__(64 * kWaves, R == 1 ? 4 : 2) void kv_statistics_ker
                     x[i] = hidden ? -__builtin_inff() : x[i];
                 }
             }
+            if (SCORES && n < rows) {
+                float *const at = scores.of(a, it.s.start * a.groups + it.row0 + n, head) + key0 + 4 * g;
+#pragma unroll
+                for (int t = 0; t < 2; ++t) *reinterpret_cast<float4 *>(at + 16 * t) = make_float4(x[4 * t] * factor[r], x[4 * t + 1] * factor[r], x[4 * t + 2] * factor[r], x[4 * t + 3] * factor[r]);
+            }
             const float high = max_of_three(max_of_three(x[0], x[1], x[2]), max_of_three(x[3], x[4], x[5]), max_of_three(x[6], x[7], x[7])) * factor[r], to = max_of_three(top[r], high, high);
             float sum = 0.0f;
 #pragma unroll
@@ -306,28 +320,104 @@ __device__ __forceinline__ float sums_of_eight(const float (&x)[8], int n)
     return s + other(s, std::integral_constant<int, 0xb1>());
 }
 
-// Second pass of few rows, on the first one's pieces.  A sequence that has more than one tile of rows all the same has its keys shared out anew among the first tile's workgroups, which go through the tiles.
-template <int D, bool BF16>
-__global__ __launch_bounds__(64 * kWaves, 3) void kv_weights_few_kernel(KvAttentionArgs a, KvPart part, float *pieces, KvWeights out, float decay)
+// A second pass' piece of few rows' first one.  A sequence that has more than one tile of rows all the same has its keys shared out anew among the first tile's workgroups, which go through the tiles.
+__device__ __forceinline__ bool few_item(const KvAttentionArgs &a, const KvPart &part, int slot, int head, const KvWeights &out, float decay, KvItem<kStep> &it, int &all_rows, int &tiles, int &first_slot, int &end,
+                                         float *&weights)
 {
-    constexpr int W = D / 32;
-    const int slot = kv_divide(blockIdx.x, a.c.by_heads), head = blockIdx.x - slot * a.c.heads, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = kv_lane(), n = lane & 15, g = lane >> 4;
-    KvItem<kStep> it;
-    if (!kv_item<kStep, kFew>(a, part, slot, it)) return;
-    const int all_rows = it.s.n * a.groups, tiles = (all_rows + kFew - 1) / kFew, tile = it.row0 / kFew, first_slot = slot - it.part - (tiles - 1 - tile) * it.pieces;  // (the last tile comes first)
-    if (tile) return;
+    if (!kv_item<kStep, kFew>(a, part, slot, it)) return false;
+    all_rows = it.s.n * a.groups;
+    tiles = (all_rows + kFew - 1) / kFew;
+    const int tile = it.row0 / kFew;
+    first_slot = slot - it.part - (tiles - 1 - tile) * it.pieces;  // (the last tile comes first)
+    if (tile) return false;
     if (tiles > 1) {
         const int steps = (it.s.keys + kStep - 1) / kStep;
         it.from = (int)((int64_t)steps * it.part / it.pieces);
         it.to = (int)((int64_t)steps * (it.part + 1) / it.pieces);
         it.sink_steps = it.gap = 0;
     }
-    float *const weights = out.data + it.b * out.sequence_stride + head * out.head_stride;
-    const int end = (int)min((int64_t)it.s.keys, out.capacity);
+    weights = out.data + it.b * out.sequence_stride + head * out.head_stride;
+    end = (int)min((int64_t)it.s.keys, out.capacity);
     if (it.gap && decay != 1.0f) {  // keys that a window hides from every row
         const int from = (it.sink_steps + (int)((int64_t)it.gap * it.part / it.pieces)) * kStep, to = min((it.sink_steps + (int)((int64_t)it.gap * (it.part + 1) / it.pieces)) * kStep, end);
         for (int key = from + (int)threadIdx.x; key < to; key += 64 * kWaves) weights[key] = decay == 0.0f ? 0.0f : decay * weights[key];
     }
+    return true;
+}
+// Row min(n, rows - 1) of a tile: its pieces' m and l, quarter g of them to a lane, joined
+__device__ __forceinline__ RowFactor tile_row(const KvAttentionArgs &a, const KvPart &part, float *pieces, const KvItem<kStep> &it, int head, int tile, int tiles, int first_slot, int rows, int n, int g)
+{
+    float top = kLowest, total = 0.0f;
+    // (there are slots for all pieces but where starts do not ascend: as in kv_note)
+    const int from = first_slot + (tiles - 1 - tile) * it.pieces, there = min(it.pieces, part.slots - from);
+#pragma unroll 4
+    for (int i = g; i < there; i += 4) {
+        const float2 p = piece_rows(a, pieces, part, from + i, head)[min(n, rows - 1)];
+        join(top, total, p.x, p.y);
+    }
+    join(top, total, __shfl_xor(top, 16), __shfl_xor(total, 16));
+    join(top, total, __shfl_xor(top, 32), __shfl_xor(total, 32));
+    RowFactor f = factor_of(top, total);
+    if (n >= rows) f.by = 0.0f;  // (the last row again)
+    return f;
+}
+
+// Second pass of few rows whose scores the first one has kept: a lane has four keys, a wave eight steps at a time.
+__global__ __launch_bounds__(64 * kWaves) void kv_weights_scored_kernel(KvAttentionArgs a, KvPart part, float *pieces, RowScores scores, KvWeights out, float decay)
+{
+    __shared__ RowFactor factors[kFew];
+    __shared__ int positions[kFew];
+    const int slot = kv_divide(blockIdx.x, a.c.by_heads), head = blockIdx.x - slot * a.c.heads, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = kv_lane(), n = lane & 15, g = lane >> 4;
+    KvItem<kStep> it;
+    int all_rows, tiles, first_slot, end;
+    float *weights;
+    if (!few_item(a, part, slot, head, out, decay, it, all_rows, tiles, first_slot, end, weights)) return;
+    for (int tile = 0; tile < tiles; ++tile) {
+        const int rows = min(all_rows - tile * kFew, kFew);
+        __syncthreads();
+        if (wave == 0) {
+            const RowFactor f = tile_row(a, part, pieces, it, head, tile, tiles, first_slot, rows, n, g);
+            if (g == 0) {
+                factors[n] = f;
+                positions[n] = it.s.first + kv_divide(tile * kFew + min(n, rows - 1), a.by_groups);
+            }
+        }
+        __syncthreads();
+        for (int v = it.from + 8 * wave + (lane >> 3); v < it.to; v += 8 * kWaves) {
+            const int key = it.key_of(v) + 4 * (lane & 7);
+            float p[4] = {}, before[4] = {};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if ((tile || decay != 0.0f) && key + i < end) before[i] = weights[key + i];
+#pragma unroll 4
+            for (int r = 0; r < rows; ++r) {
+                const float4 x = *reinterpret_cast<const float4 *>(scores.of(a, it.s.start * a.groups + tile * kFew + r, head) + key);
+                const RowFactor f = factors[r];
+                const int pos = positions[r], below = a.window ? pos - a.window : INT32_MIN;
+                const float s[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float w = __builtin_amdgcn_exp2f(s[i] + f.base) * f.by;
+                    p[i] += (key + i > pos) | ((key + i <= below) & (key + i >= a.sinks)) ? 0.0f : w;  // (what the row's tile did not visit was not written)
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (key + i < end) weights[key + i] = tile ? before[i] + p[i] : decay == 0.0f ? p[i] : fmaf(decay, before[i], p[i]);
+        }
+    }
+}
+
+// Second pass of few rows, on the first one's pieces, which makes the scores again.
+template <int D, bool BF16>
+__global__ __launch_bounds__(64 * kWaves, 3) void kv_weights_few_kernel(KvAttentionArgs a, KvPart part, float *pieces, KvWeights out, float decay)
+{
+    constexpr int W = D / 32;
+    const int slot = kv_divide(blockIdx.x, a.c.by_heads), head = blockIdx.x - slot * a.c.heads, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = kv_lane(), n = lane & 15, g = lane >> 4;
+    KvItem<kStep> it;
+    int all_rows, tiles, first_slot, end;
+    float *weights;
+    if (!few_item(a, part, slot, head, out, decay, it, all_rows, tiles, first_slot, end, weights)) return;
     int v = it.from + wave, ids = kv_page_ids(a, it, v, kWaves), id = 0;
     if (v >= it.to) return;
     KeyCodes<D> codes[2], next[2];
@@ -347,19 +437,8 @@ __global__ __launch_bounds__(64 * kWaves, 3) void kv_weights_few_kernel(KvAttent
     auto take = [&](int tile) {
         rows = min(all_rows - tile * kFew, kFew);
         const int row = tile * kFew + min(n, rows - 1);
-        float top = kLowest, total = 0.0f;
-        // (there are slots for all pieces but where starts do not ascend: as in kv_note)
-        const int from = first_slot + (tiles - 1 - tile) * it.pieces, there = min(it.pieces, part.slots - from);
-#pragma unroll 4
-        for (int i = g; i < there; i += 4) {
-            const float2 p = piece_rows(a, pieces, part, from + i, head)[min(n, rows - 1)];
-            join(top, total, p.x, p.y);
-        }
         take_rows<D, BF16>(a, it.s.start, head, row, q, factor);
-        join(top, total, __shfl_xor(top, 16), __shfl_xor(total, 16));
-        join(top, total, __shfl_xor(top, 32), __shfl_xor(total, 32));
-        f = factor_of(top, total);
-        if (n >= rows) f.by = 0.0f;  // (the last row again)
+        f = tile_row(a, part, pieces, it, head, tile, tiles, first_slot, rows, n, g);
         pos = n < rows ? it.s.first + kv_divide(row, a.by_groups) : INT32_MIN;
         first_pos = it.s.first + kv_divide(tile * kFew, a.by_groups);
         last_pos = it.s.first + kv_divide(tile * kFew + rows - 1, a.by_groups);
@@ -534,7 +613,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_weights_many_kernel(KvAtten
 template <int D, bool BF16>
 void launch(const KvAttentionArgs &a, const KvWeights &w, float decay, const KvWeightsPlan &p, hipStream_t stream)
 {
-    float *few = a.partial, *many = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(a.partial) + p.few_bytes);
+    float *few = a.partial, *many = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(a.partial) + p.few_bytes + p.score_bytes);
     RowTiles tiles;
     tiles.operands = reinterpret_cast<uint8_t *>(many) + p.many_bytes;
     tiles.factors = reinterpret_cast<RowFactor *>(tiles.operands + p.row_tiles * a.c.heads * (D / 32) * 1024);
@@ -542,12 +621,18 @@ void launch(const KvAttentionArgs &a, const KvWeights &w, float decay, const KvW
     const dim3 block(64 * kWaves);
     if (p.few.tile) {
         const dim3 groups((uint32_t)((int64_t)p.few.slots * a.c.heads));
-        kv_statistics_kernel<D, BF16, 1><<<groups, block, 0, stream>>>(a, p.few, few, RowTiles{});
-        kv_weights_few_kernel<D, BF16><<<groups, block, 0, stream>>>(a, p.few, few, w, decay);
+        if (p.score_bytes) {
+            const RowScores scores = {reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(few) + p.few_bytes), p.score_stride};
+            kv_statistics_kernel<D, BF16, 1, true><<<groups, block, 0, stream>>>(a, p.few, few, RowTiles{}, scores);
+            kv_weights_scored_kernel<<<groups, block, 0, stream>>>(a, p.few, few, scores, w, decay);
+        } else {
+            kv_statistics_kernel<D, BF16, 1, false><<<groups, block, 0, stream>>>(a, p.few, few, RowTiles{}, RowScores{});
+            kv_weights_few_kernel<D, BF16><<<groups, block, 0, stream>>>(a, p.few, few, w, decay);
+        }
     }
     if (p.many.tile) {
         const dim3 groups((uint32_t)((int64_t)p.many.slots * a.c.heads)), units((uint32_t)(p.units * a.c.heads));
-        kv_statistics_kernel<D, BF16, 4><<<groups, block, 0, stream>>>(a, p.many, many, tiles);
+        kv_statistics_kernel<D, BF16, 4, false><<<groups, block, 0, stream>>>(a, p.many, many, tiles, RowScores{});
         if (p.many.target) kv_statistics_join_kernel<<<groups, dim3(64), 0, stream>>>(a, p.many, many, tiles);
         if (p.key_tiles == 2) kv_weights_many_kernel<D, BF16, 2><<<units, block, 0, stream>>>(a, w, decay, tiles, p.many.from_rows);
         else if (p.key_tiles == 4) kv_weights_many_kernel<D, BF16, 4><<<units, block, 0, stream>>>(a, w, decay, tiles, p.many.from_rows);
@@ -582,6 +667,8 @@ KvWeightsPlan kv_weights_plan(const KvArgs &c, int groups, int window, int sinks
         p.few.least = 32;
         cut(p.few, c, groups, window, sinks, few ? std::min(c.tokens * (int64_t)((groups + kFew - 1) / kFew), rows / kFew + sequences) : sequences, 1024, 4096);  // (8 sequences of up to 32768 tokens: 78 us; 512 pieces 87, 1536 and 2048 85)
         p.few_bytes = (size_t)p.few.slots * c.heads * kFew * sizeof(float2);
+        p.score_stride = blocks_of(c, kStep) / c.sequences * kStep;
+        if (few && rows * c.heads * p.score_stride <= kMostScores) p.score_bytes = (size_t)(rows * c.heads * p.score_stride) * sizeof(float);
     }
     if (!few) {
         p.many.tile = 64;
@@ -598,7 +685,7 @@ KvWeightsPlan kv_weights_plan(const KvArgs &c, int groups, int window, int sinks
     return p;
 }
 
-size_t kv_weights_bytes(const KvWeightsPlan &p) { return p.few_bytes + p.many_bytes + p.rows_bytes; }
+size_t kv_weights_bytes(const KvWeightsPlan &p) { return p.few_bytes + p.score_bytes + p.many_bytes + p.rows_bytes; }
 int64_t kv_weights_items(const KvWeightsPlan &p, int heads) { return std::max(std::max((int64_t)p.few.slots, (int64_t)p.many.slots), p.units) * heads * 64 * kWaves; }
 
 hipError_t launch_kv_weights(const KvAttentionArgs &a, const KvWeights &w, float decay, const KvWeightsPlan &p, hipStream_t stream)

@@ -10,6 +10,7 @@ struct dim3 {
     dim3(uint32_t x, uint32_t y = 1) : x(x), y(y) {}
 };
 struct float4 { float x, y, z, w; };
+inline float4 make_float4(float x, float y, float z, float w) { return {x, y, z, w}; }
 
 namespace host_layers {
 

@@ -71,6 +71,10 @@ CASES = [  # D, heads, groups, page, lengths, new, window, sinks
     (64, 1, 1, 256, [1500], [700], 0, 0),
     (128, 1, 1, 16, [520], [520], 16, 0),
     (64, 1, 1, 16, [513], [300], 1, 0),                                      # each query sees itself alone
+    (64, 1, 2, 16, [1100] + [30] * 24, [20] + [0] * 20 + [1] * 4, 0, 0),     # no more tokens than sequences, of which one has most
+    (128, 2, 4, 16, [100] + [30] * 24, [20] + [0] * 20 + [1] * 4, 40, 3),
+    (64, 1, 8, 16, [1100] + [30] * 24, [20] + [0] * 20 + [1] * 4, 0, 0),
+    (128, 1, 5, 32, [100, 333] + [30] * 23, [20, 3] + [0] * 20 + [1] * 3, 40, 3),
 ]
 
 
@@ -91,6 +95,9 @@ def test_weights(gpu, case, dtype):
         base = before if decay else torch.zeros_like(before)
         want, near = weights_of(torch, b, b.q, base, b.starts, window, sinks, D ** -0.5 if scale is None else scale, decay)
         for i, length in enumerate(lengths):
+            if new[i] == 0:                                                  # keeps what is there, the NaN too
+                assert torch.equal(torch.nan_to_num(got[i], 7.0), torch.nan_to_num(before[i], 7.0))
+                continue
             assert bool(((got[i, :, :length].cpu().double() - want[i, :, :length]).abs() <= near[i, :, :length]).all()), (decay, i)
             assert torch.equal(torch.nan_to_num(got[i, :, length:], 7.0), torch.nan_to_num(before[i, :, length:], 7.0))
             if decay == 0 and length:                                        # each query gives 1 in all
@@ -109,6 +116,21 @@ def test_cut_rows_of_long_sequences(gpu):
         want, near = weights_of(torch, b, b.q, torch.zeros_like(w), b.starts, window, sinks, 64 ** -0.5, 1.0)
         assert bool(((w.cpu().double() - want).abs() <= near).all())
     assert binding.apmm_kv_weights_workspace_bytes(5, 6, *b.args) > 5 * 6 * 8
+
+
+def test_wide_table(gpu):
+    """Few rows whose scores, as far as the table goes, would take more room than is given to them."""
+    torch, binding = gpu
+    for D, dtype, window in ((64, torch.float16, 0), (128, torch.bfloat16, 300)):
+        b = Batch(torch, dtype, D, 2, 2, 16, [1700, 40], [1, 1], seed=15)
+        wide = torch.full((2, 1 << 20), -1, dtype=torch.int32)
+        wide[:, :b.table.shape[1]] = b.table
+        args = [b.args[0], b.args[1], wide.cuda(), b.args[3]]
+        assert binding.apmm_kv_weights_workspace_bytes(2, 4, *args) < binding.apmm_kv_weights_workspace_bytes(2, 4, *args[:2], args[2][:, :1 << 18].contiguous(), args[3])
+        for a in (b.args, args):
+            w = binding.apmm_kv_weights(b.q, *a, torch.ones((2, 2, 1700), device="cuda"), window=window, sinks=5)
+            want, near = weights_of(torch, b, b.q, torch.ones((2, 2, 1700)), b.starts, window, 5, D ** -0.5, 1.0)
+            assert bool(((w.cpu().double() - want).abs() <= near).all())
 
 
 def test_capacity_strides_streams_workspace_and_graph(gpu):

@@ -81,11 +81,11 @@ def test_weights(lib):  # noqa: F811
     assert need >= 7 * 32 * 8 and need % 8 == 0
     assert weigh(lib, workspace=0xc000, size=need - 1) == WORKSPACE and weigh(lib, workspace=0xc008, size=need) == INVALID
     assert lib.apmm_kv_weights_workspace_bytes(*structs(batch=dict(tokens=0)), 32) == 0 and lib.apmm_kv_weights_workspace_bytes(*structs(), 33) == 0
-    for tokens in (1, 3, 33, 1000, 100000):                            # whatever lengths the batch has: as much as the queries and some MiB
+    for tokens in (1, 3, 33, 1000, 100000):                            # whatever lengths the batch has: as much as the queries and 320 MiB
         for sequences in (1, 2, 64, 1000):
             for kv_heads in (1, 8, 32, 1024):
                 size = lib.apmm_kv_weights_workspace_bytes(*structs(dict(kv_heads=kv_heads), dict(tokens=tokens, sequences=sequences, table_width=1 << 16, table_stride=1 << 16)), kv_heads * 4)
-                assert 0 < size <= (tokens * 4 + 16 * (sequences + 1)) * kv_heads * (256 + 12) + min(tokens, sequences) * kv_heads * 2 * 128 + (64 << 20)
+                assert 0 < size <= (tokens * 4 + 16 * (sequences + 1)) * kv_heads * (256 + 12) + min(tokens, sequences) * kv_heads * 2 * 128 + (320 << 20)
 
 
 def test_eviction(lib):  # noqa: F811

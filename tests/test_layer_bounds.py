@@ -51,6 +51,8 @@ SMALL = [  # D, heads, groups, page, lengths, new, window, sinks
     (128, 1, 3, 16, [70, 40], [20, 3], 30, 2),
     (64, 1, 1, 64, [200, 1], [150, 1], 0, 0),
     (128, 1, 16, 16, [2100], [1], 0, 0),
+    (64, 1, 2, 16, [700] + [30] * 12, [9] + [0] * 9 + [1] * 3, 300, 3),
+    (64, 1, 5, 16, [700] + [30] * 12, [9] + [0] * 9 + [1] * 3, 300, 3),
 ]
 
 
