@@ -1,4 +1,4 @@
-// Four-bit weights with group scales times 16-bit activations (apmm_w4.h): packing, the kernel for up to sixteen tokens, and which kernel a call takes.
+// Four-bit weights with group scales times 16-bit activations (apmm_w4.h): packing, the kernel for few tokens, and which kernel a call takes.
 //
 // The codes' odd integers are exact in both types and so are their products with the activations in 32 bits; a group's sum is multiplied with its scale in 32 bits, results are rounded once.
 #include <algorithm>
@@ -42,7 +42,7 @@ __device__ __forceinline__ float4v multiply(typename W4Type<BF16>::Eight a, type
     else return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
-// Few tokens.  A workgroup has 16 C channels and 16 T tokens, its waves take blocks of 128 inputs in turn, the next block's weights and activations on their way while one is multiplied, and meet in LDS.
+// Up to 32 tokens.  A workgroup has 16 C channels and 16 T tokens, its waves take blocks of 128 inputs in turn, the next block's weights and activations on their way while one is multiplied, and meet in LDS.
 // Activations come from the caches into each wave's registers: they are no two waves' of a workgroup.  Bound by HBM and the way there: one token of 11008 x 4096 23 MB in 8.0 us, of 4096 x 4096 in 4.3 as
 // called; at sixteen tokens by the activations beside it, which every workgroup reads (9.7 us).
 template <bool BF16, int GROUP, int T, int C>
@@ -154,7 +154,11 @@ template <bool BF16, int GROUP>
 void launch(const W4Args &a, const W4Rule &r, hipStream_t stream)
 {
     const dim3 grid((uint32_t)((a.N + kW4Tile * r.c - 1) / (kW4Tile * r.c)), (uint32_t)((a.M + 16 * r.t - 1) / (16 * r.t)));
-    if (r.c == 3 && r.waves == 16) w4_rows_kernel<BF16, GROUP, 1, 3, 16><<<grid, dim3(1024), 0, stream>>>(a);
+    if (r.t == 2) {
+        if (r.c == 3) w4_rows_kernel<BF16, GROUP, 2, 3, 8><<<grid, dim3(512), 0, stream>>>(a);
+        else if (r.c == 2) w4_rows_kernel<BF16, GROUP, 2, 2, 8><<<grid, dim3(512), 0, stream>>>(a);
+        else w4_rows_kernel<BF16, GROUP, 2, 1, 8><<<grid, dim3(512), 0, stream>>>(a);
+    } else if (r.c == 3 && r.waves == 16) w4_rows_kernel<BF16, GROUP, 1, 3, 16><<<grid, dim3(1024), 0, stream>>>(a);
     else if (r.c == 3) w4_rows_kernel<BF16, GROUP, 1, 3, 8><<<grid, dim3(512), 0, stream>>>(a);
     else if (r.c == 2 && r.waves == 16) w4_rows_kernel<BF16, GROUP, 1, 2, 16><<<grid, dim3(1024), 0, stream>>>(a);
     else if (r.c == 2) w4_rows_kernel<BF16, GROUP, 1, 2, 8><<<grid, dim3(512), 0, stream>>>(a);
@@ -177,6 +181,8 @@ hipError_t launch_w4_pack(const uint8_t *codes, const uint16_t *scales, const W4
 // Up to sixteen tokens: w4_rows_kernel.  As many tiles of channels to a workgroup, up to three, as leave the compute unit that has most with the fewest, and of equals the most, since every workgroup reads all
 // activations (one and sixteen tokens, with one, two and three: 688 tiles of 4096 inputs 9.0, 9.4, 8.0 and 14.8, 12.5, 9.7 us; 320 of 13824 16.7, 15.5, 19.4 and 30.4, 19.5, 23.1; 256 of 4096 4.3, 5.4, 6.8 and 6.2,
 // 6.9, 8.2; 1376 of 4096 15.3, 13.4, 13.3 and 27.0, 17.4, 16.3; four are never the least).  Sixteen waves where each then has four blocks and more (256 tiles of 11008 inputs 10.1 and 8.3 us, of 4096 inputs no difference).
+// The same kernel with two blocks of tokens for up to 32, where the inputs and the compute units' tiles are few (17 and 32 tokens, this and w4_tiles_kernel: 11008 x 4096 11.5, 13.6 and 15.1, 16.9 us; 4096 x 4096 7.2, 9.8
+// and 9.4, 10.6; 11008 x 2048 7.1, 8.4 and 11.0, 12.6; but 4096 x 6144 10.2, 14.1 and 11.0, 12.1, 22016 x 4096 20.9, 25.0 and 20.9, 22.2).
 //
 // More: w4_tiles_kernel, with the tokens and shares that promise the least time.  A workgroup takes 0.45 + 0.2 T us a block where it is alone on its compute unit and 0.3 + 0.17 T for each on it where there
 // are more, its launch and the way to the first block are the same for all; shares cost a launch of 3.5 us and their sums' way out and in.  (77 x 5119 x 13800 in shares of 4: 39 us, 8: 34, 12: 30; 128 x 4096 x
@@ -185,16 +191,17 @@ W4Rule w4_rule(int64_t M, int64_t N, int64_t blocks)
 {
     W4Rule r = {false, 1, 1, 1, 8};
     const int64_t tiles = (N + kW4Tile - 1) / kW4Tile;
-    if (M <= 16) {
-        int64_t least = INT64_MAX;
-        for (int c = 1; c <= 3; ++c) {
-            const int64_t on_unit = ((tiles + c - 1) / c + 255) / 256 * c;
-            if (on_unit <= least) {
-                least = on_unit;
-                r.c = c;
-            }
+    int64_t tiles_on_unit = INT64_MAX;
+    for (int c = 1; c <= 3; ++c) {
+        const int64_t n = ((tiles + c - 1) / c + 255) / 256 * c;
+        if (n <= tiles_on_unit) {
+            tiles_on_unit = n;
+            r.c = c;
         }
-        r.waves = blocks >= 64 ? 16 : 8;
+    }
+    if (M <= 16 || (M <= 32 && blocks <= 32 && tiles_on_unit <= 3)) {
+        r.t = M <= 16 ? 1 : 2;
+        r.waves = M <= 16 && blocks >= 64 ? 16 : 8;
         return r;
     }
     r.tiles = true;

@@ -1,4 +1,4 @@
-// Four-bit weights with group scales times 16-bit activations (apmm_w4.h), more tokens than one block of sixteen.
+// Four-bit weights with group scales times 16-bit activations (apmm_w4.h), more tokens than few.
 //
 // A workgroup has 128 channels, 32 to each of its four waves, 32 T tokens and a share of the inputs.  Activations of 128 inputs at a time go through LDS, straight from memory, the next blocks on their way
 // while one is used; a wave's weights come into registers as codes and become operands there: no two waves unpack the same.  Where there are few tiles the inputs are cut in shares, whose sums of 32 bits

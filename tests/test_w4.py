@@ -35,7 +35,7 @@ def close(torch, got, want, near):
 
 
 SIZES = [(1, 1, 1), (1, 16, 128), (1, 17, 129), (2, 40, 31), (15, 33, 127), (16, 64, 256), (17, 100, 640), (33, 7, 1000), (48, 130, 95), (64, 257, 512), (65, 96, 384), (100, 300, 200),
-         (129, 513, 136), (200, 256, 1024), (256, 1000, 64), (300, 48, 2000), (1, 4096, 2048), (7, 1030, 4100)]
+         (129, 513, 136), (200, 256, 1024), (256, 1000, 64), (300, 48, 2000), (1, 4096, 2048), (7, 1030, 4100), (31, 600, 130), (32, 40, 4096), (20, 50, 4200), (18, 12400, 70)]
 
 
 @pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
