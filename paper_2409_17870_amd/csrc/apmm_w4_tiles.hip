@@ -4,10 +4,11 @@
 // while one is used; a wave's weights come into registers as codes and become operands there: no two waves unpack the same.  Where there are few tiles the inputs are cut in shares, whose sums of 32 bits
 // meet in a second launch.
 // A group's sum is multiplied with its scale in 32 bits, one instruction for each result and group.  (With weights times scales rounded to 16 bits it is none, a wave has registers for 64 channels, and
-// 2048 x 11008 x 4096 takes 190 us in place of 205, at 1.4 times the error of an exact product's rounding; groups of 32 inputs 205 in place of 260.)
+// 2048 x 11008 x 4096 took 190 us where this form then took 205, at 1.4 times the error of an exact product's rounding; groups of 32 inputs 205 and 260.)
 //
 // What bounds many tokens: LDS, which gives every wave all of the block's activations, 128 bytes a clock at the full rate of the matrix unit, and beside it the vector unit (unpacking 43 % (bfloat16) or 28 %
 // (binary16) of the matrix unit's time at T = 4, the groups' products 25, 50 or 100 %): two workgroups on a compute unit, so that one's vector instructions run under the other's products.
+// 2048 x 11008 x 4096 takes 196 us, 943 TFLOP/s.  (A wave with 64 channels, which halves what is read from LDS, took 207 to 260, with two waves to a vector unit or one: it is not LDS alone.)
 // What bounds a few: a workgroup's way from its first load to its first product (5 us with launch and join), then 0.45 + 0.2 T us a block for one workgroup to a compute unit.
 #include <type_traits>
 
@@ -106,19 +107,28 @@ __global__ __launch_bounds__(64 * kWaves, 2) void w4_tiles_kernel(W4Args a, int 
         // behind this block's loads there are those of R - 2 others, each as many (a last block that ends within has its rows waited for as they are loaded), or fewer at the end
         if (b + R - 2 < last) wait_and_meet<(R - 2) * kLoads>();
         else wait_and_meet<0>();
+        const uint4 w0 = weights[at].w[0], w1 = weights[at].w[1];
+        uint32_t words[8] = {w0.x, w1.x, w0.y, w1.y, w0.z, w1.z, w0.w, w1.w};  // of sixteen inputs each, this lane's half of them
+        float scales_of[kGroups];
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) scales_of[g] = w4_scale<BF16>(weights[at].s[g]);
+        // taken here, before the next loads are begun: a first use behind them would be waited for with all of them, since the compiler cannot tell how many they are (256 x 11008 x 4096 44 us in place of 51, 2048 196 in
+        // place of 205)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) asm volatile("" : "+v"(words[i]));
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) asm volatile("" : "+v"(scales_of[g]));
         if (b + R - 1 < last) {
             load_weights(b + R - 1, weights[(at + R - 1) % R]);
             stage(b + R - 1, (at + R - 1) % R);
         }
-        const uint4 w0 = weights[at].w[0], w1 = weights[at].w[1];
-        const uint32_t words[8] = {w0.x, w1.x, w0.y, w1.y, w0.z, w1.z, w0.w, w1.w};  // of sixteen inputs each, this lane's half of them
         const uint4 *here = &rows[at][n * 16];
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
             Eight w[kSteps];
 #pragma unroll
             for (int k = 0; k < kSteps; ++k) w[k] = w4_operand<BF16>(words[g * kSteps + k]);
-            const float scale = w4_scale<BF16>(weights[at].s[g]);
+            const float scale = scales_of[g];
 #pragma unroll
             for (int t = 0; t < T; ++t) {
                 float16v part;
