@@ -1,6 +1,6 @@
 // Four-bit weights with group scales times 16-bit activations (apmm_w4.h), more tokens than few.
 //
-// A workgroup has 128 channels, 32 to each of its four waves, 32 T tokens and a share of the inputs.  Activations of 128 inputs at a time go through LDS, straight from memory, the next blocks on their way
+// A workgroup has 128 channels, 32 to each of its four waves (or pairs of waves), 32 T tokens and a share of the inputs.  Activations of 128 inputs at a time go through LDS, straight from memory, the next blocks on their way
 // while one is used; a wave's weights come into registers as codes and become operands there: no two waves unpack the same.  Where there are few tiles the inputs are cut in shares, whose sums of 32 bits
 // meet in a second launch.
 // A group's sum is multiplied with its scale in 32 bits, one instruction for each result and group.  (With weights times scales rounded to 16 bits it is none, a wave has registers for 64 channels, and
@@ -41,15 +41,20 @@ __device__ __forceinline__ void wait_and_meet() { asm volatile("s_waitcnt vmcnt(
 // Blocks of activations in LDS: the one in use and those on their way.  As many as leave room for two workgroups on a compute unit (three of one block of tokens).
 constexpr int ring_of(int t) { return t == 1 ? 6 : t == 2 ? 4 : t == 3 ? 3 : 2; }
 
+// Two waves to the same channels, half of a block's inputs each, where the groups' products keep a wave busy between matrix instructions (groups of 32, with and without: 77 x 5119 x 13800 34 and 41 us, 96 x 11008 x 4096
+// 29 and 35, 64 x 5119 x 13800 26 and 31; groups of 64 31 and 36, 27 and 31, 25 and 28; of 128 no difference; one block of tokens 17 and 16 us, four have no registers for it)
+constexpr int halves_of(int group, int t) { return group < 128 && (t == 2 || t == 3) ? 2 : 1; }
+
 // DIRECT: rows of x begin at multiples of 16 bytes and a tile's lie within 2^31 bytes
 template <bool BF16, int GROUP, int T, bool DIRECT>
-__global__ __launch_bounds__(64 * kWaves, 2) void w4_tiles_kernel(W4Args a, int tiles_m, int shares)
+__global__ __launch_bounds__(64 * kWaves * halves_of(GROUP, T), 2 * halves_of(GROUP, T)) void w4_tiles_kernel(W4Args a, int tiles_m, int shares)
 {
     typedef typename W4Type<BF16>::Eight Eight;
-    constexpr int kGroups = kW4Block / GROUP, kTokens = 32 * T, kSteps = GROUP / 16, R = ring_of(T);
-    constexpr int kLoads = 2 * T + 2 + kGroups;  // of a wave for a block: activations, codes, scales
+    constexpr int H = halves_of(GROUP, T), kPart = kW4Block / H;  // inputs of a block that a wave multiplies
+    constexpr int kGroups = kPart / GROUP, kTokens = 32 * T, kSteps = GROUP / 16, R = ring_of(T);
+    constexpr int kRows = 2 * T / H, kLoads = kRows + 2 + kGroups;  // of a wave for a block: activations, codes, scales
     __shared__ uint4 rows[R][kTokens * 16];      // [token][eight of inputs, its number xor token % 16]
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
+    const int any_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = any_wave % kWaves, half = any_wave / kWaves, lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
     // a die's workgroups (every eighth) take work that follows each other: the shares of a tile, then the tiles of the same channels, whose weights meet in its L2
     const int all = gridDim.x, id = all % 8 == 0 ? (int)(blockIdx.x % 8) * (all / 8) + (int)(blockIdx.x / 8) : (int)blockIdx.x;
     const int tile = id / shares, share = id - tile * shares, tn = tile / tiles_m, tm = tile - tn * tiles_m, m0 = tm * kTokens, n0 = (tn * kWaves + wave) * kChannels;
@@ -57,38 +62,39 @@ __global__ __launch_bounds__(64 * kWaves, 2) void w4_tiles_kernel(W4Args a, int 
 
     const int last_tile = (a.N + kW4Tile - 1) / kW4Tile - 1;
     const int64_t packed_tile = min((n0 + n) / kW4Tile, last_tile);  // (channels behind the last: results that are not written)
-    const uint8_t *codes = a.packed + packed_tile * a.blocks * kW4BlockBytes + ((n & 15) + 16 * h) * 16;
-    const uint16_t *scales = reinterpret_cast<const uint16_t *>(a.packed + a.code_bytes) + packed_tile * a.blocks * kGroups * kW4Tile + (n & 15);
-    uint32_t from[DIRECT ? 2 * T : 1];
+    const uint8_t *codes = a.packed + packed_tile * a.blocks * kW4BlockBytes + ((n & 15) + 16 * h) * 16 + half * 8;
+    const uint16_t *scales = reinterpret_cast<const uint16_t *>(a.packed + a.code_bytes) + (packed_tile * a.blocks * H + half) * kGroups * kW4Tile + (n & 15);
+    uint32_t from[DIRECT ? kRows : 1];
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint4 *)&rows[0][0];
     const uint16_t *x0 = a.x + m0 * a.x_stride;
     if (DIRECT) {
 #pragma unroll
-        for (int i = 0; i < 2 * T; ++i) {
-            const int token = 4 * (wave * 2 * T + i) + (lane >> 4), eight = (lane & 15) ^ (token & 15);
+        for (int i = 0; i < kRows; ++i) {
+            const int token = 4 * (any_wave * kRows + i) + (lane >> 4), eight = (lane & 15) ^ (token & 15);
             from[i] = (uint32_t)(min(token, a.M - 1 - m0) * (int)a.x_stride * 2 + eight * 16);
         }
     }
     auto stage = [&](int b, int to) {
         if (DIRECT && (b + 1) * kW4Block <= a.K) {
 #pragma unroll
-            for (int i = 0; i < 2 * T; ++i) load_to_lds(x0 + b * kW4Block, from[i], lds0 + (uint32_t)(to * kTokens * 256 + (wave * 2 * T + i) * 1024));
+            for (int i = 0; i < kRows; ++i) load_to_lds(x0 + b * kW4Block, from[i], lds0 + (uint32_t)(to * kTokens * 256 + (any_wave * kRows + i) * 1024));
         } else {
-            for (int i = threadIdx.x; i < kTokens * 16; i += 64 * kWaves) {
+            for (int i = threadIdx.x; i < kTokens * 16; i += 64 * kWaves * H) {
                 const int token = i >> 4, eight = (i & 15) ^ (token & 15);
                 rows[to][i] = w4_row_eight<uint4>(x0 + min(token, a.M - 1 - m0) * a.x_stride, b * kW4Block + eight * 8, a.K);
             }
         }
     };
+    typedef typename std::conditional<H == 1, uint4, uint2>::type Codes;
     struct Weights {
-        uint4 w[2];
+        Codes w[2];
         uint16_t s[kGroups];
     } weights[R];
     auto load_weights = [&](int b, Weights &to) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) to.w[i] = *reinterpret_cast<const uint4 *>(codes + (int64_t)b * kW4BlockBytes + i * 512);
+        for (int i = 0; i < 2; ++i) to.w[i] = *reinterpret_cast<const Codes *>(codes + (int64_t)b * kW4BlockBytes + i * 512);
 #pragma unroll
-        for (int i = 0; i < kGroups; ++i) to.s[i] = scales[((int64_t)b * kGroups + i) * kW4Tile];
+        for (int i = 0; i < kGroups; ++i) to.s[i] = scales[((int64_t)b * H * kGroups + i) * kW4Tile];
     };
 
     float16v acc[T];
@@ -107,15 +113,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void w4_tiles_kernel(W4Args a, int 
         // behind this block's loads there are those of R - 2 others, each as many (a last block that ends within has its rows waited for as they are loaded), or fewer at the end
         if (b + R - 2 < last) wait_and_meet<(R - 2) * kLoads>();
         else wait_and_meet<0>();
-        const uint4 w0 = weights[at].w[0], w1 = weights[at].w[1];
-        uint32_t words[8] = {w0.x, w1.x, w0.y, w1.y, w0.z, w1.z, w0.w, w1.w};  // of sixteen inputs each, this lane's half of them
+        uint32_t words[8 / H];  // of sixteen inputs each, this lane's half of them
+#pragma unroll
+        for (int i = 0; i < 8 / H; ++i) words[i] = reinterpret_cast<const uint32_t *>(&weights[at].w[i & 1])[i >> 1];
         float scales_of[kGroups];
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) scales_of[g] = w4_scale<BF16>(weights[at].s[g]);
         // taken here, before the next loads are begun: a first use behind them would be waited for with all of them, since the compiler cannot tell how many they are (256 x 11008 x 4096 44 us in place of 51, 2048 196 in
         // place of 205)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) asm volatile("" : "+v"(words[i]));
+        for (int i = 0; i < 8 / H; ++i) asm volatile("" : "+v"(words[i]));
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) asm volatile("" : "+v"(scales_of[g]));
         if (b + R - 1 < last) {
@@ -136,7 +143,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void w4_tiles_kernel(W4Args a, int 
                 for (int i = 0; i < 16; ++i) part[i] = 0.0f;
 #pragma unroll
                 for (int k = 0; k < kSteps; ++k)
-                    part = multiply<BF16>(__builtin_bit_cast(Eight, here[t * 32 * 16 + ((2 * (g * kSteps + k) + h) ^ (n & 15))]), w[k], part);
+                    part = multiply<BF16>(__builtin_bit_cast(Eight, here[t * 32 * 16 + ((kPart / 8 * half + 2 * (g * kSteps + k) + h) ^ (n & 15))]), w[k], part);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[t][i] = fmaf(part[i], scale, acc[t][i]);
                 if (GROUP < 128 && T > 2) __builtin_amdgcn_sched_barrier(0);  // (the compiler would begin sums of all groups at a time, for which there are no registers)
@@ -152,6 +159,26 @@ __global__ __launch_bounds__(64 * kWaves, 2) void w4_tiles_kernel(W4Args a, int 
         if (R > 3 && b + 3 < last) block(b + 3, std::integral_constant<int, 3 % R>());
         if (R > 4 && b + 4 < last) block(b + 4, std::integral_constant<int, 4 % R>());
         if (R > 5 && b + 5 < last) block(b + 5, std::integral_constant<int, 5 % R>());
+    }
+    if (H > 1) {  // the halves meet in the place of the activations
+        float4 *const meet = reinterpret_cast<float4 *>(&rows[0][0]) + wave * T * 4 * 64 + lane;
+        static_assert(kWaves * 4 * 64 <= R * 32 * 16, "");
+        __syncthreads();
+        if (half) {
+#pragma unroll
+            for (int t = 0; t < T; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) meet[(t * 4 + i) * 64] = make_float4(acc[t][4 * i], acc[t][4 * i + 1], acc[t][4 * i + 2], acc[t][4 * i + 3]);
+        }
+        __syncthreads();
+        if (half) return;
+#pragma unroll
+        for (int t = 0; t < T; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float4 x = meet[(t * 4 + i) * 64];
+                acc[t][4 * i] += x.x; acc[t][4 * i + 1] += x.y; acc[t][4 * i + 2] += x.z; acc[t][4 * i + 3] += x.w;
+            }
     }
     const int64_t stride = w4_partial_stride(a.N);
     float *partial = a.partial + share * a.M * stride;
@@ -193,7 +220,7 @@ void launch(const W4Args &a, const W4Rule &r, hipStream_t stream)
 {
     const bool direct = (reinterpret_cast<uintptr_t>(a.x) & 15) == 0 && a.x_stride % 8 == 0 && a.x_stride < (1 << 22);
     const int tiles_m = (a.M + 32 * T - 1) / (32 * T), tiles_n = (a.N + kWaves * kChannels - 1) / (kWaves * kChannels);
-    const dim3 grid((uint32_t)((int64_t)tiles_m * tiles_n * r.shares)), block(64 * kWaves);
+    const dim3 grid((uint32_t)((int64_t)tiles_m * tiles_n * r.shares)), block(64 * kWaves * halves_of(GROUP, T));
     if (direct) w4_tiles_kernel<BF16, GROUP, T, true><<<grid, block, 0, stream>>>(a, tiles_m, r.shares);
     else w4_tiles_kernel<BF16, GROUP, T, false><<<grid, block, 0, stream>>>(a, tiles_m, r.shares);
     if (r.shares > 1) w4_join_kernel<BF16><<<dim3((uint32_t)((a.M * (w4_partial_stride(a.N) / 4) + 255) / 256)), dim3(256), 0, stream>>>(a, r.shares);
