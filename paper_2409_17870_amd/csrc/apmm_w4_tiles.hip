@@ -42,15 +42,15 @@ __device__ __forceinline__ void wait_and_meet() { asm volatile("s_waitcnt vmcnt(
 constexpr int ring_of(int t) { return t == 1 ? 6 : t == 2 ? 4 : t == 3 ? 3 : 2; }
 
 // Two waves to the same channels, half of a block's inputs each, where the groups' products keep a wave busy between matrix instructions (groups of 32, with and without: 77 x 5119 x 13800 34 and 41 us, 96 x 11008 x 4096
-// 29 and 35, 64 x 5119 x 13800 26 and 31; groups of 64 31 and 36, 27 and 31, 25 and 28; of 128 no difference; one block of tokens 17 and 16 us, four have no registers for it)
-constexpr int halves_of(int group, int t) { return group < 128 && (t == 2 || t == 3) ? 2 : 1; }
+// 29 and 35, 64 x 5119 x 13800 26 and 31; groups of 64 31 and 36, 27 and 31, 25 and 28; of 128 no difference; one block of tokens 17 and 16 us; four, and rows at any address, have no registers for it)
+constexpr int halves_of(int group, int t, bool direct) { return direct && group < 128 && (t == 2 || t == 3) ? 2 : 1; }
 
 // DIRECT: rows of x begin at multiples of 16 bytes and a tile's lie within 2^31 bytes
 template <bool BF16, int GROUP, int T, bool DIRECT>
-__global__ __launch_bounds__(64 * kWaves * halves_of(GROUP, T), 2 * halves_of(GROUP, T)) void w4_tiles_kernel(W4Args a, int tiles_m, int shares)
+__global__ __launch_bounds__(64 * kWaves * halves_of(GROUP, T, DIRECT), 2 * halves_of(GROUP, T, DIRECT)) void w4_tiles_kernel(W4Args a, int tiles_m, int shares)
 {
     typedef typename W4Type<BF16>::Eight Eight;
-    constexpr int H = halves_of(GROUP, T), kPart = kW4Block / H;  // inputs of a block that a wave multiplies
+    constexpr int H = halves_of(GROUP, T, DIRECT), kPart = kW4Block / H;  // inputs of a block that a wave multiplies
     constexpr int kGroups = kPart / GROUP, kTokens = 32 * T, kSteps = GROUP / 16, R = ring_of(T);
     constexpr int kRows = 2 * T / H, kLoads = kRows + 2 + kGroups;  // of a wave for a block: activations, codes, scales
     __shared__ uint4 rows[R][kTokens * 16];      // [token][eight of inputs, its number xor token % 16]
@@ -220,9 +220,9 @@ void launch(const W4Args &a, const W4Rule &r, hipStream_t stream)
 {
     const bool direct = (reinterpret_cast<uintptr_t>(a.x) & 15) == 0 && a.x_stride % 8 == 0 && a.x_stride < (1 << 22);
     const int tiles_m = (a.M + 32 * T - 1) / (32 * T), tiles_n = (a.N + kWaves * kChannels - 1) / (kWaves * kChannels);
-    const dim3 grid((uint32_t)((int64_t)tiles_m * tiles_n * r.shares)), block(64 * kWaves * halves_of(GROUP, T));
+    const dim3 grid((uint32_t)((int64_t)tiles_m * tiles_n * r.shares)), block(64 * kWaves * halves_of(GROUP, T, true)), one(64 * kWaves);
     if (direct) w4_tiles_kernel<BF16, GROUP, T, true><<<grid, block, 0, stream>>>(a, tiles_m, r.shares);
-    else w4_tiles_kernel<BF16, GROUP, T, false><<<grid, block, 0, stream>>>(a, tiles_m, r.shares);
+    else w4_tiles_kernel<BF16, GROUP, T, false><<<grid, one, 0, stream>>>(a, tiles_m, r.shares);
     if (r.shares > 1) w4_join_kernel<BF16><<<dim3((uint32_t)((a.M * (w4_partial_stride(a.N) / 4) + 255) / 256)), dim3(256), 0, stream>>>(a, r.shares);
 }
 
