@@ -186,6 +186,7 @@ __global__ __launch_bounds__(kThreads) void kv_select_kernel(KvEvictArgs a)
 constexpr int kMoveWaves = 4;
 
 // A wave has eight places of the new pages that follow each other, of a head, eight lanes to a token.  (The values of a token lie 16 bits a line of 16 bytes: lines are read for a token alone.)
+// Bound by these scattered reads: 24 sequences of which 1000 tokens stay, 8 heads of 64, 11 us; 4096 of 65001 tokens, 8 heads of 128, 7.
 template <int D>
 __global__ __launch_bounds__(64 * kMoveWaves) void kv_move_kernel(KvEvictArgs a, uint64_t by_heads, int eights, int64_t units)
 {
