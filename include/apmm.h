@@ -313,7 +313,8 @@ apmm_status apmm_kv_write_rotary(const apmm_kv_cache *cache, const apmm_kv_batch
  * over the keys that apmm_kv_attention with the same arguments lets query i see; a decay of 0 does not read what was there.  weights: device, sequences x kv_heads x capacity 32-bit floats with contiguous
  * tokens; tokens from `capacity` on have none, tokens behind a sequence's length and sequences without new tokens keep what is there.  A query with a score that is NaN (a scale or a number of it is) gives NaN to
  * the keys that it sees.  Results do not depend on the order of execution.
- *   workspace  device, 16-byte aligned, apmm_kv_weights_workspace_bytes() bytes of the same arguments (a call with a window needs no more); calls that may overlap need one each */
+ *   workspace  device, 16-byte aligned, apmm_kv_weights_workspace_bytes() bytes of the same arguments (a call with a window needs no more; about as much as the queries, and up to 256 MiB where
+ *              sequences have few); calls that may overlap need one each */
 size_t apmm_kv_weights_workspace_bytes(const apmm_kv_cache *cache, const apmm_kv_batch *batch, int q_heads);
 apmm_status apmm_kv_weights(const apmm_kv_cache *cache, const apmm_kv_batch *batch, int q_heads, const void *q, int64_t q_token_stride, int64_t q_head_stride,
                             float *weights, int64_t weights_sequence_stride, int64_t weights_head_stride, int64_t capacity, float decay, float scale, int64_t window, int64_t sinks,
@@ -326,10 +327,12 @@ apmm_status apmm_kv_weights(const apmm_kv_cache *cache, const apmm_kv_batch *bat
  *   to_lengths  device, sequences: tokens that stay; not `lengths` itself
  *   kept        device, sequences x kv_heads x budget: the places they had, ascending, then -1
  *   to_weights  device, sequences x kv_heads x budget: their weights (0 for those that have none), then 0
+ *   workspace   device, 16-byte aligned, apmm_kv_evict_workspace_bytes() bytes of the same sizes (0, then it may be NULL, for tables of up to 65536 tokens); calls that may overlap need one each
  * sinks + recent <= budget.  A call of 2^32 work items or more is refused: sequences x kv_heads from 2^22 on, sequences x kv_heads x budget from about 2^29 on. */
+size_t apmm_kv_evict_workspace_bytes(const apmm_kv_cache *cache, int sequences, int64_t table_width);
 apmm_status apmm_kv_evict(const apmm_kv_cache *cache, int sequences, const int32_t *lengths, const int32_t *page_table, int64_t table_stride, int64_t table_width,
                           const float *weights, int64_t weights_sequence_stride, int64_t weights_head_stride, int64_t capacity, int64_t budget, int64_t sinks, int64_t recent,
-                          const int32_t *to_table, int64_t to_stride, int64_t to_width, int32_t *to_lengths, int32_t *kept, float *to_weights, void *stream);
+                          const int32_t *to_table, int64_t to_stride, int64_t to_width, int32_t *to_lengths, int32_t *kept, float *to_weights, void *workspace, size_t workspace_bytes, void *stream);
 
 /* ---- Four-bit weights with group scales times activations of 16 bits: y = x * W^T with W[n][k] = (2 u[n][k] - 15) * scales[n][k / group], u bipolar-INT codes of four bits (paper Sec. 3.1, Eq. 1).
  * For layers whose activations are not to be quantised.  The products of a group are exact and summed in 32 bits, its sum is multiplied with the scale in 32 bits, y is rounded once.  (Activations of

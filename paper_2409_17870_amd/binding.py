@@ -22,7 +22,8 @@ EXPORTS = [
     "apmm_packed_bytes", "apmm_packed_activation_bytes", "apmm_workspace_bytes", "apmm_pack_weights", "apmm_pack_activations",
     "apmm_quantize_pack_activations", "apmm_unpack", "apmm_unpack_activations", "apmm_gemm", "apmm_gemm_ex", "apmm_gemm_from_codes", "apmm_gemm_from_codes_noalloc", "apmm_gemm_grouped",
     "apmm_kv_write", "apmm_kv_read", "apmm_kv_attention", "apmm_kv_attention_workspace_bytes",
-    "apmm_rotary", "apmm_kv_write_rotary", "apmm_kv_weights", "apmm_kv_weights_workspace_bytes", "apmm_kv_evict", "apmm_w4_packed_bytes", "apmm_w4_workspace_bytes", "apmm_w4_pack", "apmm_w4_gemm",
+    "apmm_rotary", "apmm_kv_write_rotary", "apmm_kv_weights", "apmm_kv_weights_workspace_bytes", "apmm_kv_evict", "apmm_kv_evict_workspace_bytes", "apmm_w4_packed_bytes", "apmm_w4_workspace_bytes",
+    "apmm_w4_pack", "apmm_w4_gemm",
     "apmm_time_next_gemm", "apmm_last_gemm_kernel", "apmm_status_string", "apmm_last_error", "apmm_version",
 ]
 
@@ -62,7 +63,7 @@ except ImportError as _reason:  # not built, or built for another torch or Pytho
 _CALL_FUNCTIONS = ("apmm_packed_bytes", "apmm_packed_activation_bytes", "apmm_pack_weights", "apmm_pack_activations",
                    "apmm_quantize_pack_activations", "apmm_gemm_ex", "apmm_gemm_from_codes", "apmm_kv_write", "apmm_kv_read", "apmm_kv_attention",
                    "apmm_kv_attention_workspace_bytes", "apmm_rotary", "apmm_kv_write_rotary", "apmm_kv_weights", "apmm_kv_weights_workspace_bytes", "apmm_kv_evict",
-                   "apmm_w4_packed_bytes", "apmm_w4_workspace_bytes", "apmm_w4_gemm")
+                   "apmm_kv_evict_workspace_bytes", "apmm_w4_packed_bytes", "apmm_w4_workspace_bytes", "apmm_w4_gemm")
 
 
 class ApmmError(RuntimeError):
@@ -127,7 +128,9 @@ def load():
     lib.apmm_kv_weights_workspace_bytes.restype = ctypes.c_size_t
     lib.apmm_kv_weights_workspace_bytes.argtypes = [cache, batch, ci]
     lib.apmm_kv_evict.restype = ci
-    lib.apmm_kv_evict.argtypes = [cache, ci, vp, vp, i64, i64, vp, i64, i64, i64, i64, i64, i64, vp, i64, i64, vp, vp, vp, vp]
+    lib.apmm_kv_evict.argtypes = [cache, ci, vp, vp, i64, i64, vp, i64, i64, i64, i64, i64, i64, vp, i64, i64, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.apmm_kv_evict_workspace_bytes.restype = ctypes.c_size_t
+    lib.apmm_kv_evict_workspace_bytes.argtypes = [cache, ci, i64]
     lib.apmm_w4_packed_bytes.restype = ctypes.c_size_t
     lib.apmm_w4_packed_bytes.argtypes = [i64, i64, ci]
     lib.apmm_w4_pack.restype = ci
@@ -526,9 +529,10 @@ def apmm_kv_weights_workspace_bytes(tokens, q_heads, codes, scales, page_table, 
     return int(load().apmm_kv_weights_workspace_bytes(_kv_cache(codes, scales), batch, q_heads))
 
 
-def apmm_kv_evict(codes, scales, page_table, lengths, weights, budget, to_table, sinks=0, recent=0, kept=None, to_weights=None, to_lengths=None):
+def apmm_kv_evict(codes, scales, page_table, lengths, weights, budget, to_table, sinks=0, recent=0, kept=None, to_weights=None, to_lengths=None, workspace=None):
     """Keep of each sequence and head the first `sinks` tokens, the last `recent` and the heaviest others, `budget` in all: copied in their order to the pages of to_table (int32, sequences
     x pages, none of a sequence of the call).  (places they had, int32, sequences x kv heads x budget with -1 behind the last; their weights; the new lengths.)
+    workspace: uint8 tensor of apmm_kv_evict_workspace_bytes(...) bytes, allocated if None.
     """
     cache = _kv_cache(codes, scales)
     batch = _kv_batch(codes, page_table, lengths, None, lengths.shape[0])
@@ -544,10 +548,21 @@ def apmm_kv_evict(codes, scales, page_table, lengths, weights, budget, to_table,
     for t, what, dtype, of in ((kept, "kept", torch.int32, shape), (to_weights, "to_weights", torch.float32, shape), (to_lengths, "to_lengths", torch.int32, (sequences,))):
         if t.dtype != dtype or tuple(t.shape) != of or t.device != codes.device or not t.is_contiguous():
             raise ValueError("%s must be a contiguous tensor of %s on the cache's device, %s" % (what, dtype, " x ".join(map(str, of))))
-    _check(load().apmm_kv_evict(cache, sequences, batch.lengths, batch.page_table, batch.table_stride, batch.table_width, *rows, budget, sinks, recent,
-                                to_table.data_ptr(), to_table.stride(0) if sequences > 1 else to_table.shape[1], to_table.shape[1], to_lengths.data_ptr(), kept.data_ptr(),
-                                to_weights.data_ptr(), _stream()))
+    lib = load()
+    if workspace is None:
+        need = lib.apmm_kv_evict_workspace_bytes(cache, sequences, batch.table_width)
+        workspace = torch.empty(need, dtype=torch.uint8, device=codes.device) if need else None
+    elif workspace.device != codes.device or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the cache's device")
+    _check(lib.apmm_kv_evict(cache, sequences, batch.lengths, batch.page_table, batch.table_stride, batch.table_width, *rows, budget, sinks, recent,
+                             to_table.data_ptr(), to_table.stride(0) if sequences > 1 else to_table.shape[1], to_table.shape[1], to_lengths.data_ptr(), kept.data_ptr(),
+                             to_weights.data_ptr(), _ptr(workspace), 0 if workspace is None else workspace.nbytes, _stream()))
     return kept, to_weights, to_lengths
+
+
+def apmm_kv_evict_workspace_bytes(codes, scales, page_table):
+    """Bytes of workspace that apmm_kv_evict needs for sequences with this page table."""
+    return int(load().apmm_kv_evict_workspace_bytes(_kv_cache(codes, scales), page_table.shape[0], page_table.shape[1]))
 
 
 @functools.lru_cache(maxsize=1024, typed=True)

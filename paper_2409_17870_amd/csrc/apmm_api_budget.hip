@@ -151,9 +151,17 @@ apmm_status apmm_kv_weights(const apmm_kv_cache *cache, const apmm_kv_batch *bat
     return e == hipSuccess ? APMM_OK : fail_hip(e, "apmm_kv_weights");
 }
 
+size_t apmm_kv_evict_workspace_bytes(const apmm_kv_cache *cache, int sequences, int64_t table_width)
+{
+    apmm::KvArgs a;
+    const apmm_kv_batch batch = {sequences, sequences, nullptr, nullptr, nullptr, table_width, table_width};
+    if (check_sizes(cache, &batch, a) != APMM_OK || sequences == 0) return 0;
+    return apmm::kv_evict_parts(a).bytes;
+}
+
 apmm_status apmm_kv_evict(const apmm_kv_cache *cache, int sequences, const int32_t *lengths, const int32_t *page_table, int64_t table_stride, int64_t table_width,
                           const float *weights, int64_t weights_sequence_stride, int64_t weights_head_stride, int64_t capacity, int64_t budget, int64_t sinks, int64_t recent,
-                          const int32_t *to_table, int64_t to_stride, int64_t to_width, int32_t *to_lengths, int32_t *kept, float *to_weights, void *stream)
+                          const int32_t *to_table, int64_t to_stride, int64_t to_width, int32_t *to_lengths, int32_t *kept, float *to_weights, void *workspace, size_t workspace_bytes, void *stream)
 {
     apmm::KvEvictArgs a = {};
     bool empty;
@@ -178,8 +186,15 @@ apmm_status apmm_kv_evict(const apmm_kv_cache *cache, int sequences, const int32
     a.kept = kept;
     a.to_lengths = to_lengths;
     a.to_weights = to_weights;
-    if (apmm::kv_evict_items(a) > apmm::kKvMostItems) return fail(APMM_ERR_UNSUPPORTED, "kv_evict: sequences * kv_heads * budget is more than one launch takes");
-    const hipError_t e = apmm::launch_kv_evict(a, static_cast<hipStream_t>(stream));
+    apmm::KvEvictParts parts = apmm::kv_evict_parts(a.c);
+    if (apmm::kv_evict_items(a, parts) > apmm::kKvMostItems) return fail(APMM_ERR_UNSUPPORTED, "kv_evict: sequences * kv_heads * budget is more than one launch takes");
+    if (parts.parts) {
+        if (!workspace || workspace_bytes < parts.bytes) return fail(APMM_ERR_WORKSPACE, "kv_evict: needs a workspace of apmm_kv_evict_workspace_bytes() bytes");
+        if (!aligned(workspace, 16)) return fail(APMM_ERR_INVALID_ARG, "kv_evict: workspace must be 16-byte aligned");
+        parts.counts = workspace;
+        parts.tallies = static_cast<uint8_t *>(workspace) + parts.counts_bytes;
+    }
+    const hipError_t e = apmm::launch_kv_evict(a, parts, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? APMM_OK : fail_hip(e, "apmm_kv_evict");
 }
 

@@ -36,7 +36,15 @@ struct KvEvictArgs {
     int32_t *kept, *to_lengths;  // sequences x heads x budget; sequences
     float *to_weights;           // sequences x heads x budget
 };
-int64_t kv_evict_items(const KvEvictArgs &a);
-hipError_t launch_kv_evict(const KvEvictArgs &a, hipStream_t stream);
+// Many workgroups to a sequence and head, each with `chunks` of its tokens; parts 0: one.  The workspace has their counts and, behind these, what each part has to give.
+struct KvEvictParts {
+    int parts, chunks;
+    uint64_t by_parts;  // what kv_divide divides by parts with
+    size_t counts_bytes, bytes;
+    void *counts, *tallies;
+};
+KvEvictParts kv_evict_parts(const KvArgs &c);
+int64_t kv_evict_items(const KvEvictArgs &a, const KvEvictParts &p);
+hipError_t launch_kv_evict(const KvEvictArgs &a, const KvEvictParts &p, hipStream_t stream);
 
 }  // namespace apmm

@@ -32,11 +32,42 @@ struct Tokens {
     }
 };
 
+// Numbers of tokens begin + 64 i + lane, zeros from `to` on
+template <int N>
+__device__ __forceinline__ void read_tokens(const Tokens &order, int begin, int to, uint32_t (&v)[N])
+{
+    // tokens that all have a weight and a page, and none of which stays whatever its weight, are read as they lie
+    const int lane = kv_lane(), end = min(begin + 64 * N, to), last = end - begin - 1;
+    bool plain = last >= 0 && begin >= order.sinks && end <= order.recent_from && end <= order.capacity;
+    if (plain)
+        for (int page = (begin >> order.shift) + lane; page <= (end - 1) >> order.shift; page += 64) plain &= order.table[page] >= 0 && order.table[page] < order.pages;
+    if (__ballot(!plain) == 0) {
+        const float *w = order.w + begin;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint32_t n = order_of(w[min(64 * i + lane, last)]);
+            v[i] = 64 * i + lane <= last ? n : 0u;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            v[i] = 0;
+            if (64 * i <= last) v[i] = 64 * i + lane <= last ? order(begin + 64 * i + lane) : 0u;
+            if (i % 8 == 7) __builtin_amdgcn_sched_barrier(0);  // (eight on their way at a time: of more there are no registers)
+        }
+    }
+}
+__device__ __forceinline__ Tokens tokens_of(const KvEvictArgs &a, int b, int head)
+{
+    const int length = min(max(a.c.lengths[b], 0), kKvMost), keys = (int)min((int64_t)length, (int64_t)a.c.width << a.c.page_shift);
+    return {a.w.data + b * a.w.sequence_stride + head * a.w.head_stride, a.c.table + b * a.c.table_stride, a.c.pages, a.w.capacity, keys, a.c.page_shift, a.sinks, length - a.recent};
+}
+
 // A workgroup to a sequence and head, each of its waves has a stretch of tokens.  Three passes find the budget-th largest number, digit by digit from the highest; then each wave counts those of its stretch that
-// stay, and after the counts have met writes their places in order, whose weights are fetched at the end by all.  Sequences of up to 1024 HELD tokens are read once and held in registers, the second half of 64 to a
+// stay, and after the counts have met writes their places in order, whose weights are fetched at the end by all.  Sequences of up to 1024 HELD tokens, as far as the table goes, are read once and held in registers, the second half of 64 to a
 // lane in LDS.  Bound by the instructions of the one compute unit that has a sequence and head: 65001 tokens take 102 000 cycles, 23 000 to read them, 46 000 for the three passes (a fifth of it LDS additions that
 // meet in one digit), 10 000 to count and 21 000 to write.  Reading every token with its own checks took 55 000, a weight fetched as its place is written 48 000 in place of 21 000; reading the weights anew in each of
-// five passes 150 us.  More workgroups to a head would need memory for their counts, and a launch more for calls of ordinary length, which take 31 us with the copy.
+// five passes 150 us.
 template <int HELD>
 __global__ __launch_bounds__(kThreads) void kv_select_kernel(KvEvictArgs a)
 {
@@ -45,55 +76,30 @@ __global__ __launch_bounds__(kThreads) void kv_select_kernel(KvEvictArgs a)
     __shared__ int above[kWaves], equal[kWaves];
     __shared__ uint32_t found_digit, found_rest;
     const int b = kv_divide(blockIdx.x, a.c.by_heads), head = blockIdx.x - b * a.c.heads, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = kv_lane();
-    const int length = min(max(a.c.lengths[b], 0), kKvMost), keys = (int)min((int64_t)length, (int64_t)a.c.width << a.c.page_shift);
-    const Tokens order = {a.w.data + b * a.w.sequence_stride + head * a.w.head_stride, a.c.table + b * a.c.table_stride, a.c.pages, a.w.capacity, keys, a.c.page_shift, a.sinks, length - a.recent};
-    const int stretch = ((keys + kThreads - 1) / kThreads) * 64, own_from = min(wave * stretch, keys), to = min(own_from + stretch, keys);
+    const Tokens order = tokens_of(a, b, head);
+    const int keys = order.keys, stretch = ((keys + kThreads - 1) / kThreads) * 64, own_from = min(wave * stretch, keys), to = min(own_from + stretch, keys);
     constexpr int kInRegisters = HELD < 32 ? HELD : 32;
-    uint32_t held[HELD ? kInRegisters : 1];
+    uint32_t held[kInRegisters];
     __shared__ uint32_t more[HELD > 32 ? HELD - 32 : 1][kThreads];
-    if (HELD) {
-        constexpr int kBatch = HELD < 16 ? HELD : 16;
-        auto hold = [&](int i, uint32_t v) {
-            if (i < 32) held[i < 32 ? i : 0] = v;
-            else more[i < 32 ? 0 : i - 32][threadIdx.x] = v;
-        };
+    constexpr int kBatch = HELD < 16 ? HELD : 16;
 #pragma unroll
-        for (int first = 0; first < HELD; first += kBatch) {
-            // tokens that all have a weight and a page, and none of which stays whatever its weight, are read as they lie
-            const int begin = min(own_from + 64 * first, to), end = min(begin + 64 * kBatch, to), last = end - begin - 1;
-            bool plain = last >= 0 && begin >= order.sinks && end <= order.recent_from && end <= order.capacity;
-            if (plain)
-                for (int page = (begin >> order.shift) + lane; page <= (end - 1) >> order.shift; page += 64) plain &= order.table[page] >= 0 && order.table[page] < order.pages;
-            if (__ballot(!plain) == 0) {
-                const float *w = order.w + begin;
+    for (int first = 0; first < HELD; first += kBatch) {
+        uint32_t v[kBatch];
+        read_tokens(order, min(own_from + 64 * first, to), to, v);
 #pragma unroll
-                for (int i = 0; i < kBatch; ++i) {
-                    const uint32_t v = order_of(w[min(64 * i + lane, last)]);
-                    hold(first + i, 64 * i + lane <= last ? v : 0u);
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < kBatch; ++i) {
-                    uint32_t v = 0;
-                    if (64 * i <= last) v = 64 * i + lane <= last ? order(begin + 64 * i + lane) : 0u;
-                    hold(first + i, v);
-                    if (i % 8 == 7) __builtin_amdgcn_sched_barrier(0);  // (eight on their way at a time: of more there are no registers)
-                }
-            }
+        for (int i = 0; i < kBatch; ++i) {
+            if (first + i < 32) held[first + i < 32 ? first + i : 0] = v[i];
+            else more[first + i < 32 ? 0 : first + i - 32][threadIdx.x] = v[i];
         }
     }
     // f(token, number) of this lane's tokens, sixty-four to a wave at a time
     auto each = [&](auto f) {
         int from = own_from, lane = kv_lane();
         asm volatile("" : "+s"(from), "+v"(lane));  // (places and borders of 64 tokens are not kept from one pass for the next: for those there are no registers)
-        if (HELD) {
 #pragma unroll
-            for (int i = 0; i < HELD; ++i) {
-                if (from + 64 * i < to) f(from + 64 * i + lane, i < 32 ? held[i < 32 ? i : 0] : more[i < 32 ? 0 : i - 32][threadIdx.x]);
-                if (i % 8 == 7) __builtin_amdgcn_sched_barrier(0);
-            }
-        } else {
-            for (int t = from; t < to; t += 64) f(t + lane, t + lane < to ? order(t + lane) : 0u);
+        for (int i = 0; i < HELD; ++i) {
+            if (from + 64 * i < to) f(from + 64 * i + lane, i < 32 ? held[i < 32 ? i : 0] : more[i < 32 ? 0 : i - 32][threadIdx.x]);
+            if (i % 8 == 7) __builtin_amdgcn_sched_barrier(0);
         }
     };
     uint32_t least = 0, rest = (uint32_t)a.budget;  // what the digits so far say; how many are wanted of those that begin with them
@@ -183,6 +189,213 @@ __global__ __launch_bounds__(kThreads) void kv_select_kernel(KvEvictArgs a)
     if (head == 0 && threadIdx.x == 0) a.to_lengths[b] = kept;
 }
 
+// The same by many workgroups: a part of a sequence's tokens to each, in chunks of kChunk, a launch for each digit.  Counts of a digit meet in memory by additions of whole numbers, whose order changes nothing; each
+// workgroup finds the digits before its own again.  Six launches of 2 to 12 us (65001 tokens of 8 heads: 48 in all), bound by what each has to wait for in turn: lengths, pages, weights, counts.
+constexpr int kPartThreads = 256, kPartWaves = 4, kPartHeld = 16, kChunk = kPartThreads * kPartHeld, kMostParts = 256;
+
+struct Counts {  // of a sequence and head
+    uint32_t digits[3][kDigits];
+};
+struct Tally {   // of a part: tokens above the least number that stays, and tokens that have it
+    int above, equal;
+};
+
+__global__ __launch_bounds__(kPartThreads) void kv_clear_kernel(uint32_t *at, int64_t n)
+{
+    for (int64_t i = (int64_t)blockIdx.x * kPartThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kPartThreads) at[i] = 0;
+}
+
+struct Least {
+    uint32_t number, rest;  // the digits found; how many are wanted of the tokens that have them
+    bool all;               // fewer tokens than the budget: all stay
+};
+// By all lanes of a workgroup, from the highest digit down, eight to a lane
+template <int PASSES>
+__device__ __forceinline__ Least find_least(const Counts *counts, uint32_t budget)
+{
+    __shared__ uint32_t totals[kPartWaves], digit, left;
+    const int wave = threadIdx.x >> 6, lane = kv_lane();
+    Least l = {0, budget, false};
+#pragma unroll
+    for (int pass = 0; pass < PASSES; ++pass) {
+        const uint4 *at = reinterpret_cast<const uint4 *>(counts->digits[pass] + kDigits - 8 - 8 * (int)threadIdx.x);
+        const uint4 low = at[0], high = at[1];
+        const uint32_t n[8] = {high.w, high.z, high.y, high.x, low.w, low.z, low.y, low.x};
+        uint32_t sum = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += n[i];
+        const uint32_t up_to = (uint32_t)kv_scan((int)sum);
+        if (lane == 63) totals[wave] = up_to;
+        if (threadIdx.x == 0) digit = 0xffffffffu;
+        __syncthreads();
+        uint32_t before = up_to - sum;
+        for (int i = 0; i < wave; ++i) before += totals[i];
+        if (before < l.rest && before + sum >= l.rest) {
+            int i = 0;
+            while (before + n[i] < l.rest) before += n[i++];
+            digit = kDigits - 1 - 8 * threadIdx.x - i;
+            left = l.rest - before;
+        }
+        __syncthreads();
+        if (digit == 0xffffffffu) {  // (in the first pass, and for all workgroups of the sequence and head alike)
+            l = {0, 0, true};
+            return l;
+        }
+        l.number |= digit << (pass == 0 ? 21 : pass == 1 ? 10 : 0);
+        l.rest = left;
+        __syncthreads();
+    }
+    return l;
+}
+
+struct Part {
+    int unit, part, b, head;  // unit: sequence and head
+    __device__ __forceinline__ Part(const KvEvictArgs &a, const KvEvictParts &p)
+    {
+        unit = kv_divide(blockIdx.x, p.by_parts);
+        part = blockIdx.x - unit * p.parts;
+        b = kv_divide(unit, a.c.by_heads);
+        head = unit - b * a.c.heads;
+    }
+};
+
+template <int PASS>
+__global__ __launch_bounds__(kPartThreads) void kv_count_kernel(KvEvictArgs a, KvEvictParts p)
+{
+    __shared__ uint32_t digits[kDigits];
+    const Part at(a, p);
+    const Tokens order = tokens_of(a, at.b, at.head);
+    const int from = (int)min((int64_t)at.part * p.chunks * kChunk, (int64_t)order.keys), to = (int)min((int64_t)from + (int64_t)p.chunks * kChunk, (int64_t)order.keys);
+    if (from >= to) return;
+    Counts *counts = static_cast<Counts *>(p.counts) + at.unit;
+    const Least l = find_least<PASS>(counts, (uint32_t)a.budget);
+    if (l.all) return;
+    for (int i = threadIdx.x; i < kDigits; i += kPartThreads) digits[i] = 0;
+    __syncthreads();
+    constexpr int shift = PASS == 0 ? 21 : PASS == 1 ? 10 : 0, bits = PASS == 2 ? 10 : 11;
+    constexpr uint32_t mask = (1u << bits) - 1, upper = PASS == 0 ? 0 : ~0u << (shift + bits);
+    for (int begin = from + (int)(threadIdx.x >> 6) * 64 * kPartHeld; begin < to; begin += kChunk) {
+        uint32_t v[kPartHeld];
+        read_tokens(order, begin, to, v);
+#pragma unroll
+        for (int i = 0; i < kPartHeld; ++i)
+            if (v[i] && (v[i] & upper) == (l.number & upper)) atomicAdd(&digits[v[i] >> shift & mask], 1u);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < kDigits; i += kPartThreads)
+        if (digits[i]) atomicAdd(&counts->digits[PASS][i], digits[i]);
+}
+
+// Tokens of a chunk's stretch of a wave above l.number, and of it
+__device__ __forceinline__ Tally tally_of(const uint32_t (&v)[kPartHeld], int begin, int to, const Least &l)
+{
+    Tally t = {0, 0};
+#pragma unroll
+    for (int i = 0; i < kPartHeld; ++i) {
+        t.above += v[i] > l.number;
+        t.equal += begin + 64 * i + kv_lane() < to && v[i] == l.number;
+    }
+    return {__builtin_amdgcn_readlane(kv_scan(t.above), 63), __builtin_amdgcn_readlane(kv_scan(t.equal), 63)};
+}
+
+__global__ __launch_bounds__(kPartThreads) void kv_tally_kernel(KvEvictArgs a, KvEvictParts p)
+{
+    __shared__ Tally waves[kPartWaves];
+    const Part at(a, p);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Tokens order = tokens_of(a, at.b, at.head);
+    const int from = (int)min((int64_t)at.part * p.chunks * kChunk, (int64_t)order.keys), to = (int)min((int64_t)from + (int64_t)p.chunks * kChunk, (int64_t)order.keys);
+    const Least l = find_least<3>(static_cast<const Counts *>(p.counts) + at.unit, (uint32_t)a.budget);
+    Tally sum = {0, 0};
+    for (int begin = from + wave * 64 * kPartHeld; begin < to; begin += kChunk) {
+        uint32_t v[kPartHeld];
+        read_tokens(order, begin, to, v);
+        const Tally t = tally_of(v, begin, to, l);
+        sum.above += t.above;
+        sum.equal += t.equal;
+    }
+    if (kv_lane() == 0) waves[wave] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < kPartWaves; ++i) {
+            sum.above += waves[i].above;
+            sum.equal += waves[i].equal;
+        }
+        static_cast<Tally *>(p.tallies)[(int64_t)at.unit * p.parts + at.part] = sum;
+    }
+}
+
+__global__ __launch_bounds__(kPartThreads) void kv_keep_kernel(KvEvictArgs a, KvEvictParts p)
+{
+    __shared__ Tally waves[kPartWaves], before_of[kPartWaves], all_of[kPartWaves];
+    const Part at(a, p);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = kv_lane();
+    const Tokens order = tokens_of(a, at.b, at.head);
+    const int from = (int)min((int64_t)at.part * p.chunks * kChunk, (int64_t)order.keys), to = (int)min((int64_t)from + (int64_t)p.chunks * kChunk, (int64_t)order.keys);
+    const Least l = find_least<3>(static_cast<const Counts *>(p.counts) + at.unit, (uint32_t)a.budget);
+    static_assert(kMostParts <= kPartThreads, "a part to a lane");
+    Tally mine = {0, 0};
+    if ((int)threadIdx.x < p.parts) mine = static_cast<const Tally *>(p.tallies)[(int64_t)at.unit * p.parts + threadIdx.x];
+    const bool earlier = (int)threadIdx.x < at.part;
+    const Tally some = {__builtin_amdgcn_readlane(kv_scan(earlier ? mine.above : 0), 63), __builtin_amdgcn_readlane(kv_scan(earlier ? mine.equal : 0), 63)};
+    const Tally whole = {__builtin_amdgcn_readlane(kv_scan(mine.above), 63), __builtin_amdgcn_readlane(kv_scan(mine.equal), 63)};
+    if (lane == 0) {
+        before_of[wave] = some;
+        all_of[wave] = whole;
+    }
+    __syncthreads();
+    int above = 0, equals = 0, all_above = 0, all_equal = 0;  // before this part; of all
+    for (int i = 0; i < kPartWaves; ++i) {
+        above += before_of[i].above;
+        equals += before_of[i].equal;
+        all_above += all_of[i].above;
+        all_equal += all_of[i].equal;
+    }
+    const int rest = (int)l.rest, kept = all_above + min(all_equal, rest), first = above + min(equals, rest);
+    int32_t *kept_to = a.kept + (int64_t)at.unit * a.budget;
+    float *weights_to = a.to_weights + (int64_t)at.unit * a.budget;
+    for (int chunk = from; chunk < to; chunk += kChunk) {  // (the same for all waves)
+        const int begin = min(chunk + wave * 64 * kPartHeld, to);
+        uint32_t v[kPartHeld];
+        read_tokens(order, begin, to, v);
+        const Tally t = tally_of(v, begin, to, l);
+        __syncthreads();
+        if (lane == 0) waves[wave] = t;
+        __syncthreads();
+        int a0 = above, e0 = equals;
+        for (int i = 0; i < kPartWaves; ++i) {
+            if (i < wave) {
+                a0 += waves[i].above;
+                e0 += waves[i].equal;
+            }
+            above += waves[i].above;
+            equals += waves[i].equal;
+        }
+        int place = a0 + min(e0, rest);
+#pragma unroll
+        for (int i = 0; i < kPartHeld; ++i) {
+            const int token = begin + 64 * i + lane;
+            const bool is_equal = token < to && v[i] == l.number;
+            const uint64_t same = __ballot(is_equal), below = (1ull << lane) - 1;
+            const bool stays = v[i] > l.number || (is_equal && e0 + (int)__popcll(same & below) < rest);
+            const uint64_t staying = __ballot(stays);
+            if (stays) kept_to[place + (int)__popcll(staying & below)] = token;
+            place += (int)__popcll(staying);
+            e0 += (int)__popcll(same);
+        }
+    }
+    __syncthreads();
+    for (int i = first + (int)threadIdx.x; i < above + min(equals, rest); i += kPartThreads) {
+        const int t = kept_to[i];
+        weights_to[i] = t < a.w.capacity ? order.w[t] : 0.0f;
+    }
+    for (int64_t i = kept + (int64_t)at.part * kPartThreads + threadIdx.x; i < a.budget; i += (int64_t)p.parts * kPartThreads) {
+        kept_to[i] = -1;
+        weights_to[i] = 0.0f;
+    }
+    if (at.head == 0 && at.part == 0 && threadIdx.x == 0) a.to_lengths[at.b] = kept;
+}
+
 constexpr int kMoveWaves = 4;
 
 // A wave has eight places of the new pages that follow each other, of a head, eight lanes to a token.  (The values of a token lie 16 bits a line of 16 bytes: lines are read for a token alone.)
@@ -238,23 +451,50 @@ int64_t move_units(const KvEvictArgs &a) { return (int64_t)a.c.sequences * ((a.b
 
 }  // namespace
 
-int64_t kv_evict_items(const KvEvictArgs &a)
+// Many workgroups to a sequence and head where its weights do not fit into one's registers and LDS (tokens of 8 heads, with the copy and the read back: 130000 64 us,
+// 1000000 90; of 20000, 33000 and 65000 it took 60 or 61, where one workgroup takes 43, 46 and 59)
+KvEvictParts kv_evict_parts(const KvArgs &c)
 {
-    return std::max<int64_t>((move_units(a) + kMoveWaves - 1) / kMoveWaves * 64 * kMoveWaves, (int64_t)a.c.sequences * a.c.heads * kThreads);
+    KvEvictParts p = {};
+    const int64_t most = std::min<int64_t>((int64_t)c.width << c.page_shift, kKvMost), units = (int64_t)c.sequences * c.heads;  // tokens of a sequence, as far as the page table goes
+    if (most <= 64 * kThreads) return p;
+    const int64_t chunks = (most + kChunk - 1) / kChunk, parts = std::min<int64_t>(kMostParts, std::max<int64_t>(1, ((int64_t)1 << 23) / units));
+    p.chunks = (int)((chunks + parts - 1) / parts);
+    p.parts = (int)((chunks + p.chunks - 1) / p.chunks);
+    p.by_parts = kv_divisor(p.parts);
+    p.counts_bytes = (size_t)units * sizeof(Counts);
+    p.bytes = p.counts_bytes + (size_t)units * p.parts * sizeof(Tally);
+    return p;
 }
 
-hipError_t launch_kv_evict(const KvEvictArgs &a, hipStream_t stream)
+int64_t kv_evict_items(const KvEvictArgs &a, const KvEvictParts &p)
 {
-    const int64_t most = (int64_t)a.c.width << a.c.page_shift;  // tokens of a sequence, as far as the page table goes
-    const dim3 groups((uint32_t)a.c.sequences * (uint32_t)a.c.heads), block(kThreads);
-    if (most <= 4 * kThreads) kv_select_kernel<4><<<groups, block, 0, stream>>>(a);
-    else if (most <= 16 * kThreads) kv_select_kernel<16><<<groups, block, 0, stream>>>(a);
-    else if (most <= 64 * kThreads) kv_select_kernel<64><<<groups, block, 0, stream>>>(a);
-    else kv_select_kernel<0><<<groups, block, 0, stream>>>(a);
-    const int64_t units = move_units(a);
-    const dim3 grid((uint32_t)((units + kMoveWaves - 1) / kMoveWaves)), four(64 * kMoveWaves);
-    if (a.c.head_dim == 128) kv_move_kernel<128><<<grid, four, 0, stream>>>(a, kv_divisor(a.c.heads), (a.budget + 7) / 8, units);
-    else kv_move_kernel<64><<<grid, four, 0, stream>>>(a, kv_divisor(a.c.heads), (a.budget + 7) / 8, units);
+    const int64_t units = (int64_t)a.c.sequences * a.c.heads;
+    return std::max<int64_t>((move_units(a) + kMoveWaves - 1) / kMoveWaves * 64 * kMoveWaves, p.parts ? units * p.parts * kPartThreads : units * kThreads);
+}
+
+hipError_t launch_kv_evict(const KvEvictArgs &a, const KvEvictParts &p, hipStream_t stream)
+{
+    const int64_t most = (int64_t)a.c.width << a.c.page_shift, units = (int64_t)a.c.sequences * a.c.heads;
+    if (p.parts) {
+        const int64_t words = (int64_t)(p.counts_bytes / 4);
+        const dim3 groups((uint32_t)(units * p.parts)), block(kPartThreads), clear((uint32_t)std::min<int64_t>((words + kPartThreads - 1) / kPartThreads, 4096));
+        kv_clear_kernel<<<clear, block, 0, stream>>>(static_cast<uint32_t *>(p.counts), words);
+        kv_count_kernel<0><<<groups, block, 0, stream>>>(a, p);
+        kv_count_kernel<1><<<groups, block, 0, stream>>>(a, p);
+        kv_count_kernel<2><<<groups, block, 0, stream>>>(a, p);
+        kv_tally_kernel<<<groups, block, 0, stream>>>(a, p);
+        kv_keep_kernel<<<groups, block, 0, stream>>>(a, p);
+    } else {
+        const dim3 groups((uint32_t)units), block(kThreads);
+        if (most <= 4 * kThreads) kv_select_kernel<4><<<groups, block, 0, stream>>>(a);
+        else if (most <= 16 * kThreads) kv_select_kernel<16><<<groups, block, 0, stream>>>(a);
+        else kv_select_kernel<64><<<groups, block, 0, stream>>>(a);
+    }
+    const int64_t places = move_units(a);
+    const dim3 grid((uint32_t)((places + kMoveWaves - 1) / kMoveWaves)), four(64 * kMoveWaves);
+    if (a.c.head_dim == 128) kv_move_kernel<128><<<grid, four, 0, stream>>>(a, kv_divisor(a.c.heads), (a.budget + 7) / 8, places);
+    else kv_move_kernel<64><<<grid, four, 0, stream>>>(a, kv_divisor(a.c.heads), (a.budget + 7) / 8, places);
     return hipGetLastError();
 }
 

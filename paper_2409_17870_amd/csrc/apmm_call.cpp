@@ -42,11 +42,12 @@ struct Library {
     decltype(&apmm_kv_weights) kv_weights;
     decltype(&apmm_kv_weights_workspace_bytes) kv_weights_workspace_bytes;
     decltype(&apmm_kv_evict) kv_evict;
+    decltype(&apmm_kv_evict_workspace_bytes) kv_evict_workspace_bytes;
     decltype(&apmm_w4_packed_bytes) w4_packed_bytes;
     decltype(&apmm_w4_workspace_bytes) w4_workspace_bytes;
     decltype(&apmm_w4_gemm) w4_gemm;
 };
-constexpr int kLibraryFunctions = 19;
+constexpr int kLibraryFunctions = 20;
 Library lib = {};
 bool loaded = false;
 PyObject *check = nullptr;  // binding.py's _check
@@ -74,8 +75,8 @@ Signature signatures[kFunctions] = {
     {"apmm_kv_write_rotary", 13, 8,
      {"q", "k", "v", "codes", "scales", "page_table", "lengths", "frequencies", "starts", "positions", "interleaved", "magnitude", "q_out"}, {}, nullptr},
     {"apmm_kv_weights", 12, 6, {"q", "codes", "scales", "page_table", "lengths", "weights", "starts", "window", "sinks", "scale", "decay", "workspace"}, {}, nullptr},
-    {"apmm_kv_evict", 12, 7,
-     {"codes", "scales", "page_table", "lengths", "weights", "budget", "to_table", "sinks", "recent", "kept", "to_weights", "to_lengths"}, {}, nullptr},
+    {"apmm_kv_evict", 13, 7,
+     {"codes", "scales", "page_table", "lengths", "weights", "budget", "to_table", "sinks", "recent", "kept", "to_weights", "to_lengths", "workspace"}, {}, nullptr},
     {"apmm_w4_gemm", 6, 4, {"x", "packed", "N", "group", "out", "workspace"}, {}, nullptr},
 };
 
@@ -493,15 +494,17 @@ int kv_evict(PyObject **v, PyObject *&result)
         if (!t || t->scalar_type() != (i == 10 ? at::kFloat : at::kInt) || t->sizes() != at::IntArrayRef(shape, i == 11 ? 1 : 3) || t->get_device() != lengths->get_device() || !t->is_contiguous())
             return 0;
     }
-    Output out[3];
-    int done = 1;
+    if (given(v[12]) && (!tensor(v[12]) || !tensor(v[12])->is_contiguous() || tensor(v[12])->get_device() != lengths->get_device())) return 0;
+    const size_t need = given(v[12]) ? 0 : lib.kv_evict_workspace_bytes(&c, b.sequences, b.table_width);
+    Output out[3], work;
+    int done = output(work, v[12], need != 0, *lengths, {(int64_t)need}, at::kByte);
     for (int i = 0; i < 3 && done; ++i) done = output(out[i], v[9 + i], true, *lengths, at::IntArrayRef(shape, i == 2 ? 1 : 3), i == 1 ? at::kFloat : at::kInt);
     if (done) {
         void *s = stream();
         const bool went = called([&] {
             return lib.kv_evict(&c, b.sequences, b.lengths, b.page_table, b.table_stride, b.table_width, static_cast<const float *>(w->data_ptr()), w->stride(0), w->stride(1), w->size(2), budget, sinks,
                                 recent, to.page_table, to.table_stride, to.table_width, static_cast<int32_t *>(out[2].address), static_cast<int32_t *>(out[0].address),
-                                static_cast<float *>(out[1].address), s);
+                                static_cast<float *>(out[1].address), work.address, given(v[12]) ? bytes(*tensor(v[12])) : need, s);
         });
         done = went ? 1 : -1;
     }
@@ -511,6 +514,7 @@ int kv_evict(PyObject **v, PyObject *&result)
     }
     for (Output &o : out)
         if (o.made) Py_DECREF(o.object);
+    if (work.made) Py_DECREF(work.object);
     return done;
 }
 
@@ -632,7 +636,7 @@ PyMethodDef methods[] = {
      "apmm_kv_weights(q, codes, scales, page_table, lengths, weights, starts=None, window=0, sinks=0, scale=None, decay=1.0, workspace=None)\n--\n\n"
      "What attention of the new tokens' queries gives each cached token, added to decay * weights."},
     {"apmm_kv_evict", ENTRY(kKvEvict),
-     "apmm_kv_evict(codes, scales, page_table, lengths, weights, budget, to_table, sinks=0, recent=0, kept=None, to_weights=None, to_lengths=None)\n--\n\n"
+     "apmm_kv_evict(codes, scales, page_table, lengths, weights, budget, to_table, sinks=0, recent=0, kept=None, to_weights=None, to_lengths=None, workspace=None)\n--\n\n"
      "Keep of each sequence and head the first tokens, the last and the heaviest others: (places they had, their weights, the new lengths)."},
     {"apmm_w4_gemm", ENTRY(kW4Gemm),
      "apmm_w4_gemm(x, packed, N, group, out=None, workspace=None)\n--\n\nx (M x K, float16 or bfloat16) times packed weights of N channels: M x N of x's type."},

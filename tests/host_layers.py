@@ -54,7 +54,8 @@ class Host(host_wave.Host):
         lib.apmm_kv_write_rotary.argtypes = [cache, batch, ci, vp, rotation] + rows * 4 + [vp]
         lib.apmm_kv_weights.argtypes = [cache, batch, ci] + rows + [vp, i64, i64, i64, cf, cf, i64, i64, vp, ctypes.c_size_t, vp]
         lib.apmm_kv_weights_workspace_bytes.argtypes, lib.apmm_kv_weights_workspace_bytes.restype = [cache, batch, ci], ctypes.c_size_t
-        lib.apmm_kv_evict.argtypes = [cache, ci, vp, vp, i64, i64, vp, i64, i64, i64, i64, i64, i64, vp, i64, i64, vp, vp, vp, vp]
+        lib.apmm_kv_evict.argtypes = [cache, ci, vp, vp, i64, i64, vp, i64, i64, i64, i64, i64, i64, vp, i64, i64, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        lib.apmm_kv_evict_workspace_bytes.argtypes, lib.apmm_kv_evict_workspace_bytes.restype = [cache, ci, i64], ctypes.c_size_t
         self.lib = lib
 
     def rotation(self, frequencies, interleaved, magnitude):
@@ -84,7 +85,9 @@ class Host(host_wave.Host):
     def evict(self, codes, scales, table, lengths, w, budget, to, sinks=0, recent=0):
         cache, _ = self.structs(codes, scales, table, lengths, None, lengths.shape[0])
         m, shape = Memory(), (lengths.shape[0], scales.shape[1], budget)
+        need = self.lib.apmm_kv_evict_workspace_bytes(cache, shape[0], table.shape[1])
+        work = m.empty((need,), torch.uint8).fill_(0xff)
         kept, weights, n = m.empty(shape, torch.int32), m.empty(shape, torch.float32), m.empty(shape[:1], torch.int32)
         self.call(self.lib.apmm_kv_evict, cache, shape[0], lengths.data_ptr(), table.data_ptr(), table.stride(0), table.shape[1], w.data_ptr(), w.stride(0), w.stride(1), w.shape[2], budget, sinks,
-                  recent, to.data_ptr(), to.stride(0), to.shape[1], n.data_ptr(), kept.data_ptr(), weights.data_ptr(), None)
+                  recent, to.data_ptr(), to.stride(0), to.shape[1], n.data_ptr(), kept.data_ptr(), weights.data_ptr(), work.data_ptr(), need, None)
         return kept.clone(), weights.clone(), n.clone()

@@ -278,22 +278,27 @@ def test_eviction(gpu, case, kind, dtype):
     assert torch.equal(after.view(torch.int16), before.view(torch.int16))      # (bits: the rest of the cache is as it was)
 
 
-def test_long_eviction_equals_a_stable_sort(gpu):
+@pytest.mark.parametrize("L, heads, budget", [(70001, 2, 5003), (17000, 3, 16999), (33000, 1, 4096), (300017, 2, 70001), (1200001, 1, 1), (70001, 260, 100), (20000, 300, 3000)])
+def test_long_eviction_equals_a_stable_sort(gpu, L, heads, budget):
+    """Sequences of one workgroup to a head and of many, of one chunk of tokens each and of several."""
     torch, binding = gpu
-    L, heads, budget, ps = 70001, 2, 5003, 16
+    ps = 16
     g = torch.Generator(device="cuda").manual_seed(1)
     pages = -(-L // ps) + -(-budget // ps)
-    codes = torch.randint(0, 256, (pages, heads, 2, ps * 32), generator=g, device="cuda", dtype=torch.uint8)
-    scales = torch.rand((pages, heads, 2, ps), generator=g, device="cuda").half()
+    codes = torch.empty((pages, heads, 2, ps * 32), device="cuda", dtype=torch.uint8)
+    scales = torch.empty((pages, heads, 2, ps), device="cuda", dtype=torch.float16)
     table, to = (torch.arange(a, z, dtype=torch.int32, device="cuda")[None] for a, z in ((0, -(-L // ps)), (-(-L // ps), pages)))
     lengths = torch.tensor([L], dtype=torch.int32, device="cuda")
     for step in (0.0, 0.5, 1e9):                                               # all different, many equal, all equal
         w = torch.exp(2 * torch.randn((1, heads, L), generator=g, device="cuda"))
         if step:
             w = torch.floor(w / step) * step
-        kept, weights, length = binding.apmm_kv_evict(codes, scales, table, lengths, w, budget, to, sinks=4, recent=100)
+        sinks, recent = min(4, budget), min(100, max(0, budget - 4))
+        kept, weights, length = binding.apmm_kv_evict(codes, scales, table, lengths, w, budget, to, sinks=sinks, recent=recent)
         value = w.clone()
-        value[:, :, :4] = value[:, :, -100:] = float("inf")
+        value[:, :, :sinks] = float("inf")
+        if recent:
+            value[:, :, -recent:] = float("inf")
         order = torch.sort(value, dim=2, descending=True, stable=True).indices[:, :, :budget].sort(2).values
         assert torch.equal(kept.long(), order) and torch.equal(weights, w.gather(2, order)) and length.tolist() == [budget]
 

@@ -30,8 +30,9 @@ def weigh(lib, cache={}, batch={}, q_heads=32, q=0x6000, w=0x7000, strides=(8192
 
 
 def evict(lib, cache={}, sequences=3, lengths=0x3000, table=0x5000, width=10, w=0x7000, strides=(8192, 1000), capacity=1000, budget=64, sinks=0, recent=0, to=0x5800, to_stride=4, to_width=4,
-          to_lengths=0x9000, kept=0xa000, to_weights=0xb000):
-    return lib.apmm_kv_evict(structs(cache)[0], sequences, lengths, table, width, width, w, *strides, capacity, budget, sinks, recent, to, to_stride, to_width, to_lengths, kept, to_weights, None)
+          to_lengths=0x9000, kept=0xa000, to_weights=0xb000, workspace=None, size=0):
+    return lib.apmm_kv_evict(structs(cache)[0], sequences, lengths, table, width, width, w, *strides, capacity, budget, sinks, recent, to, to_stride, to_width, to_lengths, kept, to_weights, workspace,
+                             size, None)
 
 
 @pytest.mark.parametrize("status, cache, batch", REFUSED)
@@ -96,6 +97,12 @@ def test_eviction(lib):  # noqa: F811
                            (INVALID, dict(to=None)), (INVALID, dict(to_lengths=None)), (INVALID, dict(kept=None)), (INVALID, dict(to_weights=None)), (INVALID, dict(kept=0xa002)),
                            (INVALID, dict(to_lengths=0x3000)), (UNSUPPORTED, dict(budget=1 << 28)), (UNSUPPORTED, dict(sequences=65536, cache=dict(kv_heads=64), budget=1))]:
         assert evict(lib, **change) == status, change
+    room, (c, b) = lib.apmm_kv_evict_workspace_bytes, structs()
+    assert room(c, 3, 65536 // c.page_size) == 0 and room(c, 0, 1 << 20) == 0 and room(c, -1, 1 << 20) == 0 and room(c, 3, 0) == 0
+    width = 65536 // c.page_size + 1
+    need = room(c, 3, width)
+    assert 3 * c.kv_heads * 3 * 2048 * 4 < need <= 3 * c.kv_heads * (3 * 2048 * 4 + 256 * 8) and room(c, 3, 1 << 26) <= 3 * c.kv_heads * (3 * 2048 * 4 + 256 * 8)
+    assert evict(lib, width=width) == WORKSPACE and evict(lib, width=width, workspace=0xc000, size=need - 1) == WORKSPACE and evict(lib, width=width, workspace=0xc008, size=need) == INVALID
 
 
 def test_w4(lib):  # noqa: F811

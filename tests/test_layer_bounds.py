@@ -70,7 +70,8 @@ def test_weights(host, case):
             assert bool(((got[i, :, :n].double() - want[i, :, :n]).abs() <= near[i, :, :n]).all()) and torch.equal(got[i, :, n:], w[i, :, n:])
 
 
-@pytest.mark.parametrize("ps, lengths, budget, sinks, recent, width", [(16, [100, 0, 7, 33], 20, 2, 5, 0), (64, [900, 3], 300, 0, 100, 100), (64, [700], 64, 4, 0, 300), (64, [500, 65], 70, 1, 9, 1100)])
+@pytest.mark.parametrize("ps, lengths, budget, sinks, recent, width", [(16, [100, 0, 7, 33], 20, 2, 5, 0), (64, [900, 3], 300, 0, 100, 100), (64, [700], 64, 4, 0, 300), (64, [500, 65], 70, 1, 9, 1100), (16, [9000, 5000, 30], 700, 3, 40, 4200),
+                                                                        (16, [4097, 8192], 4500, 0, 0, 4200)])
 def test_eviction(host, ps, lengths, budget, sinks, recent, width):
     """Tables of all widths that the selection tells apart."""
     heads, D = 2, 64
@@ -116,6 +117,11 @@ def test_wild_batches(host, seed):
     args = codes, scales, table, lengths
     host.write_rotary(q, k, v, *args, f, starts, r.choice([None, positions]), interleaved=seed % 2)
     host.weights(q, *args, w, starts, window=r.choice([0, 0, 50]), sinks=7, decay=r.choice([0.0, 1.0]))
+    if seed % 3 == 0:  # (a table so wide that several workgroups share a sequence)
+        wide = torch.randint(-2, codes.shape[0] + 2, (sequences, 4200), generator=g, dtype=torch.int32)
+        lengths = torch.tensor([wild(r, 12000) for _ in range(sequences)], dtype=torch.int32)
+        table, lengths = guarded(wide, lengths)
+        args, width = (codes, scales, table, lengths), 4200
     if sequences <= 12:
         budget = r.choice([1, 20, 70])
         kept, _, left = host.evict(*args, w, budget, to, sinks=r.choice([0, 1]), recent=r.choice([0, budget - 1]))

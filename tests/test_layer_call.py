@@ -57,6 +57,8 @@ def test_results_and_errors_alike():
     w4 = binding.apmm_w4_pack(torch.randint(0, 16, (48, 256), generator=g, device=dev, dtype=torch.uint8), torch.rand((48, 4), generator=g, device=dev).half(), 64)
     general_of = {name: general(name) for name in NAMES}
     room = binding.apmm_kv_weights_workspace_bytes(20, Hq, *c)
+    wide = torch.cat([table, torch.full((B, 4200), -1, dtype=torch.int32, device=dev)], 1)
+    more = binding.apmm_kv_evict_workspace_bytes(codes, scales, wide)
 
     def cache():
         return codes.clone(), scales.clone(), table, lengths
@@ -97,6 +99,10 @@ def test_results_and_errors_alike():
         ("apmm_kv_evict", PLAIN, lambda: ((*cache(), w, 50, to), {})),
         ("apmm_kv_evict", PLAIN, lambda: ((*cache(), w, 50, to, 2, 7, torch.zeros((B, H, 50), dtype=torch.int32, device=dev), torch.zeros((B, H, 50), device=dev), torch.zeros_like(lengths)), {})),
         ("apmm_kv_evict", PLAIN, lambda: ((*cache(), w, 50, to), dict(sinks=51))),
+        ("apmm_kv_evict", PLAIN, lambda: ((*cache()[:2], wide, lengths, w, 50, to), {})),
+        ("apmm_kv_evict", PLAIN, lambda: ((*cache()[:2], wide, lengths, w, 50, to), dict(recent=4, workspace=space(more)))),
+        ("apmm_kv_evict", PLAIN, lambda: ((*cache()[:2], wide, lengths, w, 50, to), dict(workspace=space(more - 1)))),
+        ("apmm_kv_evict", GENERAL, lambda: ((*cache()[:2], wide, lengths, w, 50, to), dict(workspace=space(more, device="cpu")))),
         ("apmm_kv_evict", GENERAL, lambda: ((*cache(), w, 50, to[:2]), {})),
         ("apmm_kv_evict", GENERAL, lambda: ((*cache(), w, 50, to), dict(kept=torch.zeros((B, H, 49), dtype=torch.int32, device=dev)))),
         ("apmm_kv_evict", GENERAL, lambda: ((*cache(), w.half(), 50, to), {})),
