@@ -77,8 +77,8 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryRows a)
 constexpr int kWaves = 4;
 
 // A workgroup has the up to eight tokens of an aligned eight of positions, as kv_write_kernel's waves have, and `per_wave` heads to each wave: those of keys and values first, then those of queries.
-// It makes the eight's cosines and sines once.  Four heads to a wave where there are many: 13 sequences of up to 1500 new tokens, 32 heads of 128, 184 MB read and written in 65 us; 32 single tokens of 8 and 32
-// heads 7.2, of which the way from lengths to pages to a partly filled eight is the longer part.
+// It makes the eight's cosines and sines once.  Four heads to a wave where there are many: 13 sequences of up to 1500 new tokens, 32 heads of 128, 184 MB read and written in 63 us (65 with rows that wait for the cosines and partners read
+// again; with the read back 82, two heads to a wave 85, eight 87); 32 single tokens of 8 and 32 heads 6.8, of which the way from lengths to pages to a partly filled eight is the longer part.
 template <int D, bool BF16>
 __global__ __launch_bounds__(64 * kWaves) void kv_rotary_write_kernel(KvRotaryArgs a)
 {
@@ -88,16 +88,35 @@ __global__ __launch_bounds__(64 * kWaves) void kv_rotary_write_kernel(KvRotaryAr
     const int eight = kv_divide(blockIdx.x, a.by_blocks), block = blockIdx.x - eight * a.blocks, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     Eight e;
     if (!find_eight(a.c, eight, e)) return;  // (all waves of the workgroup alike)
-    const int lane = kv_lane(), token = lane >> 3, part = lane & 7, pairs = a.r.pairs;
+    const int lane = kv_lane(), token = lane >> 3, part = lane & 7, pairs = a.r.pairs, all = a.c.heads + a.q_heads;
+    const int64_t row = e.s.start + (e.is_new ? e.first + token - e.s.first : 0);  // (a lane without one reads the first)
+    auto head_of = [&](int i) { return (block * a.per_wave + i) * kWaves + wave; };
+    auto first_row = [&](int head) { return head < a.c.heads ? a.k.data + row * a.k.token_stride + head * a.k.head_stride : a.q.data + row * a.q.token_stride + (head - a.c.heads) * a.q.head_stride; };
+    auto load = [&](int head, uint32_t (&x)[N], uint32_t (&y)[N]) {  // a query, or a key and a value
+        if (head >= all || (head < a.c.heads && e.page < 0)) return;
+        load_row(first_row(head), head < a.c.heads ? a.k.aligned : a.q.aligned, part, x);
+        if (head < a.c.heads) load_row(a.v.data + row * a.v.token_stride + head * a.v.head_stride, a.v.aligned, part, y);
+    };
+    uint32_t x[N], y[N];
+    load(head_of(0), x, y);  // (on their way while the cosines and sines are made)
     for (int i = threadIdx.x; i < 8 * pairs; i += 64 * kWaves) {
         const int t = i / pairs, place = e.first + t;
         if (place < e.s.first || place >= e.s.first + e.s.n) continue;
         turns[t][i - t * pairs] = rotary_turn(a.r, a.r.positions ? a.r.positions[e.s.start + place - e.s.first] : place, i - t * pairs);
     }
     __syncthreads();
-    const int64_t row = e.s.start + (e.is_new ? e.first + token - e.s.first : 0);  // (a lane without one reads the first)
-    auto turned = [&](const uint16_t *from, bool aligned, uint32_t (&x)[N]) {
-        load_row(from, aligned, part, x);
+    auto turned = [&](const uint16_t *from, bool aligned) {
+        if (D == 128 && pairs == 64 && !a.r.interleaved) {  // both partners are this lane's
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int second = D == 128 ? 4 + j : j;
+                const float2 c1 = turns[token][8 * part + 2 * j], c2 = turns[token][8 * part + 2 * j + 1];
+                const float a1 = kv_scale_value(x[j] & 0xffffu, BF16), a2 = kv_scale_value(x[j] >> 16, BF16), b1 = kv_scale_value(x[second] & 0xffffu, BF16), b2 = kv_scale_value(x[second] >> 16, BF16);
+                x[j] = rotary_pair(rotary_one(a1, -b1, c1.x, c1.y), rotary_one(a2, -b2, c2.x, c2.y), BF16);
+                x[second] = rotary_pair(rotary_one(b1, a1, c1.x, c1.y), rotary_one(b2, a2, c2.x, c2.y), BF16);
+            }
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < N / 4; ++i) {
             uint32_t w[4] = {x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
@@ -106,19 +125,16 @@ __global__ __launch_bounds__(64 * kWaves) void kv_rotary_write_kernel(KvRotaryAr
             for (int j = 0; j < 4; ++j) x[4 * i + j] = w[j];
         }
     };
-    const int all = a.c.heads + a.q_heads;
     for (int i = 0; i < a.per_wave; ++i) {
-        const int head = (block * a.per_wave + i) * kWaves + wave;
+        const int head = head_of(i);
         if (head >= all) break;
-        uint32_t x[N];
+        if (i) load(head, x, y);
         if (head >= a.c.heads) {
-            const int h = head - a.c.heads;
-            turned(a.q.data + row * a.q.token_stride + h * a.q.head_stride, a.q.aligned, x);
-            if (e.is_new) store_row(a.q_out.data + row * a.q_out.token_stride + h * a.q_out.head_stride, a.q_out.aligned, part, x);
+            turned(first_row(head), a.q.aligned);
+            if (e.is_new) store_row(a.q_out.data + row * a.q_out.token_stride + (head - a.c.heads) * a.q_out.head_stride, a.q_out.aligned, part, x);
         } else if (e.page >= 0) {
-            uint32_t y[N], uk[N / 4], uv[N / 4];
-            turned(a.k.data + row * a.k.token_stride + head * a.k.head_stride, a.k.aligned, x);
-            load_row(a.v.data + row * a.v.token_stride + head * a.v.head_stride, a.v.aligned, part, y);
+            uint32_t uk[N / 4], uv[N / 4];
+            turned(first_row(head), a.k.aligned);
             const uint32_t sk = quantise<N, BF16>(x, uk), sv = quantise<N, BF16>(y, uv);
             write_codes<D>(a.c, e, head, uk, sk, uv, sv, turn[wave]);
         }
