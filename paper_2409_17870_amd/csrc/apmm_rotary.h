@@ -2,8 +2,8 @@
 //
 //   (a, b) of a pair becomes (g (a cos t - b sin t), g (b cos t + a sin t)), t = position times the pair's frequency
 //
-// The angle is a product in 64 bits, taken as turns less the whole ones: positions of 2^31 leave it off by 2^-24 of a turn at most, 32 bits would be off by many turns.  Sums and products of the turn
-// itself are of 32 bits, rounded once to the rows' type.
+// The angle is a product in 64 bits, taken as turns less the whole ones: positions of 2^31 leave it off by 2^-24 of a turn at most, 32 bits would be off by many turns.  Cosine and sine are made in
+// 64 bits too; sums and products are of 32, rounded once to the rows' type.
 #pragma once
 #include "apmm_kv.h"
 
@@ -42,47 +42,77 @@ int64_t kv_rotary_items(const KvArgs &c, int q_heads);
 hipError_t launch_kv_write_rotary(const KvRotaryArgs &a, hipStream_t stream);
 
 #ifdef __HIPCC__
-// Cosine and sine of a pair at a position, times the magnitude
-__device__ __forceinline__ float2 rotary_turn(const RotaryArgs &r, int position, int pair)
+// Cosine and sine of a pair at a position, times the magnitude, made in 64 bits, as numbers of 32 and what these leave: Taylor's series over an eighth of a turn to either side, whose next terms are below 2^-45
+__device__ __forceinline__ float4 rotary_turn(const RotaryArgs &r, int position, int pair)
 {
-    const double turns = (double)position * (r.frequencies[pair] * 0.15915494309189533577), rest = turns - rint(turns);
-    // (what 32 bits leave of the angle goes in as the sums' first order: keys are quantised behind this, where an error may cost a code)
-    const float near = (float)rest, left = 6.283185307f * (float)(rest - (double)near);
-    float s, c;
-    sincospif(2.0f * near, &s, &c);
-    return make_float2(fmaf(-left, s, c) * r.magnitude, fmaf(left, c, s) * (r.magnitude * r.sign));
+    constexpr double kPerRadian = 0.15915494309189535, kPerRadianLow = -9.839338337591243e-18, kRadians = 6.283185307179586;  // 1 / (2 pi) in two parts
+    const double t = (double)position * r.frequencies[pair], high = t * kPerRadian, low = fma(t, kPerRadian, -high) + t * kPerRadianLow;
+    const double rest = (high - rint(high)) + low, quarter = rint(4.0 * rest), x = (rest - 0.25 * quarter) * kRadians, y = x * x;
+    double s = 1.0 / 6227020800.0, c = -1.0 / 87178291200.0;
+    s = fma(s, y, -1.0 / 39916800.0);
+    s = fma(s, y, 1.0 / 362880.0);
+    s = fma(s, y, -1.0 / 5040.0);
+    s = fma(s, y, 1.0 / 120.0);
+    s = fma(s, y, -1.0 / 6.0);
+    s = fma(s * y, x, x);
+    c = fma(c, y, 1.0 / 479001600.0);
+    c = fma(c, y, -1.0 / 3628800.0);
+    c = fma(c, y, 1.0 / 40320.0);
+    c = fma(c, y, -1.0 / 720.0);
+    c = fma(c, y, 1.0 / 24.0);
+    c = fma(c, y, -0.5);
+    c = fma(c, y, 1.0);
+    const int q = (int)quarter & 3;
+    const double cosine = q & 1 ? s : c, sine = q & 1 ? c : s;
+    const double cs = (q == 1 || q == 2 ? -cosine : cosine) * r.magnitude, sn = (q & 2 ? -sine : sine) * (r.magnitude * r.sign);
+    const float c1 = (float)cs, s1 = (float)sn;
+    return make_float4(c1, s1, (float)(cs - (double)c1), (float)(sn - (double)s1));
 }
-// One of a pair: `other` comes with the sign that the sine has for it.  (Always in this form, so that rows come out the same wherever they are turned.)
-__device__ __forceinline__ float rotary_one(float x, float other, float cosine, float sine) { return fmaf(x, cosine, other * sine); }
+// One of a pair: `other` comes with the sign that the sine has for it.  What the product and the rounding of cosine and sine to 32 bits have left goes in as a sum of its own, so that the result is off by two roundings
+// of 32 bits however much of the pair cancels: keys are quantised behind this, where a 16-bit number rounded the other way may cost a code.
+__device__ __forceinline__ float rotary_one(float x, float other, const float4 &t)
+{
+    const float p = other * t.y, left = fmaf(other, t.y, -p);
+    return fmaf(x, t.x, p) + fmaf(x, t.z, fmaf(other, t.w, left));
+}
+
+// A token's cosines and sines in LDS: pair p in row p % 8 or p % 4, as many rows as an eight of channels has pairs with (8) or within (4) it, so that lanes with an eight each read places that follow each other
+template <bool INTERLEAVED>
+struct RotaryTurns {
+    static constexpr int kShift = INTERLEAVED ? 2 : 3;
+    float4 *at;
+    int stride;
+    __device__ __forceinline__ float4 &operator[](int pair) const { return at[(pair & ((1 << kShift) - 1)) * stride + (pair >> kShift)]; }
+};
 
 __device__ __forceinline__ uint32_t rotary_pair(float a, float b, bool bf16) { return kv_round(a, bf16) | (uint32_t)kv_round(b, bf16) << 16; }
 
-// Eight channels from c0 on of the row that begins at `row`, w their words; t: the token's cosines and sines by pair
-template <bool BF16>
-__device__ __forceinline__ void rotary_eight(const uint16_t *row, bool aligned, int c0, uint32_t (&w)[4], const float2 *t, int pairs, bool interleaved)
+// Eight channels from c0 on of the row that begins at `row`, w their words
+template <bool BF16, bool INTERLEAVED>
+__device__ __forceinline__ void rotary_eight(const uint16_t *row, bool aligned, int c0, uint32_t (&w)[4], const RotaryTurns<INTERLEAVED> &t, int pairs)
 {
     if (c0 >= 2 * pairs) return;
-    if (interleaved) {
+    if (INTERLEAVED) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int pair = c0 / 2 + i;
             if (pair >= pairs) break;
-            const float2 cs = t[pair];
+            const float4 cs = t[pair];
             const float a = kv_scale_value(w[i] & 0xffffu, BF16), b = kv_scale_value(w[i] >> 16, BF16);
-            w[i] = rotary_pair(rotary_one(a, -b, cs.x, cs.y), rotary_one(b, a, cs.x, cs.y), BF16);
+            w[i] = rotary_pair(rotary_one(a, -b, cs), rotary_one(b, a, cs), BF16);
         }
         return;
     }
     uint32_t other[4];
     if (pairs % 8 == 0) {
         kv_load(row + (c0 < pairs ? c0 + pairs : c0 - pairs), aligned, other);
-        const float2 *at = t + (c0 < pairs ? c0 : c0 - pairs);
+        const int p0 = c0 < pairs ? c0 : c0 - pairs;
         const float by = c0 < pairs ? -1.0f : 1.0f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float2 c1 = at[2 * i], c2 = at[2 * i + 1];
-            w[i] = rotary_pair(rotary_one(kv_scale_value(w[i] & 0xffffu, BF16), by * kv_scale_value(other[i] & 0xffffu, BF16), c1.x, c1.y),
-                               rotary_one(kv_scale_value(w[i] >> 16, BF16), by * kv_scale_value(other[i] >> 16, BF16), c2.x, c2.y), BF16);
+            const float4 c1 = t[p0 + 2 * i], c2 = t[p0 + 2 * i + 1];
+            w[i] = rotary_pair(rotary_one(kv_scale_value(w[i] & 0xffffu, BF16), by * kv_scale_value(other[i] & 0xffffu, BF16), c1),
+                               rotary_one(kv_scale_value(w[i] >> 16, BF16), by * kv_scale_value(other[i] >> 16, BF16), c2), BF16);
         }
         return;
     }
@@ -90,9 +120,9 @@ __device__ __forceinline__ void rotary_eight(const uint16_t *row, bool aligned, 
     for (int i = 0; i < 8; ++i) {
         const int c = c0 + i;
         if (c >= 2 * pairs) break;
-        const float2 cs = t[c < pairs ? c : c - pairs];
+        const float4 cs = t[c < pairs ? c : c - pairs];
         const float x = kv_scale_value(i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xffffu, BF16), y = kv_scale_value(row[c < pairs ? c + pairs : c - pairs], BF16);
-        const uint32_t bits = kv_round(rotary_one(x, c < pairs ? -y : y, cs.x, cs.y), BF16);
+        const uint32_t bits = kv_round(rotary_one(x, c < pairs ? -y : y, cs), BF16);
         w[i / 2] = i & 1 ? (w[i / 2] & 0xffffu) | bits << 16 : (w[i / 2] & 0xffff0000u) | bits;
     }
 }
