@@ -303,9 +303,13 @@ def test_long_eviction_equals_a_stable_sort(gpu, L, heads, budget):
         assert torch.equal(kept.long(), order) and torch.equal(weights, w.gather(2, order)) and length.tolist() == [budget]
 
 
-def test_graph_and_stream(gpu):
+@pytest.mark.parametrize("columns", [13, 4200])                               # of a table for one workgroup to a sequence and head, and for several
+def test_graph_and_stream(gpu, columns):
     torch, binding = gpu
     b = Batch(torch, torch.float16, 64, 2, 1, 16, [200, 90], [1, 1], seed=21, spare=20)
+    table = torch.full((2, columns), -1, dtype=torch.int32)
+    table[:, :b.table.shape[1]] = b.table
+    b.args[2] = table.cuda()
     used = set(int(p) for p in b.table.flatten() if p >= 0)
     free = torch.tensor([p for p in range(b.codes.shape[0]) if p not in used][:8], dtype=torch.int32).view(2, 4).cuda()
     w = torch.rand((2, 2, 208), device="cuda")
@@ -399,3 +403,29 @@ def test_offsets_beyond_32_bits(gpu):
         one, other = binding.apmm_kv_evict(*x.args, near, 400, to.cuda(), recent=9), binding.apmm_kv_evict(*args, apart, 400, where[to.long()].cuda(), recent=9)
         assert all(torch.equal(i, j) for i, j in zip(one, other)) and torch.equal(codes[far], x.codes) and torch.equal(scales[far], x.scales)
         del apart
+
+
+def test_calls_on_two_streams_at_once(gpu):
+    """Each call has its own workspace: calls that overlap give what they give one after the other."""
+    torch, binding = gpu
+    lengths, new = [4000, 900, 2100], [1, 1, 1]
+    b, prompt = Batch(torch, torch.bfloat16, 128, 4, 4, 16, lengths, new, seed=31), Batch(torch, torch.float16, 64, 4, 1, 16, lengths, [300, 900, 40], seed=32)
+    codes, scales = torch.randint(0, 16, (1000, 2000), device="cuda", dtype=torch.uint8), torch.rand((1000, 16), device="cuda").half()
+    packed, x = binding.apmm_w4_pack(codes, scales, 128), torch.randn((50, 2000), device="cuda").half()
+    wide = torch.full((3, 4200), -1, dtype=torch.int32)
+    wide[:, :b.table.shape[1]] = b.table
+    wide, to = wide.cuda(), torch.full((3, 30), -1, dtype=torch.int32, device="cuda")
+    heavy = torch.rand((3, 4, 4000), device="cuda")
+
+    def calls():
+        return [binding.apmm_kv_weights(b.q, *b.args, torch.zeros((3, 4, 4000), device="cuda")), binding.apmm_kv_weights(prompt.q, *prompt.args, torch.zeros((3, 4, 4000), device="cuda"), prompt.starts_gpu),
+                binding.apmm_w4_gemm(x, packed, 1000, 128), *binding.apmm_kv_evict(b.codes, b.scales, wide, b.args[3], heavy, 400, to, sinks=2, recent=20)]
+    want = calls()
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], []
+    for _ in range(4):
+        for s in streams:
+            with torch.cuda.stream(s):
+                got.append(calls())
+    torch.cuda.synchronize()
+    assert all(torch.equal(i, j) for some in got for i, j in zip(some, want))
