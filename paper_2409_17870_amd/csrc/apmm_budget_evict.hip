@@ -32,6 +32,14 @@ struct Tokens {
     }
 };
 
+// Of N waves' numbers those of the waves before this one, summed
+template <int N>
+__device__ __forceinline__ uint32_t sum_before(const uint32_t (&of_waves)[N], int wave)
+{
+    const int lane = kv_lane();
+    return (uint32_t)__builtin_amdgcn_readlane(kv_scan(lane < wave ? (int)of_waves[min(lane, N - 1)] : 0), 63);
+}
+
 // Numbers of tokens begin + 64 i + lane, zeros from `to` on
 template <int N>
 __device__ __forceinline__ void read_tokens(const Tokens &order, int begin, int to, uint32_t (&v)[N])
@@ -120,8 +128,7 @@ __global__ __launch_bounds__(kThreads) void kv_select_kernel(KvEvictArgs a)
         const uint32_t up_to = (uint32_t)kv_scan((int)(high + low));
         if (lane == 63) totals[wave] = up_to;
         __syncthreads();
-        uint32_t before = up_to - high - low;
-        for (int i = 0; i < wave; ++i) before += totals[i];
+        const uint32_t before = up_to - high - low + sum_before(totals, wave);
         if (before < rest && before + high + low >= rest) {
             const bool first = before + high >= rest;
             found_digit = kDigits - 1 - 2 * threadIdx.x - (first ? 0 : 1);
@@ -228,8 +235,7 @@ __device__ __forceinline__ Least find_least(const Counts *counts, uint32_t budge
         if (lane == 63) totals[wave] = up_to;
         if (threadIdx.x == 0) digit = 0xffffffffu;
         __syncthreads();
-        uint32_t before = up_to - sum;
-        for (int i = 0; i < wave; ++i) before += totals[i];
+        uint32_t before = up_to - sum + sum_before(totals, wave);
         if (before < l.rest && before + sum >= l.rest) {
             int i = 0;
             while (before + n[i] < l.rest) before += n[i++];
