@@ -27,6 +27,7 @@ constexpr int kWaves = 4;
 constexpr int kFew = 16;      // rows of a sequence that are few
 constexpr int64_t kMostScores = 64 << 20;  // few rows' that are kept in the workspace
 constexpr int kChunk = 4;     // tiles of 16 rows that are in LDS at a time
+constexpr int kFold = 8;      // of these whose weights are one sum
 
 struct RowFactor { float base, by; };  // -m and 1 / l; zeros for a row that sees nothing
 
@@ -528,11 +529,21 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_weights_many_kernel(KvAtten
         int last_token = s.n;  // (behind the last)
         if (a.window && block0 >= a.sinks) last_token = (int)min((int64_t)s.n, max((int64_t)block0 + kBlock - 1 + a.window - s.first, (int64_t)0));
         const int row_end = min(last_token * a.groups, rows);
-        float sums[KT][4];
+        // sums of kFold chunks' rows, and of these: of 8192 tiles one after the other the sum would be off by 2^-25 of itself 52 times, as a rule (8192 / 3 roundings' root), in two steps by 10
+        float sums[KT][4], whole[KT][4];
 #pragma unroll
         for (int t = 0; t < KT; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sums[t][i] = 0.0f;
+            for (int i = 0; i < 4; ++i) sums[t][i] = whole[t][i] = 0.0f;
+        auto fold = [&] {
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    whole[t][i] += sums[t][i];
+                    sums[t][i] = 0.0f;
+                }
+        };
         Keys<D> keys[KT];
 #pragma unroll
         for (int t = 0; t < KT; ++t) make_keys<D, BF16>(codes[t], keys[t]);
@@ -547,7 +558,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_weights_many_kernel(KvAtten
             factor = in.factors[tile * 16 + n];
             scale = in.scales[tile * 16 + n];
         };
-        int row0 = first_token * a.groups / 16 * 16, place = 0;
+        int row0 = first_token * a.groups / 16 * 16, place = 0, chunks = 0;
         if (row0 < row_end) bring(row0);
         __syncthreads();  // (of the unit before nothing is read from LDS any more)
         for (; row0 < row_end; row0 += 16 * kChunk, place ^= 1) {
@@ -558,6 +569,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_weights_many_kernel(KvAtten
                 rows_f[place][wave][n] = row < rows ? float4v{scale, factor.base, factor.by, __uint_as_float((uint32_t)(s.first + kv_divide(row, a.by_groups)))} :
                                                       float4v{0.0f, 0.0f, 0.0f, __uint_as_float((uint32_t)INT32_MIN)};
             __syncthreads();
+            if (++chunks % kFold == 0) fold();
             if (row0 + 16 * kChunk < row_end) bring(row0 + 16 * kChunk);
             const int tiles = min((row_end - row0 + 15) / 16, kChunk);
             for (int tile = 0; tile < tiles; ++tile) {
@@ -598,7 +610,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_weights_many_kernel(KvAtten
         for (int t = 0; t < KT; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                float v = sums[t][i];
+                float v = whole[t][i] + sums[t][i];
 #pragma unroll
                 for (int d = 1; d < 16; d *= 2) v += __shfl_xor(v, d);
                 const int key = key0 + 16 * t + 4 * g + i;

@@ -55,7 +55,8 @@ def weights_of(torch, b, q, before, starts, window, sinks, scale, decay, table=N
                 total += w.sum(0)
             m = min(keys, capacity)
             out[i, h, :m] = total[:m] + (decay * out[i, h, :m] if decay else 0.0)
-            near[i, h, :m] = off[:m] + (n * G + 4) * 2.0 ** -24 * out[i, h, :m].abs() + 1e-30
+            # a lane's sum: up to 32 tiles' rows one after the other (or 16 rows of few), such sums one after the other, sixteen lanes'
+            near[i, h, :m] = off[:m] + (min(n * G, 32 + n * G / 512) + 8) * 2.0 ** -24 * out[i, h, :m].abs() + 1e-30
     return out, near
 
 
@@ -103,6 +104,17 @@ def test_weights(gpu, case, dtype):
             if decay == 0 and length:                                        # each query gives 1 in all
                 n = min(new[i], length)
                 assert abs(float(got[i, :, :length].double().sum()) - n * heads * groups) <= 1e-4 * n * heads * groups
+
+
+def test_sums_over_many_rows(gpu):
+    """First tokens that every query sees under a window: 65536 rows' weights to one sum, 4096 a lane.  Two steps of 32 and 128 round to 2^-25 of the sum at most at each and so are off by 2^-25 sqrt((32 + 128) / 3) as a
+    rule, 2.2e-7; one after the other 4096 would be by 1.1e-6."""
+    torch, binding = gpu
+    b = Batch(torch, torch.bfloat16, 64, 1, 16, 64, [4096], [4096], seed=16)
+    w = binding.apmm_kv_weights(b.q, *b.args, torch.zeros((1, 1, 4096), device="cuda"), b.starts_gpu, window=14, sinks=3, decay=0.0)
+    want, near = weights_of(torch, b, b.q, torch.zeros((1, 1, 4096)), b.starts, 14, 3, 64 ** -0.5, 0.0)
+    off = (w.cpu().double() - want).abs()
+    assert bool((off <= near).all()) and float((off[0, 0, :3] / want[0, 0, :3]).pow(2).mean().sqrt()) < 6e-7
 
 
 def test_cut_rows_of_long_sequences(gpu):
