@@ -104,10 +104,14 @@ __global__ __launch_bounds__(kThreads) void kv_select_kernel(KvEvictArgs a)
     auto each = [&](auto f) {
         int from = own_from, lane = kv_lane();
         asm volatile("" : "+s"(from), "+v"(lane));  // (places and borders of 64 tokens are not kept from one pass for the next: for those there are no registers)
+        constexpr int kOnce = HELD < 8 ? HELD : 8;
 #pragma unroll
-        for (int i = 0; i < HELD; ++i) {
-            if (from + 64 * i < to) f(from + 64 * i + lane, i < 32 ? held[i < 32 ? i : 0] : more[i < 32 ? 0 : i - 32][threadIdx.x]);
-            if (i % 8 == 7) __builtin_amdgcn_sched_barrier(0);
+        for (int first = 0; first < HELD; first += kOnce) {
+            if (from + 64 * first < to) {  // (behind `to` numbers are zero)
+#pragma unroll
+                for (int i = first; i < first + kOnce; ++i) f(from + 64 * i + lane, i < 32 ? held[i < 32 ? i : 0] : more[i < 32 ? 0 : i - 32][threadIdx.x]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
     uint32_t least = 0, rest = (uint32_t)a.budget;  // what the digits so far say; how many are wanted of those that begin with them
