@@ -79,7 +79,7 @@ __device__ __forceinline__ Tokens tokens_of(const KvEvictArgs &a, int b, int hea
 template <int HELD>
 __global__ __launch_bounds__(kThreads) void kv_select_kernel(KvEvictArgs a)
 {
-    __shared__ uint32_t digits[kDigits];
+    __shared__ __align__(16) uint32_t digits[kDigits][2];  // (by even and odd lanes: fewer meet in one)
     __shared__ uint32_t totals[kWaves];
     __shared__ int above[kWaves], equal[kWaves];
     __shared__ uint32_t found_digit, found_rest;
@@ -120,15 +120,17 @@ __global__ __launch_bounds__(kThreads) void kv_select_kernel(KvEvictArgs a)
     for (int pass = 0; pass < 3; ++pass) {
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
         const uint32_t mask = (1u << bits) - 1, upper = pass == 0 ? 0 : ~0u << (shift + bits);
-        for (int i = threadIdx.x; i < kDigits; i += kThreads) digits[i] = 0;
+        reinterpret_cast<uint4 *>(digits)[threadIdx.x] = make_uint4(0, 0, 0, 0);
+        static_assert(sizeof(digits) == kThreads * sizeof(uint4), "");
         if (threadIdx.x == 0) found_digit = 0xffffffffu;
         __syncthreads();
         each([&](int, uint32_t v) {
-            if (v && (v & upper) == (least & upper)) atomicAdd(&digits[v >> shift & mask], 1u);
+            if (v && (v & upper) == (least & upper)) atomicAdd(&digits[v >> shift & mask][lane & 1], 1u);
         });
         __syncthreads();
         // from the highest digit down, two to a lane
-        const uint32_t high = digits[kDigits - 1 - 2 * threadIdx.x], low = digits[kDigits - 2 - 2 * threadIdx.x];
+        const uint4 both = reinterpret_cast<const uint4 *>(digits)[kThreads - 1 - threadIdx.x];
+        const uint32_t high = both.z + both.w, low = both.x + both.y;
         const uint32_t up_to = (uint32_t)kv_scan((int)(high + low));
         if (lane == 63) totals[wave] = up_to;
         __syncthreads();
