@@ -44,17 +44,24 @@ __device__ __forceinline__ uint32_t sum_before(const uint32_t (&of_waves)[N], in
 template <int N>
 __device__ __forceinline__ void read_tokens(const Tokens &order, int begin, int to, uint32_t (&v)[N])
 {
-    // tokens that all have a weight and a page, and none of which stays whatever its weight, are read as they lie
+    // tokens that all have a weight and a page are read as they lie
     const int lane = kv_lane(), end = min(begin + 64 * N, to), last = end - begin - 1;
-    bool plain = last >= 0 && begin >= order.sinks && end <= order.recent_from && end <= order.capacity;
-    if (plain)
-        for (int page = (begin >> order.shift) + lane; page <= (end - 1) >> order.shift; page += 64) plain &= order.table[page] >= 0 && order.table[page] < order.pages;
-    if (__ballot(!plain) == 0) {
+    bool plain = last >= 0 && end <= order.capacity;
+    if (plain) {
         const float *w = order.w + begin;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const uint32_t n = order_of(w[min(64 * i + lane, last)]);
-            v[i] = 64 * i + lane <= last ? n : 0u;
+        for (int i = 0; i < N; ++i) v[i] = __float_as_uint(w[min(64 * i + lane, last)]);
+        for (int page = (begin >> order.shift) + lane; page <= (end - 1) >> order.shift; page += 64) plain &= order.table[page] >= 0 && order.table[page] < order.pages;
+    }
+    if (__ballot(!plain) == 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = 64 * i + lane <= last ? order_of(__uint_as_float(v[i])) : 0u;
+        if (begin < order.sinks || end > order.recent_from) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int t = begin + 64 * i + lane;
+                v[i] = t < end && (t < order.sinks || t >= order.recent_from) ? 0xffffffffu : v[i];
+            }
         }
     } else {
 #pragma unroll
@@ -64,6 +71,7 @@ __device__ __forceinline__ void read_tokens(const Tokens &order, int begin, int 
             if (i % 8 == 7) __builtin_amdgcn_sched_barrier(0);  // (eight on their way at a time: of more there are no registers)
         }
     }
+    __builtin_amdgcn_sched_barrier(0);
 }
 __device__ __forceinline__ Tokens tokens_of(const KvEvictArgs &a, int b, int head)
 {
