@@ -81,9 +81,9 @@ __device__ __forceinline__ Tokens tokens_of(const KvEvictArgs &a, int b, int hea
 
 // A workgroup to a sequence and head, each of its waves has a stretch of tokens.  Three passes find the budget-th largest number, digit by digit from the highest; then each wave counts those of its stretch that
 // stay, and after the counts have met writes their places in order, whose weights are fetched at the end by all.  Sequences of up to 1024 HELD tokens, as far as the table goes, are read once and held in registers, the second half of 64 to a
-// lane in LDS.  Bound by the instructions of the one compute unit that has a sequence and head: 65001 tokens take 102 000 cycles, 23 000 to read them, 46 000 for the three passes (a fifth of it LDS additions that
-// meet in one digit), 10 000 to count and 21 000 to write.  Reading every token with its own checks took 55 000, a weight fetched as its place is written 48 000 in place of 21 000; reading the weights anew in each of
-// five passes 150 us.
+// lane in LDS.  Bound by the instructions of the one compute unit that has a sequence and head: 65001 tokens take 81 000 cycles, 18 000 to read them, 36 000 for the three passes, 8 000 to count and 19 000 to write.
+// Tried and slower, of as many cycles: every token read with its own checks (55 000 to read), a weight fetched as its place is written (48 000 to write), counts of all lanes in one (19 500 for the first pass, 16 500
+// so), the end of a stretch asked for at every token (18 000 more in all).
 template <int HELD>
 __global__ __launch_bounds__(kThreads) void kv_select_kernel(KvEvictArgs a)
 {
@@ -211,7 +211,7 @@ __global__ __launch_bounds__(kThreads) void kv_select_kernel(KvEvictArgs a)
 }
 
 // The same by many workgroups: a part of a sequence's tokens to each, in chunks of kChunk, a launch for each digit.  Counts of a digit meet in memory by additions of whole numbers, whose order changes nothing; each
-// workgroup finds the digits before its own again.  Six launches of 2 to 12 us (65001 tokens of 8 heads: 48 in all), bound by what each has to wait for in turn: lengths, pages, weights, counts.
+// workgroup finds the digits before its own again.  Six launches, bound by what each has to wait for in turn: lengths, pages, weights, counts.
 constexpr int kPartThreads = 256, kPartWaves = 4, kPartHeld = 16, kChunk = kPartThreads * kPartHeld, kMostParts = 256;
 
 struct Counts {  // of a sequence and head
@@ -471,8 +471,8 @@ int64_t move_units(const KvEvictArgs &a) { return (int64_t)a.c.sequences * ((a.b
 
 }  // namespace
 
-// Many workgroups to a sequence and head where its weights do not fit into one's registers and LDS (tokens of 8 heads, with the copy and the read back: 130000 64 us,
-// 1000000 90; of 20000, 33000 and 65000 it took 60 or 61, where one workgroup takes 43, 46 and 59)
+// Many workgroups to a sequence and head where its weights do not fit into one's registers and LDS.  (Tokens of 8 heads, with the copy and the read back: 130000 51 us, a million 82; 20000, 33000 and 65000 would take 49 to
+// 51, and take 33, 39 and 49 with one workgroup.)
 KvEvictParts kv_evict_parts(const KvArgs &c)
 {
     KvEvictParts p = {};
