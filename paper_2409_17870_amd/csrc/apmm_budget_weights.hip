@@ -50,15 +50,21 @@ __device__ __forceinline__ int first_tile(const KvAttentionArgs &a, const KvSequ
 // The odd integers 2 u - 15 of a word of codes as operand words (nibbles 0 and 4, 1 and 5, 2 and 6, 3 and 7): a code in bits 1 to 4 under the upper bits of 1024 is 1024 + 2 u, in bits 4 to 7 under those of
 // 128 it is 128 + 2 u.  The attention's operands, u 2^-24, take five operations in place of eleven, and leave a score off by 2^-17 of itself where these leave 2^-24 (the matrix unit keeps fewer bits of
 // products of subnormal numbers): too much for weights that are a result of 32 bits.
+__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t bits)
+{
+    uint32_t r;  // (in one instruction with one of the two in a scalar register; of two literals the compiler makes two)
+    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "s"(mask), "v"(bits));
+    return r;
+}
 __device__ __forceinline__ half8 odd_operand(uint32_t w)
 {
     const half2v less2 = {(_Float16)-1039.0f, (_Float16)-1039.0f}, less4 = {(_Float16)-143.0f, (_Float16)-143.0f};
     const uint32_t h = w >> 8;
     uint4 r;
-    r.x = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, ((w << 1) & 0x001e001eu) | 0x64006400u) + less2);
-    r.y = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, (w & 0x00f000f0u) | 0x58005800u) + less4);
-    r.z = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, ((w >> 7) & 0x001e001eu) | 0x64006400u) + less2);
-    r.w = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, (h & 0x00f000f0u) | 0x58005800u) + less4);
+    r.x = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, and_or(w << 1, 0x001e001eu, 0x64006400u)) + less2);
+    r.y = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, and_or(w, 0x00f000f0u, 0x58005800u)) + less4);
+    r.z = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, and_or(w >> 7, 0x001e001eu, 0x64006400u)) + less2);
+    r.w = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, and_or(h, 0x00f000f0u, 0x58005800u)) + less4);
     return __builtin_bit_cast(half8, r);
 }
 
@@ -172,7 +178,7 @@ __device__ __forceinline__ float max_of_three(float x, float y, float z)
 
 // First pass.  A workgroup has R tiles of 16 rows and a piece of the keys that they see, its waves take steps in turn, the next step's codes on their way while one's scores are made.
 template <int D, bool BF16, int R, bool SCORES>
-__global__ __launch_bounds__(64 * kWaves, R == 1 ? 4 : 2) void kv_statistics_kernel(KvAttentionArgs a, KvPart part, float *pieces, RowTiles out, RowScores scores)
+__global__ __launch_bounds__(64 * kWaves, 4) void kv_statistics_kernel(KvAttentionArgs a, KvPart part, float *pieces, RowTiles out, RowScores scores)
 {
     constexpr int W = D / 32, T = 16 * R;
     __shared__ float bases[kWaves][T], totals[kWaves][T];
@@ -192,29 +198,33 @@ __global__ __launch_bounds__(64 * kWaves, R == 1 ? 4 : 2) void kv_statistics_ker
         load_keys<D>(a, head, it.key_of(v), __builtin_amdgcn_readlane(ids, 0), codes[0]);
         load_keys<D>(a, head, it.key_of(v) + 16, __builtin_amdgcn_readlane(ids, 1), codes[1]);
     }
-    half8 q[R][W];
+    // one tile's operands are in each wave's registers, several tiles' in LDS, a wave makes one
+    __shared__ __align__(16) half8 rows_q[R > 1 ? R : 1][W][R > 1 ? 64 : 1];
+    __shared__ float rows_factor[R][16];
+    half8 q[W];
     float factor[R], top[R], total[R];
     int pos[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const int row = it.row0 + min(16 * r + n, rows - 1);
-        take_rows<D, BF16>(a, it.s.start, head, row, q[r], factor[r]);
-        pos[r] = it.s.first + kv_divide(row, a.by_groups);
+        pos[r] = it.s.first + kv_divide(it.row0 + min(16 * r + n, rows - 1), a.by_groups);
         top[r] = kLowest;
         total[r] = 0.0f;
     }
+    take_rows<D, BF16>(a, it.s.start, head, it.row0 + min(16 * (R > 1 ? wave : 0) + n, rows - 1), q, factor[0]);
     if constexpr (R > 1) {
         static_assert(R == kWaves, "a tile to a wave");
+#pragma unroll
+        for (int i = 0; i < W; ++i) rows_q[wave][i][lane] = q[i];
+        if (g == 0) rows_factor[wave][n] = factor[0];
         if (it.part == 0 && 16 * wave < rows) {
             const int64_t tile = (int64_t)(first_tile(a, it.s, it.b) + it.row0 / 16 + wave) * a.c.heads + head;
 #pragma unroll
-            for (int r = 0; r < R; ++r)
-                if (r == wave) {
-#pragma unroll
-                    for (int i = 0; i < W; ++i) reinterpret_cast<half8 *>(out.operands)[(tile * W + i) * 64 + lane] = q[r][i];
-                    if (g == 0) out.scales[tile * 16 + n] = factor[r];
-                }
+            for (int i = 0; i < W; ++i) reinterpret_cast<half8 *>(out.operands)[(tile * W + i) * 64 + lane] = q[i];
+            if (g == 0) out.scales[tile * 16 + n] = factor[0];
         }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < R; ++r) factor[r] = rows_factor[r][n];
     }
     const int first_pos = it.s.first + kv_divide(it.row0, a.by_groups), last_pos = it.s.first + kv_divide(it.row0 + rows - 1, a.by_groups);
     for (; v < it.to; v += kWaves) {
@@ -234,6 +244,7 @@ __global__ __launch_bounds__(64 * kWaves, R == 1 ? 4 : 2) void kv_statistics_ker
         make_keys<D, BF16>(codes[0], keys[0]);
         make_keys<D, BF16>(codes[1], keys[1]);
         const bool all = key0 + kStep <= it.s.keys && key0 + kStep - 1 <= first_pos && page0 >= 0 && page1 >= 0 && (!a.window || key0 > last_pos - a.window || key0 + kStep <= a.sinks);
+        if (R > 1) asm volatile("" ::: "memory");  // (the rows' operands are read in each step: held from one to the next they take the registers that a fourth wave has)
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             if (16 * r >= rows) break;
@@ -242,7 +253,7 @@ __global__ __launch_bounds__(64 * kWaves, R == 1 ? 4 : 2) void kv_statistics_ker
             for (int t = 0; t < 2; ++t) {
                 float4v s = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int i = 0; i < W; ++i) s = __builtin_amdgcn_mfma_f32_16x16x32_f16(keys[t].k[i], q[r][i], s, 0, 0, 0);
+                for (int i = 0; i < W; ++i) s = __builtin_amdgcn_mfma_f32_16x16x32_f16(keys[t].k[i], R > 1 ? rows_q[r][i][R > 1 ? lane : 0] : q[i], s, 0, 0, 0);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) x[4 * t + i] = s[i] * keys[t].s[i];
             }

@@ -16,7 +16,9 @@ HEADERS = ["apmm_api.h", "apmm_budget.h", "apmm_rotary.h"]
 
 def on_host(text):
     text = re.sub(r'asm\("v_max3_f32 %0, %1, %2, %3" : "=v"\((\w+)\) : "v"\((\w+)\), "v"\((\w+)\), "v"\((\w+)\)\);', r"\1 = fmaxf(fmaxf(\2, \3), \4);", text)
-    text = re.sub(r'asm volatile\("" : [^;]*\);', "", text)
+    text = re.sub(r'asm\("v_and_or_b32 %0, %1, %2, %3" : "=v"\((\w+)\) : "v"\((\w+)\), "s"\((\w+)\), "v"\((\w+)\)\);', r"\1 = (\2 & \3) | \4;", text)
+    text = re.sub(r'(if \(R > 1\) )?asm volatile\("" ::? [^;]*\);', "", text)
+    text = re.sub(r'(if \(R > 1\) )?asm volatile\("" ::: "memory"\);', "", text)
     text = re.sub(r"(\w+(?:<[\w, ]+>)?)<<<(\w+), (dim3\([^()]*\)|\w+), 0, stream>>>\(((?:[^()]|\([^()]*\))*)\)", r"host_layers::launch(\2, \3, [&] { \1(\4); })", text)
     return host_wave.on_host(text)
 
