@@ -80,6 +80,13 @@ __device__ __forceinline__ uint32_t w4_word(const uint32_t (&u)[8])
 template <bool BF16> struct W4Type { typedef _Float16 Eight __attribute__((ext_vector_type(8))); };
 template <> struct W4Type<true> { typedef __bf16 Eight __attribute__((ext_vector_type(8))); };
 
+__device__ __forceinline__ uint32_t w4_and_or(uint32_t x, uint32_t mask, uint32_t bits)
+{
+    uint32_t r;  // (in one instruction with one of the two in a scalar register; of two literals the compiler makes two)
+    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "s"(mask), "v"(bits));
+    return r;
+}
+
 // The eight odd integers of a word as an operand
 template <bool BF16>
 __device__ __forceinline__ typename W4Type<BF16>::Eight w4_operand(uint32_t w)
@@ -100,7 +107,7 @@ __device__ __forceinline__ typename W4Type<BF16>::Eight w4_operand(uint32_t w)
         const uint32_t v = __builtin_amdgcn_alignbit(w, w, 8);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t from = i < 2 ? w : v, pair = i & 1 ? (from & 0x01e001e0u) | 0x54005400u : (from & 0x001e001eu) | 0x64006400u;
+            const uint32_t from = i < 2 ? w : v, pair = i & 1 ? w4_and_or(from, 0x01e001e0u, 0x54005400u) : w4_and_or(from, 0x001e001eu, 0x64006400u);
             const half2v less = i & 1 ? half2v{(_Float16)-79.0f, (_Float16)-79.0f} : half2v{(_Float16)-1039.0f, (_Float16)-1039.0f};
             r[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, pair) + less);
         }
