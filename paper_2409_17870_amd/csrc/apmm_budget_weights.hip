@@ -8,10 +8,10 @@
 //
 // Few rows of a sequence (up to 16: token generation): both passes have the same workgroups, a piece of the keys each; the second joins the pieces' m and l as it begins.  The first keeps its scores for the second, a
 // number for each row and key, where they are no more than 2^26; else, and for the sequences of few rows beside others of many, the second makes them again from the keys.  8 sequences of up to 32768 tokens, 8 key/value
-// heads of 128: 4 query heads to one 56 us with scores kept (38 and 14; 111 MB of keys, 26 MB of scores written and read) and 78 with scores made twice (34 and 40), 6 60 and 78; 4 sequences of 8 to one 39 and 49, 16 to one
+// heads of 128: 4 query heads to one 55 us with scores kept (36 and 14; 111 MB of keys, 26 MB of scores written and read) and 78 with scores made twice (34 and 40), 6 60 and 78; 4 sequences of 8 to one 39 and 49, 16 to one
 // of 4 heads 32 and 35; one sequence of 3000 tokens 19 and 24.  Bound by HBM and, at the beginnings, by the way from lengths to pages to codes.
 // Many: the second pass has blocks of 256 keys (fewer where there are few of them), as operands in registers, and every row that sees some of them comes by through LDS, as the first pass left it in the workspace (RowTiles).  Bound by
-// the vector unit: of a score's 7 issues the exponential takes four.  4096 tokens of 32 heads of 128: 122 us for each pass, the unit busy for 75 and 67 of them.  Half as many workgroups, each with a first and a
+// the vector unit: of a score's 7 issues the exponential takes four.  4096 tokens of 32 heads of 128: 115 and 122 us (126 for the first pass with the rows in registers, three waves to a vector unit).  Half as many workgroups, each with a first and a
 // last block, took 257 us in all for 247; the next tile's operands read ahead, or its products made ahead, take registers that a fourth wave to a SIMD has (123 and 131 us for 121).
 #include <algorithm>
 #include <type_traits>
