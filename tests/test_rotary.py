@@ -232,3 +232,26 @@ def test_offsets_beyond_32_bits(gpu):
     far.copy_(x)
     want = binding.apmm_rotary(x, at, f)
     assert torch.equal(binding.apmm_rotary(far, at, f), want) and torch.equal(binding.apmm_rotary(far, at, f, out=far), want)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_numbers_that_are_not_finite(gpu, interleaved):
+    """An infinity goes where the formula takes it, with the signs of cosine and sine, two of a pair that cancel and NaN give NaN; other pairs do not notice."""
+    torch, binding = gpu
+    inf, nan = float("inf"), float("nan")
+    for dt in (torch.float16, torch.bfloat16):
+        x = torch.randn((6, 2, 64), generator=torch.Generator().manual_seed(7)).to(dt)
+        at, f = torch.tensor([1, 2, 3, 4, 5, 6], dtype=torch.int32), binding.apmm_rotary_frequencies(64)
+        clean = binding.apmm_rotary(x.cuda(), at.cuda(), f, interleaved=interleaved).cpu()
+        x[0, 0, 3], x[1, 1, 40], x[2, 0, 10], x[3, 0, 11], x[4, 1, 32], x[4, 1, 33], x[4, 1, 0], x[4, 1, 1] = inf, -inf, nan, inf, inf, -inf, inf, inf
+        x[5, 0, 5] = torch.finfo(dt).max
+        y = binding.apmm_rotary(x.cuda(), at.cuda(), f, interleaved=interleaved).cpu()
+        want, _ = exact(torch, x, at, f, interleaved, 1.0)
+        odd = ~torch.isfinite(want)
+        assert bool(odd.any()) and torch.equal(torch.nan_to_num(y[odd].double(), 1.0, 2.0, 3.0), torch.nan_to_num(want[odd], 1.0, 2.0, 3.0))
+        same = x == x
+        partner = torch.ones_like(same)
+        for row, head, channel in torch.nonzero(~torch.isfinite(x) | (x == torch.finfo(dt).max)).tolist():
+            other = channel ^ 1 if interleaved else channel ^ 32
+            partner[row, head, channel] = partner[row, head, other] = False
+        assert torch.equal(y[partner], clean[partner])
