@@ -69,12 +69,46 @@ __device__ __forceinline__ float4 rotary_turn(const RotaryArgs &r, int position,
     return make_float4(c1, s1, (float)(cs - (double)c1), (float)(sn - (double)s1));
 }
 // One of a pair: `other` comes with the sign that the sine has for it.  What the product and the rounding of cosine and sine to 32 bits have left goes in as a sum of its own, so that the result is off by two roundings
-// of 32 bits however much of the pair cancels: keys are quantised behind this, where a 16-bit number rounded the other way may cost a code.  (Rounded from the exact
-// sum instead, by what two of 32 bits leave and an odd last bit, it takes the vector unit longer than memory: 8192 tokens of 64 heads 56 us for 46.)
-__device__ __forceinline__ float rotary_one(float x, float other, const float4 &t)
+// of 32 bits however much of the pair cancels.
+__device__ __forceinline__ float rotary_sum(float x, float other, const float4 &t)
 {
+#pragma clang fp contract(off)
     const float p = other * t.y, sum = fmaf(x, t.x, p), all = sum + fmaf(x, t.z, fmaf(other, t.w, fmaf(other, t.y, -p)));
     return all == all ? all : sum;  // (what infinities leave is an infinity of either sign or no number)
+}
+// The same with what every step leaves: the exact sum, rounded to 32 bits
+__device__ __forceinline__ float rotary_exact(float x, float other, const float4 &t)
+{
+#pragma clang fp contract(off)
+    const float q = x * t.x, p = other * t.y, sum = q + p, b = sum - q;
+    return sum + (((q - (sum - b)) + (p - b)) + ((fmaf(x, t.x, -q) + fmaf(other, t.y, -p)) + fmaf(x, t.z, other * t.w)));
+}
+// Rounding in the sum decides the one to 16 bits where the number is so near the middle between two of those: one in 1600 (binary16) or 13000.  Keys are quantised behind this, where a number rounded the other way may
+// cost a code.
+template <bool BF16>
+__device__ __forceinline__ bool rotary_near(float v)
+{
+    constexpr uint32_t kHalf = BF16 ? 0x8000 : 0x1000;
+    return ((__float_as_uint(v) - (kHalf - 2)) & (2 * kHalf - 1)) <= 4;
+}
+template <bool BF16>
+__device__ __forceinline__ float rotary_one(float x, float other, const float4 &t)
+{
+    float v = rotary_sum(x, other, t);
+    if (rotary_near<BF16>(v) && fabsf(v) < __builtin_inff()) v = rotary_exact(x, other, t);
+    return v;
+}
+// (a, b) turned
+template <bool BF16>
+__device__ __forceinline__ void rotary_both(float &a, float &b, const float4 &t)
+{
+    float first = rotary_sum(a, -b, t), second = rotary_sum(b, a, t);
+    if ((rotary_near<BF16>(first) | rotary_near<BF16>(second)) && fmaxf(fabsf(a), fabsf(b)) < __builtin_inff()) {
+        first = rotary_exact(a, -b, t);
+        second = rotary_exact(b, a, t);
+    }
+    a = first;
+    b = second;
 }
 
 // A token's cosines and sines in LDS: pair p in row p % 8 or p % 4, as many rows as an eight of channels has pairs with (8) or within (4) it, so that lanes with an eight each read places that follow each other
@@ -99,8 +133,9 @@ __device__ __forceinline__ void rotary_eight(const uint16_t *row, bool aligned, 
             const int pair = c0 / 2 + i;
             if (pair >= pairs) break;
             const float4 cs = t[pair];
-            const float a = kv_scale_value(w[i] & 0xffffu, BF16), b = kv_scale_value(w[i] >> 16, BF16);
-            w[i] = rotary_pair(rotary_one(a, -b, cs), rotary_one(b, a, cs), BF16);
+            float a = kv_scale_value(w[i] & 0xffffu, BF16), b = kv_scale_value(w[i] >> 16, BF16);
+            rotary_both<BF16>(a, b, cs);
+            w[i] = rotary_pair(a, b, BF16);
         }
         return;
     }
@@ -112,8 +147,8 @@ __device__ __forceinline__ void rotary_eight(const uint16_t *row, bool aligned, 
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float4 c1 = t[p0 + 2 * i], c2 = t[p0 + 2 * i + 1];
-            w[i] = rotary_pair(rotary_one(kv_scale_value(w[i] & 0xffffu, BF16), by * kv_scale_value(other[i] & 0xffffu, BF16), c1),
-                               rotary_one(kv_scale_value(w[i] >> 16, BF16), by * kv_scale_value(other[i] >> 16, BF16), c2), BF16);
+            w[i] = rotary_pair(rotary_one<BF16>(kv_scale_value(w[i] & 0xffffu, BF16), by * kv_scale_value(other[i] & 0xffffu, BF16), c1),
+                               rotary_one<BF16>(kv_scale_value(w[i] >> 16, BF16), by * kv_scale_value(other[i] >> 16, BF16), c2), BF16);
         }
         return;
     }
@@ -123,7 +158,7 @@ __device__ __forceinline__ void rotary_eight(const uint16_t *row, bool aligned, 
         if (c >= 2 * pairs) break;
         const float4 cs = t[c < pairs ? c : c - pairs];
         const float x = kv_scale_value(i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xffffu, BF16), y = kv_scale_value(row[c < pairs ? c + pairs : c - pairs], BF16);
-        const uint32_t bits = kv_round(rotary_one(x, c < pairs ? -y : y, cs), BF16);
+        const uint32_t bits = kv_round(rotary_one<BF16>(x, c < pairs ? -y : y, cs), BF16);
         w[i / 2] = i & 1 ? (w[i / 2] & 0xffffu) | bits << 16 : (w[i / 2] & 0xffff0000u) | bits;
     }
 }

@@ -13,7 +13,7 @@ constexpr int kThreads = 256;
 constexpr int kTurns = 1024;  // cosines and sines that a workgroup holds
 
 // A workgroup has some tokens (those whose cosines and sines it holds) and a share of their heads.  A piece is what one lane reads and writes: both partners of its pairs are its own, so rows may be
-// turned where they lie.  Bound by HBM: 8192 tokens of 64 heads of 128, 268 MB, 46 us on the device (5.8 TB/s; with sums of 64 bits 105, which the vector unit bounds); 8 tokens of 40 heads 3.3, the launch and positions -> frequencies -> rows.
+// turned where they lie.  Bound by HBM: 8192 tokens of 64 heads of 128, 268 MB, 50 us on the device (5.4 TB/s; 46 without the second look at numbers near a middle, 105 with all sums of 64 bits); 8 tokens of 40 heads 3.3, the launch and positions -> frequencies -> rows.
 template <bool BF16, bool INTERLEAVED, bool EIGHTS>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryRows a)
 {
@@ -54,9 +54,11 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryRows a)
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             const float4 c1 = t[piece * 8 + 2 * j], c2 = t[piece * 8 + 2 * j + 1];
-                            const float a1 = kv_scale_value(w[j] & 0xffffu, BF16), a2 = kv_scale_value(w[j] >> 16, BF16), b1 = kv_scale_value(v[j] & 0xffffu, BF16), b2 = kv_scale_value(v[j] >> 16, BF16);
-                            w[j] = rotary_pair(rotary_one(a1, -b1, c1), rotary_one(a2, -b2, c2), BF16);
-                            v[j] = rotary_pair(rotary_one(b1, a1, c1), rotary_one(b2, a2, c2), BF16);
+                            float a1 = kv_scale_value(w[j] & 0xffffu, BF16), a2 = kv_scale_value(w[j] >> 16, BF16), b1 = kv_scale_value(v[j] & 0xffffu, BF16), b2 = kv_scale_value(v[j] >> 16, BF16);
+                            rotary_both<BF16>(a1, b1, c1);
+                            rotary_both<BF16>(a2, b2, c2);
+                            w[j] = rotary_pair(a1, a2, BF16);
+                            v[j] = rotary_pair(b1, b2, BF16);
                         }
                         kv_store(to + piece * 8, true, w);
                         kv_store(to + piece * 8 + pairs, true, v);
@@ -66,9 +68,10 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryRows a)
                 } else {
                     const int c1 = INTERLEAVED ? 2 * piece : piece, c2 = INTERLEAVED ? c1 + 1 : piece + pairs;
                     const float4 cs = t[piece];
-                    const float x1 = kv_scale_value(from[c1], BF16), x2 = kv_scale_value(from[c2], BF16);
-                    to[c1] = kv_round(rotary_one(x1, -x2, cs), BF16);
-                    to[c2] = kv_round(rotary_one(x2, x1, cs), BF16);
+                    float x1 = kv_scale_value(from[c1], BF16), x2 = kv_scale_value(from[c2], BF16);
+                    rotary_both<BF16>(x1, x2, cs);
+                    to[c1] = kv_round(x1, BF16);
+                    to[c2] = kv_round(x2, BF16);
                 }
             }
         }
@@ -78,7 +81,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryRows a)
 constexpr int kWaves = 4;
 
 // A workgroup has the up to eight tokens of an aligned eight of positions, as kv_write_kernel's waves have, and `per_wave` heads to each wave: those of keys and values first, then those of queries.
-// It makes the eight's cosines and sines once.  Four heads to a wave where there are many: 13 sequences of up to 1500 new tokens, 32 heads of 128, 184 MB read and written in 59 us (both forms of pairs in one
+// It makes the eight's cosines and sines once.  Four heads to a wave where there are many: 13 sequences of up to 1500 new tokens, 32 heads of 128, 184 MB read and written in 60 us (both forms of pairs in one
 // kernel, which has no registers for a fourth wave, 71; two heads to a wave, or eight, 3 and 5 more); 32 single tokens of 8 and 32 heads 7.0, of which the way from lengths to pages to a partly filled eight is the longer part.
 template <int D, bool BF16, bool INTERLEAVED>
 __global__ __launch_bounds__(64 * kWaves) void kv_rotary_write_kernel(KvRotaryArgs a)
@@ -114,9 +117,11 @@ __global__ __launch_bounds__(64 * kWaves) void kv_rotary_write_kernel(KvRotaryAr
             for (int j = 0; j < 4; ++j) {
                 const int second = D == 128 ? 4 + j : j;
                 const float4 c1 = of_token[8 * part + 2 * j], c2 = of_token[8 * part + 2 * j + 1];
-                const float a1 = kv_scale_value(x[j] & 0xffffu, BF16), a2 = kv_scale_value(x[j] >> 16, BF16), b1 = kv_scale_value(x[second] & 0xffffu, BF16), b2 = kv_scale_value(x[second] >> 16, BF16);
-                x[j] = rotary_pair(rotary_one(a1, -b1, c1), rotary_one(a2, -b2, c2), BF16);
-                x[second] = rotary_pair(rotary_one(b1, a1, c1), rotary_one(b2, a2, c2), BF16);
+                float a1 = kv_scale_value(x[j] & 0xffffu, BF16), a2 = kv_scale_value(x[j] >> 16, BF16), b1 = kv_scale_value(x[second] & 0xffffu, BF16), b2 = kv_scale_value(x[second] >> 16, BF16);
+                rotary_both<BF16>(a1, b1, c1);
+                rotary_both<BF16>(a2, b2, c2);
+                x[j] = rotary_pair(a1, a2, BF16);
+                x[second] = rotary_pair(b1, b2, BF16);
             }
             return;
         }
