@@ -81,7 +81,8 @@ __device__ __forceinline__ float rotary_exact(float x, float other, const float4
 {
 #pragma clang fp contract(off)
     const float q = x * t.x, p = other * t.y, sum = q + p, b = sum - q;
-    return sum + (((q - (sum - b)) + (p - b)) + ((fmaf(x, t.x, -q) + fmaf(other, t.y, -p)) + fmaf(x, t.z, other * t.w)));
+    const float all = sum + (((q - (sum - b)) + (p - b)) + ((fmaf(x, t.x, -q) + fmaf(other, t.y, -p)) + fmaf(x, t.z, other * t.w)));
+    return all == all ? all : fmaf(x, t.x, p);  // (a product without a place in 32 bits may have a sum with one)
 }
 // Rounding in the sum decides the one to 16 bits where the number is so near the middle between two of those: one in 1600 (binary16) or 13000.  Keys are quantised behind this, where a number rounded the other way may
 // cost a code.
