@@ -1,0 +1,146 @@
+"""Rotary positions where rounding decides: pairs that nearly cancel, numbers next to the middle between two of 16 bits.  Every number has to be the pair turned in
+more than 64 bits, rounded to 32 and then to 16, whichever kernel makes it; on the CPU (host_layers.py) and on the GPU."""
+import functools
+
+import numpy as np
+import pytest
+import torch
+
+import host_layers
+import host_wave
+from test_kv_bounds import cache, rows
+
+TOKENS, HEADS, PAIRS, D = 4, 6, 32, 64
+TYPES = [torch.float16, torch.bfloat16]
+
+
+@pytest.fixture(scope="module")
+def host(tmp_path_factory):
+    if not host_wave.available():
+        pytest.skip("no clang++")
+    return host_layers.Host(host_layers.build(tmp_path_factory.mktemp("layers")))
+
+
+@pytest.fixture(scope="module")
+def gpu():
+    from paper_2409_17870_amd import binding
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    binding.load()
+    return binding
+
+
+def turned(a, b, t, magnitude=1.0):
+    """(a, b) by the angle t, a product of 64 bits, in the 64 bits of extended precision.  (Of pairs that cancel but for 2^-22 it leaves 2^-42 of the result.)"""
+    assert np.finfo(np.longdouble).nmant >= 63
+    t, a, b, g = np.asarray(t).astype(np.longdouble), a.astype(np.longdouble), b.astype(np.longdouble), np.longdouble(np.float32(magnitude))
+    c, s = np.cos(t) * g, np.sin(t) * g
+    return a * c - b * s, b * c + a * s
+
+
+def rounded(y, dtype):
+    with np.errstate(over="ignore"):
+        return torch.from_numpy(y.astype(np.float32)).to(dtype)
+
+
+def sixteen(x, dtype):
+    """Numbers of 16 bits, as 64."""
+    return torch.from_numpy(np.asarray(x, dtype=np.float32)).to(dtype).double().numpy()
+
+
+def near_middle(y, dtype):
+    """Within two units of 32 bits of the middle between two numbers of 16."""
+    low = 16 if dtype == torch.bfloat16 else 13
+    bits = np.asarray(y).astype(np.float32).view(np.uint32).astype(np.int64) & ((1 << low) - 1)
+    return np.abs(bits - (1 << (low - 1))) <= 2
+
+
+def angles(seed):
+    r = np.random.RandomState(seed)
+    positions, frequencies = r.randint(0, 100000, TOKENS).astype(np.int32), 10000.0 ** (-np.arange(PAIRS) / PAIRS)
+    return r, positions, frequencies, positions.astype(np.float64)[:, None] * frequencies
+
+
+@functools.lru_cache(maxsize=None)
+def pairs_of(kind, dtype, seed=5):
+    """Positions, frequencies, and pairs (tokens x heads x pairs) of the kind for these angles."""
+    r, positions, frequencies, t = angles(seed)
+    a, b = np.empty((TOKENS, HEADS, PAIRS)), np.empty((TOKENS, HEADS, PAIRS))
+    for i in range(TOKENS):
+        for j in range(PAIRS):
+            n = 4096 if kind == "cancel" else 200000 if dtype == torch.bfloat16 else 30000
+            if kind == "cancel":  # the partner that takes most of it away, in 16 bits
+                v = sixteen(r.randn(n), dtype)
+                u = sixteen(v * np.tan(t[i, j]), dtype)
+                y = np.abs(u * np.cos(t[i, j]) - v * np.sin(t[i, j])) / np.abs(v)
+                best = np.argsort(np.where(y > 2.0 ** -22, y, np.inf))[:HEADS]
+            else:
+                u, v = sixteen(r.randn(n), dtype), sixteen(r.randn(n), dtype)
+                y = u * np.cos(t[i, j]) - v * np.sin(t[i, j])
+                best = np.resize(np.flatnonzero(near_middle(y, dtype)), HEADS)  # (some angles have few)
+            a[i, :, j], b[i, :, j] = u[best], v[best]
+    return positions, frequencies, a, b, *turned(a, b, t[:, None])
+
+
+def rows_of(a, b, interleaved, dtype):
+    x = np.stack([a, b], -1).reshape(*a.shape[:-1], -1) if interleaved else np.concatenate([a, b], -1)
+    return torch.from_numpy(x).float().to(dtype)
+
+
+def guarded(*tensors):
+    m = host_wave.Memory()
+    return [m.copy(t) for t in tensors]
+
+
+def on_host(host, x, positions, frequencies, interleaved, magnitude=1.0):
+    """By the kernel of rows alone, of eights and of single numbers, and by the one on the way into the cache."""
+    p, f = torch.from_numpy(positions), torch.from_numpy(frequencies)
+    wide = torch.zeros((*x.shape[:2], x.shape[2] + 3), dtype=x.dtype)
+    wide[:, :, 3:] = x
+    n, k = x.shape[0], rows(x.shape[0], 1, D, x.dtype)
+    g = guarded(x, p, f, wide)
+    yield host.rotary(*g[:3], interleaved=interleaved, magnitude=magnitude)
+    yield host.rotary(g[3][:, :, 3:], *g[1:3], interleaved=interleaved, magnitude=magnitude)
+    k, starts, *args = guarded(k, torch.tensor([0, n], dtype=torch.int32), *cache([n], 1, D, 16, x.dtype))
+    yield host.write_rotary(g[0], k, k, *args, g[2], starts, g[1], interleaved=interleaved, magnitude=magnitude)
+
+
+def on_gpu(binding, x, positions, frequencies, interleaved, magnitude=1.0):
+    x, p, f = x.cuda(), torch.from_numpy(positions).cuda(), torch.from_numpy(frequencies).cuda()
+    wide = torch.zeros((*x.shape[:2], x.shape[2] + 3), dtype=x.dtype, device="cuda")
+    wide[:, :, 3:] = x
+    n = x.shape[0]
+    k, starts, args = x[:, :1], torch.tensor([0, n], dtype=torch.int32).cuda(), [t.cuda() for t in cache([n], 1, D, 16, x.dtype)]
+    one, other = ([args[0].clone(), args[1].clone()] for _ in range(2))
+    yield (y := binding.apmm_rotary(x, p, f, interleaved=interleaved, magnitude=magnitude)).cpu()
+    yield binding.apmm_rotary(wide[:, :, 3:], p, f, interleaved=interleaved, magnitude=magnitude).cpu()
+    yield binding.apmm_kv_write_rotary(x, k, k, *one, *args[2:], f, starts, positions=p, interleaved=interleaved, magnitude=magnitude).cpu()
+    binding.apmm_kv_write(y[:, :1], k, *other, *args[2:], starts)
+    assert torch.equal(one[0], other[0]) and torch.equal(one[1], other[1])
+
+
+def check(turn, where, kind, dtype, interleaved):
+    positions, frequencies, a, b, first, second = pairs_of(kind, dtype)
+    want = rows_of(rounded(first, dtype).double().numpy(), rounded(second, dtype).double().numpy(), interleaved, dtype)
+    if kind == "cancel":  # half of the pairs at least lose 16 bits and more; none is all gone
+        assert np.median(np.abs(first) / np.abs(b)) < 2.0 ** -15 and bool((first != 0).all())
+    if kind == "middle":
+        assert near_middle(first, dtype).mean() > 0.9
+    for y in turn(where, rows_of(a, b, interleaved, dtype), positions, frequencies, interleaved):
+        wrong = (y != want).sum()
+        assert wrong == 0, "%d of %d are not the exact pair's" % (wrong, want.numel())
+
+
+KINDS = [("cancel", t) for t in TYPES] + [("middle", t) for t in TYPES]
+
+
+@pytest.mark.parametrize("interleaved", [0, 1])
+@pytest.mark.parametrize("kind, dtype", KINDS)
+def test_pairs_on_the_host(host, kind, dtype, interleaved):
+    check(on_host, host, kind, dtype, interleaved)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("interleaved", [0, 1])
+@pytest.mark.parametrize("kind, dtype", KINDS)
+def test_pairs_on_the_gpu(gpu, kind, dtype, interleaved):
+    check(on_gpu, gpu, kind, dtype, interleaved)
