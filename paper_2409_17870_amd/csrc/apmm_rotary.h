@@ -69,14 +69,14 @@ __device__ __forceinline__ float4 rotary_turn(const RotaryArgs &r, int position,
     return make_float4(c1, s1, (float)(cs - (double)c1), (float)(sn - (double)s1));
 }
 // One of a pair: `other` comes with the sign that the sine has for it.  What the product and the rounding of cosine and sine to 32 bits have left goes in as a sum of its own, so that the result is off by two roundings
-// of 32 bits however much of the pair cancels.
+// of 32 bits, and by 2^-47 of the larger product, which is less wherever no more than 20 bits of the pair cancel.
 __device__ __forceinline__ float rotary_sum(float x, float other, const float4 &t)
 {
 #pragma clang fp contract(off)
     const float p = other * t.y, sum = fmaf(x, t.x, p), all = sum + fmaf(x, t.z, fmaf(other, t.w, fmaf(other, t.y, -p)));
     return all == all ? all : sum;  // (what infinities leave is an infinity of either sign or no number)
 }
-// The same with what every step leaves: the exact sum, rounded to 32 bits
+// The same with what every step leaves: the sum rounded to 32 bits once
 __device__ __forceinline__ float rotary_exact(float x, float other, const float4 &t)
 {
 #pragma clang fp contract(off)
@@ -85,18 +85,19 @@ __device__ __forceinline__ float rotary_exact(float x, float other, const float4
     return all == all ? all : fmaf(x, t.x, p);  // (a product without a place in 32 bits may have a sum with one)
 }
 // Rounding in the sum decides the one to 16 bits where the number is so near the middle between two of those: one in 1600 (binary16) or 13000.  Keys are quantised behind this, where a number rounded the other way may
-// cost a code.
+// cost a code.  Below 2^-14 binary16 numbers are equally far apart, and the middles not at one place of the bits: any of these is near.
 template <bool BF16>
 __device__ __forceinline__ bool rotary_near(float v)
 {
     constexpr uint32_t kHalf = BF16 ? 0x8000 : 0x1000;
-    return ((__float_as_uint(v) - (kHalf - 2)) & (2 * kHalf - 1)) <= 4;
+    return (((__float_as_uint(v) - (kHalf - 2)) & (2 * kHalf - 1)) <= 4) | (!BF16 && fabsf(v) < 0x1p-14f);
 }
+// Each number is made again by its own nearness alone, here and where both of a pair are a lane's: so all kernels have the same.  (What is near is finite.)
 template <bool BF16>
 __device__ __forceinline__ float rotary_one(float x, float other, const float4 &t)
 {
     float v = rotary_sum(x, other, t);
-    if (rotary_near<BF16>(v) && fabsf(v) < __builtin_inff()) v = rotary_exact(x, other, t);
+    if (rotary_near<BF16>(v)) v = rotary_exact(x, other, t);
     return v;
 }
 // (a, b) turned
@@ -104,9 +105,11 @@ template <bool BF16>
 __device__ __forceinline__ void rotary_both(float &a, float &b, const float4 &t)
 {
     float first = rotary_sum(a, -b, t), second = rotary_sum(b, a, t);
-    if ((rotary_near<BF16>(first) | rotary_near<BF16>(second)) && fmaxf(fabsf(a), fabsf(b)) < __builtin_inff()) {
-        first = rotary_exact(a, -b, t);
-        second = rotary_exact(b, a, t);
+    const bool near_first = rotary_near<BF16>(first), near_second = rotary_near<BF16>(second);
+    if (near_first | near_second) {
+        const float first_exact = rotary_exact(a, -b, t), second_exact = rotary_exact(b, a, t);
+        first = near_first ? first_exact : first;
+        second = near_second ? second_exact : second;
     }
     a = first;
     b = second;

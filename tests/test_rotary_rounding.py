@@ -1,5 +1,5 @@
-"""Rotary positions where rounding decides: pairs that nearly cancel, numbers next to the middle between two of 16 bits.  Every number has to be the pair turned in
-more than 64 bits, rounded to 32 and then to 16, whichever kernel makes it; on the CPU (host_layers.py) and on the GPU."""
+"""Rotary positions where rounding decides: pairs that nearly cancel, numbers next to the middle between two of 16 bits, binary16 numbers below 2^-14, products without a place in 32 bits.  Every
+number has to be the pair turned in more than 64 bits, rounded to 32 and then to 16, whichever kernel makes it; on the CPU (host_layers.py) and on the GPU."""
 import functools
 
 import numpy as np
@@ -74,9 +74,13 @@ def pairs_of(kind, dtype, seed=5):
                 y = np.abs(u * np.cos(t[i, j]) - v * np.sin(t[i, j])) / np.abs(v)
                 best = np.argsort(np.where(y > 2.0 ** -22, y, np.inf))[:HEADS]
             else:
-                u, v = sixteen(r.randn(n), dtype), sixteen(r.randn(n), dtype)
+                size = 2.0 ** -15 if kind == "subnormal" else 1.0
+                u, v = sixteen(r.randn(n) * size, dtype), sixteen(r.randn(n) * size, dtype)
                 y = u * np.cos(t[i, j]) - v * np.sin(t[i, j])
-                best = np.resize(np.flatnonzero(near_middle(y, dtype)), HEADS)  # (some angles have few)
+                if kind == "subnormal":  # the middles lie at odd multiples of 2^-25
+                    best = np.argsort(np.abs(np.mod(y * 2.0 ** 24, 1.0) - 0.5))[:HEADS]
+                else:
+                    best = np.resize(np.flatnonzero(near_middle(y, dtype)), HEADS)  # (some angles have few)
             a[i, :, j], b[i, :, j] = u[best], v[best]
     return positions, frequencies, a, b, *turned(a, b, t[:, None])
 
@@ -130,7 +134,7 @@ def check(turn, where, kind, dtype, interleaved):
         assert wrong == 0, "%d of %d are not the exact pair's" % (wrong, want.numel())
 
 
-KINDS = [("cancel", t) for t in TYPES] + [("middle", t) for t in TYPES]
+KINDS = [("cancel", t) for t in TYPES] + [("middle", t) for t in TYPES] + [("subnormal", torch.float16)]
 
 
 @pytest.mark.parametrize("interleaved", [0, 1])
@@ -144,3 +148,34 @@ def test_pairs_on_the_host(host, kind, dtype, interleaved):
 @pytest.mark.parametrize("kind, dtype", KINDS)
 def test_pairs_on_the_gpu(gpu, kind, dtype, interleaved):
     check(on_gpu, gpu, kind, dtype, interleaved)
+
+
+# Pairs of which one number is near a middle that is not among those of normal numbers: position, frequency, a, b
+SMALL = [(1, 2.8041749902067479, 0x09c5, 0x054e), (1, 6.1626298429616133, 0x0d92, 0x02f8), (3103, 10000.0 ** (-6 / 32), None, None)]
+
+
+def small_pairs():
+    for position, frequency, a, b in SMALL:
+        a, b = (np.array([v], dtype=np.uint16).view(np.float16).astype(np.float64) for v in (a, b)) if a else (np.array([float.fromhex(v)]) for v in ("0x1.82p-17", "-0x1.8fp-16"))
+        yield position, frequency, a, b
+
+
+def check_small(turn, where, interleaved):
+    for position, frequency, a, b in small_pairs():
+        positions, frequencies = np.array([position], dtype=np.int32), np.full(PAIRS, frequency)
+        first, second = (rounded(v, torch.float16) for v in turned(a, b, position * frequency))
+        x = rows_of(np.full((1, 1, PAIRS), a), np.full((1, 1, PAIRS), b), interleaved, torch.float16)
+        want = rows_of(np.full((1, 1, PAIRS), first.item()), np.full((1, 1, PAIRS), second.item()), interleaved, torch.float16)
+        for y in turn(where, x, positions, frequencies, interleaved):
+            assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("interleaved", [0, 1])
+def test_subnormal_pairs_on_the_host(host, interleaved):
+    check_small(on_host, host, interleaved)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("interleaved", [0, 1])
+def test_subnormal_pairs_on_the_gpu(gpu, interleaved):
+    check_small(on_gpu, gpu, interleaved)
