@@ -76,28 +76,36 @@ __device__ __forceinline__ float rotary_sum(float x, float other, const float4 &
     const float p = other * t.y, sum = fmaf(x, t.x, p), all = sum + fmaf(x, t.z, fmaf(other, t.w, fmaf(other, t.y, -p)));
     return all == all ? all : sum;  // (what infinities leave is an infinity of either sign or no number)
 }
-// The same with what every step leaves: the sum rounded to 32 bits once
-__device__ __forceinline__ float rotary_exact(float x, float other, const float4 &t)
+// The same with what every step leaves: the sum rounded to 32 bits once (NaN where a product has no place in 32 bits)
+__device__ __forceinline__ float rotary_all(float x, float other, const float4 &t)
 {
 #pragma clang fp contract(off)
     const float q = x * t.x, p = other * t.y, sum = q + p, b = sum - q;
-    const float all = sum + (((q - (sum - b)) + (p - b)) + ((fmaf(x, t.x, -q) + fmaf(other, t.y, -p)) + fmaf(x, t.z, other * t.w)));
-    return all == all ? all : fmaf(x, t.x, p);  // (a product without a place in 32 bits may have a sum with one)
+    return sum + (((q - (sum - b)) + (p - b)) + ((fmaf(x, t.x, -q) + fmaf(other, t.y, -p)) + fmaf(x, t.z, other * t.w)));
+}
+template <bool BF16>
+__device__ __forceinline__ float rotary_exact(float x, float other, const float4 &t, float v)
+{
+    float all = rotary_all(x, other, t);
+    if (BF16 && all != all)  // the sum of such products may have a place, and does as products of numbers 2^128 times smaller
+        all = rotary_all(x * 0x1p-64f, other * 0x1p-64f, make_float4(t.x * 0x1p-64f, t.y * 0x1p-64f, t.z * 0x1p-64f, t.w * 0x1p-64f)) * 0x1p64f * 0x1p64f;
+    return all == all ? all : v;
 }
 // Rounding in the sum decides the one to 16 bits where the number is so near the middle between two of those: one in 1600 (binary16) or 13000.  Keys are quantised behind this, where a number rounded the other way may
-// cost a code.  Below 2^-14 binary16 numbers are equally far apart, and the middles not at one place of the bits: any of these is near.
+// cost a code.  Below 2^-14 binary16 numbers are equally far apart, and the middles not at one place of the bits: any of these is near.  So is, of
+// bfloat16, whose largest numbers are those of 32 bits, what has become infinite on the way.
 template <bool BF16>
 __device__ __forceinline__ bool rotary_near(float v)
 {
     constexpr uint32_t kHalf = BF16 ? 0x8000 : 0x1000;
-    return (((__float_as_uint(v) - (kHalf - 2)) & (2 * kHalf - 1)) <= 4) | (!BF16 && fabsf(v) < 0x1p-14f);
+    return (((__float_as_uint(v) - (kHalf - 2)) & (2 * kHalf - 1)) <= 4) | (BF16 ? !(fabsf(v) < __builtin_inff()) : fabsf(v) < 0x1p-14f);
 }
-// Each number is made again by its own nearness alone, here and where both of a pair are a lane's: so all kernels have the same.  (What is near is finite.)
+// Each number is made again by its own nearness alone, here and where both of a pair are a lane's: so all kernels have the same.
 template <bool BF16>
 __device__ __forceinline__ float rotary_one(float x, float other, const float4 &t)
 {
     float v = rotary_sum(x, other, t);
-    if (rotary_near<BF16>(v)) v = rotary_exact(x, other, t);
+    if (rotary_near<BF16>(v)) v = rotary_exact<BF16>(x, other, t, v);
     return v;
 }
 // (a, b) turned
@@ -107,7 +115,7 @@ __device__ __forceinline__ void rotary_both(float &a, float &b, const float4 &t)
     float first = rotary_sum(a, -b, t), second = rotary_sum(b, a, t);
     const bool near_first = rotary_near<BF16>(first), near_second = rotary_near<BF16>(second);
     if (near_first | near_second) {
-        const float first_exact = rotary_exact(a, -b, t), second_exact = rotary_exact(b, a, t);
+        const float first_exact = rotary_exact<BF16>(a, -b, t, first), second_exact = rotary_exact<BF16>(b, a, t, second);
         first = near_first ? first_exact : first;
         second = near_second ? second_exact : second;
     }

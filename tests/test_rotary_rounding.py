@@ -119,7 +119,7 @@ def on_gpu(binding, x, positions, frequencies, interleaved, magnitude=1.0):
     yield binding.apmm_rotary(wide[:, :, 3:], p, f, interleaved=interleaved, magnitude=magnitude).cpu()
     yield binding.apmm_kv_write_rotary(x, k, k, *one, *args[2:], f, starts, positions=p, interleaved=interleaved, magnitude=magnitude).cpu()
     binding.apmm_kv_write(y[:, :1], k, *other, *args[2:], starts)
-    assert torch.equal(one[0], other[0]) and torch.equal(one[1], other[1])
+    assert torch.equal(one[0], other[0]) and torch.equal(one[1].view(torch.int16), other[1].view(torch.int16))
 
 
 def check(turn, where, kind, dtype, interleaved):
@@ -179,3 +179,29 @@ def test_subnormal_pairs_on_the_host(host, interleaved):
 @pytest.mark.parametrize("interleaved", [0, 1])
 def test_subnormal_pairs_on_the_gpu(gpu, interleaved):
     check_small(on_gpu, gpu, interleaved)
+
+
+def check_large(turn, where, interleaved):
+    """The largest bfloat16 numbers: products, and cosines and sines with the magnitude, of which some have no place in 32 bits where their sum has one, and sums that have none."""
+    r, positions, frequencies, t = angles(7)
+    a, b = (sixteen(np.ldexp(r.uniform(-1, 1, (TOKENS, HEADS, PAIRS)), 128), torch.bfloat16) for _ in range(2))
+    a, b = (np.clip(v, -torch.finfo(torch.bfloat16).max, torch.finfo(torch.bfloat16).max) for v in (a, b))
+    for magnitude in (1.0, 1.4375, 3e38):
+        if magnitude > 2:
+            a, b = (np.where(np.arange(PAIRS) % 4 == 1, v, sixteen(np.ldexp(v, -127), torch.bfloat16)) for v in (a, b))
+        first, second = turned(a, b, t[:, None], magnitude)
+        want = rows_of(rounded(first, torch.bfloat16).double().numpy(), rounded(second, torch.bfloat16).double().numpy(), interleaved, torch.bfloat16)
+        assert 0.02 < torch.isinf(want).float().mean() < 0.9
+        for y in turn(where, rows_of(a, b, interleaved, torch.bfloat16), positions, frequencies, interleaved, magnitude):
+            assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("interleaved", [0, 1])
+def test_large_pairs_on_the_host(host, interleaved):
+    check_large(on_host, host, interleaved)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("interleaved", [0, 1])
+def test_large_pairs_on_the_gpu(gpu, interleaved):
+    check_large(on_gpu, gpu, interleaved)
