@@ -10,7 +10,7 @@ namespace apmm {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTurns = 1024;  // cosines and sines that a workgroup holds
+constexpr int kTurns = 512;  // cosines and sines that a workgroup holds: of one token, or of several that have 256 with those that fill up a row of RotaryTurns
 
 // A workgroup has some tokens (those whose cosines and sines it holds) and a share of their heads.  A piece is what one lane reads and writes: both partners of its pairs are its own, so rows may be
 // turned where they lie.  Bound by HBM: 8192 tokens of 64 heads of 128, 268 MB, 50 us on the device (5.4 TB/s; 46 without the second look at numbers near a middle, 105 with all sums of 64 bits); 8 tokens of 40 heads 3.3, the launch and positions -> frequencies -> rows.

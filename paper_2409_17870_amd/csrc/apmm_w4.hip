@@ -11,7 +11,6 @@ namespace apmm {
 namespace {
 
 typedef float float4v __attribute__((ext_vector_type(4)));
-typedef float float16v __attribute__((ext_vector_type(16)));
 
 // A lane makes a word.  Bound by HBM: a byte a code in, half a byte out.
 template <bool BF16>
