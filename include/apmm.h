@@ -301,6 +301,7 @@ apmm_status apmm_rotary(int64_t tokens, int heads, int head_dim, int dtype, cons
 
 /* apmm_rotary of queries (into q_out, which may be q with the same strides) and of keys, and apmm_kv_write of these keys and of the values, in one launch, with the results of the calls one by one.
  *   q_heads    0 to 2048; 0: no queries, q and q_out may be NULL
+ *   q_out      rows that overlap nothing else of the call, or q
  *   positions  device, one of each new token; or NULL: its place in its sequence.  (After apmm_kv_evict places are not positions any more.)
  * Rows of q that belong to no sequence are left as they are in q_out. */
 apmm_status apmm_kv_write_rotary(const apmm_kv_cache *cache, const apmm_kv_batch *batch, int q_heads, const int32_t *positions, const apmm_rotation *rotation,
@@ -326,7 +327,7 @@ apmm_status apmm_kv_weights(const apmm_kv_cache *cache, const apmm_kv_batch *bat
  *   to_table    device, sequences x to_width (rows to_stride apart): pages that no sequence of the call has; a token without a place there is not copied.  The old pages stay as they are.
  *   to_lengths  device, sequences: tokens that stay; not `lengths` itself
  *   kept        device, sequences x kv_heads x budget: the places they had, ascending, then -1
- *   to_weights  device, sequences x kv_heads x budget: their weights (0 for those that have none), then 0
+ *   to_weights  device, sequences x kv_heads x budget: their weights (0 for those that have none), then 0; no part of `weights`
  *   workspace   device, 16-byte aligned, apmm_kv_evict_workspace_bytes() bytes of the same sizes (0, then it may be NULL, for tables of up to 65536 tokens); calls that may overlap need one each
  * sinks + recent <= budget.  A call of 2^32 work items or more is refused: sequences x kv_heads from 2^22 on, sequences x kv_heads x budget from about 2^29 on. */
 size_t apmm_kv_evict_workspace_bytes(const apmm_kv_cache *cache, int sequences, int64_t table_width);
@@ -341,7 +342,7 @@ apmm_status apmm_kv_evict(const apmm_kv_cache *cache, int sequences, const int32
  *   dtype     apmm_dtype of x, y and the scales; the packed form is made for one of them
  *   codes     device, N x K uint8, row-major, the low four bits count;  scales  device, N x ceil(K / group)
  *   packed    device, apmm_w4_packed_bytes(N, K, group) bytes, 16-byte aligned, opaque, of this version of the library
- *   x, y      device, M x K and M x N, rows x_stride and y_stride elements apart, at any address of their type's alignment; M up to 2^20, N and K up to 2^24
+ *   x, y      device, M x K and M x N, rows x_stride and y_stride elements apart, at any address of their type's alignment, y's without a part of x; M up to 2^20, N and K up to 2^24
  *   workspace device, 16-byte aligned, apmm_w4_workspace_bytes() bytes of the same sizes (0, then it may be NULL, for many of them); calls that may overlap need one each */
 size_t apmm_w4_packed_bytes(int64_t N, int64_t K, int group);
 apmm_status apmm_w4_pack(const uint8_t *codes, const void *scales, int64_t N, int64_t K, int group, int dtype, void *packed, void *stream);

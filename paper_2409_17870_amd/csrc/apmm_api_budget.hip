@@ -102,6 +102,7 @@ apmm_status apmm_kv_write_rotary(const apmm_kv_cache *cache, const apmm_kv_batch
         if ((st = check_tensor(q, q_token_stride, q_head_stride, a.q)) != APMM_OK || (st = check_tensor(q_out, q_out_token_stride, q_out_head_stride, a.q_out)) != APMM_OK) return st;
         if (q == q_out && (q_token_stride != q_out_token_stride || q_head_stride != q_out_head_stride))
             return fail(APMM_ERR_INVALID_ARG, "kv_write_rotary: queries that are turned where they lie must have one set of strides");
+        if (q_out == k || q_out == v) return fail(APMM_ERR_INVALID_ARG, "kv_write_rotary: q_out must be neither k nor v");
     }
     a.q_heads = q_heads;
     a.r.positions = positions;
@@ -176,6 +177,7 @@ apmm_status apmm_kv_evict(const apmm_kv_cache *cache, int sequences, const int32
     if ((st = check_weights(cache, weights, weights_sequence_stride, weights_head_stride, capacity, 0, a.w)) != APMM_OK) return st;
     if (!to_table || !to_lengths || !kept || !to_weights) return fail(APMM_ERR_INVALID_ARG, "kv_evict: null pointer");
     if (!aligned(to_table, 4) || !aligned(to_lengths, 4) || !aligned(kept, 4) || !aligned(to_weights, 4)) return fail(APMM_ERR_INVALID_ARG, "kv_evict: misaligned pointer");
+    if (to_weights == weights) return fail(APMM_ERR_INVALID_ARG, "kv_evict: to_weights must not be weights");
     if (to_lengths == lengths) return fail(APMM_ERR_INVALID_ARG, "kv_evict: to_lengths must not be lengths");
     a.to_table = to_table;
     a.to_stride = to_stride;

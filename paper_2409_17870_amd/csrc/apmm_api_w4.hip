@@ -60,6 +60,7 @@ apmm_status apmm_w4_gemm(int64_t M, int64_t N, int64_t K, int group, int dtype, 
     if (M == 0 || N == 0) return APMM_OK;
     if (!x || !packed || !y) return fail(APMM_ERR_INVALID_ARG, "w4: null pointer");
     if (!aligned(x, 2) || !aligned(y, 2) || !aligned(packed, 16)) return fail(APMM_ERR_INVALID_ARG, "w4: x and y must be 2-byte, packed weights 16-byte aligned");
+    if (x == y) return fail(APMM_ERR_INVALID_ARG, "w4: y must not be x, which other workgroups still read");
     if (M > 1 && (x_stride < 0 || y_stride < N)) return fail(APMM_ERR_INVALID_ARG, "w4: x_stride < 0, or rows of y that overlap");
     const apmm::W4Shape s = {N, K, group};
     const apmm::W4Rule r = apmm::w4_rule(M, N, s.blocks());
