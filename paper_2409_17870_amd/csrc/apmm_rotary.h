@@ -46,8 +46,9 @@ hipError_t launch_kv_write_rotary(const KvRotaryArgs &a, hipStream_t stream);
 __device__ __forceinline__ float4 rotary_turn(const RotaryArgs &r, int position, int pair)
 {
     constexpr double kPerRadian = 0.15915494309189535, kPerRadianLow = -9.839338337591243e-18, kRadians = 6.283185307179586;  // 1 / (2 pi) in two parts
-    const double t = (double)position * r.frequencies[pair], high = t * kPerRadian, low = fma(t, kPerRadian, -high) + t * kPerRadianLow;
-    const double rest = (high - rint(high)) + low, quarter = rint(4.0 * rest), x = (rest - 0.25 * quarter) * kRadians, y = x * x;
+    // turns less the whole ones with one rounding of what is left.  (As the product less the whole ones, and the product's rounding after it, the compiler would take the first of these in one step and the rounding twice.)
+    const double t = (double)position * r.frequencies[pair], rest = fma(t, kPerRadianLow, fma(t, kPerRadian, -rint(t * kPerRadian)));
+    const double quarter = rint(4.0 * rest), x = (rest - 0.25 * quarter) * kRadians, y = x * x;
     double s = 1.0 / 6227020800.0, c = -1.0 / 87178291200.0;
     s = fma(s, y, -1.0 / 39916800.0);
     s = fma(s, y, 1.0 / 362880.0);

@@ -205,3 +205,30 @@ def test_large_pairs_on_the_host(host, interleaved):
 @pytest.mark.parametrize("interleaved", [0, 1])
 def test_large_pairs_on_the_gpu(gpu, interleaved):
     check_large(on_gpu, gpu, interleaved)
+
+
+# Pairs of large angles of which a number lies so near the middle between two of 32 bits, next to that of two of 16, that the angle's turns have to be right to 2^-50 of a turn: a, b, position, frequency
+LARGE_ANGLES = [
+    (torch.float16, -1.76171875, -1.337890625, 1002222, 0.1539926526059492), (torch.float16, 0.42236328125, 1.6083984375, 782958, 0.4216965034285822), (torch.float16, 3.947265625, 2.1015625, 727726, 1.0),
+    (torch.float16, 1.4150390625, -1.15625, 755405, 0.7498942093324559), (torch.float16, -0.4384765625, 1.14453125, 972351, 0.042169650342858224),
+    (torch.float16, 0.22998046875, -2.4296875, 798727, 0.23713737056616552), (torch.bfloat16, 1.296875, 1.8984375, 727513, 0.4216965034285822)]
+
+
+def check_large_angles(turn, where, interleaved):
+    for dtype, a, b, position, frequency in LARGE_ANGLES:
+        positions, frequencies = np.array([position], dtype=np.int32), np.full(PAIRS, frequency)
+        first, second = (rounded(v, dtype).item() for v in turned(np.array([a]), np.array([b]), position * frequency))
+        x, want = (rows_of(np.full((1, 1, PAIRS), v), np.full((1, 1, PAIRS), w), interleaved, dtype) for v, w in ((a, b), (first, second)))
+        for y in turn(where, x, positions, frequencies, interleaved):
+            assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("interleaved", [0, 1])
+def test_large_angles_on_the_host(host, interleaved):
+    check_large_angles(on_host, host, interleaved)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("interleaved", [0, 1])
+def test_large_angles_on_the_gpu(gpu, interleaved):
+    check_large_angles(on_gpu, gpu, interleaved)
