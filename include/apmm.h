@@ -285,8 +285,8 @@ apmm_status apmm_kv_attention(const apmm_kv_cache *cache, const apmm_kv_batch *b
 /* ---- Rotary positions: pairs of a row's channels turned by an angle that its position gives.
  * Of head_dim channels the first 2 * pairs are turned: pair i is channels 2 i and 2 i + 1 (interleaved) or i and i + pairs, and with t = position * frequencies[i] its (a, b) becomes
  *   magnitude * (a cos t - b sin t), magnitude * (b cos t + a sin t);
- * the other channels stay as they are.  The angle is a product of 64 bits, so far positions lose nothing; the rest is of 32 bits, rounded once to the rows' type.  Scaling for long contexts lies in
- * the frequencies and the magnitude. */
+ * the other channels stay as they are.  The angle is a product of 64 bits, so far positions lose nothing, and the sum is that of 64 bits rounded to 32, then to the rows' type (but where more than 20 bits
+ * of a pair cancel, and for numbers below 2^-100).  Scaling for long contexts lies in the frequencies and the magnitude. */
 typedef struct apmm_rotation {
     const double *frequencies; /* device, pairs: radians a position */
     int64_t pairs;             /* 1 to head_dim / 2 */
@@ -339,7 +339,7 @@ apmm_status apmm_kv_evict(const apmm_kv_cache *cache, int sequences, const int32
  * For layers whose activations are not to be quantised.  The products of a group are exact and summed in 32 bits, its sum is multiplied with the scale in 32 bits, y is rounded once.  (Activations of
  * 2^115 and more may overflow the sums.  Infinities and NaN reach the results of their own row alone.)
  *   group     32, 64 or 128 inputs; the last one of a channel may be shorter
- *   dtype     apmm_dtype of x, y and the scales; the packed form is made for one of them
+ *   dtype     apmm_dtype of x, y and the scales; the packed form is made for one of them and for its group, and does not tell which
  *   codes     device, N x K uint8, row-major, the low four bits count;  scales  device, N x ceil(K / group)
  *   packed    device, apmm_w4_packed_bytes(N, K, group) bytes, 16-byte aligned, opaque, of this version of the library
  *   x, y      device, M x K and M x N, rows x_stride and y_stride elements apart, at any address of their type's alignment, y's without a part of x; M up to 2^20, N and K up to 2^24

@@ -599,6 +599,8 @@ def apmm_w4_workspace_bytes(M, N, K, group):
 def apmm_w4_gemm(x, packed, N, group, out=None, workspace=None):
     """x (M x K, float16 or bfloat16, rows at any distance) times packed weights of N channels: M x N of x's type.
 
+    packed: apmm_w4_pack's, of scales of x's type and of the same group (a form for others that is as long is not told apart).
+
     workspace: uint8 tensor of apmm_w4_workspace_bytes(M, N, K, group) bytes; allocated if None.
     """
     if x.dtype not in _KV_DTYPES or x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):

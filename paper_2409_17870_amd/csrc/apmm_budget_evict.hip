@@ -471,7 +471,8 @@ int64_t move_units(const KvEvictArgs &a) { return (int64_t)a.c.sequences * ((a.b
 
 }  // namespace
 
-// Many workgroups to a sequence and head where its weights do not fit into one's registers and LDS.  (Tokens of 8 heads, with the copy and the read back: 130000 51 us, a million 82; 20000, 33000 and 65000 would take 49 to
+// Many workgroups to a sequence and head where its weights do not fit into one's registers and LDS.  By the page table's width, since the host does not know lengths: short sequences under a table that wide pay for
+// six launches (24 of up to 2300 tokens, 8 heads of 64, 69 us in place of 19; one of 2300 40 and 11; 8 of up to 16000 58 and 31).  (Tokens of 8 heads, with the copy and the read back: 130000 51 us, a million 82; 20000, 33000 and 65000 would take 49 to
 // 51, and take 33, 39 and 49 with one workgroup.)
 KvEvictParts kv_evict_parts(const KvArgs &c)
 {

@@ -8,11 +8,13 @@
 //
 // Few rows of a sequence (up to 16: token generation): both passes have the same workgroups, a piece of the keys each; the second joins the pieces' m and l as it begins.  The first keeps its scores for the second, a
 // number for each row and key, where they are no more than 2^26; else, and for the sequences of few rows beside others of many, the second makes them again from the keys.  8 sequences of up to 32768 tokens, 8 key/value
-// heads of 128: 4 query heads to one 55 us with scores kept (36 and 14; 111 MB of keys, 26 MB of scores written and read) and 78 with scores made twice (34 and 40), 6 60 and 78; 4 sequences of 8 to one 39 and 49, 16 to one
+// heads of 128: 4 query heads to one 51 us with scores kept (35 and 13; 111 MB of keys, 26 MB of scores written and read) and 78 with scores made twice (34 and 40), 6 60 and 78; 4 sequences of 8 to one 39 and 49, 16 to one
 // of 4 heads 32 and 35; one sequence of 3000 tokens 19 and 24.  Bound by HBM and, at the beginnings, by the way from lengths to pages to codes.
-// Many: the second pass has blocks of 256 keys (fewer where there are few of them), as operands in registers, and every row that sees some of them comes by through LDS, as the first pass left it in the workspace (RowTiles).  Bound by
-// the vector unit: of a score's 7 issues the exponential takes four.  4096 tokens of 32 heads of 128: 115 and 122 us (126 for the first pass with the rows in registers, three waves to a vector unit).  Half as many workgroups, each with a first and a
-// last block, took 257 us in all for 247; the next tile's operands read ahead, or its products made ahead, take registers that a fourth wave to a SIMD has (123 and 131 us for 121).
+// Many: the second pass has blocks of 256 keys (fewer where there are few of them), as operands in registers, and every row that sees some of them comes by through LDS, as the first pass left it in the workspace (RowTiles).  4096 tokens
+// of 32 heads of 128: 100 and 110 us where calls follow each other (120 and 128 in the first twenty after a pause).  Bound by the vector unit in the first pass: 11 instructions a score, of which the exponential takes the time of two, busy for
+// 92 % of the cycles in which its compute unit has work, which are 88 % of all.  In the second pass (9 instructions) no unit is full: vector 72 %, LDS 58 %, matrix 30 % of the cycles with work, which are 81 % of all, since each workgroup has one
+// block here and the first ones have the most rows.  When the passes took 115 and 122 us: the first one with the rows in registers, three waves to a vector unit, 126; half as many workgroups, each with a first and a last block, 10 more in
+// all; the next tile's operands read ahead, or its products made ahead, which take registers that a fourth wave to a SIMD has, 2 and 10 more.
 #include <algorithm>
 #include <type_traits>
 

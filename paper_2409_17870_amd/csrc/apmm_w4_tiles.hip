@@ -8,7 +8,7 @@
 //
 // What bounds many tokens: LDS, which gives every wave all of the block's activations, 128 bytes a clock at the full rate of the matrix unit, and beside it the vector unit (unpacking 43 % (bfloat16) or 28 %
 // (binary16) of the matrix unit's time at T = 4, the groups' products 25, 50 or 100 %): two workgroups on a compute unit, so that one's vector instructions run under the other's products.
-// 2048 x 11008 x 4096 takes 196 us, 943 TFLOP/s.  (A wave with 64 channels, which halves what is read from LDS, took 207 to 260, with two waves to a vector unit or one: it is not LDS alone.)
+// 2048 x 11008 x 4096 takes 197 us, 937 TFLOP/s, where calls follow each other (240 in the first twenty after a pause).  (A wave with 64 channels, which halves what is read from LDS, took 207 to 260, with two waves to a vector unit or one: it is not LDS alone.)
 // What bounds a few: a workgroup's way from its first load to its first product (5 us with launch and join), then 0.45 + 0.2 T us a block for one workgroup to a compute unit.
 #include <type_traits>
 
