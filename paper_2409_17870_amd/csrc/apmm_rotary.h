@@ -94,13 +94,14 @@ __device__ __forceinline__ float rotary_exact(float x, float other, const float4
     return all == all ? all : v;
 }
 // Rounding in the sum decides the one to 16 bits where the number is so near the middle between two of those: one in 1600 (binary16) or 13000.  Keys are quantised behind this, where a number rounded the other way may
-// cost a code.  Below 2^-14 binary16 numbers are equally far apart, and the middles not at one place of the bits: any of these is near.  So is, of
+// cost a code.  Below 2^-14 binary16 numbers are equally far apart, and the middles not at one place of the bits: any of these is near (rows of
+// zeros, as batches are filled up with, would take a fifth longer if they were).  So is, of
 // bfloat16, whose largest numbers are those of 32 bits, what has become infinite on the way.
 template <bool BF16>
 __device__ __forceinline__ bool rotary_near(float v)
 {
     constexpr uint32_t kHalf = BF16 ? 0x8000 : 0x1000;
-    return (((__float_as_uint(v) - (kHalf - 2)) & (2 * kHalf - 1)) <= 4) | (BF16 ? !(fabsf(v) < __builtin_inff()) : fabsf(v) < 0x1p-14f);
+    return (((__float_as_uint(v) - (kHalf - 2)) & (2 * kHalf - 1)) <= 4) | (BF16 ? !(fabsf(v) < __builtin_inff()) : fabsf(fabsf(v) - 0x1p-15f) < 0x1p-15f);  // (zeros, and what is less than 2^-40 and will be one, are not)
 }
 // Each number is made again by its own nearness alone, here and where both of a pair are a lane's: so all kernels have the same.
 template <bool BF16>
